@@ -241,6 +241,66 @@ size_t cotten_attn_workspace_bytes_ex(int B, int H, int N, int d_h, int is_bwd,
 /* Static, NUL-terminated description of a status code. */
 const char* cotten_status_string(int status);
 
+/* ---- Gated delta rule -----------------------------------------------------------------------
+ *
+ * The recurrent form of the causal linear attention above, with a state that can forget and
+ * correct itself.  For every slice (b,h), with unit rows xhat = x / sqrt(sum_c x_c^2 + eps)
+ * of Q and K as above, a_t = exp(g_t) and the state S (d_h x d_h, row a, column c):
+ *
+ *     u_t = beta_t * (v_t - a_t * S_{t-1}^T khat_t)        what is still missing of v_t
+ *     S_t = a_t * S_{t-1} + khat_t u_t^T                   decay, then write
+ *     O_t = scale * S_t^T qhat_t
+ *
+ * g (log decays, any sign; -inf empties the state) and beta are float, [B, H, N] or, with
+ * COTTEN_BNHD, [B, N, H]; Q, K, V, O and their gradients are as above.  A masked token (mask
+ * byte 0) leaves the state as it is: a = 1, beta = 0, and its K, V, g and beta are not
+ * used, so they may hold anything; O exists for all N rows (queries are not masked).  Gradients of masked K, V, g
+ * and beta are exact zeros.  A sequence without a valid token keeps its initial state.
+ *
+ * States are fp32, [B, H, d_h, d_h].  Sums, states and norms are fp32 or wider whatever the I/O type,
+ * and operands of products are not rounded to 16 bits.  A value that is not finite in a row
+ * that takes part makes the results of its column not finite from its group of 32 tokens on.
+ *
+ * Calls enqueue on `stream` only, allocate nothing, and give the same bits for the same
+ * arguments.  d_h in {16, 32, 64, 128}.  */
+typedef struct cotten_delta_params {
+  int dtype;                  /* a cotten_dtype: of Q, K, V, O and their gradients               */
+  float scale;                /* factor of O; <= 0 selects 1                                     */
+  float eps;                  /* inside the square roots; < 0 selects 1e-6; 0 allowed            */
+  int layout;                 /* a cotten_layout                                                 */
+  void* workspace;            /* backward: device buffer of cotten_delta_workspace_bytes(), 16-byte
+                                 aligned.  Forward: not looked at                                */
+  size_t workspace_bytes;
+  const float* initial_state; /* device, [B*H, d_h, d_h], or NULL: zeros                         */
+  float* final_state;         /* forward: receives the state after row N-1, or NULL.  May be
+                                 initial_state itself (a server's state, replaced in place)      */
+  const float* dfinal_state;  /* backward: gradient of the final state, or NULL: zeros           */
+  float* dinitial_state;      /* backward: receives the gradient of the initial state, or NULL   */
+  void* kept;                 /* device buffer of cotten_delta_kept_bytes(), 16-byte aligned, or
+                                 NULL.  Forward: receives what the backward of the same inputs
+                                 needs of it.  Backward: what that forward wrote (without it the
+                                 backward walks the sequence forwards first, in its workspace,
+                                 with the same results)                                          */
+  size_t kept_bytes;
+} cotten_delta_params;
+
+/* `params` must not be NULL.  N = 1 with final_state == initial_state is one step of a server. */
+int cotten_delta_fwd(const void* Q, const void* K, const void* V, const float* g, const float* beta,
+                     const uint8_t* mask, void* O, int B, int H, int N, int d_h, void* stream,
+                     const cotten_delta_params* params);
+
+/* Gradients of all inputs from dO (and params->dfinal_state).  initial_state is read where kept is NULL: it has to hold
+ * what the forward call saw. */
+int cotten_delta_bwd(const void* Q, const void* K, const void* V, const float* g, const float* beta,
+                     const uint8_t* mask, const void* dO, void* dQ, void* dK, void* dV, float* dg,
+                     float* dbeta, int B, int H, int N, int d_h, void* stream,
+                     const cotten_delta_params* params);
+
+/* Bytes of params->kept, and of params->workspace (0 for the forward; with_kept: the backward is given params->kept).
+ * They grow like N * d_h * (d_h / 32 + 1).  0 for invalid arguments; host only. */
+size_t cotten_delta_kept_bytes(int B, int H, int N, int d_h, int dtype);
+size_t cotten_delta_workspace_bytes(int B, int H, int N, int d_h, int dtype, int is_bwd, int with_kept);
+
 #ifdef __cplusplus
 }
 #endif

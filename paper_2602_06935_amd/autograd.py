@@ -41,3 +41,40 @@ def cosine_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
     """O = scale * Qhat (Khat^T V) under the key mask, differentiable in Q, K, V and, when
     given, in the per-slice scales `slice_scale` ([B,H] float32)."""
     return _CosineAttention.apply(Q, K, V, mask, scale, eps, slice_scale, layout)
+
+
+class _GatedDelta(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, Q, K, V, g, beta, mask, scale, eps, initial_state, layout):
+        kept = binding.cotten_delta_kept(Q, layout=layout) if any(ctx.needs_input_grad) else None
+        B, H, _, d = binding._dims(Q, layout)
+        state = torch.empty(B, H, d, d, device=Q.device, dtype=torch.float32)
+        O = binding.cotten_delta_fwd(Q, K, V, g, beta, mask, scale=scale, eps=eps, layout=layout,
+                                     initial_state=initial_state, final_state=state, kept=kept)
+        ctx.save_for_backward(Q, K, V, g, beta, mask, kept, initial_state)
+        ctx.scale, ctx.eps, ctx.layout = scale, eps, layout
+        ctx.set_materialize_grads(False)
+        return O, state
+
+    @staticmethod
+    def backward(ctx, dO, dstate):
+        Q, K, V, g, beta, mask, kept, initial_state = ctx.saved_tensors
+        dO = torch.zeros_like(Q) if dO is None else dO.contiguous()
+        dfirst = None
+        if initial_state is not None and ctx.needs_input_grad[8]:
+            dfirst = torch.empty_like(initial_state)
+        grads = binding.cotten_delta_bwd(Q, K, V, g, beta, mask, dO, scale=ctx.scale, eps=ctx.eps, layout=ctx.layout,
+                                         initial_state=initial_state, dinitial_state=dfirst, kept=kept,
+                                         dfinal_state=None if dstate is None else dstate.contiguous())
+        return (*grads, None, None, None, dfirst, None)
+
+
+def gated_delta_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor, beta: torch.Tensor,
+                          mask: Optional[torch.Tensor] = None, *, scale: Optional[float] = None,
+                          eps: Optional[float] = None, initial_state: Optional[torch.Tensor] = None,
+                          return_state: bool = False, layout: str = "bhnd"):
+    """The gated delta rule of `binding.cotten_delta_fwd`, differentiable in Q, K, V, g, beta and the initial state;
+    with `return_state` (O, final state).  The states before every 32 tokens and a float32 row per token are kept for the
+    backward."""
+    O, state = _GatedDelta.apply(Q, K, V, g, beta, mask, scale, eps, initial_state, layout)
+    return (O, state) if return_state else O

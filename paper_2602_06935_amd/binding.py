@@ -35,6 +35,7 @@ EXPORTS = (
     "cotten_attn_workspace_bytes", "cotten_status_string",
     "cotten_normaliser_fwd", "cotten_normaliser_bwd", "cotten_attn_bwd_static",
     "cotten_attn_workspace_bytes_ex",
+    "cotten_delta_fwd", "cotten_delta_bwd", "cotten_delta_kept_bytes", "cotten_delta_workspace_bytes",
 )
 
 
@@ -44,6 +45,14 @@ class CottenParams(ctypes.Structure):
                 ("slice_scale", ctypes.c_void_p), ("dlog_scale", ctypes.c_void_p),
                 ("layout", ctypes.c_int), ("causal", ctypes.c_int),
                 ("saved_state", ctypes.c_void_p), ("feature_map", ctypes.c_int)]
+
+
+class CottenDeltaParams(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("scale", ctypes.c_float), ("eps", ctypes.c_float),
+                ("layout", ctypes.c_int), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+                ("initial_state", ctypes.c_void_p), ("final_state", ctypes.c_void_p),
+                ("dfinal_state", ctypes.c_void_p), ("dinitial_state", ctypes.c_void_p),
+                ("kept", ctypes.c_void_p), ("kept_bytes", ctypes.c_size_t)]
 
 
 class CottenError(RuntimeError):
@@ -82,6 +91,12 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.cotten_normaliser_fwd.argtypes = [vp, vp, vp, ip, ip, ip, vp]
     lib.cotten_normaliser_bwd.argtypes = [vp, vp, vp, ip, ip, ip, vp]
     lib.cotten_normaliser_fwd.restype = lib.cotten_normaliser_bwd.restype = ctypes.c_int
+    lib.cotten_delta_fwd.argtypes = [vp] * 7 + [ip] * 4 + [vp, ctypes.POINTER(CottenDeltaParams)]
+    lib.cotten_delta_bwd.argtypes = [vp] * 12 + [ip] * 4 + [vp, ctypes.POINTER(CottenDeltaParams)]
+    lib.cotten_delta_fwd.restype = lib.cotten_delta_bwd.restype = ctypes.c_int
+    lib.cotten_delta_kept_bytes.argtypes = [ip] * 5
+    lib.cotten_delta_workspace_bytes.argtypes = [ip] * 7
+    lib.cotten_delta_kept_bytes.restype = lib.cotten_delta_workspace_bytes.restype = ctypes.c_size_t
     lib.cotten_status_string.argtypes = [ip]
     lib.cotten_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -359,3 +374,105 @@ def cotten_normaliser_bwd(dlog_scale: torch.Tensor, n: Optional[torch.Tensor], N
                                          _lengths_ptr(n, B, dev), _f32_vector("dm", dm, H, dev),
                                          B, H, N, _stream_handle(stream)))
     return dm
+
+
+# ---- gated delta rule -----------------------------------------------------------------------------
+
+_LAYOUTS = {"bhnd": COTTEN_BHND, "bnhd": COTTEN_BNHD}
+
+
+@functools.lru_cache(maxsize=1024)
+def cotten_delta_kept_bytes(B: int, H: int, N: int, d_h: int, dtype: int) -> int:
+    return int(load_library().cotten_delta_kept_bytes(B, H, N, d_h, dtype))
+
+
+@functools.lru_cache(maxsize=1024)
+def cotten_delta_workspace_bytes(B: int, H: int, N: int, d_h: int, dtype: int, is_bwd: bool,
+                                 with_kept: bool = False) -> int:
+    return int(load_library().cotten_delta_workspace_bytes(B, H, N, d_h, dtype, int(bool(is_bwd)),
+                                                           int(bool(with_kept))))
+
+
+def cotten_delta_kept(Q: torch.Tensor, *, layout: str = "bhnd") -> torch.Tensor:
+    """A buffer for what the forward of Q's shape hands to its backward (`kept` of the two calls)."""
+    B, H, N, d = _dims(Q, layout)
+    return torch.empty(cotten_delta_kept_bytes(B, H, N, d, _dtype_code(Q)), dtype=torch.uint8, device=Q.device)
+
+
+def _buffer(name: str, t: Optional[torch.Tensor], dev) -> Tuple[Optional[int], int]:
+    if t is None:
+        return None, 0
+    if not t.is_contiguous() or t.device != dev:
+        raise ValueError(f"{name} must be a contiguous tensor on the device of Q")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def _delta_params(Q, g, beta, dims, gates, scale, eps, layout, workspace, initial_state, final_state,
+                  dfinal_state, dinitial_state, kept) -> CottenDeltaParams:
+    """The checks of what the two calls share besides Q, K and V, and their parameters."""
+    B, H, N, d = dims
+    dev = Q.device
+    lead = Q.shape[:3]
+    for name, t in gates:
+        if not (t.dtype is torch.float32 and t.shape == lead and t.device == dev and t.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous float32 tensor of shape {tuple(lead)} on the device of Q")
+    ptr = [None if t is None else _f32_vector(name, t, B * H * d * d, dev) for name, t in (
+        ("initial_state", initial_state), ("final_state", final_state), ("dfinal_state", dfinal_state),
+        ("dinitial_state", dinitial_state))]
+    space, space_bytes = _buffer("workspace", workspace, dev)
+    held, held_bytes = _buffer("kept", kept, dev)
+    return CottenDeltaParams(_dtype_code(Q), 0.0 if scale is None else float(scale), -1.0 if eps is None else float(eps),
+                             _LAYOUTS[layout], space, space_bytes, *ptr, held, held_bytes)
+
+
+def cotten_delta_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor, beta: torch.Tensor,
+                     mask: Optional[torch.Tensor], O: Optional[torch.Tensor] = None, *,
+                     scale: Optional[float] = None, eps: Optional[float] = None, stream=None,
+                     layout: str = "bhnd", initial_state: Optional[torch.Tensor] = None,
+                     final_state: Optional[torch.Tensor] = None,
+                     kept: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gated delta rule: S_t = a_t S_{t-1} + khat_t u_t^T with u_t = beta_t (v_t - a_t S_{t-1}^T khat_t) and a_t =
+    exp(g_t); O_t = scale * S_t^T qhat_t.  Enqueues on the stream and returns O.
+    `g` (log decays) and `beta` are float32, [B,H,N] ([B,N,H] with layout "bnhd"); a masked token leaves the state as it is;
+    `scale` defaults to 1.  `initial_state` and `final_state` ([B,H,d_h,d_h] float32) may be the same tensor: with N = 1 that
+    is a server's step.  `kept` (see cotten_delta_kept) receives what the backward needs of this call."""
+    lib = _lib or load_library()
+    _prep_like(Q, (("K", K), ("V", V)))
+    dims = _dims(Q, layout)
+    O = torch.empty_like(Q) if O is None else _prep("O", O, Q)
+    prm = _delta_params(Q, g, beta, dims, (("g", g), ("beta", beta)), scale, eps, layout, None, initial_state,
+                        final_state, None, None, kept)
+    _on_device(Q.device, lib.cotten_delta_fwd, Q.data_ptr(), K.data_ptr(), V.data_ptr(), g.data_ptr(),
+               beta.data_ptr(), _mask_ptr(mask, dims[0], dims[2], Q.device), O.data_ptr(), *dims,
+               _stream_handle(stream), ctypes.byref(prm))
+    return O
+
+
+def cotten_delta_bwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor, beta: torch.Tensor,
+                     mask: Optional[torch.Tensor], dO: torch.Tensor, dQ: Optional[torch.Tensor] = None,
+                     dK: Optional[torch.Tensor] = None, dV: Optional[torch.Tensor] = None,
+                     dg: Optional[torch.Tensor] = None, dbeta: Optional[torch.Tensor] = None, *,
+                     scale: Optional[float] = None, eps: Optional[float] = None, stream=None,
+                     workspace: Optional[torch.Tensor] = None, layout: str = "bhnd",
+                     initial_state: Optional[torch.Tensor] = None, dfinal_state: Optional[torch.Tensor] = None,
+                     dinitial_state: Optional[torch.Tensor] = None, kept: Optional[torch.Tensor] = None):
+    """(dQ, dK, dV, dg, dbeta) for the upstream gradients dO and, when given, `dfinal_state`; `dinitial_state`, when
+    given, receives the gradient of the initial state.  `kept`: what the forward call of the same inputs wrote (without it
+    `initial_state` has to hold what that call saw, and the sequence is walked forwards once more)."""
+    lib = _lib or load_library()
+    _prep_like(Q, (("K", K), ("V", V), ("dO", dO)))
+    dims = _dims(Q, layout)
+    dQ = torch.empty_like(Q) if dQ is None else _prep("dQ", dQ, Q)
+    dK = torch.empty_like(Q) if dK is None else _prep("dK", dK, Q)
+    dV = torch.empty_like(Q) if dV is None else _prep("dV", dV, Q)
+    dg = torch.empty_like(g) if dg is None else dg
+    dbeta = torch.empty_like(beta) if dbeta is None else dbeta
+    handle = _stream_handle(stream)
+    if workspace is None:
+        workspace = _workspace(Q, cotten_delta_workspace_bytes(*dims, _dtype_code(Q), True, kept is not None), handle)
+    prm = _delta_params(Q, g, beta, dims, (("g", g), ("beta", beta), ("dg", dg), ("dbeta", dbeta)), scale, eps, layout,
+                        workspace, initial_state, None, dfinal_state, dinitial_state, kept)
+    _on_device(Q.device, lib.cotten_delta_bwd, Q.data_ptr(), K.data_ptr(), V.data_ptr(), g.data_ptr(),
+               beta.data_ptr(), _mask_ptr(mask, dims[0], dims[2], Q.device), dO.data_ptr(), dQ.data_ptr(),
+               dK.data_ptr(), dV.data_ptr(), dg.data_ptr(), dbeta.data_ptr(), *dims, handle, ctypes.byref(prm))
+    return dQ, dK, dV, dg, dbeta

@@ -1,0 +1,234 @@
+// Forward of the gated delta rule (cotten_delta_core.h has the formulas): a recurrence for a few tokens, and chunks of 32
+// tokens on the matrix cores for more.
+#include "cotten_delta_chunk.h"
+#include "cotten_delta_launch.h"
+#include "cotten_launch.h"
+
+namespace cotten {
+namespace delta {
+namespace {
+
+extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+
+// ---- token by token -----------------------------------------------------------------------------------------------
+//
+// A wave carries up to 32 columns of a state in registers (columns do not meet: u of a column needs that column only),
+// eight lanes to a row of 128 bytes, the rows dealt to the lane groups.  k^ . S and q^ . S are sums over the groups by
+// lane permutes; no LDS, no barrier.  One token is bound by the state, read and written once.
+template <class E, int D>
+__global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
+  constexpr int kCols = D < 32 ? D : 32;         // columns of a wave
+  constexpr int kLanes = kCols / 4;              // lanes of a row
+  constexpr int kGroups = 64 / kLanes;
+  constexpr int kRows = D / kGroups;             // rows of a lane: group, group + kGroups, ...
+  static_assert(D % kGroups == 0, "rows are dealt evenly");
+  const int lane = threadIdx.x & 63;
+  const long long unit = static_cast<long long>(blockIdx.x) * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= static_cast<long long>(parts) * (D / kCols)) return;
+  const int slice = static_cast<int>(unit / (D / kCols)), col = static_cast<int>(unit % (D / kCols)) * kCols + 4 * (lane % kLanes);
+  const int group = lane / kLanes;
+  const Slice s(a, slice, D * E::kBytes);
+  const __amdgpu_buffer_rsrc_t Q = s.of(a.Q), K = s.of(a.K), V = s.of(a.V), O = s.of(a.O);
+
+  f32x4_t S[kRows];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r)
+    S[r] = a.initial_state == nullptr
+               ? f32x4_t{0, 0, 0, 0}
+               : *reinterpret_cast<const f32x4_t*>(a.initial_state + (static_cast<long long>(slice) * D + group + r * kGroups) * D + col);
+  for (int t = 0; t < a.N; ++t) {
+    const bool live = s.mask == nullptr || s.mask[t] != 0;
+    const uint32_t row = static_cast<uint32_t>(t) * a.stride_row;
+    const long long gate = s.gates + static_cast<long long>(t) * a.gate_row;
+    const float decay = live ? expf(a.g[gate]) : 1.0f, beta = live ? a.beta[gate] : 0.0f;
+    const f32x4_t v = E::load_four(V, live ? row + col * E::kBytes : kNowhere);
+    float k[kRows], q[kRows], kk = 0.0f, qq = 0.0f;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const uint32_t off = row + (group + r * kGroups) * E::kBytes;
+      k[r] = E::load_one(K, live ? off : kNowhere);
+      q[r] = E::load_one(Q, off);
+      kk = fmaf(k[r], k[r], kk);
+      qq = fmaf(q[r], q[r], qq);
+    }
+    f32x4_t p = {0, 0, 0, 0};
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      S[r] *= decay;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) p[c] = fmaf(k[r], S[r][c], p[c]);
+    }
+#pragma unroll
+    for (int m = kLanes; m < 64; m <<= 1) {
+      kk += __shfl_xor(kk, m);
+      qq += __shfl_xor(qq, m);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) p[c] += __shfl_xor(p[c], m);
+    }
+    const float rk = __builtin_amdgcn_rsqf(kk + a.eps), rq = a.scale * __builtin_amdgcn_rsqf(qq + a.eps);
+    f32x4_t u, o = {0, 0, 0, 0};
+#pragma unroll
+    for (int c = 0; c < 4; ++c) u[c] = live ? beta * (v[c] - rk * p[c]) * rk : 0.0f;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        S[r][c] = fmaf(k[r], u[c], S[r][c]);
+        o[c] = fmaf(q[r], S[r][c], o[c]);
+      }
+#pragma unroll
+    for (int m = kLanes; m < 64; m <<= 1)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] += __shfl_xor(o[c], m);
+    if (group == 0) E::store_four(O, row + col * E::kBytes, o * rq);
+  }
+  if (a.final_state != nullptr) {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+      *reinterpret_cast<f32x4_t*>(a.final_state + (static_cast<long long>(slice) * D + group + r * kGroups) * D + col) = S[r];
+  }
+}
+
+// ---- chunks ---------------------------------------------------------------------------------------------------------
+//
+// A workgroup walks the chunks of a slice: wave 0 makes the keys' side of a chunk, wave 1 the queries', the others carry 16
+// columns of the state each, a chunk behind.  Everything a consumer passes on to itself (K^ S -> U -> O, S) stays in the
+// registers it came out in; LDS only carries what the producers made.
+template <int D>
+constexpr int kConsumers = D / 16 < 4 ? D / 16 : 4;  // of a workgroup; d = 128 takes two (of ten waves, none would have the registers)
+
+template <class E, int D>
+__global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Args a) {
+  typedef ChunkBuffer<E, D> B;
+  typedef typename B::R R;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int kGroups = D / 16 / kConsumers<D>;
+  const int slice = blockIdx.x / kGroups, group = blockIdx.x % kGroups;
+  const Slice s(a, slice, D * E::kBytes);
+  Scratch* scratch = reinterpret_cast<Scratch*>(smem + 2 * B::kBytes);
+  Notes* notes = reinterpret_cast<Notes*>(scratch + 1);
+  const __amdgpu_buffer_rsrc_t K = s.of(a.K);
+
+  if (wave == 0) {
+    KeyProducer<E, D, false> producer;
+    producer.begin(a, s, K, 0, a.chunks > 1 ? 1 : -1, lane);
+    for (int c = 0; c <= a.chunks; ++c) {
+      if (c < a.chunks)
+        producer.make(a, s, K, c + 1 < a.chunks ? c + 1 : -1, c + 2 < a.chunks ? c + 2 : -1, smem + (c & 1) * B::kBytes, scratch, lane);
+      __syncthreads();
+    }
+  } else if (wave == 1) {
+    if (a.O == nullptr) {
+      for (int c = 0; c <= a.chunks; ++c) __syncthreads();
+      return;
+    }
+    const __amdgpu_buffer_rsrc_t Q = s.of(a.Q);
+    QueryProducer<E, D, false> producer;
+    producer.begin(a, s, Q, K, 0, a.chunks > 1 ? 1 : -1, lane);
+    for (int c = 0; c <= a.chunks; ++c) {
+      if (c < a.chunks)
+        producer.make(a, s, Q, K, c + 1 < a.chunks ? c + 1 : -1, c + 2 < a.chunks ? c + 2 : -1, smem + (c & 1) * B::kBytes, notes, lane);
+      __syncthreads();
+    }
+  } else {
+    const __amdgpu_buffer_rsrc_t V = s.of(a.V), O = s.of(a.O);
+    const int tile = group * kConsumers<D> + wave - 2, col = 16 * tile + (lane & 15);
+    StateColumns<D> S;
+    S.load(a.initial_state == nullptr ? nullptr : a.initial_state + static_cast<long long>(slice) * D * D, col, lane);
+    S.cut_all();
+    ColumnTile<E> v;
+    v.load(V, a.stride_row, 0, live_of(fetch_live(s, a.N, 0, lane)), col, lane);
+    int byte = a.chunks > 1 ? fetch_live(s, a.N, 1, lane) : 0;
+    __syncthreads();
+    for (int c = 0; c < a.chunks; ++c) {
+      const unsigned char* at = smem + (c & 1) * B::kBytes;
+      const float* coef = reinterpret_cast<const float*>(at + B::kCoef);
+      const long long chunk = static_cast<long long>(slice) * a.chunks + c;
+      if (a.states != nullptr) S.store(a.states + chunk * D * D, col, lane);
+      // beta (V - e^G K^ S)
+      f32x4_t u[2];
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) {
+        f32x4_t p = {0, 0, 0, 0};
+#pragma unroll
+        for (int kb = 0; kb < S.kBlocks; ++kb) p = mul(R::row_operand(at + B::kK, tt, kb, lane), S.p[kb], p);
+        u[tt] = by_rows(coef + B::kBeta, tt, lane) * (v.tile(tt) - by_rows(coef + B::kReadK, tt, lane) * p);
+      }
+      if (c + 1 < a.chunks) {
+        v.load(V, a.stride_row, c + 1, live_of(byte), col, lane);
+        byte = c + 2 < a.chunks ? fetch_live(s, a.N, c + 2, lane) : 0;
+      }
+      const Pieces<3> y = cut(u[0], u[1]);
+#pragma unroll
+      for (int tt = 0; tt < 2; ++tt) u[tt] = mul(triangle_operand(at + B::kT, tt, lane), y, f32x4_t{0, 0, 0, 0});
+      if (a.rows_u != nullptr) {
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) a.rows_u[(chunk * kChunk + 16 * tt + 4 * (lane >> 4) + r) * D + col] = u[tt][r];
+      }
+      if (a.O != nullptr) {
+        // O^T: a lane has four columns of a token
+        const Pieces<3> up = cut(u[0], u[1]);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) {
+          f32x4_t o = {0, 0, 0, 0};
+#pragma unroll
+          for (int kb = 0; kb < S.kBlocks; ++kb) o = mul(S.p[kb], R::row_operand(at + B::kQ, tt, kb, lane), o);
+          o *= coef[B::kQuery + 16 * tt + (lane & 15)];
+          o = mul(up, triangle_operand(at + B::kM, tt, lane), o);
+          const int row = kChunk * c + 16 * tt + (lane & 15);
+          if (row < a.N)
+            E::store_four(O, static_cast<uint32_t>(row) * a.stride_row + (16 * tile + 4 * (lane >> 4)) * E::kBytes, o);
+        }
+      }
+      // S' = e^(G_C) S + K^^T (e^(G_C - G) U)
+      const float whole = coef[B::kWhole];
+      const Pieces<3> w = cut(u[0] * by_rows(coef + B::kWriteK, 0, lane), u[1] * by_rows(coef + B::kWriteK, 1, lane));
+#pragma unroll
+      for (int dt = 0; dt < S.kTiles; ++dt) S.s[dt] = mul(R::column_operand(at + B::kK, dt, lane), w, S.s[dt] * whole);
+      S.cut_all();
+      __syncthreads();
+    }
+    if (a.final_state != nullptr) S.store(a.final_state + static_cast<long long>(slice) * D * D, col, lane);
+  }
+}
+
+// Up to this many tokens the recurrence is faster than a chunk.
+constexpr int kMostSteps = 8;
+
+template <class E, int D>
+hipError_t launch(const Args& a, int slices, hipStream_t stream) {
+  if (a.N <= kMostSteps && a.states == nullptr && a.O != nullptr) {
+    constexpr int kParts = D < 32 ? 1 : D / 32;
+    const long long waves = static_cast<long long>(slices) * kParts;
+    const int per = waves >= 4096 ? 4 : 1;
+    step_kernel<E, D><<<dim3(static_cast<uint32_t>((waves + per - 1) / per)), dim3(64 * per), 0, stream>>>(a, slices);
+    return hipGetLastError();
+  }
+  constexpr int kLds = 2 * ChunkBuffer<E, D>::kBytes + sizeof(Scratch) + sizeof(Notes);
+  if (hipError_t err = grant_dynamic_lds(reinterpret_cast<const void*>(chunk_fwd_kernel<E, D>), kLds); err != hipSuccess) return err;
+  chunk_fwd_kernel<E, D><<<dim3(slices * (D / 16 / kConsumers<D>)), dim3(64 * (kConsumers<D> + 2)), kLds, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <class E>
+hipError_t launch_dim(const Args& a, int D, int slices, hipStream_t stream) {
+  switch (D) {
+    case 16: return launch<E, 16>(a, slices, stream);
+    case 32: return launch<E, 32>(a, slices, stream);
+    case 64: return launch<E, 64>(a, slices, stream);
+    default: return launch<E, 128>(a, slices, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_forward(const Args& a, int dtype, int D, int slices, hipStream_t stream) {
+  return dtype == 0 ? launch_dim<F32>(a, D, slices, stream)
+         : dtype == 1 ? launch_dim<Bf16>(a, D, slices, stream)
+                      : launch_dim<F16>(a, D, slices, stream);
+}
+
+}  // namespace delta
+}  // namespace cotten

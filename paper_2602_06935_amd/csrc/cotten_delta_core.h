@@ -1,0 +1,469 @@
+// Device code shared by the kernels of the gated delta rule: the pieces that matrix-core operands are cut into, row
+// loads in the layout of the products, and what a chunk of 32 tokens needs before its state is known.
+//
+// The operation, for a slice (b,h) with unit rows k^ = k / sqrt(|k|^2 + eps), q^ likewise, a_t = exp(g_t):
+//
+//     u_t = beta_t (v_t - a_t S_{t-1}^T k^_t)      S_t = a_t S_{t-1} + k^_t u_t^T      o_t = scale * S_t^T q^_t
+//
+// (a masked token: a = 1, beta = 0).  Over a chunk, with S the state before it, G the inclusive sums of g inside it and
+// everything row by row:
+//
+//     N_ij = e^(G_i - G_j) k^_i . k^_j  (j < i)     T = (I + diag(beta) N)^-1
+//     U = T beta (V - e^G (K^ S))                   O = scale (e^G (Q^ S) + M U),  M_ij = e^(G_i - G_j) q^_i . k^_j (j <= i)
+//     S' = e^(G_C) S + K^^T (e^(G_C - G) U)
+//
+// T and M do not depend on the state: "producer" waves make them, ahead of the waves that carry the state along.
+//
+// Precision.  States and gate gradients leave in fp32, and an error of u is written into the state, so nothing is
+// rounded to 16 bits on the way: an operand is cut into bf16 pieces, x = h + m + l exactly (fp32: three pieces; fp16: two;
+// bf16: itself), and a product is the sum of the products of pieces that reach 24 bits (the norms 1 / r(x) and the
+// decays are factors of the results, so raw 16-bit rows stay exact operands).  For bf16 rows a product with the state
+// is three matrix instructions, for fp32 rows six, a fifth and 2/5 of what fp32 matrix instructions would take.
+// Sums of g are fp64: differences of sums that a strong decay has made large would lose the weak decays after it.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace cotten {
+namespace delta {
+
+typedef __bf16 bf16x2_t __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8_t __attribute__((ext_vector_type(8)));
+typedef float f32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+
+constexpr int kChunk = 32;                       // tokens of a chunk: the depth of one matrix instruction
+constexpr uint32_t kNowhere = 0x80000000u;       // a byte offset beyond every slice: such loads bring zeros
+
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+__device__ __forceinline__ f32x4_t mfma(bf16x8_t a, bf16x8_t b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4_t mfma(float a, float b, f32x4_t c) {
+  return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+// ---- pieces ----------------------------------------------------------------------------------------------------
+
+template <int P>
+struct Pieces {
+  bf16x8_t p[P];  // p[0] the leading bits
+};
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  bf16x2_t v;
+  v[0] = static_cast<__bf16>(lo);
+  v[1] = static_cast<__bf16>(hi);
+  return __builtin_bit_cast(uint32_t, v);
+}
+
+// Eight values as three pieces: h the upper half of the word, m what is left rounded to bf16, l the rest (which fits).
+__device__ __forceinline__ Pieces<3> cut(const float (&x)[8]) {
+  u32x4_t h, m, l;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t a = __float_as_uint(x[2 * i]), b = __float_as_uint(x[2 * i + 1]);
+    h[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    const float ra = x[2 * i] - __uint_as_float(a & 0xffff0000u), rb = x[2 * i + 1] - __uint_as_float(b & 0xffff0000u);
+    m[i] = pack_bf16(ra, rb);
+    l[i] = pack_bf16(ra - __uint_as_float(m[i] << 16), rb - __uint_as_float(m[i] & 0xffff0000u));
+  }
+  Pieces<3> r;
+  r.p[0] = __builtin_bit_cast(bf16x8_t, h);
+  r.p[1] = __builtin_bit_cast(bf16x8_t, m);
+  r.p[2] = __builtin_bit_cast(bf16x8_t, l);
+  return r;
+}
+__device__ __forceinline__ Pieces<3> cut(f32x4_t a, f32x4_t b) {
+  const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  return cut(x);
+}
+
+// The pieces that values of E's are made of (fewer than three where they are 16-bit values).
+template <class E>
+__device__ __forceinline__ Pieces<E::kPieces> cut_elements(f32x4_t a, f32x4_t b) {
+  const Pieces<3> c = cut(a, b);
+  Pieces<E::kPieces> r;
+#pragma unroll
+  for (int i = 0; i < E::kPieces; ++i) r.p[i] = c.p[i];
+  return r;
+}
+
+// c += A B, the products of pieces that reach 24 bits, the small ones first.
+template <int PA, int PB>
+__device__ __forceinline__ f32x4_t mul(const Pieces<PA>& a, const Pieces<PB>& b, f32x4_t c) {
+#pragma unroll
+  for (int s = 2; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i < PA; ++i)
+      if (s - i >= 0 && s - i < PB) c = mfma(a.p[i], b.p[s - i], c);
+  return c;
+}
+
+// ---- element formats: eight consecutive elements of a row ---------------------------------------------------------
+
+struct F32 {
+  static constexpr int kBytes = 4, kPieces = 3;
+  struct Raw {
+    u32x4_t a, b;
+  };
+  static __device__ __forceinline__ Raw load(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return Raw{__builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0),
+               __builtin_amdgcn_raw_buffer_load_b128(r, off + 16, 0, 0)};
+  }
+  static __device__ __forceinline__ void unpack(const Raw& w, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[i] = __uint_as_float(w.a[i]);
+      x[4 + i] = __uint_as_float(w.b[i]);
+    }
+  }
+  static __device__ __forceinline__ Pieces<3> pieces(const Raw& w) {
+    float x[8];
+    unpack(w, x);
+    return cut(x);
+  }
+  static __device__ __forceinline__ float load_one(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
+  }
+  static __device__ __forceinline__ f32x4_t load_four(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
+  }
+  static __device__ __forceinline__ void store_one(__amdgpu_buffer_rsrc_t r, uint32_t off, float x) {
+    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), r, off, 0, 0);
+  }
+  static __device__ __forceinline__ void store_four(__amdgpu_buffer_rsrc_t r, uint32_t off, f32x4_t x) {
+    __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, x), r, off, 0, 0);
+  }
+};
+
+template <class T>
+struct Half {
+  static constexpr int kBytes = 2;
+  typedef u32x4_t Raw;
+  static __device__ __forceinline__ Raw load(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0);
+  }
+  static __device__ __forceinline__ float value(uint16_t bits) { return static_cast<float>(__builtin_bit_cast(T, bits)); }
+  static __device__ __forceinline__ uint16_t bits(float x) { return __builtin_bit_cast(uint16_t, static_cast<T>(x)); }
+  static __device__ __forceinline__ void unpack(const Raw& w, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      x[2 * i] = value(static_cast<uint16_t>(w[i] & 0xffffu));
+      x[2 * i + 1] = value(static_cast<uint16_t>(w[i] >> 16));
+    }
+  }
+  static __device__ __forceinline__ float load_one(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return value(static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0)));
+  }
+  static __device__ __forceinline__ f32x4_t load_four(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    const u32x2_t w = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
+    return f32x4_t{value(w[0] & 0xffffu), value(w[0] >> 16), value(w[1] & 0xffffu), value(w[1] >> 16)};
+  }
+  static __device__ __forceinline__ void store_one(__amdgpu_buffer_rsrc_t r, uint32_t off, float x) {
+    __builtin_amdgcn_raw_buffer_store_b16(bits(x), r, off, 0, 0);
+  }
+  static __device__ __forceinline__ void store_four(__amdgpu_buffer_rsrc_t r, uint32_t off, f32x4_t x) {
+    u32x2_t w;
+    w[0] = bits(x[0]) | (static_cast<uint32_t>(bits(x[1])) << 16);
+    w[1] = bits(x[2]) | (static_cast<uint32_t>(bits(x[3])) << 16);
+    __builtin_amdgcn_raw_buffer_store_b64(w, r, off, 0, 0);
+  }
+};
+struct Bf16 : Half<__bf16> {
+  static constexpr int kPieces = 1;
+  static __device__ __forceinline__ Pieces<1> pieces(const Raw& w) {
+    Pieces<1> r;
+    r.p[0] = __builtin_bit_cast(bf16x8_t, w);
+    return r;
+  }
+};
+struct F16 : Half<_Float16> {  // 11 significant bits: two pieces
+  static constexpr int kPieces = 2;
+  static __device__ __forceinline__ Pieces<2> pieces(const Raw& w) {
+    float x[8];
+    unpack(w, x);
+    const Pieces<3> c = cut(x);
+    Pieces<2> r;
+    r.p[0] = c.p[0];
+    r.p[1] = c.p[1];
+    return r;
+  }
+};
+
+// ---- arguments --------------------------------------------------------------------------------------------------
+
+struct Args {
+  const unsigned char* Q;
+  const unsigned char* K;
+  const unsigned char* V;
+  const unsigned char* dO;
+  const float* g;
+  const float* beta;
+  const uint8_t* mask;          // [B,N] or nullptr
+  unsigned char* O;             // nullptr: states only
+  unsigned char* dQ;
+  unsigned char* dK;
+  unsigned char* dV;
+  float* dg;
+  float* dbeta;
+  const float* initial_state;   // [B*H][D][D] or nullptr
+  float* final_state;
+  const float* dfinal_state;
+  float* dinitial_state;
+  float* states;                // [slice][chunk][D][D]: the state before every chunk, or nullptr
+  float* rows_u;                // [slice][chunk * 32][D]: U, or nullptr
+  float* dstates;               // [slice][chunk][D][D]: the gradient of the state after every chunk (backward)
+  float* rows_z;                // [slice][chunk * 32][D]: Z (backward)
+  int H, N, chunks;
+  long long stride_batch, stride_head;  // of the tensors, in bytes
+  uint32_t stride_row;
+  long long gate_batch, gate_head;      // of g and beta, in elements
+  int gate_row;
+  float scale, eps;
+};
+
+// What a wave knows of its slice.
+struct Slice {
+  long long rows;       // byte offset of row 0 in Q, K, V, O ...
+  long long gates;      // element offset of token 0 in g, beta ...
+  const uint8_t* mask;  // of the sequence, or nullptr
+  uint32_t bytes;       // from row 0 to the end of row N-1
+  int index;
+  __device__ __forceinline__ Slice(const Args& a, int slice, uint32_t row_bytes) {
+    const int b = slice / a.H, h = slice - b * a.H;
+    rows = b * a.stride_batch + h * a.stride_head;
+    gates = b * a.gate_batch + h * a.gate_head;
+    mask = a.mask == nullptr ? nullptr : a.mask + static_cast<long long>(b) * a.N;
+    bytes = static_cast<uint32_t>(a.N - 1) * a.stride_row + row_bytes;
+    index = slice;
+  }
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t of(const unsigned char* base) const {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base) + rows, 0, bytes, 0x00020000);
+  }
+};
+
+// Bit t: token 32 * chunk + t exists and is not masked.  `fetch` brings the byte, `live_of` makes the bits of it.
+__device__ __forceinline__ int fetch_live(const Slice& s, int N, int chunk, int lane) {
+  const int t = kChunk * chunk + (lane & 31);
+  if (t >= N) return 0;
+  return s.mask == nullptr ? 1 : s.mask[t];
+}
+__device__ __forceinline__ uint32_t live_of(int byte) { return static_cast<uint32_t>(__ballot(byte != 0)); }
+
+// Bit t: token 32 * chunk + t exists.
+__device__ __forceinline__ uint32_t existing(int N, int chunk) {
+  const int left = N - kChunk * chunk;
+  return left >= kChunk ? ~0u : (1u << left) - 1u;
+}
+
+// ---- decays -----------------------------------------------------------------------------------------------------
+
+// 2^x of a difference of sums: the fraction goes through the hardware's 2^x, the whole part into the exponent.
+__device__ __forceinline__ float pow2(double x) {
+  const double n = __builtin_rint(x);
+  return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(static_cast<float>(x - n)),
+                                 static_cast<int>(n < -100000.0 ? -100000.0 : n > 100000.0 ? 100000.0 : n));
+}
+
+// Inclusive sums of g * log2(e) over the chunk's 32 tokens, the same in both halves of the wave (lane & 31 is the token).
+// A decay to nothing (g = -inf) counts as 2^-100000: fp32 knows no difference, and later differences stay numbers.
+__device__ __forceinline__ double scan_decays(float g, bool live, int lane) {
+  double x = live ? static_cast<double>(g) * 1.4426950408889634 : 0.0;
+  x = x < -100000.0 ? -100000.0 : x;
+#pragma unroll
+  for (int d = 1; d < 32; d <<= 1) {
+    const double y = __shfl_up(x, d, 32);
+    if ((lane & 31) >= d) x += y;
+  }
+  return x;
+}
+
+// ---- rows in LDS ------------------------------------------------------------------------------------------------
+//
+// 32 rows of a chunk, a plane per piece.  A lane of a product holds, of a block of 32 columns, the columns 4g .. 4g+3
+// and 16+4g .. 16+4g+3 (g = lane / 16): the rows of two 16-row result tiles that it holds, so a result is fed back as an
+// operand without moving between lanes.  Rows are kept in that order ("slots"): the operand is one 16-byte read.
+
+template <int D, int P>
+struct Rows {
+  static constexpr int kWidth = D < 32 ? 32 : D;          // (narrow rows are followed by zeros)
+  static constexpr int kBlocks = kWidth / 32;
+  static constexpr int kStride = kWidth * 2 + 16;         // bytes; the padding keeps 16-byte accesses free of conflicts
+  static constexpr int kPlane = kChunk * kStride;
+  static constexpr int kBytes = P * kPlane;
+
+  // columns 32 kb + 8 g .. + 7 of a row, as loads in natural order bring them
+  static __device__ __forceinline__ void put(unsigned char* at, int row, int kb, int g, const Pieces<P>& x) {
+    const int slot = (g & 1) * 32 + (g >> 1) * 8;  // bytes: columns 8g .. 8g+3 (8g+4 .. +7: 16 bytes on)
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const u32x4_t w = __builtin_bit_cast(u32x4_t, x.p[i]);
+      unsigned char* p = at + i * kPlane + row * kStride + kb * 64 + slot;
+      *reinterpret_cast<u32x2_t*>(p) = u32x2_t{w[0], w[1]};
+      *reinterpret_cast<u32x2_t*>(p + 16) = u32x2_t{w[2], w[3]};
+    }
+  }
+  // operand: row 16 tt + lane%16, depth = the columns of block kb
+  static __device__ __forceinline__ Pieces<P> row_operand(const unsigned char* at, int tt, int kb, int lane) {
+    Pieces<P> r;
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      r.p[i] = *reinterpret_cast<const bf16x8_t*>(at + i * kPlane + (16 * tt + (lane & 15)) * kStride + kb * 64 + (lane >> 4) * 16);
+    return r;
+  }
+  // operand: column 16 dt + lane%16, depth = the 32 tokens (in the slot order of a pair of result tiles)
+  static __device__ __forceinline__ Pieces<P> column_operand(const unsigned char* at, int dt, int lane) {
+    typedef bf16x4_t __attribute__((address_space(3))) * lds_v4;
+    const int s = lane & 15, g = lane >> 4;
+    const unsigned char* p = at + (4 * g + (s >> 2)) * kStride + (dt >> 1) * 64 + (s & 3) * 16 + (dt & 1) * 8;
+    Pieces<P> r;
+#pragma unroll
+    for (int i = 0; i < P; ++i) {
+      const bf16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_v4)(p + i * kPlane));
+      const bf16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_v4)(p + i * kPlane + 16 * kStride));
+      r.p[i] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    }
+    return r;
+  }
+};
+
+// A 32 x 32 triangular operand in LDS in the order the products read it: [tile][piece][lane] 16 bytes.
+constexpr int kTriangleBytes = 2 * 3 * 64 * 16;
+__device__ __forceinline__ void put_triangle(unsigned char* at, int tile, int lane, f32x4_t lo, f32x4_t hi) {
+  const Pieces<3> x = cut(lo, hi);
+#pragma unroll
+  for (int i = 0; i < 3; ++i) *reinterpret_cast<bf16x8_t*>(at + ((tile * 3 + i) * 64 + lane) * 16) = x.p[i];
+}
+__device__ __forceinline__ Pieces<3> triangle_operand(const unsigned char* at, int tile, int lane) {
+  Pieces<3> r;
+#pragma unroll
+  for (int i = 0; i < 3; ++i) r.p[i] = *reinterpret_cast<const bf16x8_t*>(at + ((tile * 3 + i) * 64 + lane) * 16);
+  return r;
+}
+
+// ---- what the producers read and make -----------------------------------------------------------------------------
+
+// The 32 rows of a chunk of Q or K straight in the layout of the products (columns in natural order).
+template <class E, int D>
+struct RowTile {
+  static constexpr int kBlocks = Rows<D, E::kPieces>::kBlocks;
+  typename E::Raw raw[2][kBlocks];
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t stride, int chunk, uint32_t live, int lane) {
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      const int row = 16 * tt + (lane & 15);
+      const uint32_t off = static_cast<uint32_t>(kChunk * chunk + row) * stride + (lane >> 4) * 8 * E::kBytes;
+#pragma unroll
+      for (int kb = 0; kb < kBlocks; ++kb) {
+        const bool there = ((live >> row) & 1u) != 0 && (D >= 32 || (lane >> 4) * 8 < D);
+        raw[tt][kb] = E::load(r, there ? off + kb * 32 * E::kBytes : kNowhere);
+      }
+    }
+  }
+  // 1 / sqrt(sum of squares + eps) of row 16 tt + lane%16, the same in the four lanes that share it; 0 for a row that was
+  // not loaded (whatever eps is: its products are zeros and stay zeros)
+  __device__ __forceinline__ float inverse_norm(int tt, float eps, uint32_t live, int lane) const {
+    float ss = 0.0f;
+#pragma unroll
+    for (int kb = 0; kb < kBlocks; ++kb) {
+      float x[8];
+      E::unpack(raw[tt][kb], x);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+    }
+    ss += __shfl_xor(ss, 16);
+    ss += __shfl_xor(ss, 32);
+    return ((live >> (16 * tt + (lane & 15))) & 1u) ? __builtin_amdgcn_rsqf(ss + eps) : 0.0f;
+  }
+  __device__ __forceinline__ Pieces<E::kPieces> operand(int tt, int kb) const { return E::pieces(raw[tt][kb]); }
+  __device__ __forceinline__ void put(unsigned char* at, int lane) const {
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+      for (int kb = 0; kb < kBlocks; ++kb)
+        Rows<D, E::kPieces>::put(at, 16 * tt + (lane & 15), kb, lane >> 4, operand(tt, kb));
+  }
+};
+
+// Result rows 4g .. 4g+3 = rows of X tile `a`, result column lane%16 = row of Y tile `b`: X_a Y_b^T.
+template <class E, int D>
+__device__ __forceinline__ f32x4_t dots(const RowTile<E, D>& X, int a, const RowTile<E, D>& Y, int b) {
+  f32x4_t c = {0, 0, 0, 0};
+#pragma unroll
+  for (int kb = 0; kb < RowTile<E, D>::kBlocks; ++kb) c = mul(X.operand(a, kb), Y.operand(b, kb), c);
+  return c;
+}
+
+// The producers' own notes of a chunk: sums of decays and 1/r of the keys by token.
+struct Notes {
+  double G[kChunk];
+  float rk[kChunk];
+  float beta[kChunk];
+};
+
+constexpr int kSquareStride = 20;                    // floats per row of a 16 x 16 square (80 bytes: free of conflicts)
+constexpr int kSquare = 16 * kSquareStride;
+struct Scratch {  // of the wave that solves
+  Notes notes;
+  float a[2][kSquare];  // diagonal blocks of diag(beta) N, transposed
+  float t[2][kSquare];  // diagonal blocks of T
+};
+
+// T = (I + A)^-1 for A = [[A0, 0], [A10, A1]], strictly lower: the diagonal blocks by substitution (as stable as solving
+// token by token; powers of A would lose digits where keys repeat), and T10 = -T1 A10 T0.  `d0`, `d1`: A0 and A1 as
+// results (row 4g + r, column lane%16).  In LDS afterwards: the rows of T0 and T1.
+__device__ __forceinline__ void solve_blocks(Scratch* s, f32x4_t d0, f32x4_t d1, int lane) {
+  const int c = lane & 15, g = lane >> 4;
+  *reinterpret_cast<f32x4_t*>(&s->a[0][c * kSquareStride + 4 * g]) = d0;
+  *reinterpret_cast<f32x4_t*>(&s->a[1][c * kSquareStride + 4 * g]) = d1;
+  wave_fence();
+  // row i = lane%16 of T of block (lane / 16) % 2: t_j = [i = j] - sum_{m > j} t_m A_mj
+  const float* A = s->a[g & 1];
+  float t[16];
+#pragma unroll
+  for (int j = 15; j >= 0; --j) {
+    float x = c == j ? 1.0f : 0.0f;
+#pragma unroll
+    for (int q = 3; q >= 0; --q) {
+      if (4 * q + 3 <= j) continue;
+      const f32x4_t w = *reinterpret_cast<const f32x4_t*>(&A[j * kSquareStride + 4 * q]);
+#pragma unroll
+      for (int e = 3; e >= 0; --e)
+        if (4 * q + e > j) x = fmaf(-t[4 * q + e], w[e], x);
+    }
+    t[j] = x;
+  }
+  if (lane < 32) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<f32x4_t*>(&s->t[g][c * kSquareStride + 4 * q]) = f32x4_t{t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
+  }
+  wave_fence();
+}
+__device__ __forceinline__ f32x4_t square_row(const float* m, int lane) {  // row lane%16, columns 4g .. 4g+3
+  return *reinterpret_cast<const f32x4_t*>(&m[(lane & 15) * kSquareStride + 4 * (lane >> 4)]);
+}
+__device__ __forceinline__ f32x4_t square_column(const float* m, int lane) {  // column lane%16, rows 4g .. 4g+3
+  f32x4_t r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = m[(4 * (lane >> 4) + i) * kSquareStride + (lane & 15)];
+  return r;
+}
+// A 16 x 16 product in fp32 over a depth of 16: lane holds row (column) lane%16 at depths 4g .. 4g+3
+__device__ __forceinline__ f32x4_t square_product(f32x4_t a, f32x4_t b) {
+  f32x4_t c = {0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) c = mfma(a[i], b[i], c);
+  return c;
+}
+
+}  // namespace delta
+}  // namespace cotten
