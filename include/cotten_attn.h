@@ -301,6 +301,40 @@ int cotten_delta_bwd(const void* Q, const void* K, const void* V, const float* g
 size_t cotten_delta_kept_bytes(int B, int H, int N, int d_h, int dtype);
 size_t cotten_delta_workspace_bytes(int B, int H, int N, int d_h, int dtype, int is_bwd, int with_kept);
 
+/* ---- Embedding of item ids -------------------------------------------------------------------
+ *
+ * The input of the layers (Cotten4Rec, "Model Description": E_t = s_t + P_t), with a factor:
+ *
+ *     E[b,n] = scale * W[ids[b,n]] + P[position_offset + n]
+ *     dW[i]  = scale * sum of dE[b,n] over the tokens with ids[b,n] = i, in the order of the tokens
+ *     dP[position_offset + n] = sum_b dE[b,n]
+ *
+ * W is [V, D], P [positions, D] (or NULL: none), E and dE [B, N, D], contiguous, all of one element type;
+ * ids [B, N], int32 or int64.  A token with padding_idx, or with an id outside 0 ... V-1, has no row:
+ * its E is its position's alone, and it gives dW nothing.  Sums are fp32, rounded once.  dW and dP are
+ * dense and written whole, zeros included.  The same arguments give the same bits.
+ *
+ * dW needs a workspace of cotten_embed_workspace_bytes() bytes (lists of the tokens sorted by id, and partial
+ * sums).  Calls enqueue on `stream` only and allocate nothing. */
+typedef struct cotten_embed_params {
+  int dtype;            /* a cotten_dtype: of W, P, E and their gradients                        */
+  int id_bytes;         /* 4 or 8                                                                */
+  float scale;          /* as it is (finite)                                                     */
+  int padding_idx;      /* -1: none                                                              */
+  int positions;        /* rows of P; position_offset + N at most                                */
+  int position_offset;
+  void* workspace;      /* backward with dW: 16-byte aligned device buffer                       */
+  size_t workspace_bytes;
+} cotten_embed_params;
+
+int cotten_embed_fwd(const void* ids, const void* W, const void* P, void* E, int B, int N, int D, int V,
+                     void* stream, const cotten_embed_params* params);
+/* dW or dP may be NULL, not both. */
+int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B, int N, int D, int V,
+                     void* stream, const cotten_embed_params* params);
+/* 0 for invalid arguments; host only. */
+size_t cotten_embed_workspace_bytes(int B, int N, int D, int V);
+
 #ifdef __cplusplus
 }
 #endif

@@ -78,3 +78,33 @@ def gated_delta_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: 
     backward."""
     O, state = _GatedDelta.apply(Q, K, V, g, beta, mask, scale, eps, initial_state, layout)
     return (O, state) if return_state else O
+
+
+class _ItemEmbedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, ids, W, positions, scale, padding_idx, position_offset):
+        ctx.save_for_backward(ids)
+        ctx.scale, ctx.padding_idx, ctx.position_offset = scale, padding_idx, position_offset
+        ctx.rows = W.shape[0]
+        ctx.positions = None if positions is None else positions.shape
+        return binding.cotten_embed_fwd(ids, W, positions, scale=scale, padding_idx=padding_idx,
+                                        position_offset=position_offset)
+
+    @staticmethod
+    def backward(ctx, dE):
+        ids, = ctx.saved_tensors
+        dP = None
+        if ctx.positions is not None and ctx.needs_input_grad[2]:
+            dP = torch.empty(ctx.positions, device=dE.device, dtype=dE.dtype)
+        elif not ctx.needs_input_grad[1]:
+            return None, None, None, None, None, None
+        dW = binding.cotten_embed_bwd(ids, dE.contiguous(), ctx.rows, dP=dP, scale=ctx.scale,
+                                      padding_idx=ctx.padding_idx, position_offset=ctx.position_offset)
+        return None, dW, dP, None, None, None
+
+
+def item_embedding(ids: torch.Tensor, W: torch.Tensor, positions: Optional[torch.Tensor] = None, *,
+                   scale: float = 1.0, padding_idx: Optional[int] = None, position_offset: int = 0) -> torch.Tensor:
+    """scale * W[ids] + positions[position_offset + n] (see `binding.cotten_embed_fwd`), differentiable in W and the
+    positions; both gradients are dense."""
+    return _ItemEmbedding.apply(ids, W, positions, scale, padding_idx, position_offset)

@@ -36,6 +36,7 @@ EXPORTS = (
     "cotten_normaliser_fwd", "cotten_normaliser_bwd", "cotten_attn_bwd_static",
     "cotten_attn_workspace_bytes_ex",
     "cotten_delta_fwd", "cotten_delta_bwd", "cotten_delta_kept_bytes", "cotten_delta_workspace_bytes",
+    "cotten_embed_fwd", "cotten_embed_bwd", "cotten_embed_workspace_bytes",
 )
 
 
@@ -53,6 +54,12 @@ class CottenDeltaParams(ctypes.Structure):
                 ("initial_state", ctypes.c_void_p), ("final_state", ctypes.c_void_p),
                 ("dfinal_state", ctypes.c_void_p), ("dinitial_state", ctypes.c_void_p),
                 ("kept", ctypes.c_void_p), ("kept_bytes", ctypes.c_size_t)]
+
+
+class CottenEmbedParams(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("id_bytes", ctypes.c_int), ("scale", ctypes.c_float),
+                ("padding_idx", ctypes.c_int), ("positions", ctypes.c_int), ("position_offset", ctypes.c_int),
+                ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
 
 
 class CottenError(RuntimeError):
@@ -97,6 +104,11 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.cotten_delta_kept_bytes.argtypes = [ip] * 5
     lib.cotten_delta_workspace_bytes.argtypes = [ip] * 7
     lib.cotten_delta_kept_bytes.restype = lib.cotten_delta_workspace_bytes.restype = ctypes.c_size_t
+    lib.cotten_embed_fwd.argtypes = lib.cotten_embed_bwd.argtypes = \
+        [vp] * 4 + [ip] * 4 + [vp, ctypes.POINTER(CottenEmbedParams)]
+    lib.cotten_embed_fwd.restype = lib.cotten_embed_bwd.restype = ctypes.c_int
+    lib.cotten_embed_workspace_bytes.argtypes = [ip] * 4
+    lib.cotten_embed_workspace_bytes.restype = ctypes.c_size_t
     lib.cotten_status_string.argtypes = [ip]
     lib.cotten_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -476,3 +488,83 @@ def cotten_delta_bwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch
                beta.data_ptr(), _mask_ptr(mask, dims[0], dims[2], Q.device), dO.data_ptr(), dQ.data_ptr(),
                dK.data_ptr(), dV.data_ptr(), dg.data_ptr(), dbeta.data_ptr(), *dims, handle, ctypes.byref(prm))
     return dQ, dK, dV, dg, dbeta
+
+
+# ---- embedding of item ids -----------------------------------------------------------------------
+
+@functools.lru_cache(maxsize=1024)
+def cotten_embed_workspace_bytes(B: int, N: int, D: int, V: int) -> int:
+    return int(load_library().cotten_embed_workspace_bytes(B, N, D, V))
+
+
+_ID_BYTES = {torch.int32: 4, torch.int64: 8}
+
+
+def _embed_params(ids: torch.Tensor, like: torch.Tensor, scale: float, padding_idx: Optional[int], positions: int,
+                  position_offset: int, workspace: Optional[torch.Tensor] = None) -> CottenEmbedParams:
+    if ids.dim() != 2 or ids.dtype not in _ID_BYTES or not ids.is_contiguous() or ids.device != like.device:
+        raise ValueError("ids must be a contiguous int32 or int64 [B,N] tensor on the same device")
+    if padding_idx is not None and padding_idx < 0:
+        raise ValueError("padding_idx must be None or an id, counted from 0")
+    space, space_bytes = _buffer("workspace", workspace, like.device)
+    return CottenEmbedParams(_dtype_code(like), _ID_BYTES[ids.dtype], float(scale),
+                             -1 if padding_idx is None else int(padding_idx), positions, int(position_offset),
+                             space, space_bytes)
+
+
+def _table(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None, dims: int = 2) -> torch.Tensor:
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor (there is no CPU path)")
+    if t.dim() != dims or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dims}-d tensor")
+    if like is not None and (t.dtype is not like.dtype or t.device != like.device or t.shape[-1] != like.shape[-1]):
+        raise ValueError(f"{name} must match the other tensors in width, dtype and device")
+    return t
+
+
+def cotten_embed_fwd(ids: torch.Tensor, W: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                     E: Optional[torch.Tensor] = None, *, scale: float = 1.0, padding_idx: Optional[int] = None,
+                     position_offset: int = 0, stream=None) -> torch.Tensor:
+    """E[b,n] = scale * W[ids[b,n]] + positions[position_offset + n]; enqueues on the stream and returns E [B,N,D].
+    `ids` int32 or int64 [B,N]; a token with `padding_idx`, or an id that W has no row for, gets no row of W."""
+    lib = _lib or load_library()
+    _table("W", W)
+    if positions is not None:
+        _table("positions", positions, W)
+    prm = _embed_params(ids, W, scale, padding_idx, 0 if positions is None else positions.shape[0], position_offset)
+    (B, N), (V, D) = ids.shape, W.shape
+    if E is None:
+        E = torch.empty(B, N, D, device=W.device, dtype=W.dtype)
+    elif _table("E", E, W, 3).shape != (B, N, D):
+        raise ValueError("E must be [B,N,D]")
+    _on_device(W.device, lib.cotten_embed_fwd, ids.data_ptr(), W.data_ptr(),
+               None if positions is None else positions.data_ptr(), E.data_ptr(), B, N, D, V, _stream_handle(stream),
+               ctypes.byref(prm))
+    return E
+
+
+def cotten_embed_bwd(ids: torch.Tensor, dE: torch.Tensor, V: int, dW: Optional[torch.Tensor] = None,
+                     dP: Optional[torch.Tensor] = None, *, scale: float = 1.0, padding_idx: Optional[int] = None,
+                     position_offset: int = 0, stream=None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The gradient dW [V,D] of the table (written whole) for the upstream gradient dE; `dP`, the shape of the table of
+    positions, receives its gradient when given."""
+    lib = _lib or load_library()
+    _table("dE", dE, None, 3)
+    B, N, D = dE.shape
+    if ids.shape != (B, N):
+        raise ValueError("ids must be [B,N] and dE [B,N,D]")
+    if dW is None:
+        dW = torch.empty(V, D, device=dE.device, dtype=dE.dtype)
+    elif _table("dW", dW, dE).shape[0] != V:
+        raise ValueError("dW must be [V,D]")
+    if dP is not None:
+        _table("dP", dP, dE)
+    handle = _stream_handle(stream)
+    if workspace is None:
+        need = cotten_embed_workspace_bytes(B, N, D, V)
+        if need != 0:
+            workspace = _workspace(dE, need, handle)
+    prm = _embed_params(ids, dE, scale, padding_idx, 0 if dP is None else dP.shape[0], position_offset, workspace)
+    _on_device(dE.device, lib.cotten_embed_bwd, ids.data_ptr(), dE.data_ptr(), dW.data_ptr(),
+               None if dP is None else dP.data_ptr(), B, N, D, V, handle, ctypes.byref(prm))
+    return dW

@@ -1,0 +1,638 @@
+// Embedding of item ids, E[b,n] = scale * W[id] + P[offset + n], and its gradient:
+//
+//     dW[i] = scale * sum over the tokens with id i of dE (in the order of the tokens)      dP[offset + n] = sum_b dE[b,n]
+//
+// Everything here moves memory.  The gradient of the table sorts the tokens by id (stable, so a row's sum has one order
+// and a call one result) and sums the sorted rows in units of a few tokens, whatever ids they have: a popular item is
+// many units, a rare one a part of one, and no workgroup waits for the most popular item.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include <cmath>
+
+#include "../../include/cotten_attn.h"
+
+namespace cotten {
+namespace embed {
+namespace {
+
+typedef uint32_t u32x2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+
+// ---- VEC elements of a row ------------------------------------------------------------------------------------------
+
+template <int BYTES>
+struct Word;
+template <>
+struct Word<2> { typedef uint16_t type; };
+template <>
+struct Word<4> { typedef uint32_t type; };
+template <>
+struct Word<8> { typedef u32x2_t type; };
+template <>
+struct Word<16> { typedef u32x4_t type; };
+
+template <class T, int VEC>
+struct Vec {
+  typedef typename Word<sizeof(T) * VEC>::type word;
+  typedef T elems __attribute__((ext_vector_type(VEC)));
+  static __device__ __forceinline__ void load(const T* p, float (&x)[VEC]) {
+    const word w = *reinterpret_cast<const word*>(p);
+    if constexpr (VEC == 1) {
+      x[0] = static_cast<float>(__builtin_bit_cast(T, w));
+    } else {
+      const elems e = __builtin_bit_cast(elems, w);
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) x[i] = static_cast<float>(e[i]);
+    }
+  }
+  static __device__ __forceinline__ void store(T* p, const float (&x)[VEC]) {
+    if constexpr (VEC == 1) {
+      *reinterpret_cast<word*>(p) = __builtin_bit_cast(word, static_cast<T>(x[0]));
+    } else {
+      elems e;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) e[i] = static_cast<T>(x[i]);
+      *reinterpret_cast<word*>(p) = __builtin_bit_cast(word, e);
+    }
+  }
+};
+
+struct Ids {
+  const void* ids;
+  int wide;       // int64
+  int V, padding; // rows of the table; the id that stands for no item (-1: none)
+  // the id, or V for a token without a row: padding, or outside the table
+  __device__ __forceinline__ uint32_t row(long long i) const {
+    const long long id = wide ? static_cast<const long long*>(ids)[i] : static_cast<const int*>(ids)[i];
+    return id >= 0 && id < V && id != padding ? static_cast<uint32_t>(id) : static_cast<uint32_t>(V);
+  }
+};
+
+// ---- forward ----------------------------------------------------------------------------------------------------------
+
+constexpr int kThreads = 256;
+constexpr int kUnroll = 4;  // pieces of a thread: their ids, then their rows, are on the way together
+
+// A piece is VEC elements; pieces are numbered through the rows of a workgroup's tokens.
+template <class T, int VEC>
+__global__ __launch_bounds__(kThreads) void lookup_kernel(Ids ids, const T* __restrict__ W, const T* __restrict__ P,
+                                                          T* __restrict__ E, long long tokens, int N, int D, int pieces,
+                                                          int block_tokens, int offset, float scale) {
+  const long long first = static_cast<long long>(blockIdx.x) * block_tokens;
+  const int rows = static_cast<int>(tokens - first < block_tokens ? tokens - first : block_tokens);
+  const uint32_t end = static_cast<uint32_t>(rows) * pieces;
+  for (uint32_t at = threadIdx.x; at < end; at += kThreads * kUnroll) {
+    uint32_t row[kUnroll], col[kUnroll], id[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const uint32_t i = at + u * kThreads;
+      row[u] = i / pieces;
+      col[u] = (i - row[u] * pieces) * VEC;
+      id[u] = i < end ? ids.row(first + row[u]) : ids.V;
+    }
+    float x[kUnroll][VEC];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (id[u] < static_cast<uint32_t>(ids.V)) {
+        Vec<T, VEC>::load(W + static_cast<long long>(id[u]) * D + col[u], x[u]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) x[u][e] = 0.0f;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      if (at + u * kThreads >= end) break;
+      const long long token = first + row[u];
+      float p[VEC] = {};
+      if (P != nullptr) Vec<T, VEC>::load(P + (offset + token % N) * D + col[u], p);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) x[u][e] = id[u] < static_cast<uint32_t>(ids.V) ? fmaf(scale, x[u][e], p[e]) : p[e];
+      Vec<T, VEC>::store(E + token * D + col[u], x[u]);
+    }
+  }
+}
+
+// ---- sorting tokens by id ------------------------------------------------------------------------------------------------
+//
+// Least significant digits first, up to 9 bits each (two passes for tables of up to 2^18 rows).  A pass: counts of every
+// digit in every block, their sums over the blocks before, and the move, which keeps the order of equal digits: a wave
+// takes 64 tokens at a time in order, and a token's place among those with its digit is a count of lanes.
+
+constexpr int kDigits = 512;
+constexpr int kStrips = 8;                                       // of 64 tokens, per wave of the sort's blocks
+constexpr int kBlockTokens = (kThreads / 64) * kStrips * 64;
+constexpr int kSoloWaves = 16;                                   // one workgroup sorts up to ...
+constexpr int kSoloTokens = kSoloWaves * kStrips * 64;           // ... this many tokens, all passes in one launch
+
+struct Sort {
+  Ids ids;
+  const uint32_t* keys;    // of the pass before; nullptr: the ids
+  const uint32_t* tokens;
+  uint32_t* keys_out;
+  uint32_t* tokens_out;
+  uint32_t* counts;        // [digit][block], then (after the sums) tokens of that digit in the blocks before
+  uint32_t* totals;        // [digit]
+  uint32_t n;
+  int blocks, shift, bits;
+  __device__ __forceinline__ uint32_t key(uint32_t i) const { return keys != nullptr ? keys[i] : ids.row(i); }
+};
+
+__global__ __launch_bounds__(kThreads) void count_kernel(Sort s) {
+  __shared__ uint32_t hist[kDigits];
+  for (int d = threadIdx.x; d < kDigits; d += kThreads) hist[d] = 0;
+  __syncthreads();
+  const uint32_t first = blockIdx.x * kBlockTokens, mask = (1u << s.bits) - 1u;
+#pragma unroll
+  for (int i = 0; i < kBlockTokens / kThreads; ++i) {
+    const uint32_t at = first + i * kThreads + threadIdx.x;
+    if (at < s.n) atomicAdd(&hist[(s.key(at) >> s.shift) & mask], 1u);
+  }
+  __syncthreads();
+  for (uint32_t d = threadIdx.x; d <= mask; d += kThreads) s.counts[static_cast<size_t>(d) * s.blocks + blockIdx.x] = hist[d];
+}
+
+// A wave per digit.
+__global__ __launch_bounds__(kThreads) void sums_kernel(Sort s) {
+  const int lane = threadIdx.x & 63;
+  const uint32_t d = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
+  if (d >= (1u << s.bits)) return;
+  uint32_t* row = s.counts + static_cast<size_t>(d) * s.blocks;
+  uint32_t before = 0;
+  for (int b = 0; b < s.blocks; b += 64) {
+    const uint32_t own = b + lane < s.blocks ? row[b + lane] : 0;
+    uint32_t x = own;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const uint32_t y = __shfl_up(x, m);
+      if (lane >= m) x += y;
+    }
+    if (b + lane < s.blocks) row[b + lane] = before + x - own;
+    before += __shfl(x, 63);
+  }
+  if (lane == 0) s.totals[d] = before;
+}
+
+// Exclusive sums of base[0 ... 511], by 256 or more threads; `part`: a word per wave.
+__device__ __forceinline__ void exclusive_sums(uint32_t* base, uint32_t* part) {
+  const int t = threadIdx.x, lane = t & 63;
+  uint32_t a = 0, b = 0, x = 0;
+  if (t < kDigits / 2) {
+    a = base[2 * t];
+    b = base[2 * t + 1];
+    x = a + b;
+#pragma unroll
+    for (int m = 1; m < 64; m <<= 1) {
+      const uint32_t y = __shfl_up(x, m);
+      if (lane >= m) x += y;
+    }
+    if (lane == 63) part[t >> 6] = x;
+  }
+  __syncthreads();
+  if (t < kDigits / 2) {
+    uint32_t before = x - a - b;
+    for (int w = 0; w < (t >> 6); ++w) before += part[w];
+    base[2 * t] = before;
+    base[2 * t + 1] = before + a;
+  }
+  __syncthreads();
+}
+
+// The tokens first ... first + WAVES * kStrips * 64 - 1 to their places.  place[w][d] counts up from where wave w's next
+// token with digit d goes.  `alone`: there is no other block, base holds nothing yet.
+template <int WAVES>
+__device__ __forceinline__ void move_block(const Sort& s, uint32_t first, uint32_t (*place)[kDigits], uint32_t* base,
+                                           uint32_t* part, bool alone) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t mask = (1u << s.bits) - 1u;
+  for (int i = threadIdx.x; i < WAVES * kDigits; i += WAVES * 64) place[0][i] = 0;
+  __syncthreads();
+  uint32_t key[kStrips], token[kStrips];
+  const uint32_t mine = first + wave * (kStrips * 64) + lane;
+#pragma unroll
+  for (int i = 0; i < kStrips; ++i) {
+    const uint32_t at = mine + 64 * i;
+    key[i] = at < s.n ? s.key(at) : 0;
+    token[i] = at < s.n && s.keys != nullptr ? s.tokens[at] : at;
+  }
+#pragma unroll
+  for (int i = 0; i < kStrips; ++i)
+    if (mine + 64 * i < s.n) atomicAdd(&place[wave][(key[i] >> s.shift) & mask], 1u);
+  if (!alone)
+    for (uint32_t d = threadIdx.x; d < kDigits; d += WAVES * 64) base[d] = d <= mask ? s.totals[d] : 0;
+  __syncthreads();
+  if (alone) {
+    for (int d = threadIdx.x; d < kDigits; d += WAVES * 64) {
+      uint32_t x = 0;
+      for (int w = 0; w < WAVES; ++w) x += place[w][d];
+      base[d] = x;
+    }
+    __syncthreads();
+  }
+  exclusive_sums(base, part);
+  for (uint32_t d = threadIdx.x; d <= mask; d += WAVES * 64) {
+    uint32_t at = base[d] + (alone ? 0 : s.counts[static_cast<size_t>(d) * s.blocks + blockIdx.x]);
+    for (int w = 0; w < WAVES; ++w) {
+      const uint32_t x = place[w][d];
+      place[w][d] = at;
+      at += x;
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kStrips; ++i) {
+    const bool on = mine + 64 * i < s.n;
+    const uint32_t d = (key[i] >> s.shift) & mask;
+    uint64_t same = __ballot(on);
+    for (int b = 0; b < s.bits; ++b) {
+      const uint64_t set = __ballot((d >> b) & 1u);
+      same &= ((d >> b) & 1u) ? set : ~set;
+    }
+    const int rank = __popcll(same & ((1ull << lane) - 1ull));
+    uint32_t to = 0;
+    if (on) to = place[wave][d] + rank;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (on && rank == 0) place[wave][d] = to + __popcll(same);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    if (on) {
+      s.keys_out[to] = key[i];
+      s.tokens_out[to] = token[i];
+    }
+  }
+}
+
+__global__ __launch_bounds__(kThreads) void move_kernel(Sort s) {
+  __shared__ uint32_t place[kThreads / 64][kDigits], base[kDigits], part[kThreads / 64];
+  move_block<kThreads / 64>(s, blockIdx.x * kBlockTokens, place, base, part, false);
+}
+
+// All passes of up to kSoloTokens tokens.
+__global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(Sort s, int passes, int digit_bits, int key_bits, uint32_t* other_keys,
+                                                               uint32_t* other_tokens) {
+  __shared__ uint32_t place[kSoloWaves][kDigits], base[kDigits], part[kSoloWaves];
+  for (int p = 0; p < passes; ++p) {
+    s.shift = p * digit_bits;
+    s.bits = key_bits - s.shift < digit_bits ? key_bits - s.shift : digit_bits;
+    move_block<kSoloWaves>(s, 0, place, base, part, true);
+    uint32_t *keys = s.keys_out, *tokens = s.tokens_out;
+    s.keys = keys;
+    s.tokens = tokens;
+    s.keys_out = other_keys;
+    s.tokens_out = other_tokens;
+    other_keys = keys;
+    other_tokens = tokens;
+    __threadfence_block();
+    __syncthreads();
+  }
+}
+
+// ---- sums of sorted rows -------------------------------------------------------------------------------------------------
+//
+// A unit is kUnit consecutive sorted tokens; lanes of a power of two take its columns.  A row whose tokens all lie in one
+// unit is written at once.  One that goes on leaves its sum so far: of the unit that it starts in as the tail, of the
+// units after that as their head; join_kernel adds these in order.
+
+constexpr int kUnit = 16;
+
+struct Rows {
+  const uint32_t* keys;
+  const uint32_t* tokens;
+  uint32_t n;
+  int V, D, lanes;          // lanes: of a row, a power of two
+  uint32_t units;
+  float* heads;             // [unit][D]
+  float* tails;
+  float scale;
+};
+
+template <class T, int VEC>
+__global__ __launch_bounds__(kThreads) void zero_kernel(T* to, size_t elements) {
+  size_t i = (static_cast<size_t>(blockIdx.x) * kThreads * kUnroll + threadIdx.x) * VEC;
+  const float x[VEC] = {};
+#pragma unroll
+  for (int u = 0; u < kUnroll; ++u, i += static_cast<size_t>(kThreads) * VEC)
+    if (i < elements) Vec<T, VEC>::store(to + i, x);
+}
+
+template <class T, int VEC>
+__global__ __launch_bounds__(kThreads) void sum_kernel(Rows s, const T* __restrict__ dE, T* __restrict__ dW) {
+  const uint32_t unit = blockIdx.x * (kThreads / s.lanes) + threadIdx.x / s.lanes;
+  const int col = (blockIdx.y * s.lanes + threadIdx.x % s.lanes) * VEC;
+  if (unit >= s.units || col >= s.D) return;
+  const uint32_t first = unit * kUnit, end = first + kUnit < s.n ? first + kUnit : s.n;
+  const uint32_t V = s.V;
+  uint32_t key[kUnit + 1], token[kUnit];
+#pragma unroll
+  for (int i = 0; i < kUnit; ++i) {
+    key[i] = first + i < end ? s.keys[first + i] : V;
+    token[i] = first + i < end ? s.tokens[first + i] : 0;
+  }
+  key[kUnit] = end < s.n ? s.keys[end] : V;
+  if (key[0] == V) return;  // tokens without a row are the last
+  const uint32_t before = first > 0 ? s.keys[first - 1] : V;
+  bool begun = before != key[0];  // the present row starts in this unit
+  float sum[VEC] = {};
+  constexpr int kAhead = 8;  // rows on the way together
+#pragma unroll
+  for (int half = 0; half < kUnit; half += kAhead) {
+    float x[kAhead][VEC];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      if (key[half + i] != V) {
+        Vec<T, VEC>::load(dE + static_cast<size_t>(token[half + i]) * s.D + col, x[i]);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const uint32_t k = key[half + i], next = key[half + i + 1];
+      if (k == V) continue;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sum[e] += x[i][e];
+      const bool ends = next != k, last = half + i == kUnit - 1;
+      if (!ends && !last) continue;
+      if (ends && begun) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) sum[e] *= s.scale;
+        Vec<T, VEC>::store(dW + static_cast<size_t>(k) * s.D + col, sum);
+      } else {
+        float* to = (begun ? s.tails : s.heads) + static_cast<size_t>(unit) * s.D + col;
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) to[e] = sum[e];
+      }
+      begun = true;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
+    }
+  }
+}
+
+// A workgroup per unit: where a row starts in it and goes on, its tail and the heads of the units that it goes on in.
+template <class T>
+__global__ __launch_bounds__(kThreads) void join_kernel(Rows s, T* __restrict__ dW) {
+  const uint32_t unit = blockIdx.x, first = unit * kUnit, next = first + kUnit;
+  if (next >= s.n) return;
+  const uint32_t key = s.keys[next - 1];
+  if (key == static_cast<uint32_t>(s.V) || s.keys[next] != key) return;                     // nothing goes on
+  if (s.keys[first] == key && first > 0 && s.keys[first - 1] == key) return;                  // it started before
+  const int lane = threadIdx.x & 63;
+  uint32_t heads = 0;
+  for (;;) {  // units whose first token has the key: they follow one another
+    const uint32_t u = unit + 1 + heads + lane;
+    const uint64_t same = __ballot(u < s.units && s.keys[u < s.units ? u * kUnit : 0] == key);
+    const int run = same == ~0ull ? 64 : __ffsll(static_cast<long long>(~same)) - 1;
+    heads += run;
+    if (run < 64) break;
+  }
+  // partial sums 0 (the tail) ... heads, a contiguous share for each group of lanes
+  __shared__ float part[kThreads];
+  const int groups = kThreads / s.lanes, group = threadIdx.x / s.lanes;
+  const uint32_t share = (heads + groups) / groups;
+  for (int c0 = 0; c0 < s.D; c0 += s.lanes) {
+    const int col = c0 + threadIdx.x % s.lanes;
+    float sum = 0.0f;
+    if (col < s.D) {
+      const uint32_t from = group * share, to = from + share < heads + 1 ? from + share : heads + 1;
+#pragma unroll 8
+      for (uint32_t i = from; i < to; ++i)
+        sum += i == 0 ? s.tails[static_cast<size_t>(unit) * s.D + col] : s.heads[static_cast<size_t>(unit + i) * s.D + col];
+    }
+    part[threadIdx.x] = sum;
+    __syncthreads();
+    if (group == 0 && col < s.D) {
+      float x = 0.0f;
+      for (int g = 0; g < groups; ++g) x += part[g * s.lanes + threadIdx.x];
+      dW[static_cast<size_t>(key) * s.D + col] = static_cast<T>(x * s.scale);
+    }
+    __syncthreads();
+  }
+}
+
+// ---- positions ----------------------------------------------------------------------------------------------------------
+
+// dP: a workgroup per row of the table and `lanes` * VEC columns; rows that no token has are zeros.
+template <class T, int VEC>
+__global__ __launch_bounds__(1024) void positions_kernel(const T* __restrict__ dE, T* __restrict__ dP, int B, int N, int D,
+                                                         int offset, int lanes) {
+  __shared__ float part[1024 * VEC];
+  const int groups = 1024 / lanes, group = threadIdx.x / lanes, lane = threadIdx.x % lanes;
+  const int col = (blockIdx.y * lanes + lane) * VEC, n = static_cast<int>(blockIdx.x) - offset;
+  float sum[VEC] = {};
+  if (n >= 0 && n < N && col < D) {
+#pragma unroll 4
+    for (int b = group; b < B; b += groups) {
+      float x[VEC];
+      Vec<T, VEC>::load(dE + (static_cast<size_t>(b) * N + n) * D + col, x);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) sum[e] += x[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) part[e * 1024 + threadIdx.x] = sum[e];
+  __syncthreads();
+  for (int half = groups / 2; half > 0; half /= 2) {
+    if (group < half)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) part[e * 1024 + threadIdx.x] += part[e * 1024 + threadIdx.x + half * lanes];
+    __syncthreads();
+  }
+  if (group == 0 && col < D) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) sum[e] = part[e * 1024 + threadIdx.x];
+    Vec<T, VEC>::store(dP + static_cast<size_t>(blockIdx.x) * D + col, sum);
+  }
+}
+
+// ---- host ----------------------------------------------------------------------------------------------------------------
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+int key_bits(int V) {  // of 0 ... V
+  int bits = 1;
+  while (V >> bits) ++bits;
+  return bits;
+}
+
+// Where things are in the workspace, in 4-byte words.
+struct Layout {
+  uint32_t blocks, units;
+  int passes, digit_bits;
+  size_t list, counts, sums, words;  // list: of each of the four lists
+  Layout(long long n, int D, int V) {
+    blocks = static_cast<uint32_t>((n + kBlockTokens - 1) / kBlockTokens);
+    units = static_cast<uint32_t>((n + kUnit - 1) / kUnit);
+    const int bits = key_bits(V);
+    passes = (bits + 8) / 9;
+    digit_bits = (bits + passes - 1) / passes;
+    list = (static_cast<size_t>(n) + 3) & ~size_t{3};
+    counts = static_cast<size_t>(kDigits) * blocks + kDigits;
+    sums = (static_cast<size_t>(units) * D + 3) & ~size_t{3};
+    words = 4 * list + counts + 2 * sums;
+  }
+};
+
+// The widest pieces that rows consist of.
+int piece_bytes(int D, int elem) {
+  int b = 16;
+  while ((static_cast<long long>(D) * elem) % b) b /= 2;
+  return b;
+}
+int lanes_of(int pieces) {
+  int l = 1;
+  while (l < pieces && l < 64) l *= 2;
+  return l;
+}
+
+// f(Vec<T, VEC> tag) for the pieces of D elements of a type
+template <class T, int VEC>
+struct Tag {
+  typedef T type;
+  static constexpr int vec = VEC;
+};
+template <class T, class F>
+void by_piece(int D, F&& f) {
+  const int vec = piece_bytes(D, sizeof(T)) / static_cast<int>(sizeof(T));
+  if (vec == 8) {
+    if constexpr (sizeof(T) == 2) f(Tag<T, 8>());
+  } else if (vec == 4) {
+    f(Tag<T, 4>());
+  } else if (vec == 2) {
+    f(Tag<T, 2>());
+  } else {
+    f(Tag<T, 1>());
+  }
+}
+template <class F>
+void by_type(int dtype, int D, F&& f) {
+  if (dtype == COTTEN_F32) by_piece<float>(D, f);
+  else if (dtype == COTTEN_BF16) by_piece<__bf16>(D, f);
+  else by_piece<_Float16>(D, f);
+}
+
+int check(const void* ids, int B, int N, int D, int V, const cotten_embed_params* prm, bool positions) {
+  if (prm == nullptr || ids == nullptr) return COTTEN_ERR_NULL_POINTER;
+  if (prm->dtype != COTTEN_F32 && prm->dtype != COTTEN_BF16 && prm->dtype != COTTEN_F16) return COTTEN_ERR_BAD_DTYPE;
+  if (prm->id_bytes != 4 && prm->id_bytes != 8) return COTTEN_ERR_BAD_DTYPE;
+  if (B < 1 || N < 1 || D < 1 || V < 1) return COTTEN_ERR_BAD_SHAPE;
+  if (D > 65536 || static_cast<long long>(B) * N >= (1ll << 31) || V >= (1 << 30)) return COTTEN_ERR_BAD_SHAPE;
+  if (positions && (prm->position_offset < 0 || prm->positions < 1 ||
+                    static_cast<long long>(prm->position_offset) + N > prm->positions))
+    return COTTEN_ERR_BAD_SHAPE;
+  if (!std::isfinite(prm->scale)) return COTTEN_ERR_BAD_PARAM;
+  if (reinterpret_cast<uintptr_t>(ids) & (prm->id_bytes - 1)) return COTTEN_ERR_MISALIGNED;
+  if (!aligned16(prm->workspace)) return COTTEN_ERR_MISALIGNED;
+  return COTTEN_OK;
+}
+
+}  // namespace
+}  // namespace embed
+}  // namespace cotten
+
+using namespace cotten::embed;
+
+extern "C" {
+
+size_t cotten_embed_workspace_bytes(int B, int N, int D, int V) {
+  if (B < 1 || N < 1 || D < 1 || V < 1 || D > 65536 || static_cast<long long>(B) * N >= (1ll << 31) || V >= (1 << 30)) return 0;
+  return Layout(static_cast<long long>(B) * N, D, V).words * 4;
+}
+
+int cotten_embed_fwd(const void* ids, const void* W, const void* P, void* E, int B, int N, int D, int V, void* stream,
+                     const cotten_embed_params* params) {
+  if (W == nullptr || E == nullptr) return COTTEN_ERR_NULL_POINTER;
+  if (int rc = check(ids, B, N, D, V, params, P != nullptr)) return rc;
+  if (!aligned16(W) || !aligned16(P) || !aligned16(E)) return COTTEN_ERR_MISALIGNED;
+  const Ids of{ids, params->id_bytes == 8, V, params->padding_idx};
+  const long long tokens = static_cast<long long>(B) * N;
+  by_type(params->dtype, D, [&](auto tag) {
+    typedef typename decltype(tag)::type T;
+    constexpr int VEC = decltype(tag)::vec;
+    const int pieces = D / VEC;
+    int block_tokens = kThreads * kUnroll / pieces;
+    if (block_tokens < 1) block_tokens = 1;
+    lookup_kernel<T, VEC><<<dim3(static_cast<uint32_t>((tokens + block_tokens - 1) / block_tokens)), dim3(kThreads), 0,
+                            static_cast<hipStream_t>(stream)>>>(
+        of, static_cast<const T*>(W), static_cast<const T*>(P), static_cast<T*>(E), tokens, N, D, pieces, block_tokens,
+        params->position_offset, params->scale);
+  });
+  return hipGetLastError() == hipSuccess ? COTTEN_OK : COTTEN_ERR_LAUNCH;
+}
+
+int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B, int N, int D, int V, void* stream,
+                     const cotten_embed_params* params) {
+  if (dE == nullptr || (dW == nullptr && dP == nullptr)) return COTTEN_ERR_NULL_POINTER;
+  if (int rc = check(ids, B, N, D, V, params, dP != nullptr)) return rc;
+  if (!aligned16(dE) || !aligned16(dW) || !aligned16(dP)) return COTTEN_ERR_MISALIGNED;
+  const long long n = static_cast<long long>(B) * N;
+  const Layout at(n, D, V);
+  if (dW != nullptr && (params->workspace == nullptr || params->workspace_bytes < at.words * 4)) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  hipError_t err = hipSuccess;
+  if (dW != nullptr) {
+    uint32_t* w = static_cast<uint32_t*>(params->workspace);
+    uint32_t *keys[2] = {w, w + 2 * at.list}, *tokens[2] = {w + at.list, w + 3 * at.list};
+    Sort sort{};
+    sort.ids = Ids{ids, params->id_bytes == 8, V, params->padding_idx};
+    sort.counts = w + 4 * at.list;
+    sort.totals = sort.counts + static_cast<size_t>(kDigits) * at.blocks;
+    sort.n = static_cast<uint32_t>(n);
+    sort.blocks = at.blocks;
+    sort.keys_out = keys[0];
+    sort.tokens_out = tokens[0];
+    const int bits = key_bits(V);
+    if (n <= kSoloTokens) {
+      solo_kernel<<<dim3(1), dim3(64 * kSoloWaves), 0, s>>>(sort, at.passes, at.digit_bits, bits, keys[1], tokens[1]);
+    } else {
+      for (int p = 0; p < at.passes; ++p) {
+        sort.shift = p * at.digit_bits;
+        sort.bits = bits - sort.shift < at.digit_bits ? bits - sort.shift : at.digit_bits;
+        sort.keys = p == 0 ? nullptr : keys[(p - 1) & 1];
+        sort.tokens = p == 0 ? nullptr : tokens[(p - 1) & 1];
+        sort.keys_out = keys[p & 1];
+        sort.tokens_out = tokens[p & 1];
+        count_kernel<<<dim3(at.blocks), dim3(kThreads), 0, s>>>(sort);
+        sums_kernel<<<dim3(((1 << sort.bits) + kThreads / 64 - 1) / (kThreads / 64)), dim3(kThreads), 0, s>>>(sort);
+        move_kernel<<<dim3(at.blocks), dim3(kThreads), 0, s>>>(sort);
+      }
+    }
+    err = hipGetLastError();
+    Rows rows{};
+    rows.keys = keys[(at.passes - 1) & 1];
+    rows.tokens = tokens[(at.passes - 1) & 1];
+    rows.n = static_cast<uint32_t>(n);
+    rows.V = V;
+    rows.D = D;
+    rows.units = at.units;
+    rows.heads = reinterpret_cast<float*>(w + 4 * at.list + at.counts);
+    rows.tails = rows.heads + at.sums;
+    rows.scale = params->scale;
+    by_type(params->dtype, D, [&](auto tag) {
+      typedef typename decltype(tag)::type T;
+      constexpr int VEC = decltype(tag)::vec;
+      const size_t elements = static_cast<size_t>(V) * D, per = static_cast<size_t>(kThreads) * kUnroll * VEC;
+      zero_kernel<T, VEC><<<dim3(static_cast<uint32_t>((elements + per - 1) / per)), dim3(kThreads), 0, s>>>(static_cast<T*>(dW), elements);
+      rows.lanes = lanes_of(D / VEC);
+      const uint32_t units = kThreads / rows.lanes;
+      sum_kernel<T, VEC><<<dim3((at.units + units - 1) / units, (D / VEC + rows.lanes - 1) / rows.lanes), dim3(kThreads), 0, s>>>(
+          rows, static_cast<const T*>(dE), static_cast<T*>(dW));
+      rows.lanes = lanes_of(D);
+      join_kernel<T><<<dim3(at.units), dim3(kThreads), 0, s>>>(rows, static_cast<T*>(dW));
+    });
+    if (err == hipSuccess) err = hipGetLastError();
+  }
+  if (dP != nullptr) {
+    by_type(params->dtype, D, [&](auto tag) {
+      typedef typename decltype(tag)::type T;
+      constexpr int VEC = decltype(tag)::vec;
+      const int lanes = lanes_of(D / VEC);
+      positions_kernel<T, VEC><<<dim3(params->positions, (D / VEC + lanes - 1) / lanes), dim3(1024), 0, s>>>(
+          static_cast<const T*>(dE), static_cast<T*>(dP), B, N, D, params->position_offset, lanes);
+    });
+    if (err == hipSuccess) err = hipGetLastError();
+  }
+  return err == hipSuccess ? COTTEN_OK : COTTEN_ERR_LAUNCH;
+}
+
+}  // extern "C"
