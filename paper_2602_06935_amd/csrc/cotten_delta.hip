@@ -46,8 +46,8 @@ __global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
       const uint32_t off = row + (group + r * kGroups) * E::kBytes;
-      k[r] = E::load_one(K, live ? off : kNowhere);
-      q[r] = E::load_one(Q, off);
+      k[r] = E::value(E::load_one(K, live ? off : kNowhere));
+      q[r] = E::value(E::load_one(Q, off));
       kk = fmaf(k[r], k[r], kk);
       qq = fmaf(q[r], q[r], qq);
     }
@@ -97,7 +97,8 @@ __global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
 template <int D>
 constexpr int kConsumers = D / 16 < 4 ? D / 16 : 4;  // of a workgroup; d = 128 takes two (of ten waves, none would have the registers)
 
-template <class E, int D>
+// OUT: O is wanted; KEPT: what a backward needs is.
+template <class E, int D, bool OUT, bool KEPT>
 __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Args a) {
   typedef ChunkBuffer<E, D> B;
   typedef typename B::R R;
@@ -107,28 +108,24 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Arg
   const Slice s(a, slice, D * E::kBytes);
   Scratch* scratch = reinterpret_cast<Scratch*>(smem + 2 * B::kBytes);
   Notes* notes = reinterpret_cast<Notes*>(scratch + 1);
-  const __amdgpu_buffer_rsrc_t K = s.of(a.K);
 
   if (wave == 0) {
-    KeyProducer<E, D, false> producer;
-    producer.begin(a, s, K, 0, a.chunks > 1 ? 1 : -1, lane);
+    KeyProducer<E, D, false> producer(a, s);
+    producer.begin(0, 1, lane);
     for (int c = 0; c <= a.chunks; ++c) {
-      if (c < a.chunks)
-        producer.make(a, s, K, c + 1 < a.chunks ? c + 1 : -1, c + 2 < a.chunks ? c + 2 : -1, smem + (c & 1) * B::kBytes, scratch, lane);
-      __syncthreads();
+      if (c < a.chunks) producer.make(c + 1, c + 2, smem + (c & 1) * B::kBytes, scratch, lane);
+      lds_barrier();
     }
   } else if (wave == 1) {
-    if (a.O == nullptr) {
-      for (int c = 0; c <= a.chunks; ++c) __syncthreads();
+    if (!OUT) {
+      for (int c = 0; c <= a.chunks; ++c) lds_barrier();
       return;
     }
-    const __amdgpu_buffer_rsrc_t Q = s.of(a.Q);
-    QueryProducer<E, D, false> producer;
-    producer.begin(a, s, Q, K, 0, a.chunks > 1 ? 1 : -1, lane);
+    QueryProducer<E, D, false> producer(a, s);
+    producer.begin(0, 1, lane);
     for (int c = 0; c <= a.chunks; ++c) {
-      if (c < a.chunks)
-        producer.make(a, s, Q, K, c + 1 < a.chunks ? c + 1 : -1, c + 2 < a.chunks ? c + 2 : -1, smem + (c & 1) * B::kBytes, notes, lane);
-      __syncthreads();
+      if (c < a.chunks) producer.make(c + 1, c + 2, smem + (c & 1) * B::kBytes, notes, lane);
+      lds_barrier();
     }
   } else {
     const __amdgpu_buffer_rsrc_t V = s.of(a.V), O = s.of(a.O);
@@ -137,14 +134,15 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Arg
     S.load(a.initial_state == nullptr ? nullptr : a.initial_state + static_cast<long long>(slice) * D * D, col, lane);
     S.cut_all();
     ColumnTile<E> v;
-    v.load(V, a.stride_row, 0, live_of(fetch_live(s, a.N, 0, lane)), col, lane);
-    int byte = a.chunks > 1 ? fetch_live(s, a.N, 1, lane) : 0;
-    __syncthreads();
+    const Live lives(a, s);
+    v.load(V, a.stride_row, 0, lives.bits(lives.fetch(0, lane), 0), col, lane);
+    uint8_t byte = lives.fetch(1, lane);
+    lds_barrier();
     for (int c = 0; c < a.chunks; ++c) {
       const unsigned char* at = smem + (c & 1) * B::kBytes;
       const float* coef = reinterpret_cast<const float*>(at + B::kCoef);
       const long long chunk = static_cast<long long>(slice) * a.chunks + c;
-      if (a.states != nullptr) S.store(a.states + chunk * D * D, col, lane);
+      if (KEPT) S.store(a.states + chunk * D * D, col, lane);
       // beta (V - e^G K^ S)
       f32x4_t u[2];
 #pragma unroll
@@ -155,19 +153,19 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Arg
         u[tt] = by_rows(coef + B::kBeta, tt, lane) * (v.tile(tt) - by_rows(coef + B::kReadK, tt, lane) * p);
       }
       if (c + 1 < a.chunks) {
-        v.load(V, a.stride_row, c + 1, live_of(byte), col, lane);
-        byte = c + 2 < a.chunks ? fetch_live(s, a.N, c + 2, lane) : 0;
+        v.load(V, a.stride_row, c + 1, lives.bits(byte, c + 1), col, lane);
+        byte = lives.fetch(c + 2, lane);
       }
       const Pieces<3> y = cut(u[0], u[1]);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) u[tt] = mul(triangle_operand(at + B::kT, tt, lane), y, f32x4_t{0, 0, 0, 0});
-      if (a.rows_u != nullptr) {
+      if (KEPT) {
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
           for (int r = 0; r < 4; ++r) a.rows_u[(chunk * kChunk + 16 * tt + 4 * (lane >> 4) + r) * D + col] = u[tt][r];
       }
-      if (a.O != nullptr) {
+      if (OUT) {
         // O^T: a lane has four columns of a token
         const Pieces<3> up = cut(u[0], u[1]);
 #pragma unroll
@@ -188,7 +186,7 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Arg
 #pragma unroll
       for (int dt = 0; dt < S.kTiles; ++dt) S.s[dt] = mul(R::column_operand(at + B::kK, dt, lane), w, S.s[dt] * whole);
       S.cut_all();
-      __syncthreads();
+      lds_barrier();
     }
     if (a.final_state != nullptr) S.store(a.final_state + static_cast<long long>(slice) * D * D, col, lane);
   }
@@ -197,19 +195,28 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Arg
 // Up to this many tokens the recurrence is faster than a chunk.
 constexpr int kMostSteps = 8;
 
+template <class E, int D, bool OUT, bool KEPT>
+hipError_t launch_chunks(const Args& a, int slices, hipStream_t stream) {
+  constexpr int kLds = 2 * ChunkBuffer<E, D>::kBytes + sizeof(Scratch) + sizeof(Notes);
+  const auto kernel = chunk_fwd_kernel<E, D, OUT, KEPT>;
+  if (hipError_t err = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds); err != hipSuccess) return err;
+  kernel<<<dim3(slices * (D / 16 / kConsumers<D>)), dim3(64 * (kConsumers<D> + 2)), kLds, stream>>>(a);
+  return hipGetLastError();
+}
+
 template <class E, int D>
 hipError_t launch(const Args& a, int slices, hipStream_t stream) {
-  if (a.N <= kMostSteps && a.states == nullptr && a.O != nullptr) {
+  const bool out = a.O != nullptr, kept = a.states != nullptr;
+  if (a.N <= kMostSteps && out && !kept) {
     constexpr int kParts = D < 32 ? 1 : D / 32;
     const long long waves = static_cast<long long>(slices) * kParts;
     const int per = waves >= 4096 ? 4 : 1;
     step_kernel<E, D><<<dim3(static_cast<uint32_t>((waves + per - 1) / per)), dim3(64 * per), 0, stream>>>(a, slices);
     return hipGetLastError();
   }
-  constexpr int kLds = 2 * ChunkBuffer<E, D>::kBytes + sizeof(Scratch) + sizeof(Notes);
-  if (hipError_t err = grant_dynamic_lds(reinterpret_cast<const void*>(chunk_fwd_kernel<E, D>), kLds); err != hipSuccess) return err;
-  chunk_fwd_kernel<E, D><<<dim3(slices * (D / 16 / kConsumers<D>)), dim3(64 * (kConsumers<D> + 2)), kLds, stream>>>(a);
-  return hipGetLastError();
+  return !out   ? launch_chunks<E, D, false, true>(a, slices, stream)
+         : kept ? launch_chunks<E, D, true, true>(a, slices, stream)
+                : launch_chunks<E, D, true, false>(a, slices, stream);
 }
 
 template <class E>

@@ -43,23 +43,21 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel
   const Slice s(a, slice, D * E::kBytes);
   Scratch* scratch = reinterpret_cast<Scratch*>(smem + 2 * B::kBytes);
   Notes* notes = reinterpret_cast<Notes*>(scratch + 1);
-  const __amdgpu_buffer_rsrc_t K = s.of(a.K);
   const int last = a.chunks - 1;
 
   if (wave == 0) {
-    KeyProducer<E, D, true> producer;
-    producer.begin(a, s, K, last, last - 1, lane);  // (-1: none)
+    KeyProducer<E, D, true> producer(a, s);
+    producer.begin(last, last > 0 ? last - 1 : 0, lane);
     for (int c = last; c >= -1; --c) {
-      if (c >= 0) producer.make(a, s, K, c - 1, c > 0 ? c - 2 : -1, smem + (c & 1) * B::kBytes, scratch, lane);
-      __syncthreads();
+      if (c >= 0) producer.make(c - 1, c > 1 ? c - 2 : 0, smem + (c & 1) * B::kBytes, scratch, lane);
+      lds_barrier();
     }
   } else if (wave == 1) {
-    const __amdgpu_buffer_rsrc_t Q = s.of(a.Q);
-    QueryProducer<E, D, true> producer;
-    producer.begin(a, s, Q, K, last, last - 1, lane);
+    QueryProducer<E, D, true> producer(a, s);
+    producer.begin(last, last > 0 ? last - 1 : 0, lane);
     for (int c = last; c >= -1; --c) {
-      if (c >= 0) producer.make(a, s, Q, K, c - 1, c > 0 ? c - 2 : -1, smem + (c & 1) * B::kBytes, notes, lane);
-      __syncthreads();
+      if (c >= 0) producer.make(c - 1, c > 1 ? c - 2 : 0, smem + (c & 1) * B::kBytes, notes, lane);
+      lds_barrier();
     }
   } else {
     const __amdgpu_buffer_rsrc_t G = s.of(a.dO), dV = s.of(a.dV);
@@ -70,14 +68,15 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel
     dS.cut_all();
     ColumnTile<E> g;
     g.load(G, a.stride_row, last, existing(a.N, last), col, lane);
-    uint32_t live = live_of(fetch_live(s, a.N, last, lane));
-    __syncthreads();
+    const Live lives(a, s);
+    uint32_t live = lives.bits(lives.fetch(last, lane), last);
+    lds_barrier();
     for (int c = last; c >= 0; --c) {
       const unsigned char* at = smem + (c & 1) * B::kBytes;
       const float* coef = reinterpret_cast<const float*>(at + B::kCoef);
       const long long chunk = static_cast<long long>(slice) * a.chunks + c;
       dS.store(a.dstates + chunk * D * D, col, lane);
-      const int byte = c > 0 ? fetch_live(s, a.N, c - 1, lane) : 0;
+      const uint8_t byte = lives.fetch(c > 0 ? c - 1 : 0, lane);
       const Pieces<E::kPieces> up = cut_elements<E>(g.tile(0), g.tile(1));
       const Pieces<3> write = cut(g.tile(0) * by_rows(coef + B::kQuery, 0, lane), g.tile(1) * by_rows(coef + B::kQuery, 1, lane));
       if (c > 0) g.load(G, a.stride_row, c - 1, ~0u, col, lane);
@@ -111,8 +110,8 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel
         dS.s[dt] = mul(R::column_operand(at + B::kK, dt, lane), w, dS.s[dt]);
       }
       dS.cut_all();
-      live = live_of(byte);
-      __syncthreads();
+      live = lives.bits(byte, c - 1);
+      lds_barrier();
     }
     if (a.dinitial_state != nullptr) dS.store(a.dinitial_state + state, col, lane);
   }
@@ -124,37 +123,18 @@ template <class E, int D>
 struct GradientLds {
   typedef Rows<D, E::kPieces> R;
   typedef Rows<D, 3> R3;
-  static constexpr int kK = 0, kQ = R::kBytes, kG = 2 * R::kBytes, kU = 3 * R::kBytes, kZ = kU + R3::kBytes;
-  static constexpr int kTriangles = kZ + R3::kBytes, kSums = kTriangles + 4 * kTriangleBytes;
   static constexpr int kWaves = D / 16;
+  static constexpr int kK = 0, kQ = R::kBytes, kG = 2 * R::kBytes, kU = 3 * R::kBytes, kZ = kU + R3::kBytes;
+  // the four triangles take the place of U and Z (and, for narrow rows, of what follows), when these have been read
+  static constexpr int kTriangles = kU, kRowsEnd = kZ + R3::kBytes, kTrianglesEnd = kTriangles + 4 * kTriangleBytes;
+  static constexpr int kSums = kRowsEnd > kTrianglesEnd ? kRowsEnd : kTrianglesEnd;
   // per wave: q^ . dq^, k^ . p, k^ . w, Z . v, r and c by token, <S, dS'>
   static constexpr int kOfWave = 6 * kChunk + 4;
-  static constexpr int kPairs = kSums + kWaves * kOfWave * 4;  // sums of F by token, of its two terms
-  static constexpr int kNotes = kPairs + 2 * kChunk * 4, kBytes = kNotes + 2 * kChunk * 4;
+  static constexpr int kPairs = kSums + kWaves * kOfWave * 4;                 // sums of F by token, of its two terms
+  static constexpr int kSquares = kPairs + 2 * kChunk * 4;                     // of K's and Q's rows, by block of columns
+  static constexpr int kNotes = kSquares + 2 * R::kBlocks * kChunk * 4;        // per wave: what it knows of the tokens
+  static constexpr int kBytes = kNotes + kWaves * 5 * kChunk * 4;
 };
-
-// Rows 16 tt .. of a chunk into LDS; returns 1/r of row lane%16 of them.
-template <class E, int D>
-__device__ __forceinline__ float stage(unsigned char* at, __amdgpu_buffer_rsrc_t r, uint32_t stride, int first, uint32_t live,
-                                       int tt, float eps, int lane) {
-  typedef Rows<D, E::kPieces> R;
-  const int row = 16 * tt + (lane & 15), g = lane >> 4;
-  const bool on = ((live >> row) & 1u) != 0;
-  const uint32_t off = static_cast<uint32_t>(first + row) * stride + g * 8 * E::kBytes;
-  float ss = 0.0f;
-#pragma unroll
-  for (int kb = 0; kb < R::kBlocks; ++kb) {
-    const typename E::Raw raw = E::load(r, on && (D >= 32 || g * 8 < D) ? off + kb * 32 * E::kBytes : kNowhere);
-    float x[8];
-    E::unpack(raw, x);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-    R::put(at, row, kb, g, E::pieces(raw));
-  }
-  ss += __shfl_xor(ss, 16);
-  ss += __shfl_xor(ss, 32);
-  return on ? __builtin_amdgcn_rsqf(ss + eps) : 0.0f;
-}
 
 // Row 16 dt + lane%16 of a state [D][D] as an operand with the depth in slot order (see Rows).
 template <int D>
@@ -171,10 +151,14 @@ struct StateRows {
   }
 };
 
-__device__ __forceinline__ float over_groups(float x) {  // sum over the four lanes with the same lane%16
-  x += __shfl_xor(x, 16);
-  return x + __shfl_xor(x, 32);
-}
+// What a wave notes of the tokens: sums of decays, beta, 1/r of keys and queries.
+struct Tokens {
+  float hi[kChunk], lo[kChunk], beta[kChunk], rk[kChunk], rq[kChunk];
+  static __device__ __forceinline__ f32x4_t rows(const float* x, int tt, int lane) {  // 16 tt + 4g ... + 3
+    return *reinterpret_cast<const f32x4_t*>(x + 16 * tt + 4 * (lane >> 4));
+  }
+  __device__ __forceinline__ Sum G(int t) const { return Sum{hi[t], lo[t]}; }
+};
 
 // sum over i >= t > j of F, t = 0 ... 31, from its tiles (i tile, j tile) (0,0), (1,1), (1,0) as results (row i, column j).
 __device__ __forceinline__ void pair_sums(f32x4_t f00, f32x4_t f11, f32x4_t f10, float* to, int lane) {
@@ -183,286 +167,351 @@ __device__ __forceinline__ void pair_sums(f32x4_t f00, f32x4_t f11, f32x4_t f10,
   auto suffix = [&](f32x4_t f) {
 #pragma unroll
     for (int r = 2; r >= 0; --r) f[r] += f[r + 1];
-    const float own = f[0];
-    float behind = 0.0f;
-#pragma unroll
-    for (int d = 1; d < 4; ++d) {
-      const float x = __shfl(own, (lane + 16 * d) & 63);
-      behind += g + d < 4 ? x : 0.0f;
-    }
-    return f + behind;
+    const float x1 = __shfl(f[0], (lane + 16) & 63), x2 = __shfl(f[0], (lane + 32) & 63), x3 = __shfl(f[0], (lane + 48) & 63);
+    return f + ((g < 3 ? x1 : 0.0f) + (g < 2 ? x2 : 0.0f) + (g < 1 ? x3 : 0.0f));
   };
   const f32x4_t s00 = suffix(f00), s11 = suffix(f11), s10 = suffix(f10);
   const float all10 = __shfl(s10[0], c);
+  f32x4_t x, y;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
-    const int t = 4 * g + r;
-    float x = c < t ? s00[r] + all10 : 0.0f, y = s10[r] + (c < t ? s11[r] : 0.0f);
-#pragma unroll
-    for (int m = 1; m < 16; m <<= 1) {
-      x += __shfl_xor(x, m);
-      y += __shfl_xor(y, m);
-    }
-    if (c == 0) {
-      to[t] = x;
-      to[16 + t] = y;
-    }
+    const bool before = c < 4 * g + r;
+    const float own = s00[r] + all10, lower = s10[r] + s11[r];
+    x[r] = sum_of_row(before ? own : 0.0f);
+    y[r] = sum_of_row(before ? lower : s10[r]);
+  }
+  if (c == 15) {
+    *reinterpret_cast<f32x4_t*>(to + 4 * g) = x;
+    *reinterpret_cast<f32x4_t*>(to + 16 + 4 * g) = y;
   }
 }
 
-template <class E, int D>
-__global__ __launch_bounds__(64 * (D / 16)) void chunk_gradient_kernel(Args a) {
+// The four triangles (query i, key j; both factors of the unit rows of the operand they meet are in them):
+//   0  rows j, columns i:  scale D rk_j (dO U^T)        1  rows i, columns j:  scale D rq_i (dO U^T)
+//   2  rows j, columns i: -D rk_j (Z U^T), j < i        3  rows i, columns j: -beta_i D rk_i (Z U^T), j < i
+// as tiles (i tile, j tile) (0,0), (1,1), (1,0); of 1 and 3 the sums of F as well.
+template <class E, int D, int JOB>
+__device__ __forceinline__ void make_triangle(f32x4_t (&m)[3], const unsigned char* at, const Tokens& n, float scale, float* pairs,
+                                              int lane) {
   typedef GradientLds<E, D> L;
   typedef typename L::R R;
   typedef typename L::R3 R3;
-  constexpr int kWaves = L::kWaves;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int c16 = lane & 15, gr = lane >> 4;
-  const long long chunk = blockIdx.x;
-  const int slice = static_cast<int>(chunk / a.chunks), c = static_cast<int>(chunk - static_cast<long long>(slice) * a.chunks);
-  const Slice s(a, slice, D * E::kBytes);
-  const uint32_t live = live_of(fetch_live(s, a.N, c, lane)), there = existing(a.N, c);
-  float* rk = reinterpret_cast<float*>(smem + L::kNotes);
-  float* rq = rk + kChunk;
-  const __amdgpu_buffer_rsrc_t Q = s.of(a.Q), K = s.of(a.K), V = s.of(a.V);
-
-  StateRows<D> before, after;
-  before.load(a.states + chunk * D * D, wave, lane);
-  after.load(a.dstates + chunk * D * D, wave, lane);
-  const bool on = (live >> (lane & 31)) & 1u;
-  const long long gate = s.gates + (static_cast<long long>(kChunk) * c + (lane & 31)) * a.gate_row;
-  const float g = on ? a.g[gate] : 0.0f, beta = on ? a.beta[gate] : 0.0f;
-  // K, Q, dO, U, Z, half a chunk at a time, dealt to the waves
-  for (int item = wave; item < 10; item += kWaves) {
-    const int tt = item & 1;
-    if (item < 2) {
-      const float r = stage<E, D>(smem + L::kK, K, a.stride_row, kChunk * c, live, tt, a.eps, lane);
-      if (lane < 16) rk[16 * tt + lane] = r;
-    } else if (item < 4) {
-      const float r = stage<E, D>(smem + L::kQ, Q, a.stride_row, kChunk * c, there, tt, a.eps, lane);
-      if (lane < 16) rq[16 * tt + lane] = r;
-    } else if (item < 6) {
-      stage<E, D>(smem + L::kG, s.of(a.dO), a.stride_row, kChunk * c, there, tt, 1.0f, lane);
-    } else {
-      const float* rows = (item < 8 ? a.rows_u : a.rows_z) + chunk * kChunk * D;
-      const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(rows), 0, kChunk * D * 4, 0x00020000);
-      stage<F32, D>(smem + (item < 8 ? L::kU : L::kZ), r, D * 4, 0, ~0u, tt, 1.0f, lane);
+  constexpr bool kByI = (JOB & 1) != 0, kOuter = JOB < 2;
+  const int c = lane & 15, g = lane >> 4;
+  const f32x4_t zero = {0, 0, 0, 0};
+  m[0] = m[1] = m[2] = zero;
+  f32x4_t d00 = zero, d11 = zero, d10 = zero;
+#pragma unroll
+  for (int kb = 0; kb < R::kBlocks; ++kb) {
+    const Pieces<3> u0 = R3::row_operand(at + L::kU, 0, kb, lane), u1 = R3::row_operand(at + L::kU, 1, kb, lane);
+    auto products = [&](const auto& x0, const auto& x1) {
+      m[0] = kByI ? mul(x0, u0, m[0]) : mul(u0, x0, m[0]);
+      m[1] = kByI ? mul(x1, u1, m[1]) : mul(u1, x1, m[1]);
+      m[2] = kByI ? mul(x1, u0, m[2]) : mul(u0, x1, m[2]);
+    };
+    if constexpr (kOuter) products(R::row_operand(at + L::kG, 0, kb, lane), R::row_operand(at + L::kG, 1, kb, lane));
+    else products(R3::row_operand(at + L::kZ, 0, kb, lane), R3::row_operand(at + L::kZ, 1, kb, lane));
+    if constexpr (kByI) {
+      const auto x0 = R::row_operand(at + (kOuter ? L::kQ : L::kK), 0, kb, lane), x1 = R::row_operand(at + (kOuter ? L::kQ : L::kK), 1, kb, lane);
+      const auto k0 = R::row_operand(at + L::kK, 0, kb, lane), k1 = R::row_operand(at + L::kK, 1, kb, lane);
+      d00 = mul(x0, k0, d00);
+      d11 = mul(x1, k1, d11);
+      d10 = mul(x1, k0, d10);
     }
   }
-  const double G = scan_decays(g, on, lane), G_end = __shfl(G, 31);
-  __syncthreads();
-
-  // the four triangles (query i, key j; both factors of the unit rows of the operand they meet are in them):
-  //   0  rows j, columns i:  scale D rk_j (dO U^T)        1  rows i, columns j:  scale D rq_i (dO U^T)
-  //   2  rows j, columns i: -D rk_j (Z U^T), j < i        3  rows i, columns j: -beta_i D rk_i (Z U^T), j < i
-  for (int job = wave; job < 4; job += kWaves) {
-    const bool by_i = (job & 1) != 0;  // rows are i
-    const unsigned char* left = smem + (job < 2 ? L::kG : L::kZ);
-    f32x4_t m[3] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};  // (i tile, j tile): (0,0), (1,1), (1,0)
+  const float* factor = JOB == 1 ? n.rq : n.rk;
+  f32x4_t f0 = Tokens::rows(factor, 0, lane), f1 = Tokens::rows(factor, 1, lane);
+  if (kOuter) {
+    f0 *= scale;
+    f1 *= scale;
+  } else {
+    f0 *= kByI ? -Tokens::rows(n.beta, 0, lane) : f32x4_t{-1, -1, -1, -1};
+    f1 *= kByI ? -Tokens::rows(n.beta, 1, lane) : f32x4_t{-1, -1, -1, -1};
+  }
+  const f32x4_t hi0 = Tokens::rows(n.hi, 0, lane), hi1 = Tokens::rows(n.hi, 1, lane), lo0 = Tokens::rows(n.lo, 0, lane),
+                lo1 = Tokens::rows(n.lo, 1, lane);
+  const Sum c0 = n.G(c), c1 = n.G(16 + c);
 #pragma unroll
-    for (int kb = 0; kb < R::kBlocks; ++kb) {
-      const Pieces<3> u0 = R3::row_operand(smem + L::kU, 0, kb, lane), u1 = R3::row_operand(smem + L::kU, 1, kb, lane);
-      auto products = [&](auto x0, auto x1) {
-        if (by_i) {
-          m[0] = mul(x0, u0, m[0]);
-          m[1] = mul(x1, u1, m[1]);
-          m[2] = mul(x1, u0, m[2]);
-        } else {
-          m[0] = mul(u0, x0, m[0]);
-          m[1] = mul(u1, x1, m[1]);
-          m[2] = mul(u0, x1, m[2]);
-        }
-      };
-      if (job < 2) products(R::row_operand(left, 0, kb, lane), R::row_operand(left, 1, kb, lane));
-      else products(R3::row_operand(left, 0, kb, lane), R3::row_operand(left, 1, kb, lane));
-    }
-    const double Gc[2] = {__shfl(G, c16), __shfl(G, 16 + c16)};
+  for (int r = 0; r < 4; ++r) {
+    const int o = 4 * g + r;
+    const Sum o0{hi0[r], lo0[r]}, o1{hi1[r], lo1[r]};
+    const float x0 = m[0][r] * f0[r] * (kByI ? pow2(o0, c0) : pow2(c0, o0));
+    const float x1 = m[1][r] * f1[r] * (kByI ? pow2(o1, c1) : pow2(c1, o1));
+    const bool in = kByI ? (kOuter ? o >= c : o > c) : (kOuter ? o <= c : o < c);
+    m[0][r] = in ? x0 : 0.0f;
+    m[1][r] = in ? x1 : 0.0f;
+    m[2][r] *= kByI ? f1[r] * pow2(o1, c0) : f0[r] * pow2(c1, o0);
+  }
+  if constexpr (kByI) {
+    const float r0 = n.rk[c], r1 = n.rk[16 + c];
+    d00 *= m[0] * r0;
+    d11 *= m[1] * r1;
+    d10 *= m[2] * r0;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int o = 4 * gr + r;
-      const double Go[2] = {__shfl(G, o), __shfl(G, 16 + o)};
-      const float* factor = job == 1 ? rq : rk;
-      float f[2] = {factor[o], factor[16 + o]};
-      if (job < 2) {
-        f[0] *= a.scale;
-        f[1] *= a.scale;
-      } else {
-        const float b0 = __shfl(beta, o), b1 = __shfl(beta, 16 + o);
-        f[0] *= by_i ? -b0 : -1.0f;
-        f[1] *= by_i ? -b1 : -1.0f;
-      }
-      const bool diagonal = by_i ? (job < 2 ? o >= c16 : o > c16) : (job < 2 ? o <= c16 : o < c16);
-      m[0][r] = diagonal ? m[0][r] * f[0] * pow2(by_i ? Go[0] - Gc[0] : Gc[0] - Go[0]) : 0.0f;
-      m[1][r] = diagonal ? m[1][r] * f[1] * pow2(by_i ? Go[1] - Gc[1] : Gc[1] - Go[1]) : 0.0f;
-      m[2][r] *= by_i ? f[1] * pow2(Go[1] - Gc[0]) : f[0] * pow2(Gc[1] - Go[0]);
+      const bool in = 4 * g + r > c;
+      d00[r] = in ? d00[r] : 0.0f;
+      d11[r] = in ? d11[r] : 0.0f;
     }
-    const f32x4_t zero = {0, 0, 0, 0};
-    if (by_i) {
-      const unsigned char* rows = smem + (job == 1 ? L::kQ : L::kK);
-      f32x4_t d00 = zero, d11 = zero, d10 = zero;
-#pragma unroll
-      for (int kb = 0; kb < R::kBlocks; ++kb) {
-        const auto x0 = R::row_operand(rows, 0, kb, lane), x1 = R::row_operand(rows, 1, kb, lane);
-        const auto k0 = R::row_operand(smem + L::kK, 0, kb, lane), k1 = R::row_operand(smem + L::kK, 1, kb, lane);
-        d00 = mul(x0, k0, d00);
-        d11 = mul(x1, k1, d11);
-        d10 = mul(x1, k0, d10);
-      }
-      d00 *= m[0] * rk[c16];
-      d11 *= m[1] * rk[16 + c16];
-      d10 *= m[2] * rk[c16];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        if (4 * gr + r <= c16) d00[r] = d11[r] = 0.0f;
-      }
-      pair_sums(d00, d11, d10, reinterpret_cast<float*>(smem + L::kPairs) + (job >> 1) * kChunk, lane);
-    }
-    unsigned char* at = smem + L::kTriangles + job * kTriangleBytes;
-    put_triangle(at, 0, lane, m[0], by_i ? m[2] : zero);
-    put_triangle(at, 1, lane, by_i ? zero : m[2], m[1]);
+    pair_sums(d00, d11, d10, pairs + (JOB >> 1) * kChunk, lane);
   }
+}
+template <int JOB>
+__device__ __forceinline__ void put_tiles(unsigned char* at, const f32x4_t (&m)[3], int lane) {
+  const f32x4_t zero = {0, 0, 0, 0};
+  put_triangle(at + JOB * kTriangleBytes, 0, lane, m[0], (JOB & 1) ? m[2] : zero);
+  put_triangle(at + JOB * kTriangleBytes, 1, lane, (JOB & 1) ? zero : m[2], m[1]);
+}
 
-  // what the states give, tokens in columns
-  f32x4_t dq[2], p[2], w[2];
-  {
-    Pieces<3> S[R::kBlocks];
+template <class E, int D>
+__global__ __launch_bounds__(64 * (D / 16), D == 128 ? 2 : 3) void chunk_gradient_kernel(Args a) {
+  typedef GradientLds<E, D> L;
+  typedef typename L::R R;
+  typedef typename L::R3 R3;
+  constexpr int kWaves = L::kWaves, kBlocks = R::kBlocks;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int c16 = lane & 15, gr = lane >> 4;
+  const uint32_t chunk = blockIdx.x;
+  const int slice = chunk / a.chunks, c = chunk - slice * a.chunks;
+  const Slice s(a, slice, D * E::kBytes);
+  const Live lives(a, s);
+  const uint32_t live = lives.bits(lives.fetch(c, lane), c), there = existing(a.N, c);
+  const __amdgpu_buffer_rsrc_t Q = s.of(a.Q), K = s.of(a.K), V = s.of(a.V);
+  Tokens& n = *reinterpret_cast<Tokens*>(smem + L::kNotes + wave * sizeof(Tokens));
+
+  // K, Q, dO, U, Z: a wave brings 16 rows of 32 columns of each (d = 16: all of them), everything at once
+  constexpr int kUnits = kWaves == 1 ? 2 : 1;
+  typename E::Raw raw[kUnits][3];
+  F32::Raw wide[kUnits][2];
+  const int kb0 = kWaves == 1 ? 0 : wave >> 1;
+  const uint32_t state_rows = kChunk * D * 4;
+  const __amdgpu_buffer_rsrc_t rows_u = __builtin_amdgcn_make_buffer_rsrc(a.rows_u + static_cast<long long>(chunk) * kChunk * D, 0, state_rows, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rows_z = __builtin_amdgcn_make_buffer_rsrc(a.rows_z + static_cast<long long>(chunk) * kChunk * D, 0, state_rows, 0x00020000);
 #pragma unroll
-    for (int kb = 0; kb < R::kBlocks; ++kb) S[kb] = cut(before.lo[kb], before.hi[kb]);
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      dq[tt] = p[tt] = f32x4_t{0, 0, 0, 0};
-#pragma unroll
-      for (int kb = 0; kb < R::kBlocks; ++kb) {
-        dq[tt] = mul(S[kb], R::row_operand(smem + L::kG, tt, kb, lane), dq[tt]);
-        p[tt] = mul(S[kb], R3::row_operand(smem + L::kZ, tt, kb, lane), p[tt]);
-      }
-    }
+  for (int u = 0; u < kUnits; ++u) {
+    const int row = 16 * (kWaves == 1 ? u : wave & 1) + c16, col = 32 * kb0 + 8 * gr;
+    const bool inside = D >= 32 || col < D;
+    const uint32_t off = static_cast<uint32_t>(kChunk * c + row) * a.stride_row + col * E::kBytes;
+    const bool query = inside && ((there >> row) & 1u), key = inside && ((live >> row) & 1u);
+    raw[u][0] = E::load(K, key ? off : kNowhere);
+    raw[u][1] = E::load(Q, query ? off : kNowhere);
+    raw[u][2] = E::load(s.of(a.dO), query ? off : kNowhere);
+    wide[u][0] = F32::load(rows_u, inside ? (row * D + col) * 4 : kNowhere);
+    wide[u][1] = F32::load(rows_z, inside ? (row * D + col) * 4 : kNowhere);
   }
-  float inner = 0.0f;  // <S, dS'> over the wave's columns
-#pragma unroll
-  for (int kb = 0; kb < R::kBlocks; ++kb)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) inner += before.lo[kb][r] * after.lo[kb][r] + before.hi[kb][r] * after.hi[kb][r];
-  {
-    Pieces<3> S[R::kBlocks];
-#pragma unroll
-    for (int kb = 0; kb < R::kBlocks; ++kb) S[kb] = cut(after.lo[kb], after.hi[kb]);
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      w[tt] = f32x4_t{0, 0, 0, 0};
-#pragma unroll
-      for (int kb = 0; kb < R::kBlocks; ++kb) w[tt] = mul(S[kb], R3::row_operand(smem + L::kU, tt, kb, lane), w[tt]);
-    }
-  }
-  const float whole = pow2(G_end);
-  inner *= whole;
-  f32x4_t q[2], k[2];
-  float beta_t[2], rk_t[2], rq_t[2], read[2] = {0.0f, 0.0f}, write[2] = {0.0f, 0.0f};
+  const bool on = (live >> (lane & 31)) & 1u;
+  const float g = __uint_as_float(fetch_gate(a, s.of_gate(a, a.g), c, live, lane)),
+              beta = __uint_as_float(fetch_gate(a, s.of_gate(a, a.beta), c, live, lane));
+  StateRows<D> before, after;
+  before.load(a.states + static_cast<long long>(chunk) * D * D, wave, lane);
+  after.load(a.dstates + static_cast<long long>(chunk) * D * D, wave, lane);
+  // a lane's four columns of its two tokens
+  f32x4_t q[2], k[2], zv[2];
   uint32_t off[2];
 #pragma unroll
   for (int tt = 0; tt < 2; ++tt) {
     const int t = 16 * tt + c16;
-    const double Gt = __shfl(G, t);
-    const float eG = pow2(Gt);
-    beta_t[tt] = __shfl(beta, t);
-    rk_t[tt] = rk[t];
-    rq_t[tt] = rq[t];
     off[tt] = static_cast<uint32_t>(kChunk * c + t) * a.stride_row + (16 * wave + 4 * gr) * E::kBytes;
-    q[tt] = E::load_four(Q, ((there >> t) & 1u) ? off[tt] : kNowhere) * rq_t[tt];
-    k[tt] = E::load_four(K, ((live >> t) & 1u) ? off[tt] : kNowhere) * rk_t[tt];
-    dq[tt] *= a.scale * eG;
-    p[tt] *= -eG;
-    w[tt] *= pow2(G_end - Gt);
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      read[tt] = fmaf(q[tt][r], dq[tt][r], fmaf(beta_t[tt] * k[tt][r], p[tt][r], read[tt]));
-      write[tt] = fmaf(k[tt][r], w[tt][r], write[tt]);
-    }
+    q[tt] = E::load_four(Q, ((there >> t) & 1u) ? off[tt] : kNowhere);
+    k[tt] = E::load_four(K, ((live >> t) & 1u) ? off[tt] : kNowhere);
+    zv[tt] = E::load_four(V, ((live >> t) & 1u) ? off[tt] : kNowhere) * F32::load_four(rows_z, (t * D + 16 * wave + 4 * gr) * 4);
   }
-  __syncthreads();
+  float* squares = reinterpret_cast<float*>(smem + L::kSquares);
+#pragma unroll
+  for (int u = 0; u < kUnits; ++u) {
+    const int row = 16 * (kWaves == 1 ? u : wave & 1) + c16;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float x[8], ss = 0.0f;
+      E::unpack(raw[u][i], x);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) ss = fmaf(x[e], x[e], ss);
+      ss = over_groups(ss);
+      squares[(i * kBlocks + kb0) * kChunk + row] = ss;  // (the four lanes of a row: the same)
+    }
+    R::put(smem + L::kK, row, kb0, gr, E::pieces(raw[u][0]));
+    R::put(smem + L::kQ, row, kb0, gr, E::pieces(raw[u][1]));
+    R::put(smem + L::kG, row, kb0, gr, E::pieces(raw[u][2]));
+    R3::put(smem + L::kU, row, kb0, gr, F32::pieces(wide[u][0]));
+    R3::put(smem + L::kZ, row, kb0, gr, F32::pieces(wide[u][1]));
+  }
+  const Sum G = scan_decays(g, lane), G_end = last_of_scan(G);
+  lds_barrier();
   {
-    const Pieces<E::kPieces> kc = R::column_operand(smem + L::kK, wave, lane), qc = R::column_operand(smem + L::kQ, wave, lane);
-    const unsigned char* at = smem + L::kTriangles;
+    const int t = lane & 31;
+    float kk = a.eps, qq = a.eps;
+#pragma unroll
+    for (int kb = 0; kb < kBlocks; ++kb) {
+      kk += squares[kb * kChunk + t];
+      qq += squares[(kBlocks + kb) * kChunk + t];
+    }
+    n.hi[t] = G.hi;
+    n.lo[t] = G.lo;
+    n.beta[t] = beta;
+    n.rk[t] = on ? __builtin_amdgcn_rsqf(kk) : 0.0f;  // (rows that were not loaded: 0 whatever eps is)
+    n.rq[t] = ((there >> t) & 1u) ? __builtin_amdgcn_rsqf(qq) : 0.0f;
+  }
+  wave_fence();
+
+  float* pairs = reinterpret_cast<float*>(smem + L::kPairs);
+  f32x4_t m[kWaves >= 4 ? 1 : 4 / kWaves][3];
+  if constexpr (kWaves >= 4) {
+    if (wave == 0) make_triangle<E, D, 0>(m[0], smem, n, a.scale, pairs, lane);
+    else if (wave == 1) make_triangle<E, D, 1>(m[0], smem, n, a.scale, pairs, lane);
+    else if (wave == 2) make_triangle<E, D, 2>(m[0], smem, n, a.scale, pairs, lane);
+    else if (wave == 3) make_triangle<E, D, 3>(m[0], smem, n, a.scale, pairs, lane);
+  } else if constexpr (kWaves == 2) {
+    if (wave == 0) {
+      make_triangle<E, D, 0>(m[0], smem, n, a.scale, pairs, lane);
+      make_triangle<E, D, 3>(m[1], smem, n, a.scale, pairs, lane);
+    } else {
+      make_triangle<E, D, 1>(m[0], smem, n, a.scale, pairs, lane);
+      make_triangle<E, D, 2>(m[1], smem, n, a.scale, pairs, lane);
+    }
+  } else {
+    make_triangle<E, D, 0>(m[0], smem, n, a.scale, pairs, lane);
+    make_triangle<E, D, 1>(m[1], smem, n, a.scale, pairs, lane);
+    make_triangle<E, D, 2>(m[2], smem, n, a.scale, pairs, lane);
+    make_triangle<E, D, 3>(m[3], smem, n, a.scale, pairs, lane);
+  }
+
+  // what the states give, tokens in columns
+  f32x4_t dq[2], p[2], w[2];
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt) dq[tt] = p[tt] = w[tt] = f32x4_t{0, 0, 0, 0};
+  float inner = 0.0f;  // <S, dS'> over the wave's columns
+#pragma unroll
+  for (int kb = 0; kb < kBlocks; ++kb) {
+    const Pieces<3> S = cut(before.lo[kb], before.hi[kb]), dS = cut(after.lo[kb], after.hi[kb]);
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
-      dq[tt] = mul(kc, triangle_operand(at, tt, lane), dq[tt]);
-      p[tt] = mul(kc, triangle_operand(at + 2 * kTriangleBytes, tt, lane), p[tt]);
-      w[tt] = mul(qc, triangle_operand(at + kTriangleBytes, tt, lane), w[tt]);
-      w[tt] = mul(kc, triangle_operand(at + 3 * kTriangleBytes, tt, lane), w[tt]);
+      dq[tt] = mul(S, R::row_operand(smem + L::kG, tt, kb, lane), dq[tt]);
+      p[tt] = mul(S, R3::row_operand(smem + L::kZ, tt, kb, lane), p[tt]);
+      w[tt] = mul(dS, R3::row_operand(smem + L::kU, tt, kb, lane), w[tt]);
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) inner += before.lo[kb][r] * after.lo[kb][r] + before.hi[kb][r] * after.hi[kb][r];
+  }
+  lds_barrier();  // U and Z have been read
+  unsigned char* triangles = smem + L::kTriangles;
+  if constexpr (kWaves >= 4) {
+    if (wave == 0) put_tiles<0>(triangles, m[0], lane);
+    else if (wave == 1) put_tiles<1>(triangles, m[0], lane);
+    else if (wave == 2) put_tiles<2>(triangles, m[0], lane);
+    else if (wave == 3) put_tiles<3>(triangles, m[0], lane);
+  } else if constexpr (kWaves == 2) {
+    if (wave == 0) {
+      put_tiles<0>(triangles, m[0], lane);
+      put_tiles<3>(triangles, m[1], lane);
+    } else {
+      put_tiles<1>(triangles, m[0], lane);
+      put_tiles<2>(triangles, m[1], lane);
+    }
+  } else {
+    put_tiles<0>(triangles, m[0], lane);
+    put_tiles<1>(triangles, m[1], lane);
+    put_tiles<2>(triangles, m[2], lane);
+    put_tiles<3>(triangles, m[3], lane);
+  }
+  inner *= pow2(G_end);
+  float read[2], write[2];
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt) {
+    const int t = 16 * tt + c16;
+    const Sum Gt = n.G(t);
+    const float eG = pow2(Gt);
+    q[tt] *= n.rq[t];
+    k[tt] *= n.rk[t];
+    dq[tt] *= a.scale * eG;
+    p[tt] *= -eG;
+    w[tt] *= pow2(G_end, Gt);
+    float x = 0.0f, y = 0.0f, z = 0.0f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      x = fmaf(q[tt][r], dq[tt][r], x);
+      y = fmaf(k[tt][r], p[tt][r], y);
+      z = fmaf(k[tt][r], w[tt][r], z);
+    }
+    read[tt] = fmaf(n.beta[t], y, x);
+    write[tt] = z;
+  }
+  lds_barrier();
+  {
+    const Pieces<E::kPieces> kc = R::column_operand(smem + L::kK, wave, lane), qc = R::column_operand(smem + L::kQ, wave, lane);
+#pragma unroll
+    for (int tt = 0; tt < 2; ++tt) {
+      dq[tt] = mul(kc, triangle_operand(triangles, tt, lane), dq[tt]);
+      p[tt] = mul(kc, triangle_operand(triangles + 2 * kTriangleBytes, tt, lane), p[tt]);
+      w[tt] = mul(qc, triangle_operand(triangles + kTriangleBytes, tt, lane), w[tt]);
+      w[tt] = mul(kc, triangle_operand(triangles + 3 * kTriangleBytes, tt, lane), w[tt]);
     }
   }
   // products of a row with its gradients, over all columns
   float* sums = reinterpret_cast<float*>(smem + L::kSums);
-  constexpr int kSumsOfWave = L::kOfWave;
+  float* own = sums + wave * L::kOfWave;
 #pragma unroll
   for (int tt = 0; tt < 2; ++tt) {
     const int t = 16 * tt + c16;
-    const f32x4_t v = E::load_four(V, ((live >> t) & 1u) ? off[tt] : kNowhere);
-    const f32x4_t z = *reinterpret_cast<const f32x4_t*>(a.rows_z + (chunk * kChunk + t) * D + 16 * wave + 4 * gr);
-    float qd = 0.0f, kp = 0.0f, kw = 0.0f, zv = 0.0f;
+    float qd = 0.0f, kp = 0.0f, kw = 0.0f, v = 0.0f;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       qd = fmaf(q[tt][r], dq[tt][r], qd);
       kp = fmaf(k[tt][r], p[tt][r], kp);
       kw = fmaf(k[tt][r], w[tt][r], kw);
-      zv = fmaf(z[r], v[r], zv);
+      v += zv[tt][r];
     }
     qd = over_groups(qd);
     kp = over_groups(kp);
     kw = over_groups(kw);
-    zv = over_groups(zv);
-    // lane group gr keeps the gr-th of them
-    sums[wave * kSumsOfWave + gr * kChunk + t] = gr == 0 ? qd : gr == 1 ? kp : gr == 2 ? kw : zv;
+    v = over_groups(v);
     const float reads = over_groups(read[tt]), writes = over_groups(write[tt]);
-    if (gr < 2) sums[wave * kSumsOfWave + (4 + gr) * kChunk + t] = gr == 0 ? reads : writes;
+    // lane group gr keeps the gr-th of them
+    own[gr * kChunk + t] = (gr & 2) ? ((gr & 1) ? v : kw) : ((gr & 1) ? kp : qd);
+    if (gr < 2) own[(4 + gr) * kChunk + t] = gr == 0 ? reads : writes;
   }
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) inner += __shfl_xor(inner, m);
-  if (lane == 0) sums[wave * kSumsOfWave + 6 * kChunk] = inner;
-  __syncthreads();
+  inner = over_groups(sum_of_row(inner));
+  if (lane == 15) own[6 * kChunk] = inner;
+  lds_barrier();
 #pragma unroll
   for (int tt = 0; tt < 2; ++tt) {
     const int t = 16 * tt + c16;
-    float qd = 0.0f, kd = 0.0f;
+    const float b = n.beta[t];
+    float qd = 0.0f, kp = 0.0f, kw = 0.0f;
 #pragma unroll
     for (int i = 0; i < kWaves; ++i) {
-      qd += sums[i * kSumsOfWave + t];
-      kd += beta_t[tt] * sums[i * kSumsOfWave + kChunk + t] + sums[i * kSumsOfWave + 2 * kChunk + t];
+      qd += sums[i * L::kOfWave + t];
+      kp += sums[i * L::kOfWave + kChunk + t];
+      kw += sums[i * L::kOfWave + 2 * kChunk + t];
     }
+    const float kd = fmaf(b, kp, kw), rq = n.rq[t], rk = n.rk[t];
     f32x4_t x, y;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      x[r] = (dq[tt][r] - q[tt][r] * qd) * rq_t[tt];
-      y[r] = ((live >> t) & 1u) ? (beta_t[tt] * p[tt][r] + w[tt][r] - k[tt][r] * kd) * rk_t[tt] : 0.0f;
+      x[r] = (dq[tt][r] - q[tt][r] * qd) * rq;
+      y[r] = (fmaf(b, p[tt][r], w[tt][r]) - k[tt][r] * kd) * rk;
+      y[r] = ((live >> t) & 1u) ? y[r] : 0.0f;
     }
     const uint32_t to = ((there >> t) & 1u) ? off[tt] : kNowhere;
     E::store_four(s.of(a.dQ), to, x);
     E::store_four(s.of(a.dK), to, y);
   }
-  if (wave == 0) {
+  if (wave == kWaves - 1) {
     const int t = lane & 31;
-    float kp = 0.0f, zv = 0.0f, reads = 0.0f, writes = 0.0f, end = 0.0f;
+    float kp = 0.0f, v = 0.0f, reads = 0.0f, writes = 0.0f, end = 0.0f;
+#pragma unroll
     for (int i = 0; i < kWaves; ++i) {
-      const float* of = sums + i * kSumsOfWave;
+      const float* of = sums + i * L::kOfWave;
       kp += of[kChunk + t];
-      zv += of[3 * kChunk + t];
+      v += of[3 * kChunk + t];
       reads += of[4 * kChunk + t];
-      writes += of[5 * kChunk + t];
+      writes += t > 0 ? of[5 * kChunk + t - 1] : 0.0f;  // of the tokens before
       end += of[6 * kChunk];
     }
-    const float* pairs = reinterpret_cast<const float*>(smem + L::kPairs);
-    writes = __shfl_up(writes, 1, 32);
-    if (t == 0) writes = 0.0f;
-#pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-      const float r = __shfl_down(reads, d, 32), w1 = __shfl_up(writes, d, 32);
-      if (t + d < 32) reads += r;
-      if (t >= d) writes += w1;
-    }
-    const float x = pairs[t] + pairs[kChunk + t] + reads + writes + end;
+    const float x = pairs[t] + pairs[kChunk + t] + sums_from(reads, lane) + sums_up_to(writes, lane) + end;
+    const long long gate = s.gates + (static_cast<long long>(kChunk) * c + t) * a.gate_row;
     if (lane < 32 && ((there >> t) & 1u)) {
       a.dg[gate] = on ? x : 0.0f;
-      a.dbeta[gate] = on ? zv + kp : 0.0f;
+      a.dbeta[gate] = on ? v + kp : 0.0f;
     }
   }
 }

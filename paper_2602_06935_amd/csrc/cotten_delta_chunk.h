@@ -21,64 +21,71 @@ struct ChunkBuffer {
 template <class E, int D, bool BWD>
 struct KeyProducer {
   typedef ChunkBuffer<E, D> B;
+  const Args& a;
+  const Live lives;
+  const __amdgpu_buffer_rsrc_t K, decays, betas;
   RowTile<E, D> k;
-  uint32_t live;
-  int byte;
-  float g, beta;
+  uint32_t live, g, beta;  // (gates as they were loaded)
+  uint8_t byte;
 
-  __device__ __forceinline__ void gates(const Args& a, const Slice& s, int chunk, int lane) {
-    const int t = kChunk * chunk + (lane & 31);
-    const bool on = (live >> (lane & 31)) & 1u;
-    g = on ? a.g[s.gates + static_cast<long long>(t) * a.gate_row] : 0.0f;
-    beta = on ? a.beta[s.gates + static_cast<long long>(t) * a.gate_row] : 0.0f;
-  }
-  __device__ __forceinline__ void begin(const Args& a, const Slice& s, __amdgpu_buffer_rsrc_t K, int chunk, int next, int lane) {
-    live = live_of(fetch_live(s, a.N, chunk, lane));
+  __device__ __forceinline__ KeyProducer(const Args& args, const Slice& s)
+      : a(args), lives(args, s), K(s.of(args.K)), decays(s.of_gate(args, args.g)), betas(s.of_gate(args, args.beta)) {}
+  __device__ __forceinline__ void fetch(int chunk, int lane) {
+    live = lives.bits(byte, chunk);
     k.load(K, a.stride_row, chunk, live, lane);
-    gates(a, s, chunk, lane);
-    byte = next >= 0 ? fetch_live(s, a.N, next, lane) : 0;
+    g = fetch_gate(a, decays, chunk, live, lane);
+    beta = fetch_gate(a, betas, chunk, live, lane);
   }
-  // makes `chunk` and begins the loads of `next` (-1: none) and of the mask of `after`
-  __device__ __forceinline__ void make(const Args& a, const Slice& s, __amdgpu_buffer_rsrc_t K, int next, int after,
-                                       unsigned char* at, Scratch* scratch, int lane) {
+  // the first chunk, and the mask of the next
+  __device__ __forceinline__ void begin(int chunk, int next, int lane) {
+    byte = lives.fetch(chunk, lane);
+    fetch(chunk, lane);
+    byte = lives.fetch(next, lane);
+  }
+  // makes the chunk that was fetched; begins the loads of `next` (negative or beyond the last: none), and of the mask of `after`
+  __device__ __forceinline__ void make(int next, int after, unsigned char* at, Scratch* scratch, int lane) {
     const int c = lane & 15, gr = lane >> 4;
     float* coef = reinterpret_cast<float*>(at + B::kCoef);
-    const float rn0 = k.inverse_norm(0, a.eps, live, lane), rn1 = k.inverse_norm(1, a.eps, live, lane);
     k.put(at + B::kK, lane);
-    const double G = scan_decays(g, (live >> (lane & 31)) & 1u, lane);
-    const double G_end = __shfl(G, 31);
+    const Sum G = scan_decays(__uint_as_float(g), lane), G_end = last_of_scan(G);
     // k_i . k_j: backward keeps the lower block as its transpose, see below
     const f32x4_t d00 = dots(k, 0, k, 0), d11 = dots(k, 1, k, 1), d10 = BWD ? dots(k, 0, k, 1) : dots(k, 1, k, 0);
+    const float rn0 = inverse_norm(d00, 0, a.eps, live, lane), rn1 = inverse_norm(d11, 1, a.eps, live, lane);
     if (lane < 32) {
-      const float r = lane < 16 ? rn0 : rn1, eG = pow2(G);
-      scratch->notes.G[lane] = G;
-      scratch->notes.rk[lane] = r;
-      scratch->notes.beta[lane] = beta;
-      coef[B::kBeta + lane] = beta;
+      const float r = lane < 16 ? rn0 : rn1, eG = pow2(G), b = __uint_as_float(beta);
+      scratch->notes.hi[lane] = G.hi;
+      scratch->notes.lo[lane] = G.lo;
+      scratch->notes.factor[lane] = b * r;
+      if (BWD) scratch->notes.other[lane] = r;
+      coef[B::kBeta + lane] = b;
       coef[B::kReadK + lane] = r * eG;
-      coef[B::kWriteK + lane] = r * pow2(G_end - G);
-      if (BWD) coef[B::kAdjoint + lane] = -beta * eG * r;
+      coef[B::kWriteK + lane] = r * pow2(G_end, G);
+      if (BWD) coef[B::kAdjoint + lane] = -b * eG * r;
       if (lane == 31) coef[B::kWhole] = eG;
     }
     // the next chunk's rows, while this one is worked on
-    if (next >= 0) {
-      live = live_of(byte);
-      k.load(K, a.stride_row, next, live, lane);
-      gates(a, s, next, lane);
-      byte = after >= 0 ? fetch_live(s, a.N, after, lane) : 0;
+    if (next >= 0 && next < a.chunks) {
+      fetch(next, lane);
+      byte = lives.fetch(after, lane);
     }
     wave_fence();
-    const Notes& n = scratch->notes;
+    const Noted n(scratch->notes, lane);
     f32x4_t a00, a11, a10;
-    const double Gc0 = n.G[c], Gc1 = n.G[16 + c];
+    f32x4_t by_key = {0, 0, 0, 0};
+    float by_row = 0.0f;
+    if (BWD) {
+      by_key = *reinterpret_cast<const f32x4_t*>(&scratch->notes.other[4 * gr]);
+      by_row = scratch->notes.factor[16 + c];
+    }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int i = 4 * gr + r;
-      const float f0 = n.beta[i] * n.rk[i], f1 = n.beta[16 + i] * n.rk[16 + i];
-      a00[r] = i > c ? d00[r] * f0 * rn0 * pow2(n.G[i] - Gc0) : 0.0f;
-      a11[r] = i > c ? d11[r] * f1 * rn1 * pow2(n.G[16 + i] - Gc1) : 0.0f;
-      if (!BWD) a10[r] = d10[r] * f1 * rn0 * pow2(n.G[16 + i] - Gc0);            // row 16+i, column c
-      else a10[r] = d10[r] * (n.beta[16 + c] * rn1) * n.rk[i] * pow2(Gc1 - n.G[i]);  // row 16+c, column i
+      const bool below = 4 * gr + r > c;
+      const float x0 = d00[r] * n.factor[0][r] * rn0 * pow2(n.G(0, r), n.Gc[0]);
+      const float x1 = d11[r] * n.factor[1][r] * rn1 * pow2(n.G(1, r), n.Gc[1]);
+      a00[r] = below ? x0 : 0.0f;
+      a11[r] = below ? x1 : 0.0f;
+      a10[r] = BWD ? d10[r] * by_key[r] * by_row * pow2(n.Gc[1], n.G(0, r))           // row 16 + lane%16, column 4g + r
+                   : d10[r] * n.factor[1][r] * rn0 * pow2(n.G(1, r), n.Gc[0]);        // row 16 + 4g + r, column lane%16
     }
     solve_blocks(scratch, a00, a11, lane);
     const f32x4_t zero = {0, 0, 0, 0};
@@ -102,63 +109,63 @@ struct KeyProducer {
 template <class E, int D, bool BWD>
 struct QueryProducer {
   typedef ChunkBuffer<E, D> B;
+  const Args& a;
+  const Live lives;
+  const __amdgpu_buffer_rsrc_t Q, K, decays;
   RowTile<E, D> q, k;
-  uint32_t live, there;  // keys that take part; rows that exist
-  int byte;
-  float g;
+  uint32_t live, there, g;  // keys that take part; rows that exist
+  uint8_t byte;
 
-  __device__ __forceinline__ void fetch(const Args& a, const Slice& s, __amdgpu_buffer_rsrc_t Q, __amdgpu_buffer_rsrc_t K,
-                                        int chunk, int lane) {
+  __device__ __forceinline__ QueryProducer(const Args& args, const Slice& s)
+      : a(args), lives(args, s), Q(s.of(args.Q)), K(s.of(args.K)), decays(s.of_gate(args, args.g)) {}
+  __device__ __forceinline__ void fetch(int chunk, int lane) {
+    live = lives.bits(byte, chunk);
     there = existing(a.N, chunk);
     q.load(Q, a.stride_row, chunk, there, lane);
     k.load(K, a.stride_row, chunk, live, lane);
-    const int t = kChunk * chunk + (lane & 31);
-    g = ((live >> (lane & 31)) & 1u) ? a.g[s.gates + static_cast<long long>(t) * a.gate_row] : 0.0f;
+    g = fetch_gate(a, decays, chunk, live, lane);
   }
-  __device__ __forceinline__ void begin(const Args& a, const Slice& s, __amdgpu_buffer_rsrc_t Q, __amdgpu_buffer_rsrc_t K,
-                                        int chunk, int next, int lane) {
-    live = live_of(fetch_live(s, a.N, chunk, lane));
-    fetch(a, s, Q, K, chunk, lane);
-    byte = next >= 0 ? fetch_live(s, a.N, next, lane) : 0;
+  __device__ __forceinline__ void begin(int chunk, int next, int lane) {
+    byte = lives.fetch(chunk, lane);
+    fetch(chunk, lane);
+    byte = lives.fetch(next, lane);
   }
-  __device__ __forceinline__ void make(const Args& a, const Slice& s, __amdgpu_buffer_rsrc_t Q, __amdgpu_buffer_rsrc_t K,
-                                       int next, int after, unsigned char* at, Notes* n, int lane) {
+  __device__ __forceinline__ void make(int next, int after, unsigned char* at, Notes* n, int lane) {
     const int c = lane & 15, gr = lane >> 4;
     float* coef = reinterpret_cast<float*>(at + B::kCoef);
-    const float rq0 = a.scale * q.inverse_norm(0, a.eps, there, lane), rq1 = a.scale * q.inverse_norm(1, a.eps, there, lane);
-    const float rk0 = k.inverse_norm(0, a.eps, live, lane), rk1 = k.inverse_norm(1, a.eps, live, lane);
+    const float rq0 = a.scale * inverse_norm(dots(q, 0, q, 0), 0, a.eps, there, lane);
+    const float rq1 = a.scale * inverse_norm(dots(q, 1, q, 1), 1, a.eps, there, lane);
+    const float rk0 = inverse_norm(dots(k, 0, k, 0), 0, a.eps, live, lane);
+    const float rk1 = inverse_norm(dots(k, 1, k, 1), 1, a.eps, live, lane);
     q.put(at + B::kQ, lane);
-    const double G = scan_decays(g, (live >> (lane & 31)) & 1u, lane);
+    const Sum G = scan_decays(__uint_as_float(g), lane);
     // forward: rows j (keys), columns i (queries); backward: rows i, columns j
     const f32x4_t d00 = BWD ? dots(q, 0, k, 0) : dots(k, 0, q, 0), d11 = BWD ? dots(q, 1, k, 1) : dots(k, 1, q, 1),
                   d10 = BWD ? dots(q, 1, k, 0) : dots(k, 0, q, 1);
     if (lane < 32) {
-      n->G[lane] = G;
-      n->rk[lane] = BWD ? (lane < 16 ? rq0 : rq1) : (lane < 16 ? rk0 : rk1);  // of the rows of the results
+      n->hi[lane] = G.hi;
+      n->lo[lane] = G.lo;
+      n->factor[lane] = BWD ? (lane < 16 ? rq0 : rq1) : (lane < 16 ? rk0 : rk1);  // of the rows of the results
       coef[B::kQuery + lane] = (lane < 16 ? rq0 : rq1) * pow2(G);
     }
-    if (next >= 0) {
-      live = live_of(byte);
-      fetch(a, s, Q, K, next, lane);
-      byte = after >= 0 ? fetch_live(s, a.N, after, lane) : 0;
+    if (next >= 0 && next < a.chunks) {
+      fetch(next, lane);
+      byte = lives.fetch(after, lane);
     }
     wave_fence();
+    // rows o = 4g + r, columns lane%16: keys and queries, or queries and keys
+    const Noted o(*n, lane);
     f32x4_t m00, m11, m10;
-    const double Gc0 = n->G[c], Gc1 = n->G[16 + c];
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      const int o = 4 * gr + r;  // the other index: c and o are query and key, or key and query
-      const double Go0 = n->G[o], Go1 = n->G[16 + o];
-      const float fo0 = n->rk[o], fo1 = n->rk[16 + o];
-      if (!BWD) {
-        m00[r] = o <= c ? d00[r] * fo0 * rq0 * pow2(Gc0 - Go0) : 0.0f;
-        m11[r] = o <= c ? d11[r] * fo1 * rq1 * pow2(Gc1 - Go1) : 0.0f;
-        m10[r] = d10[r] * fo0 * rq1 * pow2(Gc1 - Go0);
-      } else {
-        m00[r] = o >= c ? d00[r] * fo0 * rk0 * pow2(Go0 - Gc0) : 0.0f;
-        m11[r] = o >= c ? d11[r] * fo1 * rk1 * pow2(Go1 - Gc1) : 0.0f;
-        m10[r] = d10[r] * fo1 * rk0 * pow2(Go1 - Gc0);
-      }
+      const int row = 4 * gr + r;
+      const float x0 = d00[r] * o.factor[0][r] * (BWD ? rk0 : rq0) * (BWD ? pow2(o.G(0, r), o.Gc[0]) : pow2(o.Gc[0], o.G(0, r)));
+      const float x1 = d11[r] * o.factor[1][r] * (BWD ? rk1 : rq1) * (BWD ? pow2(o.G(1, r), o.Gc[1]) : pow2(o.Gc[1], o.G(1, r)));
+      const bool in = BWD ? row >= c : row <= c;
+      m00[r] = in ? x0 : 0.0f;
+      m11[r] = in ? x1 : 0.0f;
+      m10[r] = BWD ? d10[r] * o.factor[1][r] * rk0 * pow2(o.G(1, r), o.Gc[0])
+                   : d10[r] * o.factor[0][r] * rq1 * pow2(o.Gc[1], o.G(0, r));
     }
     const f32x4_t zero = {0, 0, 0, 0};
     put_triangle(at + B::kM, 0, lane, m00, BWD ? m10 : zero);
@@ -169,7 +176,7 @@ struct QueryProducer {
 // Rows of V or dO in the layout of a result: column `col`, tokens 16 tt + 4g + r.
 template <class E>
 struct ColumnTile {
-  float x[2][4];
+  typename E::One x[2][4];
   __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t stride, int chunk, uint32_t live, int col, int lane) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt)
@@ -180,7 +187,7 @@ struct ColumnTile {
         x[tt][i] = E::load_one(r, ((live >> row) & 1u) ? off : kNowhere);
       }
   }
-  __device__ __forceinline__ f32x4_t tile(int tt) const { return f32x4_t{x[tt][0], x[tt][1], x[tt][2], x[tt][3]}; }
+  __device__ __forceinline__ f32x4_t tile(int tt) const { return f32x4_t{E::value(x[tt][0]), E::value(x[tt][1]), E::value(x[tt][2]), E::value(x[tt][3])}; }
 };
 
 // 16 columns of a state: rows 16 dt + 4g + r, column lane%16 of the wave's; and its pieces, by blocks of 32 rows.

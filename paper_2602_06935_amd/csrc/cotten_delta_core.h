@@ -39,8 +39,16 @@ constexpr int kChunk = 32;                       // tokens of a chunk: the depth
 constexpr uint32_t kNowhere = 0x80000000u;       // a byte offset beyond every slice: such loads bring zeros
 
 __device__ __forceinline__ void wave_fence() {
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
   __builtin_amdgcn_wave_barrier();
+}
+
+// A barrier for what waves pass each other through LDS: loads and stores of global memory stay on their way across it
+// (a full barrier waits for them: 2.1 us a chunk for the keys' producer, and nothing it had asked for early came early).
+__device__ __forceinline__ void lds_barrier() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
 __device__ __forceinline__ f32x4_t mfma(bf16x8_t a, bf16x8_t b, f32x4_t c) {
@@ -72,7 +80,9 @@ __device__ __forceinline__ Pieces<3> cut(const float (&x)[8]) {
     const uint32_t a = __float_as_uint(x[2 * i]), b = __float_as_uint(x[2 * i + 1]);
     h[i] = __builtin_amdgcn_perm(b, a, 0x07060302u);
     const float ra = x[2 * i] - __uint_as_float(a & 0xffff0000u), rb = x[2 * i + 1] - __uint_as_float(b & 0xffff0000u);
-    m[i] = pack_bf16(ra, rb);
+    uint32_t w = pack_bf16(ra, rb);
+    asm("" : "+v"(w));  // (both halves from the one conversion: the compiler would make the lower one again)
+    m[i] = w;
     l[i] = pack_bf16(ra - __uint_as_float(m[i] << 16), rb - __uint_as_float(m[i] & 0xffff0000u));
   }
   Pieces<3> r;
@@ -130,9 +140,11 @@ struct F32 {
     unpack(w, x);
     return cut(x);
   }
-  static __device__ __forceinline__ float load_one(__amdgpu_buffer_rsrc_t r, uint32_t off) {
-    return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0));
+  typedef uint32_t One;  // an element as it was loaded: turned into a float where it is used, not where it would be waited for
+  static __device__ __forceinline__ One load_one(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return __builtin_amdgcn_raw_buffer_load_b32(r, off, 0, 0);
   }
+  static __device__ __forceinline__ float value(One w) { return __uint_as_float(w); }
   static __device__ __forceinline__ f32x4_t load_four(__amdgpu_buffer_rsrc_t r, uint32_t off) {
     return __builtin_bit_cast(f32x4_t, __builtin_amdgcn_raw_buffer_load_b128(r, off, 0, 0));
   }
@@ -160,8 +172,9 @@ struct Half {
       x[2 * i + 1] = value(static_cast<uint16_t>(w[i] >> 16));
     }
   }
-  static __device__ __forceinline__ float load_one(__amdgpu_buffer_rsrc_t r, uint32_t off) {
-    return value(static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0)));
+  typedef uint16_t One;
+  static __device__ __forceinline__ One load_one(__amdgpu_buffer_rsrc_t r, uint32_t off) {
+    return static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0));
   }
   static __device__ __forceinline__ f32x4_t load_four(__amdgpu_buffer_rsrc_t r, uint32_t off) {
     const u32x2_t w = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
@@ -236,27 +249,37 @@ struct Slice {
   long long gates;      // element offset of token 0 in g, beta ...
   const uint8_t* mask;  // of the sequence, or nullptr
   uint32_t bytes;       // from row 0 to the end of row N-1
-  int index;
   __device__ __forceinline__ Slice(const Args& a, int slice, uint32_t row_bytes) {
     const int b = slice / a.H, h = slice - b * a.H;
     rows = b * a.stride_batch + h * a.stride_head;
     gates = b * a.gate_batch + h * a.gate_head;
     mask = a.mask == nullptr ? nullptr : a.mask + static_cast<long long>(b) * a.N;
     bytes = static_cast<uint32_t>(a.N - 1) * a.stride_row + row_bytes;
-    index = slice;
   }
   __device__ __forceinline__ __amdgpu_buffer_rsrc_t of(const unsigned char* base) const {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base) + rows, 0, bytes, 0x00020000);
   }
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t of_gate(const Args& a, const float* base) const {
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base) + gates, 0, ((a.N - 1) * a.gate_row + 1) * 4, 0x00020000);
+  }
 };
 
-// Bit t: token 32 * chunk + t exists and is not masked.  `fetch` brings the byte, `live_of` makes the bits of it.
-__device__ __forceinline__ int fetch_live(const Slice& s, int N, int chunk, int lane) {
-  const int t = kChunk * chunk + (lane & 31);
-  if (t >= N) return 0;
-  return s.mask == nullptr ? 1 : s.mask[t];
-}
-__device__ __forceinline__ uint32_t live_of(int byte) { return static_cast<uint32_t>(__ballot(byte != 0)); }
+// The tokens of a chunk that take part.  A byte of the mask is asked for a chunk ahead of the rows that hang on it.
+struct Live {
+  __amdgpu_buffer_rsrc_t mask;
+  bool all;
+  int N;
+  __device__ __forceinline__ Live(const Args& a, const Slice& s)
+      : mask(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(s.mask), 0, s.mask == nullptr ? 0 : a.N, 0x00020000)),
+        all(s.mask == nullptr),
+        N(a.N) {}
+  // of token 32 * chunk + lane%32 (beyond the sequence: 0)
+  __device__ __forceinline__ uint8_t fetch(int chunk, int lane) const {
+    return __builtin_amdgcn_raw_buffer_load_b8(mask, static_cast<uint32_t>(kChunk * chunk + (lane & 31)), 0, 0);
+  }
+  // bit t: token 32 * chunk + t takes part
+  __device__ __forceinline__ uint32_t bits(uint8_t byte, int chunk) const;
+};
 
 // Bit t: token 32 * chunk + t exists.
 __device__ __forceinline__ uint32_t existing(int N, int chunk) {
@@ -264,26 +287,90 @@ __device__ __forceinline__ uint32_t existing(int N, int chunk) {
   return left >= kChunk ? ~0u : (1u << left) - 1u;
 }
 
+__device__ __forceinline__ uint32_t Live::bits(uint8_t byte, int chunk) const {
+  return all ? existing(N, chunk) : static_cast<uint32_t>(__ballot(byte != 0));
+}
+// A gate of token 32 * chunk + lane%32; 0 where it takes no part.
+__device__ __forceinline__ uint32_t fetch_gate(const Args& a, __amdgpu_buffer_rsrc_t r, int chunk, uint32_t live, int lane) {
+  const uint32_t off = static_cast<uint32_t>(kChunk * chunk + (lane & 31)) * a.gate_row * 4;
+  return __builtin_amdgcn_raw_buffer_load_b32(r, ((live >> (lane & 31)) & 1u) ? off : kNowhere, 0, 0);
+}
+
 // ---- decays -----------------------------------------------------------------------------------------------------
 
-// 2^x of a difference of sums: the fraction goes through the hardware's 2^x, the whole part into the exponent.
-__device__ __forceinline__ float pow2(double x) {
-  const double n = __builtin_rint(x);
-  return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(static_cast<float>(x - n)),
-                                 static_cast<int>(n < -100000.0 ? -100000.0 : n > 100000.0 ? 100000.0 : n));
+// A sum of g * log2(e) as two floats.  Their differences are formed part by part: what rounding is left costs
+// 2^x |x| 2^-24 at most, which for decays is less than a rounding of 1, the largest of the factors it is summed with.
+struct Sum {
+  float hi, lo;
+};
+__device__ __forceinline__ Sum split(double x) {
+  const float hi = static_cast<float>(x);
+  return Sum{hi, static_cast<float>(x - hi)};
+}
+// 2^(a - b)
+__device__ __forceinline__ float pow2(Sum a, Sum b) { return __builtin_amdgcn_exp2f((a.hi - b.hi) + (a.lo - b.lo)); }
+__device__ __forceinline__ float pow2(Sum a) { return __builtin_amdgcn_exp2f(a.hi + a.lo); }
+__device__ __forceinline__ Sum of_lane(Sum x, int lane) { return Sum{__shfl(x.hi, lane), __shfl(x.lo, lane)}; }
+
+// The lanes of a row of 16 shifted right by N (lanes without a source: 0).
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ double move_lanes(double x) {
+  const uint64_t w = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, static_cast<int>(w), CTRL, ROWS, 0xF, true);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, static_cast<int>(w >> 32), CTRL, ROWS, 0xF, true);
+  return __builtin_bit_cast(double, (static_cast<uint64_t>(hi) << 32) | lo);
 }
 
 // Inclusive sums of g * log2(e) over the chunk's 32 tokens, the same in both halves of the wave (lane & 31 is the token).
 // A decay to nothing (g = -inf) counts as 2^-100000: fp32 knows no difference, and later differences stay numbers.
-__device__ __forceinline__ double scan_decays(float g, bool live, int lane) {
-  double x = live ? static_cast<double>(g) * 1.4426950408889634 : 0.0;
+__device__ __forceinline__ Sum scan_decays(float g, int lane) {
+  double x = static_cast<double>(g) * 1.4426950408889634;
   x = x < -100000.0 ? -100000.0 : x;
-#pragma unroll
-  for (int d = 1; d < 32; d <<= 1) {
-    const double y = __shfl_up(x, d, 32);
-    if ((lane & 31) >= d) x += y;
-  }
-  return x;
+  x += move_lanes<0x111>(x);  // row_shr 1, 2, 4, 8: sums inside rows of 16
+  x += move_lanes<0x112>(x);
+  x += move_lanes<0x114>(x);
+  x += move_lanes<0x118>(x);
+  const double first = move_lanes<0x15F>(x);  // the last lane of every row, to all of its lanes
+  const uint64_t w = __builtin_bit_cast(uint64_t, first);
+  const uint32_t lo = __builtin_amdgcn_readlane(static_cast<int>(w), 0), hi = __builtin_amdgcn_readlane(static_cast<int>(w >> 32), 0);
+  const double row0 = __builtin_bit_cast(double, (static_cast<uint64_t>(hi) << 32) | lo);
+  return split((lane & 16) ? x + row0 : x);
+}
+// ... of the whole chunk
+__device__ __forceinline__ Sum last_of_scan(Sum x) {
+  return Sum{__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x.hi), 31)),
+             __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x.lo), 31))};
+}
+
+// Inclusive sums over the chunk's tokens (lane & 31) of the lower half of a wave: of those up to the lane's, and from it on.
+template <int CTRL>
+__device__ __forceinline__ float add_moved(float x) {
+  return x + __uint_as_float(__builtin_amdgcn_update_dpp(0, static_cast<int>(__float_as_uint(x)), CTRL, 0xF, 0xF, true));
+}
+__device__ __forceinline__ float of_fixed_lane(float x, int lane) {
+  return __uint_as_float(__builtin_amdgcn_readlane(static_cast<int>(__float_as_uint(x)), lane));
+}
+__device__ __forceinline__ float sums_up_to(float x, int lane) {
+  x = add_moved<0x118>(add_moved<0x114>(add_moved<0x112>(add_moved<0x111>(x))));  // row_shr 1, 2, 4, 8
+  const float row0 = of_fixed_lane(x, 15);
+  return (lane & 16) ? x + row0 : x;
+}
+__device__ __forceinline__ float sums_from(float x, int lane) {
+  x = add_moved<0x108>(add_moved<0x104>(add_moved<0x102>(add_moved<0x101>(x))));  // row_shl 1, 2, 4, 8
+  const float row1 = of_fixed_lane(x, 16);
+  return (lane & 16) ? x : x + row1;
+}
+// Sum over the 16 lanes of a row, in its last lane.
+__device__ __forceinline__ float sum_of_row(float x) {
+  return add_moved<0x118>(add_moved<0x114>(add_moved<0x112>(add_moved<0x111>(x))));
+}
+
+// Sum over the four lanes with the same lane % 16.
+__device__ __forceinline__ float over_groups(float x) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 
 // ---- rows in LDS ------------------------------------------------------------------------------------------------
@@ -368,21 +455,6 @@ struct RowTile {
       }
     }
   }
-  // 1 / sqrt(sum of squares + eps) of row 16 tt + lane%16, the same in the four lanes that share it; 0 for a row that was
-  // not loaded (whatever eps is: its products are zeros and stay zeros)
-  __device__ __forceinline__ float inverse_norm(int tt, float eps, uint32_t live, int lane) const {
-    float ss = 0.0f;
-#pragma unroll
-    for (int kb = 0; kb < kBlocks; ++kb) {
-      float x[8];
-      E::unpack(raw[tt][kb], x);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-    }
-    ss += __shfl_xor(ss, 16);
-    ss += __shfl_xor(ss, 32);
-    return ((live >> (16 * tt + (lane & 15))) & 1u) ? __builtin_amdgcn_rsqf(ss + eps) : 0.0f;
-  }
   __device__ __forceinline__ Pieces<E::kPieces> operand(int tt, int kb) const { return E::pieces(raw[tt][kb]); }
   __device__ __forceinline__ void put(unsigned char* at, int lane) const {
 #pragma unroll
@@ -402,11 +474,37 @@ __device__ __forceinline__ f32x4_t dots(const RowTile<E, D>& X, int a, const Row
   return c;
 }
 
-// The producers' own notes of a chunk: sums of decays and 1/r of the keys by token.
+// 1 / sqrt(square + eps) of row 16 tt + lane%16, the same in the four lanes that share it, from the products of the tile's
+// rows with one another, whose diagonal are the squares; 0 for a row that was not loaded (whatever eps is: its products
+// are zeros and stay zeros).
+__device__ __forceinline__ float inverse_norm(f32x4_t products, int tt, float eps, uint32_t live, int lane) {
+  const int c = lane & 15;
+  const float x = (c & 2) ? ((c & 1) ? products[3] : products[2]) : ((c & 1) ? products[1] : products[0]);
+  const float square = over_groups((c >> 2) == (lane >> 4) ? x : 0.0f);
+  return ((live >> (16 * tt + c)) & 1u) ? __builtin_amdgcn_rsqf(square + eps) : 0.0f;
+}
+
+// A producer's own notes of a chunk, by token: sums of decays, and the factor of the row in the products it makes.
 struct Notes {
-  double G[kChunk];
-  float rk[kChunk];
-  float beta[kChunk];
+  float hi[kChunk], lo[kChunk];
+  float factor[kChunk];
+  float other[kChunk];  // (keys, backward: the factor without beta)
+};
+// ... of the rows 4g .. 4g+3 of both halves, and of row lane%16
+struct Noted {
+  f32x4_t hi[2], lo[2], factor[2];
+  Sum Gc[2];
+  __device__ __forceinline__ Noted(const Notes& n, int lane) {
+    const int c = lane & 15, g = lane >> 4;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      Gc[t] = Sum{n.hi[16 * t + c], n.lo[16 * t + c]};
+      hi[t] = *reinterpret_cast<const f32x4_t*>(&n.hi[16 * t + 4 * g]);
+      lo[t] = *reinterpret_cast<const f32x4_t*>(&n.lo[16 * t + 4 * g]);
+      factor[t] = *reinterpret_cast<const f32x4_t*>(&n.factor[16 * t + 4 * g]);
+    }
+  }
+  __device__ __forceinline__ Sum G(int t, int r) const { return Sum{hi[t][r], lo[t][r]}; }
 };
 
 constexpr int kSquareStride = 20;                    // floats per row of a 16 x 16 square (80 bytes: free of conflicts)
@@ -417,6 +515,23 @@ struct Scratch {  // of the wave that solves
   float t[2][kSquare];  // diagonal blocks of T
 };
 
+// x + (a of lane J of each 16 lanes) * t, in one instruction.
+template <int J>
+__device__ __forceinline__ float add_from_lane(float a, float t, float x) {
+  asm("v_fmac_f32_dpp %0, %1, %2 row_newbcast:%3 row_mask:0xf bank_mask:0xf" : "+v"(x) : "v"(a), "v"(t), "n"(J));
+  return x;
+}
+template <int J, int M>
+__device__ __forceinline__ float solve_sum(const float (&A)[16], const float (&t)[16], float x) {
+  if constexpr (M > J) return solve_sum<J, M - 1>(A, t, add_from_lane<J>(A[M], t[M], x));
+  else return x;
+}
+template <int J>
+__device__ __forceinline__ void solve_row(const float (&A)[16], float (&t)[16], int i) {
+  t[J] = solve_sum<J, 15>(A, t, i == J ? 1.0f : 0.0f);
+  if constexpr (J > 0) solve_row<J - 1>(A, t, i);
+}
+
 // T = (I + A)^-1 for A = [[A0, 0], [A10, A1]], strictly lower: the diagonal blocks by substitution (as stable as solving
 // token by token; powers of A would lose digits where keys repeat), and T10 = -T1 A10 T0.  `d0`, `d1`: A0 and A1 as
 // results (row 4g + r, column lane%16).  In LDS afterwards: the rows of T0 and T1.
@@ -425,27 +540,21 @@ __device__ __forceinline__ void solve_blocks(Scratch* s, f32x4_t d0, f32x4_t d1,
   *reinterpret_cast<f32x4_t*>(&s->a[0][c * kSquareStride + 4 * g]) = d0;
   *reinterpret_cast<f32x4_t*>(&s->a[1][c * kSquareStride + 4 * g]) = d1;
   wave_fence();
-  // row i = lane%16 of T of block (lane / 16) % 2: t_j = [i = j] - sum_{m > j} t_m A_mj
-  const float* A = s->a[g & 1];
-  float t[16];
+  // row i = lane%16 of T of block (lane / 16) % 2: t_j = [i = j] - sum_{m > j} t_m A_mj.  Lane j has column j of A: what
+  // all lanes need of it comes by a broadcast inside the 16 lanes.
+  float A[16], t[16];
 #pragma unroll
-  for (int j = 15; j >= 0; --j) {
-    float x = c == j ? 1.0f : 0.0f;
+  for (int q = 0; q < 4; ++q) {
+    const f32x4_t w = *reinterpret_cast<const f32x4_t*>(&s->a[g & 1][c * kSquareStride + 4 * q]);
 #pragma unroll
-    for (int q = 3; q >= 0; --q) {
-      if (4 * q + 3 <= j) continue;
-      const f32x4_t w = *reinterpret_cast<const f32x4_t*>(&A[j * kSquareStride + 4 * q]);
-#pragma unroll
-      for (int e = 3; e >= 0; --e)
-        if (4 * q + e > j) x = fmaf(-t[4 * q + e], w[e], x);
-    }
-    t[j] = x;
+    for (int e = 0; e < 4; ++e) A[4 * q + e] = -w[e];
   }
-  if (lane < 32) {
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<f32x4_t*>(&s->t[g][c * kSquareStride + 4 * q]) = f32x4_t{t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
-  }
+  for (int e = 0; e < 16; ++e) asm("s_nop 1" : "+v"(A[e]));  // (two states between a result and its use in other lanes)
+  solve_row<15>(A, t, c);
+#pragma unroll
+  for (int q = 0; q < 4; ++q)  // (two lane groups write the same; a branch would keep the broadcasts out of the sums)
+    *reinterpret_cast<f32x4_t*>(&s->t[g & 1][c * kSquareStride + 4 * q]) = f32x4_t{t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
   wave_fence();
 }
 __device__ __forceinline__ f32x4_t square_row(const float* m, int lane) {  // row lane%16, columns 4g .. 4g+3
