@@ -128,14 +128,13 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Arg
       lds_barrier();
     }
   } else {
-    const __amdgpu_buffer_rsrc_t V = s.of(a.V), O = s.of(a.O);
     const int tile = group * kConsumers<D> + wave - 2, col = 16 * tile + (lane & 15);
     StateColumns<D> S;
     S.load(a.initial_state == nullptr ? nullptr : a.initial_state + static_cast<long long>(slice) * D * D, col, lane);
     S.cut_all();
     ColumnTile<E> v;
     const Live lives(a, s);
-    v.load(V, a.stride_row, 0, lives.bits(lives.fetch(0, lane), 0), col, lane);
+    v.load(s.of(a.V, 0, a.stride_row), a.stride_row, lives.bits(lives.fetch(0, lane), 0), col, lane);
     uint8_t byte = lives.fetch(1, lane);
     lds_barrier();
     for (int c = 0; c < a.chunks; ++c) {
@@ -153,20 +152,16 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Arg
         u[tt] = by_rows(coef + B::kBeta, tt, lane) * (v.tile(tt) - by_rows(coef + B::kReadK, tt, lane) * p);
       }
       if (c + 1 < a.chunks) {
-        v.load(V, a.stride_row, c + 1, lives.bits(byte, c + 1), col, lane);
+        v.load(s.of(a.V, c + 1, a.stride_row), a.stride_row, lives.bits(byte, c + 1), col, lane);
         byte = lives.fetch(c + 2, lane);
       }
       const Pieces<3> y = cut(u[0], u[1]);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) u[tt] = mul(triangle_operand(at + B::kT, tt, lane), y, f32x4_t{0, 0, 0, 0});
-      if (KEPT) {
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) a.rows_u[(chunk * kChunk + 16 * tt + 4 * (lane >> 4) + r) * D + col] = u[tt][r];
-      }
+      if (KEPT) store_rows<D>(a.rows_u + chunk * kChunk * D, u, col, lane);
       if (OUT) {
         // O^T: a lane has four columns of a token
+        const __amdgpu_buffer_rsrc_t O = s.of(a.O, c, a.stride_row);
         const Pieces<3> up = cut(u[0], u[1]);
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) {
@@ -175,9 +170,7 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Arg
           for (int kb = 0; kb < S.kBlocks; ++kb) o = mul(S.p[kb], R::row_operand(at + B::kQ, tt, kb, lane), o);
           o *= coef[B::kQuery + 16 * tt + (lane & 15)];
           o = mul(up, triangle_operand(at + B::kM, tt, lane), o);
-          const int row = kChunk * c + 16 * tt + (lane & 15);
-          if (row < a.N)
-            E::store_four(O, static_cast<uint32_t>(row) * a.stride_row + (16 * tile + 4 * (lane >> 4)) * E::kBytes, o);
+          E::store_four(O, static_cast<uint32_t>(16 * tt + (lane & 15)) * a.stride_row + (16 * tile + 4 * (lane >> 4)) * E::kBytes, o);
         }
       }
       // S' = e^(G_C) S + K^^T (e^(G_C - G) U)

@@ -60,14 +60,13 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel
       lds_barrier();
     }
   } else {
-    const __amdgpu_buffer_rsrc_t G = s.of(a.dO), dV = s.of(a.dV);
     const int tile = group * kConsumers<D> + wave - 2, col = 16 * tile + (lane & 15);
     const long long state = static_cast<long long>(slice) * D * D;
     StateColumns<D> dS;
     dS.load(a.dfinal_state == nullptr ? nullptr : a.dfinal_state + state, col, lane);
     dS.cut_all();
     ColumnTile<E> g;
-    g.load(G, a.stride_row, last, existing(a.N, last), col, lane);
+    g.load(s.of(a.dO, last, a.stride_row), a.stride_row, ~0u, col, lane);
     const Live lives(a, s);
     uint32_t live = lives.bits(lives.fetch(last, lane), last);
     lds_barrier();
@@ -79,7 +78,7 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel
       const uint8_t byte = lives.fetch(c > 0 ? c - 1 : 0, lane);
       const Pieces<E::kPieces> up = cut_elements<E>(g.tile(0), g.tile(1));
       const Pieces<3> write = cut(g.tile(0) * by_rows(coef + B::kQuery, 0, lane), g.tile(1) * by_rows(coef + B::kQuery, 1, lane));
-      if (c > 0) g.load(G, a.stride_row, c - 1, ~0u, col, lane);
+      if (c > 0) g.load(s.of(a.dO, c - 1, a.stride_row), a.stride_row, ~0u, col, lane);
       f32x4_t z[2];
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
@@ -91,15 +90,15 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel
       const Pieces<3> y = cut(z[0], z[1]);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) z[tt] = mul(triangle_operand(at + B::kT, tt, lane), y, f32x4_t{0, 0, 0, 0});
+      store_rows<D>(a.rows_z + chunk * kChunk * D, z, col, lane);
+      const __amdgpu_buffer_rsrc_t dV = s.of(a.dV, c, a.stride_row);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
         const f32x4_t beta = by_rows(coef + B::kBeta, tt, lane);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          const int t = 16 * tt + 4 * (lane >> 4) + r, row = kChunk * c + t;
-          a.rows_z[(chunk * kChunk + t) * D + col] = z[tt][r];
-          E::store_one(dV, row < a.N ? static_cast<uint32_t>(row) * a.stride_row + col * E::kBytes : kNowhere,
-                       ((live >> t) & 1u) ? beta[r] * z[tt][r] : 0.0f);
+          const int t = 16 * tt + 4 * (lane >> 4) + r;
+          E::store_one(dV, static_cast<uint32_t>(t) * a.stride_row + col * E::kBytes, ((live >> t) & 1u) ? beta[r] * z[tt][r] : 0.0f);
         }
       }
       const float whole = coef[B::kWhole];
@@ -276,7 +275,7 @@ __global__ __launch_bounds__(64 * (D / 16), D == 128 ? 2 : 3) void chunk_gradien
   const Slice s(a, slice, D * E::kBytes);
   const Live lives(a, s);
   const uint32_t live = lives.bits(lives.fetch(c, lane), c), there = existing(a.N, c);
-  const __amdgpu_buffer_rsrc_t Q = s.of(a.Q), K = s.of(a.K), V = s.of(a.V);
+  const __amdgpu_buffer_rsrc_t Q = s.of(a.Q, c, a.stride_row), K = s.of(a.K, c, a.stride_row), V = s.of(a.V, c, a.stride_row);
   Tokens& n = *reinterpret_cast<Tokens*>(smem + L::kNotes + wave * sizeof(Tokens));
 
   // K, Q, dO, U, Z: a wave brings 16 rows of 32 columns of each (d = 16: all of them), everything at once
@@ -285,17 +284,16 @@ __global__ __launch_bounds__(64 * (D / 16), D == 128 ? 2 : 3) void chunk_gradien
   F32::Raw wide[kUnits][2];
   const int kb0 = kWaves == 1 ? 0 : wave >> 1;
   const uint32_t state_rows = kChunk * D * 4;
-  const __amdgpu_buffer_rsrc_t rows_u = __builtin_amdgcn_make_buffer_rsrc(a.rows_u + static_cast<long long>(chunk) * kChunk * D, 0, state_rows, 0x00020000);
-  const __amdgpu_buffer_rsrc_t rows_z = __builtin_amdgcn_make_buffer_rsrc(a.rows_z + static_cast<long long>(chunk) * kChunk * D, 0, state_rows, 0x00020000);
+  const __amdgpu_buffer_rsrc_t rows_u = buffer(a.rows_u + static_cast<long long>(chunk) * kChunk * D, state_rows);
+  const __amdgpu_buffer_rsrc_t rows_z = buffer(a.rows_z + static_cast<long long>(chunk) * kChunk * D, state_rows);
 #pragma unroll
   for (int u = 0; u < kUnits; ++u) {
     const int row = 16 * (kWaves == 1 ? u : wave & 1) + c16, col = 32 * kb0 + 8 * gr;
     const bool inside = D >= 32 || col < D;
-    const uint32_t off = static_cast<uint32_t>(kChunk * c + row) * a.stride_row + col * E::kBytes;
-    const bool query = inside && ((there >> row) & 1u), key = inside && ((live >> row) & 1u);
-    raw[u][0] = E::load(K, key ? off : kNowhere);
-    raw[u][1] = E::load(Q, query ? off : kNowhere);
-    raw[u][2] = E::load(s.of(a.dO), query ? off : kNowhere);
+    const uint32_t off = inside ? static_cast<uint32_t>(row) * a.stride_row + col * E::kBytes : kNowhere;
+    raw[u][0] = E::load(K, offset_if(live, row, off));
+    raw[u][1] = E::load(Q, off);
+    raw[u][2] = E::load(s.of(a.dO, c, a.stride_row), off);
     wide[u][0] = F32::load(rows_u, inside ? (row * D + col) * 4 : kNowhere);
     wide[u][1] = F32::load(rows_z, inside ? (row * D + col) * 4 : kNowhere);
   }
@@ -311,10 +309,10 @@ __global__ __launch_bounds__(64 * (D / 16), D == 128 ? 2 : 3) void chunk_gradien
 #pragma unroll
   for (int tt = 0; tt < 2; ++tt) {
     const int t = 16 * tt + c16;
-    off[tt] = static_cast<uint32_t>(kChunk * c + t) * a.stride_row + (16 * wave + 4 * gr) * E::kBytes;
-    q[tt] = E::load_four(Q, ((there >> t) & 1u) ? off[tt] : kNowhere);
-    k[tt] = E::load_four(K, ((live >> t) & 1u) ? off[tt] : kNowhere);
-    zv[tt] = E::load_four(V, ((live >> t) & 1u) ? off[tt] : kNowhere) * F32::load_four(rows_z, (t * D + 16 * wave + 4 * gr) * 4);
+    off[tt] = static_cast<uint32_t>(t) * a.stride_row + (16 * wave + 4 * gr) * E::kBytes;
+    q[tt] = E::load_four(Q, off[tt]);
+    k[tt] = E::load_four(K, offset_if(live, t, off[tt]));
+    zv[tt] = E::load_four(V, offset_if(live, t, off[tt])) * F32::load_four(rows_z, (t * D + 16 * wave + 4 * gr) * 4);
   }
   float* squares = reinterpret_cast<float*>(smem + L::kSquares);
 #pragma unroll
@@ -491,9 +489,8 @@ __global__ __launch_bounds__(64 * (D / 16), D == 128 ? 2 : 3) void chunk_gradien
       y[r] = (fmaf(b, p[tt][r], w[tt][r]) - k[tt][r] * kd) * rk;
       y[r] = ((live >> t) & 1u) ? y[r] : 0.0f;
     }
-    const uint32_t to = ((there >> t) & 1u) ? off[tt] : kNowhere;
-    E::store_four(s.of(a.dQ), to, x);
-    E::store_four(s.of(a.dK), to, y);
+    E::store_four(s.of(a.dQ, c, a.stride_row), off[tt], x);
+    E::store_four(s.of(a.dK, c, a.stride_row), off[tt], y);
   }
   if (wave == kWaves - 1) {
     const int t = lane & 31;

@@ -23,16 +23,17 @@ struct KeyProducer {
   typedef ChunkBuffer<E, D> B;
   const Args& a;
   const Live lives;
-  const __amdgpu_buffer_rsrc_t K, decays, betas;
+  const Slice& s;
+  const __amdgpu_buffer_rsrc_t decays, betas;
   RowTile<E, D> k;
   uint32_t live, g, beta;  // (gates as they were loaded)
   uint8_t byte;
 
-  __device__ __forceinline__ KeyProducer(const Args& args, const Slice& s)
-      : a(args), lives(args, s), K(s.of(args.K)), decays(s.of_gate(args, args.g)), betas(s.of_gate(args, args.beta)) {}
+  __device__ __forceinline__ KeyProducer(const Args& args, const Slice& slice)
+      : a(args), lives(args, slice), s(slice), decays(slice.of_gate(args, args.g)), betas(slice.of_gate(args, args.beta)) {}
   __device__ __forceinline__ void fetch(int chunk, int lane) {
     live = lives.bits(byte, chunk);
-    k.load(K, a.stride_row, chunk, live, lane);
+    k.load(s.of(a.K, chunk, a.stride_row), a.stride_row, live, lane);
     g = fetch_gate(a, decays, chunk, live, lane);
     beta = fetch_gate(a, betas, chunk, live, lane);
   }
@@ -111,18 +112,19 @@ struct QueryProducer {
   typedef ChunkBuffer<E, D> B;
   const Args& a;
   const Live lives;
-  const __amdgpu_buffer_rsrc_t Q, K, decays;
+  const Slice& s;
+  const __amdgpu_buffer_rsrc_t decays;
   RowTile<E, D> q, k;
   uint32_t live, there, g;  // keys that take part; rows that exist
   uint8_t byte;
 
-  __device__ __forceinline__ QueryProducer(const Args& args, const Slice& s)
-      : a(args), lives(args, s), Q(s.of(args.Q)), K(s.of(args.K)), decays(s.of_gate(args, args.g)) {}
+  __device__ __forceinline__ QueryProducer(const Args& args, const Slice& slice)
+      : a(args), lives(args, slice), s(slice), decays(slice.of_gate(args, args.g)) {}
   __device__ __forceinline__ void fetch(int chunk, int lane) {
     live = lives.bits(byte, chunk);
     there = existing(a.N, chunk);
-    q.load(Q, a.stride_row, chunk, there, lane);
-    k.load(K, a.stride_row, chunk, live, lane);
+    q.load(s.of(a.Q, chunk, a.stride_row), a.stride_row, ~0u, lane);
+    k.load(s.of(a.K, chunk, a.stride_row), a.stride_row, live, lane);
     g = fetch_gate(a, decays, chunk, live, lane);
   }
   __device__ __forceinline__ void begin(int chunk, int next, int lane) {
@@ -177,15 +179,14 @@ struct QueryProducer {
 template <class E>
 struct ColumnTile {
   typename E::One x[2][4];
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t stride, int chunk, uint32_t live, int col, int lane) {
+  // r: from the chunk's first row on
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t stride, uint32_t live, int col, int lane) {
+    const uint32_t first = 4 * (lane >> 4) * stride + col * E::kBytes;
+    const uint32_t of_lane = live >> (4 * (lane >> 4));
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int row = 16 * tt + 4 * (lane >> 4) + i;
-        const uint32_t off = static_cast<uint32_t>(kChunk * chunk + row) * stride + col * E::kBytes;
-        x[tt][i] = E::load_one(r, ((live >> row) & 1u) ? off : kNowhere);
-      }
+      for (int i = 0; i < 4; ++i) x[tt][i] = E::load_one(r, offset_if(of_lane, 16 * tt + i, first + (16 * tt + i) * stride));
   }
   __device__ __forceinline__ f32x4_t tile(int tt) const { return f32x4_t{E::value(x[tt][0]), E::value(x[tt][1]), E::value(x[tt][2]), E::value(x[tt][3])}; }
 };
@@ -196,24 +197,42 @@ struct StateColumns {
   static constexpr int kTiles = D / 16, kBlocks = D < 32 ? 1 : D / 32;
   f32x4_t s[kBlocks * 2];
   Pieces<3> p[kBlocks];
-  __device__ __forceinline__ void load(const float* from, int col, int lane) {  // from: [D][D] or nullptr
+  static __device__ __forceinline__ __amdgpu_buffer_rsrc_t of(const float* state) {  // [D][D]; nullptr: loads bring zeros
+    return buffer(state, state == nullptr ? 0 : D * D * 4);
+  }
+  __device__ __forceinline__ void load(const float* from, int col, int lane) {
+    const __amdgpu_buffer_rsrc_t r = of(from);
+    const uint32_t first = (4 * (lane >> 4) * D + col) * 4;
 #pragma unroll
     for (int dt = 0; dt < 2 * kBlocks; ++dt)
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-        s[dt][r] = dt < kTiles && from != nullptr ? from[(16 * dt + 4 * (lane >> 4) + r) * D + col] : 0.0f;
+      for (int i = 0; i < 4; ++i)
+        s[dt][i] = dt < kTiles ? __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, first + (16 * dt + i) * D * 4, 0, 0)) : 0.0f;
   }
   __device__ __forceinline__ void store(float* to, int col, int lane) const {
+    const __amdgpu_buffer_rsrc_t r = of(to);
+    const uint32_t first = (4 * (lane >> 4) * D + col) * 4;
 #pragma unroll
     for (int dt = 0; dt < kTiles; ++dt)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) to[(16 * dt + 4 * (lane >> 4) + r) * D + col] = s[dt][r];
+      for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(s[dt][i]), r, first + (16 * dt + i) * D * 4, 0, 0);
   }
   __device__ __forceinline__ void cut_all() {
 #pragma unroll
     for (int kb = 0; kb < kBlocks; ++kb) p[kb] = cut(s[2 * kb], s[2 * kb + 1]);
   }
 };
+
+// A pair of result tiles (tokens 16 tt + 4g + r, column `col`) into the rows of a chunk [32][D].
+template <int D>
+__device__ __forceinline__ void store_rows(float* to, const f32x4_t (&x)[2], int col, int lane) {
+  const __amdgpu_buffer_rsrc_t r = buffer(to, kChunk * D * 4);
+  const uint32_t first = (4 * (lane >> 4) * D + col) * 4;
+#pragma unroll
+  for (int tt = 0; tt < 2; ++tt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[tt][i]), r, first + (16 * tt + i) * D * 4, 0, 0);
+}
 
 __device__ __forceinline__ f32x4_t by_rows(const float* coef, int tt, int lane) {
   return *reinterpret_cast<const f32x4_t*>(coef + 16 * tt + 4 * (lane >> 4));

@@ -243,6 +243,15 @@ struct Args {
   float scale, eps;
 };
 
+// A buffer of `bytes` from `base`, which are the same in all lanes: kept in scalar registers (left to itself the compiler
+// has put descriptors made inside a loop into vector registers, and a loop over lanes around every load).
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const void* base, uint32_t bytes) {
+  const uint64_t p = reinterpret_cast<uint64_t>(base);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<int>(p)), hi = __builtin_amdgcn_readfirstlane(static_cast<int>(p >> 32));
+  return __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<void*>((static_cast<uint64_t>(hi) << 32) | lo), 0,
+                                           __builtin_amdgcn_readfirstlane(static_cast<int>(bytes)), 0x00020000);
+}
+
 // What a wave knows of its slice.
 struct Slice {
   long long rows;       // byte offset of row 0 in Q, K, V, O ...
@@ -257,10 +266,16 @@ struct Slice {
     bytes = static_cast<uint32_t>(a.N - 1) * a.stride_row + row_bytes;
   }
   __device__ __forceinline__ __amdgpu_buffer_rsrc_t of(const unsigned char* base) const {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<unsigned char*>(base) + rows, 0, bytes, 0x00020000);
+    return buffer(base + rows, bytes);
+  }
+  // from a chunk's first row on: a lane's offsets are the same in every chunk, and rows beyond the sequence are beyond the
+  // buffer (loads bring zeros, stores are dropped)
+  __device__ __forceinline__ __amdgpu_buffer_rsrc_t of(const unsigned char* base, int chunk, uint32_t stride) const {
+    const uint32_t skip = static_cast<uint32_t>(kChunk * chunk) * stride;
+    return buffer(base + rows + skip, skip < bytes ? bytes - skip : 0);
   }
   __device__ __forceinline__ __amdgpu_buffer_rsrc_t of_gate(const Args& a, const float* base) const {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(base) + gates, 0, ((a.N - 1) * a.gate_row + 1) * 4, 0x00020000);
+    return buffer(base + gates, ((a.N - 1) * a.gate_row + 1) * 4);
   }
 };
 
@@ -270,7 +285,7 @@ struct Live {
   bool all;
   int N;
   __device__ __forceinline__ Live(const Args& a, const Slice& s)
-      : mask(__builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(s.mask), 0, s.mask == nullptr ? 0 : a.N, 0x00020000)),
+      : mask(buffer(s.mask, s.mask == nullptr ? 0 : a.N)),
         all(s.mask == nullptr),
         N(a.N) {}
   // of token 32 * chunk + lane%32 (beyond the sequence: 0)
@@ -295,6 +310,9 @@ __device__ __forceinline__ uint32_t fetch_gate(const Args& a, __amdgpu_buffer_rs
   const uint32_t off = static_cast<uint32_t>(kChunk * chunk + (lane & 31)) * a.gate_row * 4;
   return __builtin_amdgcn_raw_buffer_load_b32(r, ((live >> (lane & 31)) & 1u) ? off : kNowhere, 0, 0);
 }
+
+// An offset, or one beyond every buffer where the token of the chunk takes no part.
+__device__ __forceinline__ uint32_t offset_if(uint32_t live, int token, uint32_t off) { return ((~live >> token) << 31) | off; }
 
 // ---- decays -----------------------------------------------------------------------------------------------------
 
@@ -443,16 +461,15 @@ template <class E, int D>
 struct RowTile {
   static constexpr int kBlocks = Rows<D, E::kPieces>::kBlocks;
   typename E::Raw raw[2][kBlocks];
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t stride, int chunk, uint32_t live, int lane) {
+  // r: from the chunk's first row on
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t r, uint32_t stride, uint32_t live, int lane) {
 #pragma unroll
     for (int tt = 0; tt < 2; ++tt) {
       const int row = 16 * tt + (lane & 15);
-      const uint32_t off = static_cast<uint32_t>(kChunk * chunk + row) * stride + (lane >> 4) * 8 * E::kBytes;
+      const uint32_t off = static_cast<uint32_t>(row) * stride + (lane >> 4) * 8 * E::kBytes;
+      const uint32_t at = offset_if(live, row, D >= 32 || (lane >> 4) * 8 < D ? off : kNowhere);
 #pragma unroll
-      for (int kb = 0; kb < kBlocks; ++kb) {
-        const bool there = ((live >> row) & 1u) != 0 && (D >= 32 || (lane >> 4) * 8 < D);
-        raw[tt][kb] = E::load(r, there ? off + kb * 32 * E::kBytes : kNowhere);
-      }
+      for (int kb = 0; kb < kBlocks; ++kb) raw[tt][kb] = E::load(r, at + kb * 32 * E::kBytes);
     }
   }
   __device__ __forceinline__ Pieces<E::kPieces> operand(int tt, int kb) const { return E::pieces(raw[tt][kb]); }
