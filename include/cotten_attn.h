@@ -268,8 +268,9 @@ typedef struct cotten_delta_params {
   float scale;                /* factor of O; <= 0 selects 1                                     */
   float eps;                  /* inside the square roots; < 0 selects 1e-6; 0 allowed            */
   int layout;                 /* a cotten_layout                                                 */
-  void* workspace;            /* backward: device buffer of cotten_delta_workspace_bytes(), 16-byte
-                                 aligned.  Forward: not looked at                                */
+  void* workspace;            /* device buffer of cotten_delta_workspace_bytes(), 16-byte aligned;
+                                 may be NULL where that is 0 (any forward but those of few and
+                                 long sequences without kept)                                    */
   size_t workspace_bytes;
   const float* initial_state; /* device, [B*H, d_h, d_h], or NULL: zeros                         */
   float* final_state;         /* forward: receives the state after row N-1, or NULL.  May be
@@ -296,8 +297,8 @@ int cotten_delta_bwd(const void* Q, const void* K, const void* V, const float* g
                      float* dbeta, int B, int H, int N, int d_h, void* stream,
                      const cotten_delta_params* params);
 
-/* Bytes of params->kept, and of params->workspace (0 for the forward; with_kept: the backward is given params->kept).
- * They grow like N * d_h * (d_h / 32 + 1).  0 for invalid arguments; host only. */
+/* Bytes of params->kept, and of params->workspace (with_kept: the call is given params->kept).
+ * They grow like N * d_h * (d_h / 32 + 1), a forward's workspace like d_h * d_h.  0 for invalid arguments; host only. */
 size_t cotten_delta_kept_bytes(int B, int H, int N, int d_h, int dtype);
 size_t cotten_delta_workspace_bytes(int B, int H, int N, int d_h, int dtype, int is_bwd, int with_kept);
 

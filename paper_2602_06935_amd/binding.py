@@ -440,7 +440,8 @@ def _delta_params(Q, g, beta, dims, gates, scale, eps, layout, workspace, initia
 def cotten_delta_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor, beta: torch.Tensor,
                      mask: Optional[torch.Tensor], O: Optional[torch.Tensor] = None, *,
                      scale: Optional[float] = None, eps: Optional[float] = None, stream=None,
-                     layout: str = "bhnd", initial_state: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None, layout: str = "bhnd",
+                     initial_state: Optional[torch.Tensor] = None,
                      final_state: Optional[torch.Tensor] = None,
                      kept: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Gated delta rule: S_t = a_t S_{t-1} + khat_t u_t^T with u_t = beta_t (v_t - a_t S_{t-1}^T khat_t) and a_t =
@@ -452,11 +453,16 @@ def cotten_delta_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch
     _prep_like(Q, (("K", K), ("V", V)))
     dims = _dims(Q, layout)
     O = torch.empty_like(Q) if O is None else _prep("O", O, Q)
-    prm = _delta_params(Q, g, beta, dims, (("g", g), ("beta", beta)), scale, eps, layout, None, initial_state,
+    handle = _stream_handle(stream)
+    if workspace is None and kept is None:
+        need = cotten_delta_workspace_bytes(*dims, _dtype_code(Q), False)
+        if need != 0:
+            workspace = _workspace(Q, need, handle)
+    prm = _delta_params(Q, g, beta, dims, (("g", g), ("beta", beta)), scale, eps, layout, workspace, initial_state,
                         final_state, None, None, kept)
     _on_device(Q.device, lib.cotten_delta_fwd, Q.data_ptr(), K.data_ptr(), V.data_ptr(), g.data_ptr(),
-               beta.data_ptr(), _mask_ptr(mask, dims[0], dims[2], Q.device), O.data_ptr(), *dims,
-               _stream_handle(stream), ctypes.byref(prm))
+               beta.data_ptr(), _mask_ptr(mask, dims[0], dims[2], Q.device), O.data_ptr(), *dims, handle,
+               ctypes.byref(prm))
     return O
 
 

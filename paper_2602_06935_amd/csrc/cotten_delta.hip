@@ -97,51 +97,74 @@ __global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
 template <int D>
 constexpr int kConsumers = D / 16 < 4 ? D / 16 : 4;  // of a workgroup; d = 128 takes two (of ten waves, none would have the registers)
 
-// OUT: O is wanted; KEPT: what a backward needs is.
-template <class E, int D, bool OUT, bool KEPT>
+// What a walk is for: O; O and what a backward needs; the latter alone; a segment's R or M (see segments_of).
+enum Walk { kOutput, kTraining, kStates, kTransition };
+
+template <class E, int D, Walk WALK>
 __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Args a) {
-  typedef ChunkBuffer<E, D> B;
+  constexpr bool kOut = WALK == kOutput || WALK == kTraining;
+  typedef ChunkBuffer<E, D, kOut> B;
   typedef typename B::R R;
+  constexpr bool kKept = WALK == kTraining || WALK == kStates;
+  constexpr int kGroups = D / 16 / kConsumers<D>, kProducers = kOut ? 2 : 1;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  constexpr int kGroups = D / 16 / kConsumers<D>;
-  const int slice = blockIdx.x / kGroups, group = blockIdx.x % kGroups;
+  const int unit = blockIdx.x / kGroups, group = blockIdx.x % kGroups;
+  // transitions: R of segments 0 ... count - 2, then M of 1 ... count - 2
+  const int walked = WALK == kTransition ? 2 * a.segments - 3 : a.segments;
+  const int slice = unit / walked;
+  int segment = unit - slice * walked;
+  const bool is_m = WALK == kTransition && segment > a.segments - 2;
+  if (is_m) segment -= a.segments - 2;
   const Slice s(a, slice, D * E::kBytes);
   Scratch* scratch = reinterpret_cast<Scratch*>(smem + 2 * B::kBytes);
   Notes* notes = reinterpret_cast<Notes*>(scratch + 1);
+  const int first = segment * a.segment_chunks;
+  const int end = first + a.segment_chunks < a.chunks ? first + a.segment_chunks : a.chunks;
 
   if (wave == 0) {
-    KeyProducer<E, D, false> producer(a, s);
-    producer.begin(0, 1, lane);
-    for (int c = 0; c <= a.chunks; ++c) {
-      if (c < a.chunks) producer.make(c + 1, c + 2, smem + (c & 1) * B::kBytes, scratch, lane);
+    KeyProducer<E, D, false, kOut> producer(a, s);
+    producer.begin(first, first + 1, lane);
+    for (int c = first; c <= end; ++c) {
+      if (c < end) producer.make(c + 1, c + 2, smem + (c & 1) * B::kBytes, scratch, lane);
       lds_barrier();
     }
-  } else if (wave == 1) {
-    if (!OUT) {
-      for (int c = 0; c <= a.chunks; ++c) lds_barrier();
-      return;
-    }
+  } else if (kOut && wave == 1) {
     QueryProducer<E, D, false> producer(a, s);
-    producer.begin(0, 1, lane);
-    for (int c = 0; c <= a.chunks; ++c) {
-      if (c < a.chunks) producer.make(c + 1, c + 2, smem + (c & 1) * B::kBytes, notes, lane);
+    producer.begin(first, first + 1, lane);
+    for (int c = first; c <= end; ++c) {
+      if (c < end) producer.make(c + 1, c + 2, smem + (c & 1) * B::kBytes, notes, lane);
       lds_barrier();
     }
   } else {
-    const int tile = group * kConsumers<D> + wave - 2, col = 16 * tile + (lane & 15);
+    const int tile = group * kConsumers<D> + wave - kProducers, col = 16 * tile + (lane & 15);
+    const long long of_segment = static_cast<long long>(slice) * a.segments;
     StateColumns<D> S;
-    S.load(a.initial_state == nullptr ? nullptr : a.initial_state + static_cast<long long>(slice) * D * D, col, lane);
+    if (is_m) {
+      S.unit(col, lane);
+    } else if (segment == 0) {
+      S.load(a.initial_state == nullptr ? nullptr : a.initial_state + static_cast<long long>(slice) * D * D, col, lane);
+    } else if (WALK == kTransition) {
+      S.load(nullptr, col, lane);
+    } else {  // from the segments before: the first one's R has the initial state in it
+      S.load(a.transitions + of_segment * 2 * D * D, col, lane);
+      S.cut_all();
+      for (int j = 1; j < segment; ++j) {
+        const float* R = a.transitions + (of_segment + j) * 2 * D * D;
+        advance<D, false>(S, R + D * D, R, col, lane);
+      }
+    }
     S.cut_all();
     ColumnTile<E> v;
     const Live lives(a, s);
-    v.load(s.of(a.V, 0, a.stride_row), a.stride_row, lives.bits(lives.fetch(0, lane), 0), col, lane);
-    uint8_t byte = lives.fetch(1, lane);
+    const uint32_t with_v = is_m ? 0u : ~0u;
+    v.load(s.of(a.V, first, a.stride_row), a.stride_row, with_v & lives.bits(lives.fetch(first, lane), first), col, lane);
+    uint8_t byte = lives.fetch(first + 1, lane);
     lds_barrier();
-    for (int c = 0; c < a.chunks; ++c) {
+    for (int c = first; c < end; ++c) {
       const unsigned char* at = smem + (c & 1) * B::kBytes;
       const float* coef = reinterpret_cast<const float*>(at + B::kCoef);
       const long long chunk = static_cast<long long>(slice) * a.chunks + c;
-      if (KEPT) S.store(a.states + chunk * D * D, col, lane);
+      if (kKept) S.store(a.states + chunk * D * D, col, lane);
       // beta (V - e^G K^ S)
       f32x4_t u[2];
 #pragma unroll
@@ -151,15 +174,15 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Arg
         for (int kb = 0; kb < S.kBlocks; ++kb) p = mul(R::row_operand(at + B::kK, tt, kb, lane), S.p[kb], p);
         u[tt] = by_rows(coef + B::kBeta, tt, lane) * (v.tile(tt) - by_rows(coef + B::kReadK, tt, lane) * p);
       }
-      if (c + 1 < a.chunks) {
-        v.load(s.of(a.V, c + 1, a.stride_row), a.stride_row, lives.bits(byte, c + 1), col, lane);
+      if (c + 1 < end) {
+        v.load(s.of(a.V, c + 1, a.stride_row), a.stride_row, with_v & lives.bits(byte, c + 1), col, lane);
         byte = lives.fetch(c + 2, lane);
       }
       const Pieces<3> y = cut(u[0], u[1]);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) u[tt] = mul(triangle_operand(at + B::kT, tt, lane), y, f32x4_t{0, 0, 0, 0});
-      if (KEPT) store_rows<D>(a.rows_u + chunk * kChunk * D, u, col, lane);
-      if (OUT) {
+      if (kKept) store_rows<D>(a.rows_u + chunk * kChunk * D, u, col, lane);
+      if (kOut) {
         // O^T: a lane has four columns of a token
         const __amdgpu_buffer_rsrc_t O = s.of(a.O, c, a.stride_row);
         const Pieces<3> up = cut(u[0], u[1]);
@@ -181,19 +204,22 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Arg
       S.cut_all();
       lds_barrier();
     }
-    if (a.final_state != nullptr) S.store(a.final_state + static_cast<long long>(slice) * D * D, col, lane);
+    if (WALK == kTransition) S.store(a.transitions + ((of_segment + segment) * 2 + (is_m ? 1 : 0)) * D * D, col, lane);
+    else if (end == a.chunks && a.final_state != nullptr) S.store(a.final_state + static_cast<long long>(slice) * D * D, col, lane);
   }
 }
 
 // Up to this many tokens the recurrence is faster than a chunk.
 constexpr int kMostSteps = 8;
 
-template <class E, int D, bool OUT, bool KEPT>
+template <class E, int D, Walk WALK>
 hipError_t launch_chunks(const Args& a, int slices, hipStream_t stream) {
-  constexpr int kLds = 2 * ChunkBuffer<E, D>::kBytes + sizeof(Scratch) + sizeof(Notes);
-  const auto kernel = chunk_fwd_kernel<E, D, OUT, KEPT>;
+  constexpr bool kOut = WALK == kOutput || WALK == kTraining;
+  constexpr int kLds = 2 * ChunkBuffer<E, D, kOut>::kBytes + sizeof(Scratch) + sizeof(Notes);
+  const auto kernel = chunk_fwd_kernel<E, D, WALK>;
   if (hipError_t err = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds); err != hipSuccess) return err;
-  kernel<<<dim3(slices * (D / 16 / kConsumers<D>)), dim3(64 * (kConsumers<D> + 2)), kLds, stream>>>(a);
+  const int walked = WALK == kTransition ? 2 * a.segments - 3 : a.segments;
+  kernel<<<dim3(slices * walked * (D / 16 / kConsumers<D>)), dim3(64 * (kConsumers<D> + (kOut ? 2 : 1))), kLds, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -207,9 +233,11 @@ hipError_t launch(const Args& a, int slices, hipStream_t stream) {
     step_kernel<E, D><<<dim3(static_cast<uint32_t>((waves + per - 1) / per)), dim3(64 * per), 0, stream>>>(a, slices);
     return hipGetLastError();
   }
-  return !out   ? launch_chunks<E, D, false, true>(a, slices, stream)
-         : kept ? launch_chunks<E, D, true, true>(a, slices, stream)
-                : launch_chunks<E, D, true, false>(a, slices, stream);
+  if (a.segments > 1)
+    if (hipError_t err = launch_chunks<E, D, kTransition>(a, slices, stream); err != hipSuccess) return err;
+  return !out   ? launch_chunks<E, D, kStates>(a, slices, stream)
+         : kept ? launch_chunks<E, D, kTraining>(a, slices, stream)
+                : launch_chunks<E, D, kOutput>(a, slices, stream);
 }
 
 template <class E>
@@ -223,6 +251,19 @@ hipError_t launch_dim(const Args& a, int D, int slices, hipStream_t stream) {
 }
 
 }  // namespace
+
+Segments segments_of(long long slices, int chunks, int D) {
+  // about two workgroups for each of the 256 compute units; not more segments than make up for the steps M S + R over them
+  // (one takes about as long as half a chunk in each of the two launches); with fewer than four the first launch takes
+  // what the second saves
+  constexpr int kWorkgroups = 512, kFewest = 4;
+  const long long groups = slices * (D > 64 ? D / 64 : 1);
+  long long count = kWorkgroups / groups < chunks ? kWorkgroups / groups : chunks;
+  while (count * count > 2ll * chunks) --count;
+  if (count < kFewest) return Segments{1, chunks};
+  const int each = static_cast<int>((chunks + count - 1) / count);
+  return Segments{(chunks + each - 1) / each, each};
+}
 
 hipError_t launch_forward(const Args& a, int dtype, int D, int slices, hipStream_t stream) {
   return dtype == 0 ? launch_dim<F32>(a, D, slices, stream)

@@ -20,15 +20,23 @@ int check_shape(int B, int H, int N, int d_h, int dtype) {
   return COTTEN_OK;
 }
 
-// Floats of the state before (or the gradient after) every chunk, and of a row per token behind them.
+// Floats of the buffers: the state before (or the gradient after) every chunk, a row per token; and, where sequences are
+// cut into segments, what each makes of a state (forward) and the gradient before each (backward).
 struct Sizes {
-  size_t states, rows;
+  size_t states, rows, transitions, carries;
+  cotten::delta::Segments segments;
   Sizes(int B, int H, int N, int d_h) {
+    const size_t slices = static_cast<size_t>(B) * H, state = static_cast<size_t>(d_h) * d_h;
     const size_t chunks = (static_cast<size_t>(N) + cotten::delta::kChunk - 1) / cotten::delta::kChunk;
-    states = static_cast<size_t>(B) * H * chunks * d_h * d_h;
-    rows = static_cast<size_t>(B) * H * chunks * cotten::delta::kChunk * d_h;
+    segments = cotten::delta::segments_of(static_cast<long long>(slices), static_cast<int>(chunks), d_h);
+    states = slices * chunks * state;
+    rows = slices * chunks * cotten::delta::kChunk * d_h;
+    carries = segments.count > 1 ? slices * segments.count * state : 0;
+    transitions = 2 * carries;
   }
-  size_t bytes() const { return (states + rows) * sizeof(float); }
+  size_t kept() const { return (states + rows + transitions) * sizeof(float); }
+  size_t backward(bool with_kept) const { return (states + rows + carries) * sizeof(float) + (with_kept ? 0 : kept()); }
+  size_t forward(bool with_kept) const { return with_kept ? 0 : transitions * sizeof(float); }
 };
 
 // Checks what both directions share and fills the arguments.
@@ -73,17 +81,24 @@ int prepare(cotten::delta::Args* a, const void* Q, const void* K, const void* V,
   return COTTEN_OK;
 }
 
+void use_kept(cotten::delta::Args* a, float* at, const Sizes& size) {
+  a->states = at;
+  a->rows_u = at + size.states;
+  a->transitions = a->rows_u + size.rows;
+}
+
 }  // namespace
 
 extern "C" {
 
 size_t cotten_delta_kept_bytes(int B, int H, int N, int d_h, int dtype) {
-  return check_shape(B, H, N, d_h, dtype) == COTTEN_OK ? Sizes(B, H, N, d_h).bytes() : 0;
+  return check_shape(B, H, N, d_h, dtype) == COTTEN_OK ? Sizes(B, H, N, d_h).kept() : 0;
 }
 
 size_t cotten_delta_workspace_bytes(int B, int H, int N, int d_h, int dtype, int is_bwd, int with_kept) {
-  if (check_shape(B, H, N, d_h, dtype) != COTTEN_OK || !is_bwd) return 0;
-  return Sizes(B, H, N, d_h).bytes() * (with_kept ? 1 : 2);
+  if (check_shape(B, H, N, d_h, dtype) != COTTEN_OK) return 0;
+  const Sizes size(B, H, N, d_h);
+  return is_bwd ? size.backward(with_kept != 0) : size.forward(with_kept != 0);
 }
 
 int cotten_delta_fwd(const void* Q, const void* K, const void* V, const float* g, const float* beta, const uint8_t* mask,
@@ -94,11 +109,15 @@ int cotten_delta_fwd(const void* Q, const void* K, const void* V, const float* g
   if (!aligned16(O)) return COTTEN_ERR_MISALIGNED;
   a.O = static_cast<unsigned char*>(O);
   a.final_state = params->final_state;
+  const Sizes size(B, H, N, d_h);
+  a.segments = size.segments.count;
+  a.segment_chunks = size.segments.chunks;
   if (params->kept != nullptr) {
-    const Sizes size(B, H, N, d_h);
-    if (params->kept_bytes < size.bytes()) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
-    a.states = static_cast<float*>(params->kept);
-    a.rows_u = a.states + size.states;
+    if (params->kept_bytes < size.kept()) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
+    use_kept(&a, static_cast<float*>(params->kept), size);
+  } else if (size.transitions != 0) {
+    if (params->workspace == nullptr || params->workspace_bytes < size.forward(false)) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
+    a.transitions = static_cast<float*>(params->workspace);
   }
   return cotten::delta::launch_forward(a, params->dtype, d_h, B * H, static_cast<hipStream_t>(stream)) == hipSuccess
              ? COTTEN_OK
@@ -115,14 +134,15 @@ int cotten_delta_bwd(const void* Q, const void* K, const void* V, const float* g
   if (!aligned16(dO) || !aligned16(dQ) || !aligned16(dK) || !aligned16(dV)) return COTTEN_ERR_MISALIGNED;
   if ((reinterpret_cast<uintptr_t>(dg) | reinterpret_cast<uintptr_t>(dbeta)) & 3u) return COTTEN_ERR_MISALIGNED;
   const Sizes size(B, H, N, d_h);
+  a.segments = size.segments.count;
+  a.segment_chunks = size.segments.chunks;
   const bool kept = params->kept != nullptr;
-  if (kept && params->kept_bytes < size.bytes()) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
-  if (params->workspace == nullptr || params->workspace_bytes < size.bytes() * (kept ? 1 : 2))
-    return COTTEN_ERR_WORKSPACE_TOO_SMALL;
+  if (kept && params->kept_bytes < size.kept()) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
+  if (params->workspace == nullptr || params->workspace_bytes < size.backward(kept)) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
   a.dstates = static_cast<float*>(params->workspace);
   a.rows_z = a.dstates + size.states;
-  a.states = kept ? static_cast<float*>(params->kept) : a.rows_z + size.rows;
-  a.rows_u = a.states + size.states;
+  a.carries = a.rows_z + size.rows;
+  use_kept(&a, kept ? static_cast<float*>(params->kept) : a.carries + size.carries, size);
   const hipStream_t s = static_cast<hipStream_t>(stream);
   if (!kept && cotten::delta::launch_forward(a, params->dtype, d_h, B * H, s) != hipSuccess) return COTTEN_ERR_LAUNCH;
   a.dO = static_cast<const unsigned char*>(dO);

@@ -32,53 +32,66 @@ template <int D>
 constexpr int kConsumers = D / 16 < 4 ? D / 16 : 4;
 
 // The forward's walk in reverse: two producers, and waves with 16 columns of dS each.  Writes dS' and Z for the second
-// kernel, and dV.
-template <class E, int D>
+// kernel, and dV.  CARRY: only the gradient of the state before a segment, of segments 1 ...
+template <class E, int D, bool CARRY>
 __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel(Args a) {
-  typedef ChunkBuffer<E, D> B;
+  typedef ChunkBuffer<E, D, true> B;
   typedef typename B::R R;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   constexpr int kGroups = D / 16 / kConsumers<D>;
-  const int slice = blockIdx.x / kGroups, group = blockIdx.x % kGroups;
+  const int unit = blockIdx.x / kGroups, group = blockIdx.x % kGroups;
+  const int walked = CARRY ? a.segments - 1 : a.segments;
+  const int slice = unit / walked, segment = unit - slice * walked + (CARRY ? 1 : 0);
   const Slice s(a, slice, D * E::kBytes);
   Scratch* scratch = reinterpret_cast<Scratch*>(smem + 2 * B::kBytes);
   Notes* notes = reinterpret_cast<Notes*>(scratch + 1);
-  const int last = a.chunks - 1;
+  const int first = segment * a.segment_chunks;
+  const int last = (first + a.segment_chunks < a.chunks ? first + a.segment_chunks : a.chunks) - 1;
 
   if (wave == 0) {
-    KeyProducer<E, D, true> producer(a, s);
+    KeyProducer<E, D, true, true> producer(a, s);
     producer.begin(last, last > 0 ? last - 1 : 0, lane);
-    for (int c = last; c >= -1; --c) {
-      if (c >= 0) producer.make(c - 1, c > 1 ? c - 2 : 0, smem + (c & 1) * B::kBytes, scratch, lane);
+    for (int c = last; c >= first - 1; --c) {
+      if (c >= first) producer.make(c - 1, c > 1 ? c - 2 : 0, smem + (c & 1) * B::kBytes, scratch, lane);
       lds_barrier();
     }
   } else if (wave == 1) {
     QueryProducer<E, D, true> producer(a, s);
     producer.begin(last, last > 0 ? last - 1 : 0, lane);
-    for (int c = last; c >= -1; --c) {
-      if (c >= 0) producer.make(c - 1, c > 1 ? c - 2 : 0, smem + (c & 1) * B::kBytes, notes, lane);
+    for (int c = last; c >= first - 1; --c) {
+      if (c >= first) producer.make(c - 1, c > 1 ? c - 2 : 0, smem + (c & 1) * B::kBytes, notes, lane);
       lds_barrier();
     }
   } else {
     const int tile = group * kConsumers<D> + wave - 2, col = 16 * tile + (lane & 15);
     const long long state = static_cast<long long>(slice) * D * D;
+    const long long of_segment = static_cast<long long>(slice) * a.segments;
     StateColumns<D> dS;
-    dS.load(a.dfinal_state == nullptr ? nullptr : a.dfinal_state + state, col, lane);
+    if (segment == a.segments - 1) {
+      dS.load(a.dfinal_state == nullptr ? nullptr : a.dfinal_state + state, col, lane);
+    } else if (CARRY) {
+      dS.load(nullptr, col, lane);
+    } else {  // from the segments behind: the last one's is whole
+      dS.load(a.carries + (of_segment + a.segments - 1) * D * D, col, lane);
+      dS.cut_all();
+      for (int j = a.segments - 2; j > segment; --j)
+        advance<D, true>(dS, a.transitions + ((of_segment + j) * 2 + 1) * D * D, a.carries + (of_segment + j) * D * D, col, lane);
+    }
     dS.cut_all();
     ColumnTile<E> g;
     g.load(s.of(a.dO, last, a.stride_row), a.stride_row, ~0u, col, lane);
     const Live lives(a, s);
     uint32_t live = lives.bits(lives.fetch(last, lane), last);
     lds_barrier();
-    for (int c = last; c >= 0; --c) {
+    for (int c = last; c >= first; --c) {
       const unsigned char* at = smem + (c & 1) * B::kBytes;
       const float* coef = reinterpret_cast<const float*>(at + B::kCoef);
       const long long chunk = static_cast<long long>(slice) * a.chunks + c;
-      dS.store(a.dstates + chunk * D * D, col, lane);
+      if (!CARRY) dS.store(a.dstates + chunk * D * D, col, lane);
       const uint8_t byte = lives.fetch(c > 0 ? c - 1 : 0, lane);
       const Pieces<E::kPieces> up = cut_elements<E>(g.tile(0), g.tile(1));
       const Pieces<3> write = cut(g.tile(0) * by_rows(coef + B::kQuery, 0, lane), g.tile(1) * by_rows(coef + B::kQuery, 1, lane));
-      if (c > 0) g.load(s.of(a.dO, c - 1, a.stride_row), a.stride_row, ~0u, col, lane);
+      if (c > first) g.load(s.of(a.dO, c - 1, a.stride_row), a.stride_row, ~0u, col, lane);
       f32x4_t z[2];
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) {
@@ -90,15 +103,17 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel
       const Pieces<3> y = cut(z[0], z[1]);
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) z[tt] = mul(triangle_operand(at + B::kT, tt, lane), y, f32x4_t{0, 0, 0, 0});
-      store_rows<D>(a.rows_z + chunk * kChunk * D, z, col, lane);
-      const __amdgpu_buffer_rsrc_t dV = s.of(a.dV, c, a.stride_row);
+      if (!CARRY) {
+        store_rows<D>(a.rows_z + chunk * kChunk * D, z, col, lane);
+        const __amdgpu_buffer_rsrc_t dV = s.of(a.dV, c, a.stride_row);
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        const f32x4_t beta = by_rows(coef + B::kBeta, tt, lane);
+        for (int tt = 0; tt < 2; ++tt) {
+          const f32x4_t beta = by_rows(coef + B::kBeta, tt, lane);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int t = 16 * tt + 4 * (lane >> 4) + r;
-          E::store_one(dV, static_cast<uint32_t>(t) * a.stride_row + col * E::kBytes, ((live >> t) & 1u) ? beta[r] * z[tt][r] : 0.0f);
+          for (int r = 0; r < 4; ++r) {
+            const int t = 16 * tt + 4 * (lane >> 4) + r;
+            E::store_one(dV, static_cast<uint32_t>(t) * a.stride_row + col * E::kBytes, ((live >> t) & 1u) ? beta[r] * z[tt][r] : 0.0f);
+          }
         }
       }
       const float whole = coef[B::kWhole];
@@ -112,7 +127,8 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel
       live = lives.bits(byte, c - 1);
       lds_barrier();
     }
-    if (a.dinitial_state != nullptr) dS.store(a.dinitial_state + state, col, lane);
+    if (CARRY) dS.store(a.carries + (of_segment + segment) * D * D, col, lane);
+    else if (segment == 0 && a.dinitial_state != nullptr) dS.store(a.dinitial_state + state, col, lane);
   }
 }
 
@@ -133,21 +149,6 @@ struct GradientLds {
   static constexpr int kSquares = kPairs + 2 * kChunk * 4;                     // of K's and Q's rows, by block of columns
   static constexpr int kNotes = kSquares + 2 * R::kBlocks * kChunk * 4;        // per wave: what it knows of the tokens
   static constexpr int kBytes = kNotes + kWaves * 5 * kChunk * 4;
-};
-
-// Row 16 dt + lane%16 of a state [D][D] as an operand with the depth in slot order (see Rows).
-template <int D>
-struct StateRows {
-  static constexpr int kBlocks = D < 32 ? 1 : D / 32;
-  f32x4_t lo[kBlocks], hi[kBlocks];
-  __device__ __forceinline__ void load(const float* from, int dt, int lane) {
-    const float* p = from + (16 * dt + (lane & 15)) * D + 4 * (lane >> 4);
-#pragma unroll
-    for (int kb = 0; kb < kBlocks; ++kb) {
-      lo[kb] = *reinterpret_cast<const f32x4_t*>(p + 32 * kb);
-      hi[kb] = D < 32 ? f32x4_t{0, 0, 0, 0} : *reinterpret_cast<const f32x4_t*>(p + 32 * kb + (D < 32 ? 0 : 16));
-    }
-  }
 };
 
 // What a wave notes of the tokens: sums of decays, beta, 1/r of keys and queries.
@@ -513,12 +514,21 @@ __global__ __launch_bounds__(64 * (D / 16), D == 128 ? 2 : 3) void chunk_gradien
   }
 }
 
+template <class E, int D, bool CARRY>
+hipError_t launch_walk(const Args& a, int slices, hipStream_t stream) {
+  constexpr int kLds = 2 * ChunkBuffer<E, D, true>::kBytes + sizeof(Scratch) + sizeof(Notes);
+  const auto kernel = chunk_adjoint_kernel<E, D, CARRY>;
+  if (hipError_t err = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds); err != hipSuccess) return err;
+  const int walked = CARRY ? a.segments - 1 : a.segments;
+  kernel<<<dim3(slices * walked * (D / 16 / kConsumers<D>)), dim3(64 * (kConsumers<D> + 2)), kLds, stream>>>(a);
+  return hipGetLastError();
+}
+
 template <class E, int D>
 hipError_t launch(const Args& a, int slices, hipStream_t stream) {
-  constexpr int kLds = 2 * ChunkBuffer<E, D>::kBytes + sizeof(Scratch) + sizeof(Notes);
-  if (hipError_t err = grant_dynamic_lds(reinterpret_cast<const void*>(chunk_adjoint_kernel<E, D>), kLds); err != hipSuccess) return err;
-  chunk_adjoint_kernel<E, D><<<dim3(slices * (D / 16 / kConsumers<D>)), dim3(64 * (kConsumers<D> + 2)), kLds, stream>>>(a);
-  if (hipError_t err = hipGetLastError(); err != hipSuccess) return err;
+  if (a.segments > 1)
+    if (hipError_t err = launch_walk<E, D, true>(a, slices, stream); err != hipSuccess) return err;
+  if (hipError_t err = launch_walk<E, D, false>(a, slices, stream); err != hipSuccess) return err;
   typedef GradientLds<E, D> L;
   static_assert(L::kBytes <= 160 * 1024, "fits the LDS of a compute unit");
   if (hipError_t err = grant_dynamic_lds(reinterpret_cast<const void*>(chunk_gradient_kernel<E, D>), L::kBytes); err != hipSuccess) return err;

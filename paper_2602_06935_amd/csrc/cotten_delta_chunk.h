@@ -7,10 +7,11 @@ namespace cotten {
 namespace delta {
 
 // One chunk's place in LDS.  The producers fill one while the consumers read the other.
-template <class E, int D>
+template <class E, int D, bool QUERIES>
 struct ChunkBuffer {
   typedef Rows<D, E::kPieces> R;
-  static constexpr int kK = 0, kQ = R::kBytes, kT = 2 * R::kBytes, kM = kT + kTriangleBytes, kCoef = kM + kTriangleBytes;
+  static constexpr int kK = 0, kT = R::kBytes, kQ = kT + kTriangleBytes, kM = kQ + R::kBytes;
+  static constexpr int kCoef = QUERIES ? kM + kTriangleBytes : kQ;
   static constexpr int kBytes = kCoef + (5 * kChunk + 4) * 4;
   // coefficients by token: four columns, and e^(G_C) behind them
   enum { kBeta = 0, kReadK = kChunk, kWriteK = 2 * kChunk, kQuery = 3 * kChunk, kAdjoint = 4 * kChunk, kWhole = 5 * kChunk };
@@ -18,9 +19,9 @@ struct ChunkBuffer {
 
 // Producer of the keys: rows of K in pieces, T (backward: T^T), and the coefficients
 //     kReadK  r e^G (what K S is multiplied with)     kWriteK  r e^(G_C - G)     kAdjoint  -beta e^G r (backward)
-template <class E, int D, bool BWD>
+template <class E, int D, bool BWD, bool QUERIES>
 struct KeyProducer {
-  typedef ChunkBuffer<E, D> B;
+  typedef ChunkBuffer<E, D, QUERIES> B;
   const Args& a;
   const Live lives;
   const Slice& s;
@@ -109,7 +110,7 @@ struct KeyProducer {
 // Producer of the queries: rows of Q in pieces, M (backward: M^T) and the coefficient kQuery = scale r e^G.
 template <class E, int D, bool BWD>
 struct QueryProducer {
-  typedef ChunkBuffer<E, D> B;
+  typedef ChunkBuffer<E, D, true> B;
   const Args& a;
   const Live lives;
   const Slice& s;
@@ -209,6 +210,12 @@ struct StateColumns {
       for (int i = 0; i < 4; ++i)
         s[dt][i] = dt < kTiles ? __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, first + (16 * dt + i) * D * 4, 0, 0)) : 0.0f;
   }
+  __device__ __forceinline__ void unit(int col, int lane) {
+#pragma unroll
+    for (int dt = 0; dt < 2 * kBlocks; ++dt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[dt][i] = 16 * dt + 4 * (lane >> 4) + i == col ? 1.0f : 0.0f;
+  }
   __device__ __forceinline__ void store(float* to, int col, int lane) const {
     const __amdgpu_buffer_rsrc_t r = of(to);
     const uint32_t first = (4 * (lane >> 4) * D + col) * 4;
@@ -222,6 +229,42 @@ struct StateColumns {
     for (int kb = 0; kb < kBlocks; ++kb) p[kb] = cut(s[2 * kb], s[2 * kb + 1]);
   }
 };
+
+// Row 16 dt + lane%16 of a state [D][D] as an operand with the depth in slot order (see Rows).
+template <int D>
+struct StateRows {
+  static constexpr int kBlocks = D < 32 ? 1 : D / 32;
+  f32x4_t lo[kBlocks], hi[kBlocks];
+  __device__ __forceinline__ void load(const float* from, int dt, int lane) {
+    const float* p = from + (16 * dt + (lane & 15)) * D + 4 * (lane >> 4);
+#pragma unroll
+    for (int kb = 0; kb < kBlocks; ++kb) {
+      lo[kb] = *reinterpret_cast<const f32x4_t*>(p + 32 * kb);
+      hi[kb] = D < 32 ? f32x4_t{0, 0, 0, 0} : *reinterpret_cast<const f32x4_t*>(p + 32 * kb + (D < 32 ? 0 : 16));
+    }
+  }
+};
+
+// S <- M S + R (TRANSPOSED: M^T S + R), cut.
+template <int D, bool TRANSPOSED>
+__device__ __forceinline__ void advance(StateColumns<D>& S, const float* M, const float* R, int col, int lane) {
+  S.load(R, col, lane);
+#pragma unroll
+  for (int dt = 0; dt < StateColumns<D>::kTiles; ++dt) {
+    if (TRANSPOSED) {
+      StateColumns<D> m;
+      m.load(M, 16 * dt + (lane & 15), lane);
+#pragma unroll
+      for (int kb = 0; kb < S.kBlocks; ++kb) S.s[dt] = mul(cut(m.s[2 * kb], m.s[2 * kb + 1]), S.p[kb], S.s[dt]);
+    } else {
+      StateRows<D> m;
+      m.load(M, dt, lane);
+#pragma unroll
+      for (int kb = 0; kb < S.kBlocks; ++kb) S.s[dt] = mul(cut(m.lo[kb], m.hi[kb]), S.p[kb], S.s[dt]);
+    }
+  }
+  S.cut_all();
+}
 
 // A pair of result tiles (tokens 16 tt + 4g + r, column `col`) into the rows of a chunk [32][D].
 template <int D>

@@ -235,6 +235,11 @@ struct Args {
   float* rows_u;                // [slice][chunk * 32][D]: U, or nullptr
   float* dstates;               // [slice][chunk][D][D]: the gradient of the state after every chunk (backward)
   float* rows_z;                // [slice][chunk * 32][D]: Z (backward)
+  // Sequences cut into segments (see segments_of): what a segment makes of the state before it, S -> M S + R, and the
+  // gradient of the state before it where that of the state after it is zero.
+  float* transitions;           // [slice][segment][2][D][D]: R, M
+  float* carries;               // [slice][segment][D][D] (backward)
+  int segments, segment_chunks;
   int H, N, chunks;
   long long stride_batch, stride_head;  // of the tensors, in bytes
   uint32_t stride_row;

@@ -81,6 +81,7 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(Ids ids, const T* __re
                                                           int block_tokens, int offset, float scale) {
   const long long first = static_cast<long long>(blockIdx.x) * block_tokens;
   const int rows = static_cast<int>(tokens - first < block_tokens ? tokens - first : block_tokens);
+  const uint32_t n0 = static_cast<uint32_t>(first % N);
   const uint32_t end = static_cast<uint32_t>(rows) * pieces;
   for (uint32_t at = threadIdx.x; at < end; at += kThreads * kUnroll) {
     uint32_t row[kUnroll], col[kUnroll], id[kUnroll];
@@ -106,7 +107,7 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(Ids ids, const T* __re
       if (at + u * kThreads >= end) break;
       const long long token = first + row[u];
       float p[VEC] = {};
-      if (P != nullptr) Vec<T, VEC>::load(P + (offset + token % N) * D + col[u], p);
+      if (P != nullptr) Vec<T, VEC>::load(P + static_cast<size_t>(offset + (n0 + row[u]) % static_cast<uint32_t>(N)) * D + col[u], p);
 #pragma unroll
       for (int e = 0; e < VEC; ++e) x[u][e] = id[u] < static_cast<uint32_t>(ids.V) ? fmaf(scale, x[u][e], p[e]) : p[e];
       Vec<T, VEC>::store(E + token * D + col[u], x[u]);
@@ -121,10 +122,29 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(Ids ids, const T* __re
 // takes 64 tokens at a time in order, and a token's place among those with its digit is a count of lanes.
 
 constexpr int kDigits = 512;
-constexpr int kStrips = 8;                                       // of 64 tokens, per wave of the sort's blocks
+constexpr int kStrips = 2;                                       // of 64 tokens, per wave of the sort's blocks
 constexpr int kBlockTokens = (kThreads / 64) * kStrips * 64;
-constexpr int kSoloWaves = 16;                                   // one workgroup sorts up to ...
-constexpr int kSoloTokens = kSoloWaves * kStrips * 64;           // ... this many tokens, all passes in one launch
+constexpr int kSoloWaves = 16, kSoloStrips = 8;                  // one workgroup sorts up to ...
+constexpr int kSoloTokens = kSoloWaves * kSoloStrips * 64;       // ... this many tokens, all passes in one launch
+
+// The launches of a sort wait more than they move: workgroups behind those of the sort write a share of dW's zeros
+// (120000 rows of 256 floats take 17 us by themselves).
+struct Zeros {
+  unsigned char* at;
+  size_t bytes;
+  uint32_t sort_blocks;  // workgroups before the first that writes
+};
+constexpr int kZeroBytes = 64 * 1024;  // of a workgroup
+
+template <int THREADS>
+__device__ __forceinline__ bool wrote_zeros(const Zeros& z) {
+  if (blockIdx.x < z.sort_blocks) return false;
+  const size_t first = static_cast<size_t>(blockIdx.x - z.sort_blocks) * kZeroBytes;
+  const size_t end = first + kZeroBytes < z.bytes ? first + kZeroBytes : z.bytes, whole = end & ~size_t{15};
+  for (size_t i = first + threadIdx.x * 16; i < whole; i += THREADS * 16) *reinterpret_cast<u32x4_t*>(z.at + i) = u32x4_t{0, 0, 0, 0};
+  if (whole + threadIdx.x < end) z.at[whole + threadIdx.x] = 0;
+  return true;
+}
 
 struct Sort {
   Ids ids;
@@ -139,7 +159,8 @@ struct Sort {
   __device__ __forceinline__ uint32_t key(uint32_t i) const { return keys != nullptr ? keys[i] : ids.row(i); }
 };
 
-__global__ __launch_bounds__(kThreads) void count_kernel(Sort s) {
+__global__ __launch_bounds__(kThreads) void count_kernel(Sort s, Zeros z) {
+  if (wrote_zeros<kThreads>(z)) return;
   __shared__ uint32_t hist[kDigits];
   for (int d = threadIdx.x; d < kDigits; d += kThreads) hist[d] = 0;
   __syncthreads();
@@ -154,7 +175,8 @@ __global__ __launch_bounds__(kThreads) void count_kernel(Sort s) {
 }
 
 // A wave per digit.
-__global__ __launch_bounds__(kThreads) void sums_kernel(Sort s) {
+__global__ __launch_bounds__(kThreads) void sums_kernel(Sort s, Zeros z) {
+  if (wrote_zeros<kThreads>(z)) return;
   const int lane = threadIdx.x & 63;
   const uint32_t d = blockIdx.x * (kThreads / 64) + (threadIdx.x >> 6);
   if (d >= (1u << s.bits)) return;
@@ -199,32 +221,26 @@ __device__ __forceinline__ void exclusive_sums(uint32_t* base, uint32_t* part) {
   __syncthreads();
 }
 
-// The tokens first ... first + WAVES * kStrips * 64 - 1 to their places.  place[w][d] counts up from where wave w's next
-// token with digit d goes.  `alone`: there is no other block, base holds nothing yet.
-template <int WAVES>
-__device__ __forceinline__ void move_block(const Sort& s, uint32_t first, uint32_t (*place)[kDigits], uint32_t* base,
-                                           uint32_t* part, bool alone) {
+// Tokens to their places: wave w of WAVES has `strips` (STRIPS at most) times 64 of them, from `mine` (a lane's first) on.
+// place[w][d] counts up from where wave w's next token with digit d goes.  `alone`: there is no other block, base holds
+// nothing yet.
+template <int WAVES, int STRIPS, class Put>
+__device__ __forceinline__ void move_block(const Sort& s, uint32_t mine, int strips, const uint32_t (&key)[STRIPS],
+                                           uint32_t (*place)[kDigits], uint32_t* base, uint32_t* part, bool alone, Put&& put) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint32_t mask = (1u << s.bits) - 1u;
   for (int i = threadIdx.x; i < WAVES * kDigits; i += WAVES * 64) place[0][i] = 0;
   __syncthreads();
-  uint32_t key[kStrips], token[kStrips];
-  const uint32_t mine = first + wave * (kStrips * 64) + lane;
 #pragma unroll
-  for (int i = 0; i < kStrips; ++i) {
-    const uint32_t at = mine + 64 * i;
-    key[i] = at < s.n ? s.key(at) : 0;
-    token[i] = at < s.n && s.keys != nullptr ? s.tokens[at] : at;
-  }
-#pragma unroll
-  for (int i = 0; i < kStrips; ++i)
-    if (mine + 64 * i < s.n) atomicAdd(&place[wave][(key[i] >> s.shift) & mask], 1u);
+  for (int i = 0; i < STRIPS; ++i)
+    if (i < strips && mine + 64 * i < s.n) atomicAdd(&place[wave][(key[i] >> s.shift) & mask], 1u);
   if (!alone)
     for (uint32_t d = threadIdx.x; d < kDigits; d += WAVES * 64) base[d] = d <= mask ? s.totals[d] : 0;
   __syncthreads();
   if (alone) {
     for (int d = threadIdx.x; d < kDigits; d += WAVES * 64) {
       uint32_t x = 0;
+#pragma unroll
       for (int w = 0; w < WAVES; ++w) x += place[w][d];
       base[d] = x;
     }
@@ -233,6 +249,7 @@ __device__ __forceinline__ void move_block(const Sort& s, uint32_t first, uint32
   exclusive_sums(base, part);
   for (uint32_t d = threadIdx.x; d <= mask; d += WAVES * 64) {
     uint32_t at = base[d] + (alone ? 0 : s.counts[static_cast<size_t>(d) * s.blocks + blockIdx.x]);
+#pragma unroll
     for (int w = 0; w < WAVES; ++w) {
       const uint32_t x = place[w][d];
       place[w][d] = at;
@@ -241,7 +258,8 @@ __device__ __forceinline__ void move_block(const Sort& s, uint32_t first, uint32
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kStrips; ++i) {
+  for (int i = 0; i < STRIPS; ++i) {
+    if (i >= strips) break;
     const bool on = mine + 64 * i < s.n;
     const uint32_t d = (key[i] >> s.shift) & mask;
     uint64_t same = __ballot(on);
@@ -252,39 +270,71 @@ __device__ __forceinline__ void move_block(const Sort& s, uint32_t first, uint32
     const int rank = __popcll(same & ((1ull << lane) - 1ull));
     uint32_t to = 0;
     if (on) to = place[wave][d] + rank;
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
     __builtin_amdgcn_wave_barrier();
     if (on && rank == 0) place[wave][d] = to + __popcll(same);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
     __builtin_amdgcn_wave_barrier();
-    if (on) {
-      s.keys_out[to] = key[i];
-      s.tokens_out[to] = token[i];
-    }
+    if (on) put(i, to);
   }
 }
 
-__global__ __launch_bounds__(kThreads) void move_kernel(Sort s) {
+__global__ __launch_bounds__(kThreads) void move_kernel(Sort s, Zeros z) {
+  if (wrote_zeros<kThreads>(z)) return;
   __shared__ uint32_t place[kThreads / 64][kDigits], base[kDigits], part[kThreads / 64];
-  move_block<kThreads / 64>(s, blockIdx.x * kBlockTokens, place, base, part, false);
+  const uint32_t mine = blockIdx.x * kBlockTokens + (threadIdx.x >> 6) * (kStrips * 64) + (threadIdx.x & 63);
+  uint32_t key[kStrips], token[kStrips];
+#pragma unroll
+  for (int i = 0; i < kStrips; ++i) {
+    const uint32_t at = mine + 64 * i;
+    key[i] = at < s.n ? s.key(at) : 0;
+    token[i] = at < s.n && s.keys != nullptr ? s.tokens[at] : at;
+  }
+  move_block<kThreads / 64>(s, mine, kStrips, key, place, base, part, false, [&](int i, uint32_t to) {
+    s.keys_out[to] = key[i];
+    s.tokens_out[to] = token[i];
+  });
 }
 
-// All passes of up to kSoloTokens tokens.
-__global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(Sort s, int passes, int digit_bits, int key_bits, uint32_t* other_keys,
-                                                               uint32_t* other_tokens) {
+// All passes of up to kSoloTokens tokens; between passes the lists stay in LDS.
+__global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(Sort s, int passes, int digit_bits, int key_bits, Zeros z) {
+  if (wrote_zeros<64 * kSoloWaves>(z)) return;
   __shared__ uint32_t place[kSoloWaves][kDigits], base[kDigits], part[kSoloWaves];
+  __shared__ uint32_t keys[kSoloTokens];
+  __shared__ uint16_t tokens[kSoloTokens];
+  static_assert(kSoloTokens <= 1 << 16, "a token fits 16 bits");
+  const int strips = static_cast<int>((s.n + kSoloWaves * 64 - 1) / (kSoloWaves * 64));
+  const uint32_t mine = (threadIdx.x >> 6) * (strips * 64) + (threadIdx.x & 63);
+  uint32_t key[kSoloStrips], token[kSoloStrips];
+#pragma unroll
+  for (int i = 0; i < kSoloStrips; ++i) {
+    const uint32_t at = mine + 64 * i;
+    key[i] = i < strips && at < s.n ? s.key(at) : 0;
+    token[i] = at;
+  }
   for (int p = 0; p < passes; ++p) {
     s.shift = p * digit_bits;
     s.bits = key_bits - s.shift < digit_bits ? key_bits - s.shift : digit_bits;
-    move_block<kSoloWaves>(s, 0, place, base, part, true);
-    uint32_t *keys = s.keys_out, *tokens = s.tokens_out;
-    s.keys = keys;
-    s.tokens = tokens;
-    s.keys_out = other_keys;
-    s.tokens_out = other_tokens;
-    other_keys = keys;
-    other_tokens = tokens;
-    __threadfence_block();
+    const bool last = p == passes - 1;
+    move_block<kSoloWaves>(s, mine, strips, key, place, base, part, true, [&](int i, uint32_t to) {
+      if (last) {
+        s.keys_out[to] = key[i];
+        s.tokens_out[to] = token[i];
+      } else {
+        keys[to] = key[i];
+        tokens[to] = static_cast<uint16_t>(token[i]);
+      }
+    });
+    if (last) return;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSoloStrips; ++i) {
+      const uint32_t at = mine + 64 * i;
+      if (i < strips && at < s.n) {
+        key[i] = keys[at];
+        token[i] = tokens[at];
+      }
+    }
     __syncthreads();
   }
 }
@@ -308,18 +358,55 @@ struct Rows {
   float scale;
 };
 
+// dP, by the workgroups of sum_kernel behind its units: one per row of the table of positions and `lanes` * VEC columns;
+// rows that no token has are zeros.
+template <class T>
+struct Positions {
+  T* dP;  // nullptr: not wanted
+  int B, N, offset;
+};
+
+constexpr int kSumThreads = 512;
+
 template <class T, int VEC>
-__global__ __launch_bounds__(kThreads) void zero_kernel(T* to, size_t elements) {
-  size_t i = (static_cast<size_t>(blockIdx.x) * kThreads * kUnroll + threadIdx.x) * VEC;
-  const float x[VEC] = {};
+__device__ __forceinline__ void sum_positions(const Positions<T>& p, const T* __restrict__ dE, int row, int lanes, int D, float* part) {
+  const int groups = kSumThreads / lanes, group = threadIdx.x / lanes;
+  const int col = (blockIdx.y * lanes + threadIdx.x % lanes) * VEC, n = row - p.offset;
+  float sum[VEC] = {};
+  if (n >= 0 && n < p.N && col < D) {
+#pragma unroll 8
+    for (int b = group; b < p.B; b += groups) {
+      float x[VEC];
+      Vec<T, VEC>::load(dE + (static_cast<size_t>(b) * p.N + n) * D + col, x);
 #pragma unroll
-  for (int u = 0; u < kUnroll; ++u, i += static_cast<size_t>(kThreads) * VEC)
-    if (i < elements) Vec<T, VEC>::store(to + i, x);
+      for (int e = 0; e < VEC; ++e) sum[e] += x[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) part[e * kSumThreads + threadIdx.x] = sum[e];
+  __syncthreads();
+  for (int half = groups / 2; half > 0; half /= 2) {
+    if (group < half)
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) part[e * kSumThreads + threadIdx.x] += part[e * kSumThreads + threadIdx.x + half * lanes];
+    __syncthreads();
+  }
+  if (group == 0 && col < D) {
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) sum[e] = part[e * kSumThreads + threadIdx.x];
+    Vec<T, VEC>::store(p.dP + static_cast<size_t>(row) * D + col, sum);
+  }
 }
 
 template <class T, int VEC>
-__global__ __launch_bounds__(kThreads) void sum_kernel(Rows s, const T* __restrict__ dE, T* __restrict__ dW) {
-  const uint32_t unit = blockIdx.x * (kThreads / s.lanes) + threadIdx.x / s.lanes;
+__global__ __launch_bounds__(kSumThreads) void sum_kernel(Rows s, const T* __restrict__ dE, T* __restrict__ dW, Positions<T> p,
+                                                          uint32_t unit_blocks) {
+  __shared__ float part[kSumThreads * VEC];
+  if (blockIdx.x >= unit_blocks) {
+    sum_positions<T, VEC>(p, dE, blockIdx.x - unit_blocks, s.lanes, s.D, part);
+    return;
+  }
+  const uint32_t unit = blockIdx.x * (kSumThreads / s.lanes) + threadIdx.x / s.lanes;
   const int col = (blockIdx.y * s.lanes + threadIdx.x % s.lanes) * VEC;
   if (unit >= s.units || col >= s.D) return;
   const uint32_t first = unit * kUnit, end = first + kUnit < s.n ? first + kUnit : s.n;
@@ -369,79 +456,82 @@ __global__ __launch_bounds__(kThreads) void sum_kernel(Rows s, const T* __restri
   }
 }
 
-// A workgroup per unit: where a row starts in it and goes on, its tail and the heads of the units that it goes on in.
-template <class T>
-__global__ __launch_bounds__(kThreads) void join_kernel(Rows s, T* __restrict__ dW) {
-  const uint32_t unit = blockIdx.x, first = unit * kUnit, next = first + kUnit;
-  if (next >= s.n) return;
-  const uint32_t key = s.keys[next - 1];
-  if (key == static_cast<uint32_t>(s.V) || s.keys[next] != key) return;                     // nothing goes on
-  if (s.keys[first] == key && first > 0 && s.keys[first - 1] == key) return;                  // it started before
-  const int lane = threadIdx.x & 63;
-  uint32_t heads = 0;
-  for (;;) {  // units whose first token has the key: they follow one another
-    const uint32_t u = unit + 1 + heads + lane;
-    const uint64_t same = __ballot(u < s.units && s.keys[u < s.units ? u * kUnit : 0] == key);
-    const int run = same == ~0ull ? 64 : __ffsll(static_cast<long long>(~same)) - 1;
-    heads += run;
-    if (run < 64) break;
-  }
-  // partial sums 0 (the tail) ... heads, a contiguous share for each group of lanes
-  __shared__ float part[kThreads];
-  const int groups = kThreads / s.lanes, group = threadIdx.x / s.lanes;
-  const uint32_t share = (heads + groups) / groups;
-  for (int c0 = 0; c0 < s.D; c0 += s.lanes) {
-    const int col = c0 + threadIdx.x % s.lanes;
-    float sum = 0.0f;
-    if (col < s.D) {
-      const uint32_t from = group * share, to = from + share < heads + 1 ? from + share : heads + 1;
-#pragma unroll 8
-      for (uint32_t i = from; i < to; ++i)
-        sum += i == 0 ? s.tails[static_cast<size_t>(unit) * s.D + col] : s.heads[static_cast<size_t>(unit + i) * s.D + col];
-    }
-    part[threadIdx.x] = sum;
-    __syncthreads();
-    if (group == 0 && col < s.D) {
-      float x = 0.0f;
-      for (int g = 0; g < groups; ++g) x += part[g * s.lanes + threadIdx.x];
-      dW[static_cast<size_t>(key) * s.D + col] = static_cast<T>(x * s.scale);
-    }
-    __syncthreads();
-  }
-}
+// A wave per unit: where a row starts in it and goes on, its tail and the heads of the units that it goes on in.  Rows of
+// more than kMostHeads are shared by the workgroup's waves afterwards.
+constexpr int kJoinWaves = 16, kMostHeads = 16;
 
-// ---- positions ----------------------------------------------------------------------------------------------------------
-
-// dP: a workgroup per row of the table and `lanes` * VEC columns; rows that no token has are zeros.
 template <class T, int VEC>
-__global__ __launch_bounds__(1024) void positions_kernel(const T* __restrict__ dE, T* __restrict__ dP, int B, int N, int D,
-                                                         int offset, int lanes) {
-  __shared__ float part[1024 * VEC];
-  const int groups = 1024 / lanes, group = threadIdx.x / lanes, lane = threadIdx.x % lanes;
-  const int col = (blockIdx.y * lanes + lane) * VEC, n = static_cast<int>(blockIdx.x) - offset;
-  float sum[VEC] = {};
-  if (n >= 0 && n < N && col < D) {
-#pragma unroll 4
-    for (int b = group; b < B; b += groups) {
-      float x[VEC];
-      Vec<T, VEC>::load(dE + (static_cast<size_t>(b) * N + n) * D + col, x);
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) sum[e] += x[e];
+__global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(Rows s, T* __restrict__ dW) {
+  __shared__ uint32_t long_heads[kJoinWaves];
+  __shared__ float part[kJoinWaves][64 * VEC];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t V = s.V, first_unit = blockIdx.x * kJoinWaves;
+  const uint32_t unit = first_unit + wave, first = unit * kUnit, next = first + kUnit;
+  uint32_t heads = 0, key = V;
+  if (unit < s.units && next < s.n) {
+    key = s.keys[next - 1];
+    const uint32_t after = s.keys[next], begin = s.keys[first], before = first > 0 ? s.keys[first - 1] : V;
+    const bool starts = !(begin == key && before == key);
+    if (key != V && after == key && starts) {
+      for (;;) {  // units whose first token has the key: they follow one another
+        const uint32_t u = unit + 1 + heads + lane;
+        const uint64_t same = __ballot(u < s.units && s.keys[u < s.units ? u * kUnit : 0] == key);
+        const int run = same == ~0ull ? 64 : __ffsll(static_cast<long long>(~same)) - 1;
+        heads += run;
+        if (run < 64) break;
+      }
     }
   }
+  if (lane == 0) long_heads[wave] = heads > kMostHeads ? heads : 0;
+  if (heads > 0 && heads <= kMostHeads) {
+    for (int col = lane * VEC; col < s.D; col += 64 * VEC) {
+      float sum[VEC];
+      Vec<float, VEC>::load(s.tails + static_cast<size_t>(unit) * s.D + col, sum);
+#pragma unroll 4
+      for (uint32_t i = 1; i <= heads; ++i) {
+        float x[VEC];
+        Vec<float, VEC>::load(s.heads + static_cast<size_t>(unit + i) * s.D + col, x);
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) part[e * 1024 + threadIdx.x] = sum[e];
-  __syncthreads();
-  for (int half = groups / 2; half > 0; half /= 2) {
-    if (group < half)
+        for (int e = 0; e < VEC; ++e) sum[e] += x[e];
+      }
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) part[e * 1024 + threadIdx.x] += part[e * 1024 + threadIdx.x + half * lanes];
-    __syncthreads();
+      for (int e = 0; e < VEC; ++e) sum[e] *= s.scale;
+      Vec<T, VEC>::store(dW + static_cast<size_t>(key) * s.D + col, sum);
+    }
   }
-  if (group == 0 && col < D) {
+  __syncthreads();
+  for (int w = 0; w < kJoinWaves; ++w) {
+    const uint32_t all = long_heads[w];
+    if (all == 0) continue;
+    const uint32_t owner = first_unit + w, share = (all + kJoinWaves) / kJoinWaves;
+    // partial sums 0 (the tail) ... `all`, a contiguous share for each wave
+    const uint32_t from = wave * share, to = from + share < all + 1 ? from + share : all + 1;
+    for (int c0 = 0; c0 < s.D; c0 += 64 * VEC) {
+      const int col = c0 + lane * VEC;
+      float sum[VEC] = {};
+      if (col < s.D) {
+#pragma unroll 8
+        for (uint32_t i = from; i < to; ++i) {
+          float x[VEC];
+          Vec<float, VEC>::load((i == 0 ? s.tails : s.heads) + static_cast<size_t>(owner + i) * s.D + col, x);
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) sum[e] = part[e * 1024 + threadIdx.x];
-    Vec<T, VEC>::store(dP + static_cast<size_t>(blockIdx.x) * D + col, sum);
+          for (int e = 0; e < VEC; ++e) sum[e] += x[e];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) part[wave][lane * VEC + e] = sum[e];
+      __syncthreads();
+      if (wave == 0 && col < s.D) {
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) {
+          float x = 0.0f;
+          for (int i = 0; i < kJoinWaves; ++i) x += part[i][lane * VEC + e];
+          sum[e] = x * s.scale;
+        }
+        Vec<T, VEC>::store(dW + static_cast<size_t>(s.keys[(owner + 1) * kUnit]) * s.D + col, sum);
+      }
+      __syncthreads();
+    }
   }
 }
 
@@ -570,6 +660,9 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
   if (dW != nullptr && (params->workspace == nullptr || params->workspace_bytes < at.words * 4)) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t err = hipSuccess;
+  Rows rows{};
+  rows.V = V;
+  rows.D = D;
   if (dW != nullptr) {
     uint32_t* w = static_cast<uint32_t*>(params->workspace);
     uint32_t *keys[2] = {w, w + 2 * at.list}, *tokens[2] = {w + at.list, w + 3 * at.list};
@@ -579,11 +672,25 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
     sort.totals = sort.counts + static_cast<size_t>(kDigits) * at.blocks;
     sort.n = static_cast<uint32_t>(n);
     sort.blocks = at.blocks;
-    sort.keys_out = keys[0];
-    sort.tokens_out = tokens[0];
-    const int bits = key_bits(V);
-    if (n <= kSoloTokens) {
-      solo_kernel<<<dim3(1), dim3(64 * kSoloWaves), 0, s>>>(sort, at.passes, at.digit_bits, bits, keys[1], tokens[1]);
+    const int bits = key_bits(V), last = (at.passes - 1) & 1;
+    const bool solo = n <= kSoloTokens;
+    // every launch of the sort with its share of the zeros
+    const size_t table = static_cast<size_t>(V) * D * (params->dtype == COTTEN_F32 ? 4 : 2);
+    const size_t launches = solo ? 1 : 3 * at.passes;
+    const size_t share = ((table + launches - 1) / launches + kZeroBytes - 1) / kZeroBytes * kZeroBytes;
+    size_t written = 0;
+    auto with_zeros = [&](uint32_t blocks, Zeros* z) {
+      const size_t bytes = table - written < share ? table - written : share;
+      *z = Zeros{static_cast<unsigned char*>(dW) + written, bytes, blocks};
+      written += bytes;
+      return dim3(blocks + static_cast<uint32_t>((bytes + kZeroBytes - 1) / kZeroBytes));
+    };
+    Zeros z;
+    if (solo) {
+      sort.keys_out = keys[last];
+      sort.tokens_out = tokens[last];
+      const dim3 grid = with_zeros(1, &z);
+      solo_kernel<<<grid, dim3(64 * kSoloWaves), 0, s>>>(sort, at.passes, at.digit_bits, bits, z);
     } else {
       for (int p = 0; p < at.passes; ++p) {
         sort.shift = p * at.digit_bits;
@@ -592,46 +699,38 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
         sort.tokens = p == 0 ? nullptr : tokens[(p - 1) & 1];
         sort.keys_out = keys[p & 1];
         sort.tokens_out = tokens[p & 1];
-        count_kernel<<<dim3(at.blocks), dim3(kThreads), 0, s>>>(sort);
-        sums_kernel<<<dim3(((1 << sort.bits) + kThreads / 64 - 1) / (kThreads / 64)), dim3(kThreads), 0, s>>>(sort);
-        move_kernel<<<dim3(at.blocks), dim3(kThreads), 0, s>>>(sort);
+        dim3 grid = with_zeros(at.blocks, &z);
+        count_kernel<<<grid, dim3(kThreads), 0, s>>>(sort, z);
+        grid = with_zeros(((1 << sort.bits) + kThreads / 64 - 1) / (kThreads / 64), &z);
+        sums_kernel<<<grid, dim3(kThreads), 0, s>>>(sort, z);
+        grid = with_zeros(at.blocks, &z);
+        move_kernel<<<grid, dim3(kThreads), 0, s>>>(sort, z);
       }
     }
     err = hipGetLastError();
-    Rows rows{};
-    rows.keys = keys[(at.passes - 1) & 1];
-    rows.tokens = tokens[(at.passes - 1) & 1];
+    rows.keys = keys[last];
+    rows.tokens = tokens[last];
     rows.n = static_cast<uint32_t>(n);
-    rows.V = V;
-    rows.D = D;
     rows.units = at.units;
     rows.heads = reinterpret_cast<float*>(w + 4 * at.list + at.counts);
     rows.tails = rows.heads + at.sums;
     rows.scale = params->scale;
-    by_type(params->dtype, D, [&](auto tag) {
-      typedef typename decltype(tag)::type T;
-      constexpr int VEC = decltype(tag)::vec;
-      const size_t elements = static_cast<size_t>(V) * D, per = static_cast<size_t>(kThreads) * kUnroll * VEC;
-      zero_kernel<T, VEC><<<dim3(static_cast<uint32_t>((elements + per - 1) / per)), dim3(kThreads), 0, s>>>(static_cast<T*>(dW), elements);
-      rows.lanes = lanes_of(D / VEC);
-      const uint32_t units = kThreads / rows.lanes;
-      sum_kernel<T, VEC><<<dim3((at.units + units - 1) / units, (D / VEC + rows.lanes - 1) / rows.lanes), dim3(kThreads), 0, s>>>(
-          rows, static_cast<const T*>(dE), static_cast<T*>(dW));
-      rows.lanes = lanes_of(D);
-      join_kernel<T><<<dim3(at.units), dim3(kThreads), 0, s>>>(rows, static_cast<T*>(dW));
-    });
-    if (err == hipSuccess) err = hipGetLastError();
   }
-  if (dP != nullptr) {
-    by_type(params->dtype, D, [&](auto tag) {
-      typedef typename decltype(tag)::type T;
-      constexpr int VEC = decltype(tag)::vec;
-      const int lanes = lanes_of(D / VEC);
-      positions_kernel<T, VEC><<<dim3(params->positions, (D / VEC + lanes - 1) / lanes), dim3(1024), 0, s>>>(
-          static_cast<const T*>(dE), static_cast<T*>(dP), B, N, D, params->position_offset, lanes);
-    });
-    if (err == hipSuccess) err = hipGetLastError();
-  }
+  by_type(params->dtype, D, [&](auto tag) {
+    typedef typename decltype(tag)::type T;
+    constexpr int VEC = decltype(tag)::vec;
+    rows.lanes = lanes_of(D / VEC);
+    const uint32_t of_block = kSumThreads / rows.lanes, unit_blocks = (rows.units + of_block - 1) / of_block;
+    const Positions<T> positions{static_cast<T*>(dP), B, N, params->position_offset};
+    sum_kernel<T, VEC><<<dim3(unit_blocks + (dP != nullptr ? params->positions : 0), (D / VEC + rows.lanes - 1) / rows.lanes),
+                         dim3(kSumThreads), 0, s>>>(rows, static_cast<const T*>(dE), static_cast<T*>(dW), positions, unit_blocks);
+    if (dW != nullptr && at.units > 1) {
+      const dim3 grid((at.units + kJoinWaves - 1) / kJoinWaves);
+      if (D % 4 == 0) join_kernel<T, 4><<<grid, dim3(64 * kJoinWaves), 0, s>>>(rows, static_cast<T*>(dW));
+      else join_kernel<T, 1><<<grid, dim3(64 * kJoinWaves), 0, s>>>(rows, static_cast<T*>(dW));
+    }
+  });
+  if (err == hipSuccess) err = hipGetLastError();
   return err == hipSuccess ? COTTEN_OK : COTTEN_ERR_LAUNCH;
 }
 

@@ -219,6 +219,32 @@ def test_long_history(dtype):
     both(inputs(1, 2, 1501, 32, DTYPES[dtype], seed=16, mask="left", states=True), "bnhd")
 
 
+@pytest.mark.parametrize("N", [513, 1024, 1500])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_segments(dtype, d, N):
+    """Few long sequences are cut into segments that run side by side."""
+    x = inputs(1, 2, N, d, DTYPES[dtype], seed=N + d, mask="holes" if N == 1500 else None, states=True)
+    if x["mask"] is not None:
+        x["mask"][:] = (torch.rand(N, generator=torch.Generator().manual_seed(1)) < 0.7).to(torch.uint8)
+    O, S1, _ = both(x, "bnhd" if N == 1024 else "bhnd", scale=0.5)
+    if N != 1024:    # without what the backward needs, the same bits
+        O2, S2, _ = forward(x, scale=0.5)
+        assert torch.equal(O, O2) and torch.equal(S1, S2)
+
+
+def test_segments_without_states():
+    both(inputs(2, 1, 700, 32, torch.bfloat16, seed=21, mask="left"))
+
+
+def test_segments_backward_without_kept_gives_the_same_bits():
+    x = inputs(1, 3, 900, 64, torch.bfloat16, seed=22, mask="left", states=True)
+    _, _, held = forward(x, kept=True)
+    first, alone = backward(x, kept=held), backward(x)
+    for n in first:
+        assert torch.equal(first[n], alone[n]), n
+
+
 def test_gradient_against_differences():
     x = inputs(1, 2, 50, 32, torch.float32, seed=17, mask="left", states=True)
     _, _, held = forward(x, kept=True)
