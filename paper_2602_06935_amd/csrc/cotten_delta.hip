@@ -97,24 +97,25 @@ __global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
 template <int D>
 constexpr int kConsumers = D / 16 < 4 ? D / 16 : 4;  // of a workgroup; d = 128 takes two (of ten waves, none would have the registers)
 
-// What a walk is for: O; O and what a backward needs; the latter alone; a segment's R or M (see segments_of).
+// What a walk is for: O; O and what a backward needs; the latter alone; a segment's R and M (see segments_of).
 enum Walk { kOutput, kTraining, kStates, kTransition };
 
+template <int D, Walk WALK>
+constexpr int kProducers = WALK == kOutput || WALK == kTraining ? 2 : 1;
+template <int D, Walk WALK>
+constexpr int kWaves = kProducers<D, WALK> + kConsumers<D> * (WALK == kTransition ? 2 : 1);
+
 template <class E, int D, Walk WALK>
-__global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Args a) {
+__global__ __launch_bounds__(64 * (kWaves<D, WALK>)) void chunk_fwd_kernel(Args a) {
   constexpr bool kOut = WALK == kOutput || WALK == kTraining;
   typedef ChunkBuffer<E, D, kOut> B;
   typedef typename B::R R;
   constexpr bool kKept = WALK == kTraining || WALK == kStates;
-  constexpr int kGroups = D / 16 / kConsumers<D>, kProducers = kOut ? 2 : 1;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  constexpr int kGroups = D / 16 / kConsumers<D>;
+  const int lane = threadIdx.x & 63, wave = role_of_wave<(kWaves<D, WALK>)>();
   const int unit = blockIdx.x / kGroups, group = blockIdx.x % kGroups;
-  // transitions: R of segments 0 ... count - 2, then M of 1 ... count - 2
-  const int walked = WALK == kTransition ? 2 * a.segments - 3 : a.segments;
-  const int slice = unit / walked;
-  int segment = unit - slice * walked;
-  const bool is_m = WALK == kTransition && segment > a.segments - 2;
-  if (is_m) segment -= a.segments - 2;
+  const int walked = WALK == kTransition ? a.segments - 1 : a.segments;
+  const int slice = unit / walked, segment = unit - slice * walked;
   const Slice s(a, slice, D * E::kBytes);
   Scratch* scratch = reinterpret_cast<Scratch*>(smem + 2 * B::kBytes);
   Notes* notes = reinterpret_cast<Notes*>(scratch + 1);
@@ -136,7 +137,13 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_fwd_kernel(Arg
       lds_barrier();
     }
   } else {
-    const int tile = group * kConsumers<D> + wave - kProducers, col = 16 * tile + (lane & 15);
+    const int consumer = wave - kProducers<D, WALK>;
+    const bool is_m = WALK == kTransition && consumer >= kConsumers<D>;
+    if (is_m && segment == 0) {  // (its R has the initial state in it)
+      for (int c = first; c <= end; ++c) lds_barrier();
+      return;
+    }
+    const int tile = group * kConsumers<D> + consumer % kConsumers<D>, col = 16 * tile + (lane & 15);
     const long long of_segment = static_cast<long long>(slice) * a.segments;
     StateColumns<D> S;
     if (is_m) {
@@ -218,8 +225,8 @@ hipError_t launch_chunks(const Args& a, int slices, hipStream_t stream) {
   constexpr int kLds = 2 * ChunkBuffer<E, D, kOut>::kBytes + sizeof(Scratch) + sizeof(Notes);
   const auto kernel = chunk_fwd_kernel<E, D, WALK>;
   if (hipError_t err = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds); err != hipSuccess) return err;
-  const int walked = WALK == kTransition ? 2 * a.segments - 3 : a.segments;
-  kernel<<<dim3(slices * walked * (D / 16 / kConsumers<D>)), dim3(64 * (kConsumers<D> + (kOut ? 2 : 1))), kLds, stream>>>(a);
+  const int walked = WALK == kTransition ? a.segments - 1 : a.segments;
+  kernel<<<dim3(slices * walked * (D / 16 / kConsumers<D>)), dim3(64 * kWaves<D, WALK>), kLds, stream>>>(a);
   return hipGetLastError();
 }
 

@@ -37,7 +37,7 @@ template <class E, int D, bool CARRY>
 __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel(Args a) {
   typedef ChunkBuffer<E, D, true> B;
   typedef typename B::R R;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, wave = role_of_wave<(kConsumers<D> + 2)>();
   constexpr int kGroups = D / 16 / kConsumers<D>;
   const int unit = blockIdx.x / kGroups, group = blockIdx.x % kGroups;
   const int walked = CARRY ? a.segments - 1 : a.segments;

@@ -6,6 +6,15 @@
 namespace cotten {
 namespace delta {
 
+// The role of a wave in a workgroup of WAVES.  Four waves take one SIMD each, and the producers would sit on the same two in
+// every workgroup of a compute unit: they move on by one from each 256 workgroups to the next (256 x 2 x 200 x 32 fp32,
+// forward: 23.7 -> 20.7 us; workgroups of six waves are spread by the hardware, and lose by it).
+template <int WAVES>
+__device__ __forceinline__ int role_of_wave() {
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  return WAVES == 4 ? (wave + 3 * (blockIdx.x >> 8)) % 4 : wave;
+}
+
 // One chunk's place in LDS.  The producers fill one while the consumers read the other.
 template <class E, int D, bool QUERIES>
 struct ChunkBuffer {
