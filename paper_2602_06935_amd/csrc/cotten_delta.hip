@@ -106,7 +106,10 @@ template <int D, Walk WALK>
 constexpr int kWaves = kProducers<D, WALK> + kConsumers<D> * (WALK == kTransition ? 2 : 1);
 
 template <class E, int D, Walk WALK>
-__global__ __launch_bounds__(64 * (kWaves<D, WALK>)) void chunk_fwd_kernel(Args a) {
+constexpr int kLds = 2 * ChunkBuffer<E, D, kProducers<D, WALK> == 2>::kBytes + sizeof(Scratch) + sizeof(Notes);
+
+template <class E, int D, Walk WALK>
+__global__ __launch_bounds__(64 * (kWaves<D, WALK>), waves_per_simd(kWaves<D, WALK>, kLds<E, D, WALK>)) void chunk_fwd_kernel(Args a) {
   constexpr bool kOut = WALK == kOutput || WALK == kTraining;
   typedef ChunkBuffer<E, D, kOut> B;
   typedef typename B::R R;
@@ -173,41 +176,40 @@ __global__ __launch_bounds__(64 * (kWaves<D, WALK>)) void chunk_fwd_kernel(Args 
       const long long chunk = static_cast<long long>(slice) * a.chunks + c;
       if (kKept) S.store(a.states + chunk * D * D, col, lane);
       // beta (V - e^G K^ S)
-      f32x4_t u[2];
+      f32x4_t u[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+      add_rows_times<R, D, false>(at + B::kK, S, u, lane);
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        f32x4_t p = {0, 0, 0, 0};
-#pragma unroll
-        for (int kb = 0; kb < S.kBlocks; ++kb) p = mul(R::row_operand(at + B::kK, tt, kb, lane), S.p[kb], p);
-        u[tt] = by_rows(coef + B::kBeta, tt, lane) * (v.tile(tt) - by_rows(coef + B::kReadK, tt, lane) * p);
-      }
+      for (int tt = 0; tt < 2; ++tt)
+        u[tt] = by_rows(coef + B::kBeta, tt, lane) * (v.tile(tt) - by_rows(coef + B::kReadK, tt, lane) * u[tt]);
       if (c + 1 < end) {
         v.load(s.of(a.V, c + 1, a.stride_row), a.stride_row, with_v & lives.bits(byte, c + 1), col, lane);
         byte = lives.fetch(c + 2, lane);
       }
       const Pieces<3> y = cut(u[0], u[1]);
-#pragma unroll
-      for (int tt = 0; tt < 2; ++tt) u[tt] = mul(triangle_operand(at + B::kT, tt, lane), y, f32x4_t{0, 0, 0, 0});
+      const Pieces<3> T[2] = {triangle_operand(at + B::kT, 0, lane), triangle_operand(at + B::kT, 1, lane)};
+      u[0] = u[1] = f32x4_t{0, 0, 0, 0};
+      mul_left(T, y, u);
+      // O^T: a lane has four columns of a token; the state's part of it while U comes
+      f32x4_t o[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+      if (kOut) add_rows_times<R, D, true>(at + B::kQ, S, o, lane);
       if (kKept) store_rows<D>(a.rows_u + chunk * kChunk * D, u, col, lane);
-      if (kOut) {
-        // O^T: a lane has four columns of a token
-        const __amdgpu_buffer_rsrc_t O = s.of(a.O, c, a.stride_row);
-        const Pieces<3> up = cut(u[0], u[1]);
-#pragma unroll
-        for (int tt = 0; tt < 2; ++tt) {
-          f32x4_t o = {0, 0, 0, 0};
-#pragma unroll
-          for (int kb = 0; kb < S.kBlocks; ++kb) o = mul(S.p[kb], R::row_operand(at + B::kQ, tt, kb, lane), o);
-          o *= coef[B::kQuery + 16 * tt + (lane & 15)];
-          o = mul(up, triangle_operand(at + B::kM, tt, lane), o);
-          E::store_four(O, static_cast<uint32_t>(16 * tt + (lane & 15)) * a.stride_row + (16 * tile + 4 * (lane >> 4)) * E::kBytes, o);
-        }
-      }
       // S' = e^(G_C) S + K^^T (e^(G_C - G) U)
       const float whole = coef[B::kWhole];
       const Pieces<3> w = cut(u[0] * by_rows(coef + B::kWriteK, 0, lane), u[1] * by_rows(coef + B::kWriteK, 1, lane));
 #pragma unroll
-      for (int dt = 0; dt < S.kTiles; ++dt) S.s[dt] = mul(R::column_operand(at + B::kK, dt, lane), w, S.s[dt] * whole);
+      for (int dt = 0; dt < S.kTiles; ++dt) S.s[dt] *= whole;
+      add_outer<R, D>(S, at + B::kK, w, lane);
+      if (kOut) {
+        const __amdgpu_buffer_rsrc_t O = s.of(a.O, c, a.stride_row);
+        const Pieces<3> up = cut(u[0], u[1]);
+        const Pieces<3> M[2] = {triangle_operand(at + B::kM, 0, lane), triangle_operand(at + B::kM, 1, lane)};
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt) o[tt] *= coef[B::kQuery + 16 * tt + (lane & 15)];
+        mul_right(up, M, o);
+#pragma unroll
+        for (int tt = 0; tt < 2; ++tt)
+          E::store_four(O, static_cast<uint32_t>(16 * tt + (lane & 15)) * a.stride_row + (16 * tile + 4 * (lane >> 4)) * E::kBytes, o[tt]);
+      }
       S.cut_all();
       lds_barrier();
     }
@@ -221,12 +223,11 @@ constexpr int kMostSteps = 8;
 
 template <class E, int D, Walk WALK>
 hipError_t launch_chunks(const Args& a, int slices, hipStream_t stream) {
-  constexpr bool kOut = WALK == kOutput || WALK == kTraining;
-  constexpr int kLds = 2 * ChunkBuffer<E, D, kOut>::kBytes + sizeof(Scratch) + sizeof(Notes);
+  constexpr int lds = kLds<E, D, WALK>;
   const auto kernel = chunk_fwd_kernel<E, D, WALK>;
-  if (hipError_t err = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds); err != hipSuccess) return err;
+  if (hipError_t err = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), lds); err != hipSuccess) return err;
   const int walked = WALK == kTransition ? a.segments - 1 : a.segments;
-  kernel<<<dim3(slices * walked * (D / 16 / kConsumers<D>)), dim3(64 * kWaves<D, WALK>), kLds, stream>>>(a);
+  kernel<<<dim3(slices * walked * (D / 16 / kConsumers<D>)), dim3(64 * kWaves<D, WALK>), lds, stream>>>(a);
   return hipGetLastError();
 }
 

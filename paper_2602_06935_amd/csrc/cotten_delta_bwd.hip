@@ -33,8 +33,11 @@ constexpr int kConsumers = D / 16 < 4 ? D / 16 : 4;
 
 // The forward's walk in reverse: two producers, and waves with 16 columns of dS each.  Writes dS' and Z for the second
 // kernel, and dV.  CARRY: only the gradient of the state before a segment, of segments 1 ...
+template <class E, int D>
+constexpr int kWalkLds = 2 * ChunkBuffer<E, D, true>::kBytes + sizeof(Scratch) + sizeof(Notes);
+
 template <class E, int D, bool CARRY>
-__global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel(Args a) {
+__global__ __launch_bounds__(64 * (kConsumers<D> + 2), waves_per_simd(kConsumers<D> + 2, kWalkLds<E, D>)) void chunk_adjoint_kernel(Args a) {
   typedef ChunkBuffer<E, D, true> B;
   typedef typename B::R R;
   const int lane = threadIdx.x & 63, wave = role_of_wave<(kConsumers<D> + 2)>();
@@ -92,17 +95,20 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel
       const Pieces<E::kPieces> up = cut_elements<E>(g.tile(0), g.tile(1));
       const Pieces<3> write = cut(g.tile(0) * by_rows(coef + B::kQuery, 0, lane), g.tile(1) * by_rows(coef + B::kQuery, 1, lane));
       if (c > first) g.load(s.of(a.dO, c - 1, a.stride_row), a.stride_row, ~0u, col, lane);
-      f32x4_t z[2];
+      const Pieces<3> M[2] = {triangle_operand(at + B::kM, 0, lane), triangle_operand(at + B::kM, 1, lane)};
+      f32x4_t z[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+      add_rows_times<R, D, false>(at + B::kK, dS, z, lane);
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) {
-        f32x4_t p = {0, 0, 0, 0};
-#pragma unroll
-        for (int kb = 0; kb < dS.kBlocks; ++kb) p = mul(R::row_operand(at + B::kK, tt, kb, lane), dS.p[kb], p);
-        z[tt] = mul(triangle_operand(at + B::kM, tt, lane), up, by_rows(coef + B::kWriteK, tt, lane) * p);
-      }
+      for (int tt = 0; tt < 2; ++tt) z[tt] *= by_rows(coef + B::kWriteK, tt, lane);
+      mul_left(M, up, z);
       const Pieces<3> y = cut(z[0], z[1]);
+      const Pieces<3> T[2] = {triangle_operand(at + B::kT, 0, lane), triangle_operand(at + B::kT, 1, lane)};
+      z[0] = z[1] = f32x4_t{0, 0, 0, 0};
+      mul_left(T, y, z);
+      const float whole = coef[B::kWhole];
 #pragma unroll
-      for (int tt = 0; tt < 2; ++tt) z[tt] = mul(triangle_operand(at + B::kT, tt, lane), y, f32x4_t{0, 0, 0, 0});
+      for (int dt = 0; dt < dS.kTiles; ++dt) dS.s[dt] *= whole;
+      add_outer<R, D>(dS, at + B::kQ, write, lane);
       if (!CARRY) {
         store_rows<D>(a.rows_z + chunk * kChunk * D, z, col, lane);
         const __amdgpu_buffer_rsrc_t dV = s.of(a.dV, c, a.stride_row);
@@ -116,13 +122,8 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2)) void chunk_adjoint_kernel
           }
         }
       }
-      const float whole = coef[B::kWhole];
       const Pieces<3> w = cut(z[0] * by_rows(coef + B::kAdjoint, 0, lane), z[1] * by_rows(coef + B::kAdjoint, 1, lane));
-#pragma unroll
-      for (int dt = 0; dt < dS.kTiles; ++dt) {
-        dS.s[dt] = mul(R::column_operand(at + B::kQ, dt, lane), write, dS.s[dt] * whole);
-        dS.s[dt] = mul(R::column_operand(at + B::kK, dt, lane), w, dS.s[dt]);
-      }
+      add_outer<R, D>(dS, at + B::kK, w, lane);
       dS.cut_all();
       live = lives.bits(byte, c - 1);
       lds_barrier();
@@ -382,12 +383,12 @@ __global__ __launch_bounds__(64 * (D / 16), D == 128 ? 2 : 3) void chunk_gradien
 #pragma unroll
   for (int kb = 0; kb < kBlocks; ++kb) {
     const Pieces<3> S = cut(before.lo[kb], before.hi[kb]), dS = cut(after.lo[kb], after.hi[kb]);
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      dq[tt] = mul(S, R::row_operand(smem + L::kG, tt, kb, lane), dq[tt]);
-      p[tt] = mul(S, R3::row_operand(smem + L::kZ, tt, kb, lane), p[tt]);
-      w[tt] = mul(dS, R3::row_operand(smem + L::kU, tt, kb, lane), w[tt]);
-    }
+    const Pieces<E::kPieces> up[2] = {R::row_operand(smem + L::kG, 0, kb, lane), R::row_operand(smem + L::kG, 1, kb, lane)};
+    mul_right(S, up, dq);
+    const Pieces<3> z[2] = {R3::row_operand(smem + L::kZ, 0, kb, lane), R3::row_operand(smem + L::kZ, 1, kb, lane)};
+    mul_right(S, z, p);
+    const Pieces<3> u[2] = {R3::row_operand(smem + L::kU, 0, kb, lane), R3::row_operand(smem + L::kU, 1, kb, lane)};
+    mul_right(dS, u, w);
 #pragma unroll
     for (int r = 0; r < 4; ++r) inner += before.lo[kb][r] * after.lo[kb][r] + before.hi[kb][r] * after.hi[kb][r];
   }
@@ -437,13 +438,15 @@ __global__ __launch_bounds__(64 * (D / 16), D == 128 ? 2 : 3) void chunk_gradien
   lds_barrier();
   {
     const Pieces<E::kPieces> kc = R::column_operand(smem + L::kK, wave, lane), qc = R::column_operand(smem + L::kQ, wave, lane);
-#pragma unroll
-    for (int tt = 0; tt < 2; ++tt) {
-      dq[tt] = mul(kc, triangle_operand(triangles, tt, lane), dq[tt]);
-      p[tt] = mul(kc, triangle_operand(triangles + 2 * kTriangleBytes, tt, lane), p[tt]);
-      w[tt] = mul(qc, triangle_operand(triangles + kTriangleBytes, tt, lane), w[tt]);
-      w[tt] = mul(kc, triangle_operand(triangles + 3 * kTriangleBytes, tt, lane), w[tt]);
-    }
+    auto add = [&](const Pieces<E::kPieces>& x, int triangle, f32x4_t (&c)[2]) {
+      const unsigned char* at = triangles + triangle * kTriangleBytes;
+      const Pieces<3> t[2] = {triangle_operand(at, 0, lane), triangle_operand(at, 1, lane)};
+      mul_right(x, t, c);
+    };
+    add(kc, 0, dq);
+    add(kc, 2, p);
+    add(qc, 1, w);
+    add(kc, 3, w);
   }
   // products of a row with its gradients, over all columns
   float* sums = reinterpret_cast<float*>(smem + L::kSums);
@@ -516,7 +519,7 @@ __global__ __launch_bounds__(64 * (D / 16), D == 128 ? 2 : 3) void chunk_gradien
 
 template <class E, int D, bool CARRY>
 hipError_t launch_walk(const Args& a, int slices, hipStream_t stream) {
-  constexpr int kLds = 2 * ChunkBuffer<E, D, true>::kBytes + sizeof(Scratch) + sizeof(Notes);
+  constexpr int kLds = kWalkLds<E, D>;
   const auto kernel = chunk_adjoint_kernel<E, D, CARRY>;
   if (hipError_t err = grant_dynamic_lds(reinterpret_cast<const void*>(kernel), kLds); err != hipSuccess) return err;
   const int walked = CARRY ? a.segments - 1 : a.segments;

@@ -26,6 +26,14 @@ struct ChunkBuffer {
   enum { kBeta = 0, kReadK = kChunk, kWriteK = 2 * kChunk, kQuery = 3 * kChunk, kAdjoint = 4 * kChunk, kWhole = 5 * kChunk };
 };
 
+// Waves on a SIMD that the registers of a walk must leave room for: those of two workgroups of WAVES on a compute unit, where
+// their LDS leaves room for two (128 x 4 x 200 x 64 bf16: 26 us, and 32 where registers admit one), but not more than three
+// (168 registers; the nine waves of a transition would get 96, and spill).
+constexpr int waves_per_simd(int waves, int lds) {
+  const int of_two = (2 * waves + 3) / 4;
+  return lds > 80 * 1024 ? (waves + 3) / 4 : of_two < 3 ? of_two : 3;
+}
+
 // Producer of the keys: rows of K in pieces, T (backward: T^T), and the coefficients
 //     kReadK  r e^G (what K S is multiplied with)     kWriteK  r e^(G_C - G)     kAdjoint  -beta e^G r (backward)
 template <class E, int D, bool BWD, bool QUERIES>
@@ -284,6 +292,33 @@ __device__ __forceinline__ void store_rows(float* to, const f32x4_t (&x)[2], int
   for (int tt = 0; tt < 2; ++tt)
 #pragma unroll
     for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[tt][i]), r, first + (16 * tt + i) * D * 4, 0, 0);
+}
+
+// S += X w: X the columns of the chunk's rows at `rows`, w a chunk's rows in pieces; two tiles of S at a time.
+template <class R, int D>
+__device__ __forceinline__ void add_outer(StateColumns<D>& S, const unsigned char* rows, const Pieces<3>& w, int lane) {
+  if constexpr (D == 16) {
+    S.s[0] = mul(R::column_operand(rows, 0, lane), w, S.s[0]);
+  } else {
+#pragma unroll
+    for (int dt = 0; dt < S.kTiles; dt += 2) {
+      const decltype(R::column_operand(rows, 0, lane)) x[2] = {R::column_operand(rows, dt, lane), R::column_operand(rows, dt + 1, lane)};
+      f32x4_t c[2] = {S.s[dt], S.s[dt + 1]};
+      mul_left(x, w, c);
+      S.s[dt] = c[0];
+      S.s[dt + 1] = c[1];
+    }
+  }
+}
+// c[tt] += (rows 16 tt ... of the chunk's rows at `rows`) S; TRANSPOSED: of the same product's transpose
+template <class R, int D, bool TRANSPOSED>
+__device__ __forceinline__ void add_rows_times(const unsigned char* rows, const StateColumns<D>& S, f32x4_t (&c)[2], int lane) {
+#pragma unroll
+  for (int kb = 0; kb < S.kBlocks; ++kb) {
+    const decltype(R::row_operand(rows, 0, kb, lane)) x[2] = {R::row_operand(rows, 0, kb, lane), R::row_operand(rows, 1, kb, lane)};
+    if constexpr (TRANSPOSED) mul_right(S.p[kb], x, c);
+    else mul_left(x, S.p[kb], c);
+  }
 }
 
 __device__ __forceinline__ f32x4_t by_rows(const float* coef, int tt, int lane) {

@@ -117,6 +117,28 @@ __device__ __forceinline__ f32x4_t mul(const Pieces<PA>& a, const Pieces<PB>& b,
   return c;
 }
 
+// N products side by side: no matrix instruction waits for the one before it.
+template <int N, int PA, int PB>
+__device__ __forceinline__ void mul_left(const Pieces<PA> (&a)[N], const Pieces<PB>& b, f32x4_t (&c)[N]) {
+#pragma unroll
+  for (int s = 2; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i < PA; ++i)
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        if (s - i >= 0 && s - i < PB) c[n] = mfma(a[n].p[i], b.p[s - i], c[n]);
+}
+template <int N, int PA, int PB>
+__device__ __forceinline__ void mul_right(const Pieces<PA>& a, const Pieces<PB> (&b)[N], f32x4_t (&c)[N]) {
+#pragma unroll
+  for (int s = 2; s >= 0; --s)
+#pragma unroll
+    for (int i = 0; i < PA; ++i)
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+        if (s - i >= 0 && s - i < PB) c[n] = mfma(a.p[i], b[n].p[s - i], c[n]);
+}
+
 // ---- element formats: eight consecutive elements of a row ---------------------------------------------------------
 
 struct F32 {
