@@ -168,7 +168,7 @@ __global__ __launch_bounds__(64 * (kWaves<D, WALK>), waves_per_simd(kWaves<D, WA
     const Live lives(a, s);
     const uint32_t with_v = is_m ? 0u : ~0u;
     v.load(s.of(a.V, first, a.stride_row), a.stride_row, with_v & lives.bits(lives.fetch(first, lane), first), col, lane);
-    uint8_t byte = lives.fetch(first + 1, lane);
+    uint32_t byte = lives.fetch(first + 1, lane);
     lds_barrier();
     for (int c = first; c < end; ++c) {
       const unsigned char* at = smem + (c & 1) * B::kBytes;

@@ -91,7 +91,7 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2), waves_per_simd(kConsumers
       const float* coef = reinterpret_cast<const float*>(at + B::kCoef);
       const long long chunk = static_cast<long long>(slice) * a.chunks + c;
       if (!CARRY) dS.store(a.dstates + chunk * D * D, col, lane);
-      const uint8_t byte = lives.fetch(c > 0 ? c - 1 : 0, lane);
+      const uint32_t byte = lives.fetch(c > 0 ? c - 1 : 0, lane);
       const Pieces<E::kPieces> up = cut_elements<E>(g.tile(0), g.tile(1));
       const Pieces<3> write = cut(g.tile(0) * by_rows(coef + B::kQuery, 0, lane), g.tile(1) * by_rows(coef + B::kQuery, 1, lane));
       if (c > first) g.load(s.of(a.dO, c - 1, a.stride_row), a.stride_row, ~0u, col, lane);

@@ -45,7 +45,7 @@ struct KeyProducer {
   const __amdgpu_buffer_rsrc_t decays, betas;
   RowTile<E, D> k;
   uint32_t live, g, beta;  // (gates as they were loaded)
-  uint8_t byte;
+  uint32_t byte;
 
   __device__ __forceinline__ KeyProducer(const Args& args, const Slice& slice)
       : a(args), lives(args, slice), s(slice), decays(slice.of_gate(args, args.g)), betas(slice.of_gate(args, args.beta)) {}
@@ -134,7 +134,7 @@ struct QueryProducer {
   const __amdgpu_buffer_rsrc_t decays;
   RowTile<E, D> q, k;
   uint32_t live, there, g;  // keys that take part; rows that exist
-  uint8_t byte;
+  uint32_t byte;
 
   __device__ __forceinline__ QueryProducer(const Args& args, const Slice& slice)
       : a(args), lives(args, slice), s(slice), decays(slice.of_gate(args, args.g)) {}
@@ -206,7 +206,18 @@ struct ColumnTile {
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[tt][i] = E::load_one(r, offset_if(of_lane, 16 * tt + i, first + (16 * tt + i) * stride));
   }
-  __device__ __forceinline__ f32x4_t tile(int tt) const { return f32x4_t{E::value(x[tt][0]), E::value(x[tt][1]), E::value(x[tt][2]), E::value(x[tt][3])}; }
+  // (kept as loaded, 32 bits each, by the empty statement: the compiler would pack 16-bit values in pairs, and wait for them,
+  // right behind the loads)
+  __device__ __forceinline__ f32x4_t tile(int tt) const {
+    f32x4_t r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      uint32_t w = x[tt][i];
+      asm("" : "+v"(w));
+      r[i] = E::value(w);
+    }
+    return r;
+  }
 };
 
 // 16 columns of a state: rows 16 dt + 4g + r, column lane%16 of the wave's; and its pieces, by blocks of 32 rows.

@@ -194,13 +194,14 @@ struct Half {
       x[2 * i + 1] = value(static_cast<uint16_t>(w[i] >> 16));
     }
   }
-  typedef uint16_t One;
+  typedef uint32_t One;  // (a 16-bit variable would be masked, and waited for, where it is loaded)
   static __device__ __forceinline__ One load_one(__amdgpu_buffer_rsrc_t r, uint32_t off) {
     return static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(r, off, 0, 0));
   }
+  static __device__ __forceinline__ float value(One w) { return value(static_cast<uint16_t>(w)); }
   static __device__ __forceinline__ f32x4_t load_four(__amdgpu_buffer_rsrc_t r, uint32_t off) {
     const u32x2_t w = __builtin_amdgcn_raw_buffer_load_b64(r, off, 0, 0);
-    return f32x4_t{value(w[0] & 0xffffu), value(w[0] >> 16), value(w[1] & 0xffffu), value(w[1] >> 16)};
+    return f32x4_t{value(w[0]), value(w[0] >> 16), value(w[1]), value(w[1] >> 16)};
   }
   static __device__ __forceinline__ void store_one(__amdgpu_buffer_rsrc_t r, uint32_t off, float x) {
     __builtin_amdgcn_raw_buffer_store_b16(bits(x), r, off, 0, 0);
@@ -316,11 +317,11 @@ struct Live {
         all(s.mask == nullptr),
         N(a.N) {}
   // of token 32 * chunk + lane%32 (beyond the sequence: 0)
-  __device__ __forceinline__ uint8_t fetch(int chunk, int lane) const {
+  __device__ __forceinline__ uint32_t fetch(int chunk, int lane) const {
     return __builtin_amdgcn_raw_buffer_load_b8(mask, static_cast<uint32_t>(kChunk * chunk + (lane & 31)), 0, 0);
   }
   // bit t: token 32 * chunk + t takes part
-  __device__ __forceinline__ uint32_t bits(uint8_t byte, int chunk) const;
+  __device__ __forceinline__ uint32_t bits(uint32_t byte, int chunk) const;
 };
 
 // Bit t: token 32 * chunk + t exists.
@@ -329,7 +330,7 @@ __device__ __forceinline__ uint32_t existing(int N, int chunk) {
   return left >= kChunk ? ~0u : (1u << left) - 1u;
 }
 
-__device__ __forceinline__ uint32_t Live::bits(uint8_t byte, int chunk) const {
+__device__ __forceinline__ uint32_t Live::bits(uint32_t byte, int chunk) const {
   return all ? existing(N, chunk) : static_cast<uint32_t>(__ballot(byte != 0));
 }
 // A gate of token 32 * chunk + lane%32; 0 where it takes no part.
