@@ -419,22 +419,33 @@ def _buffer(name: str, t: Optional[torch.Tensor], dev) -> Tuple[Optional[int], i
     return t.data_ptr(), t.numel() * t.element_size()
 
 
-def _delta_params(Q, g, beta, dims, gates, scale, eps, layout, workspace, initial_state, final_state,
-                  dfinal_state, dinitial_state, kept) -> CottenDeltaParams:
+def _check_gate(name: str, t: torch.Tensor, lead, dev) -> None:
+    if not (t.dtype is torch.float32 and t.shape == lead and t.device == dev and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous float32 tensor of shape {tuple(lead)} on the device of Q")
+
+
+def _delta_params(Q, dims, gates, scale, eps, layout, workspace, kept, initial_state=None, final_state=None,
+                  dfinal_state=None, dinitial_state=None) -> CottenDeltaParams:
     """The checks of what the two calls share besides Q, K and V, and their parameters."""
     B, H, N, d = dims
-    dev = Q.device
-    lead = Q.shape[:3]
+    dev, lead = Q.device, Q.shape[:3]
     for name, t in gates:
-        if not (t.dtype is torch.float32 and t.shape == lead and t.device == dev and t.is_contiguous()):
-            raise ValueError(f"{name} must be a contiguous float32 tensor of shape {tuple(lead)} on the device of Q")
-    ptr = [None if t is None else _f32_vector(name, t, B * H * d * d, dev) for name, t in (
-        ("initial_state", initial_state), ("final_state", final_state), ("dfinal_state", dfinal_state),
-        ("dinitial_state", dinitial_state))]
-    space, space_bytes = _buffer("workspace", workspace, dev)
-    held, held_bytes = _buffer("kept", kept, dev)
-    return CottenDeltaParams(_dtype_code(Q), 0.0 if scale is None else float(scale), -1.0 if eps is None else float(eps),
-                             _LAYOUTS[layout], space, space_bytes, *ptr, held, held_bytes)
+        _check_gate(name, t, lead, dev)
+    prm = CottenDeltaParams(_DTYPE_CODES[Q.dtype], 0.0 if scale is None else scale, -1.0 if eps is None else eps,
+                            _LAYOUTS[layout])
+    if initial_state is not None:
+        prm.initial_state = _f32_vector("initial_state", initial_state, B * H * d * d, dev)
+    if final_state is not None:
+        prm.final_state = _f32_vector("final_state", final_state, B * H * d * d, dev)
+    if dfinal_state is not None:
+        prm.dfinal_state = _f32_vector("dfinal_state", dfinal_state, B * H * d * d, dev)
+    if dinitial_state is not None:
+        prm.dinitial_state = _f32_vector("dinitial_state", dinitial_state, B * H * d * d, dev)
+    if workspace is not None:
+        prm.workspace, prm.workspace_bytes = _buffer("workspace", workspace, dev)
+    if kept is not None:
+        prm.kept, prm.kept_bytes = _buffer("kept", kept, dev)
+    return prm
 
 
 def cotten_delta_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor, beta: torch.Tensor,
@@ -452,14 +463,15 @@ def cotten_delta_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch
     lib = _lib or load_library()
     _prep_like(Q, (("K", K), ("V", V)))
     dims = _dims(Q, layout)
+    dtype = _dtype_code(Q)
     O = torch.empty_like(Q) if O is None else _prep("O", O, Q)
     handle = _stream_handle(stream)
     if workspace is None and kept is None:
-        need = cotten_delta_workspace_bytes(*dims, _dtype_code(Q), False)
+        need = cotten_delta_workspace_bytes(*dims, dtype, False)
         if need != 0:
             workspace = _workspace(Q, need, handle)
-    prm = _delta_params(Q, g, beta, dims, (("g", g), ("beta", beta)), scale, eps, layout, workspace, initial_state,
-                        final_state, None, None, kept)
+    prm = _delta_params(Q, dims, (("g", g), ("beta", beta)), scale, eps, layout, workspace, kept, initial_state,
+                        final_state)
     _on_device(Q.device, lib.cotten_delta_fwd, Q.data_ptr(), K.data_ptr(), V.data_ptr(), g.data_ptr(),
                beta.data_ptr(), _mask_ptr(mask, dims[0], dims[2], Q.device), O.data_ptr(), *dims, handle,
                ctypes.byref(prm))
@@ -488,8 +500,8 @@ def cotten_delta_bwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch
     handle = _stream_handle(stream)
     if workspace is None:
         workspace = _workspace(Q, cotten_delta_workspace_bytes(*dims, _dtype_code(Q), True, kept is not None), handle)
-    prm = _delta_params(Q, g, beta, dims, (("g", g), ("beta", beta), ("dg", dg), ("dbeta", dbeta)), scale, eps, layout,
-                        workspace, initial_state, None, dfinal_state, dinitial_state, kept)
+    prm = _delta_params(Q, dims, (("g", g), ("beta", beta), ("dg", dg), ("dbeta", dbeta)), scale, eps, layout, workspace,
+                        kept, initial_state, None, dfinal_state, dinitial_state)
     _on_device(Q.device, lib.cotten_delta_bwd, Q.data_ptr(), K.data_ptr(), V.data_ptr(), g.data_ptr(),
                beta.data_ptr(), _mask_ptr(mask, dims[0], dims[2], Q.device), dO.data_ptr(), dQ.data_ptr(),
                dK.data_ptr(), dV.data_ptr(), dg.data_ptr(), dbeta.data_ptr(), *dims, handle, ctypes.byref(prm))
@@ -512,10 +524,9 @@ def _embed_params(ids: torch.Tensor, like: torch.Tensor, scale: float, padding_i
         raise ValueError("ids must be a contiguous int32 or int64 [B,N] tensor on the same device")
     if padding_idx is not None and padding_idx < 0:
         raise ValueError("padding_idx must be None or an id, counted from 0")
-    space, space_bytes = _buffer("workspace", workspace, like.device)
-    return CottenEmbedParams(_dtype_code(like), _ID_BYTES[ids.dtype], float(scale),
-                             -1 if padding_idx is None else int(padding_idx), positions, int(position_offset),
-                             space, space_bytes)
+    space, space_bytes = (None, 0) if workspace is None else _buffer("workspace", workspace, like.device)
+    return CottenEmbedParams(_dtype_code(like), _ID_BYTES[ids.dtype], scale, -1 if padding_idx is None else padding_idx,
+                             positions, position_offset, space, space_bytes)
 
 
 def _table(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None, dims: int = 2) -> torch.Tensor:

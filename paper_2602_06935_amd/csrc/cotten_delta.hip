@@ -218,8 +218,16 @@ __global__ __launch_bounds__(64 * (kWaves<D, WALK>), waves_per_simd(kWaves<D, WA
   }
 }
 
-// Up to this many tokens the recurrence is faster than a chunk.
-constexpr int kMostSteps = 8;
+// Up to how many tokens a call runs as a recurrence.  Every token takes it a microsecond or two more; a chunk takes what it
+// takes, which grows with the workgroups that share a compute unit, more where operands are three pieces.  Measured (us,
+// recurrence / chunk):  256 slices of d = 64, bf16: 6 tokens 9.8 / 9.5, 8 tokens 11.2 / 9.5;  1024: 8 tokens 15.1 / 15.6, 10
+// tokens 18.3 / 15.7;  2048: 10 tokens about 26 / 28, fp32: 16 tokens 38 / 47, 24 tokens 52 / 47;  1024 of d = 128, bf16: 10
+// tokens 40 / 42, 12 tokens 44 / 43, fp16: 12 tokens 51 / 55, 16 tokens 63 / 56.
+template <class E, int D>
+int most_steps(int slices) {
+  const long long workgroups = static_cast<long long>(slices) * (D / 16 / kConsumers<D>);
+  return workgroups <= 512 ? 6 : workgroups <= 1024 ? 8 : E::kPieces == 3 ? 16 : 10;
+}
 
 template <class E, int D, Walk WALK>
 hipError_t launch_chunks(const Args& a, int slices, hipStream_t stream) {
@@ -234,7 +242,7 @@ hipError_t launch_chunks(const Args& a, int slices, hipStream_t stream) {
 template <class E, int D>
 hipError_t launch(const Args& a, int slices, hipStream_t stream) {
   const bool out = a.O != nullptr, kept = a.states != nullptr;
-  if (a.N <= kMostSteps && out && !kept) {
+  if (out && !kept && a.N <= most_steps<E, D>(slices)) {
     constexpr int kParts = D < 32 ? 1 : D / 32;
     const long long waves = static_cast<long long>(slices) * kParts;
     const int per = waves >= 4096 ? 4 : 1;

@@ -229,7 +229,7 @@ __device__ __forceinline__ void move_block(const Sort& s, uint32_t mine, int str
                                            uint32_t (*place)[kDigits], uint32_t* base, uint32_t* part, bool alone, Put&& put) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const uint32_t mask = (1u << s.bits) - 1u;
-  for (int i = threadIdx.x; i < WAVES * kDigits; i += WAVES * 64) place[0][i] = 0;
+  for (uint32_t i = threadIdx.x; i < (static_cast<uint32_t>(WAVES) << s.bits); i += WAVES * 64) place[i >> s.bits][i & mask] = 0;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < STRIPS; ++i)
@@ -238,10 +238,11 @@ __device__ __forceinline__ void move_block(const Sort& s, uint32_t mine, int str
     for (uint32_t d = threadIdx.x; d < kDigits; d += WAVES * 64) base[d] = d <= mask ? s.totals[d] : 0;
   __syncthreads();
   if (alone) {
-    for (int d = threadIdx.x; d < kDigits; d += WAVES * 64) {
+    for (uint32_t d = threadIdx.x; d < kDigits; d += WAVES * 64) {
       uint32_t x = 0;
+      if (d <= mask)
 #pragma unroll
-      for (int w = 0; w < WAVES; ++w) x += place[w][d];
+        for (int w = 0; w < WAVES; ++w) x += place[w][d];
       base[d] = x;
     }
     __syncthreads();

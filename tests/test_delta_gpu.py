@@ -214,6 +214,20 @@ def test_many_slices():
         check(n, t[:1, :1], ref[n])
 
 
+@pytest.mark.parametrize("slices", [600, 1200])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_tokens_around_the_recurrence_of_many_slices(dtype, slices):
+    """Both sides of the numbers of tokens up to which calls of many slices run as a recurrence."""
+    for N in (8, 9, 10, 11, 16, 17):
+        x = inputs(2, 1, N, 16, DTYPES[dtype], seed=N, states=True)
+        ref = reference(x, grads=False)
+        many = {n: (t if t is None else t.repeat(slices // 2, *[1] * (t.dim() - 1))) for n, t in x.items()}
+        O, S1, _ = forward(many)
+        check("O", O[:2], ref["O"])
+        check("S1", S1[-2:], ref["S1"])
+        assert torch.equal(O, O[:2].repeat(slices // 2, 1, 1, 1)) and torch.equal(S1, S1[:2].repeat(slices // 2, 1, 1, 1))
+
+
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_long_history(dtype):
     both(inputs(1, 2, 1501, 32, DTYPES[dtype], seed=16, mask="left", states=True), "bnhd")
