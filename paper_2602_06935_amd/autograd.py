@@ -45,19 +45,21 @@ def cosine_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
 
 class _GatedDelta(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, Q, K, V, g, beta, mask, scale, eps, initial_state, layout):
+    def forward(ctx, Q, K, V, g, beta, mask, scale, eps, initial_state, layout, return_state):
         kept = binding.cotten_delta_kept(Q, layout=layout) if any(ctx.needs_input_grad) else None
-        B, H, _, d = binding._dims(Q, layout)
-        state = torch.empty(B, H, d, d, device=Q.device, dtype=torch.float32)
+        state = None
+        if return_state:
+            B, H, _, d = binding._dims(Q, layout)
+            state = g.new_empty((B, H, d, d))
         O = binding.cotten_delta_fwd(Q, K, V, g, beta, mask, scale=scale, eps=eps, layout=layout,
                                      initial_state=initial_state, final_state=state, kept=kept)
         ctx.save_for_backward(Q, K, V, g, beta, mask, kept, initial_state)
         ctx.scale, ctx.eps, ctx.layout = scale, eps, layout
         ctx.set_materialize_grads(False)
-        return O, state
+        return (O, state) if return_state else O
 
     @staticmethod
-    def backward(ctx, dO, dstate):
+    def backward(ctx, dO, dstate=None):
         Q, K, V, g, beta, mask, kept, initial_state = ctx.saved_tensors
         dO = torch.zeros_like(Q) if dO is None else dO.contiguous()
         dfirst = None
@@ -66,7 +68,7 @@ class _GatedDelta(torch.autograd.Function):
         grads = binding.cotten_delta_bwd(Q, K, V, g, beta, mask, dO, scale=ctx.scale, eps=ctx.eps, layout=ctx.layout,
                                          initial_state=initial_state, dinitial_state=dfirst, kept=kept,
                                          dfinal_state=None if dstate is None else dstate.contiguous())
-        return (*grads, None, None, None, dfirst, None)
+        return (*grads, None, None, None, dfirst, None, None)
 
 
 def gated_delta_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor, beta: torch.Tensor,
@@ -76,8 +78,7 @@ def gated_delta_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: 
     """The gated delta rule of `binding.cotten_delta_fwd`, differentiable in Q, K, V, g, beta and the initial state;
     with `return_state` (O, final state).  The states before every 32 tokens and a float32 row per token are kept for the
     backward."""
-    O, state = _GatedDelta.apply(Q, K, V, g, beta, mask, scale, eps, initial_state, layout)
-    return (O, state) if return_state else O
+    return _GatedDelta.apply(Q, K, V, g, beta, mask, scale, eps, initial_state, layout, return_state)
 
 
 class _ItemEmbedding(torch.autograd.Function):
@@ -95,7 +96,7 @@ class _ItemEmbedding(torch.autograd.Function):
         ids, = ctx.saved_tensors
         dP = None
         if ctx.positions is not None and ctx.needs_input_grad[2]:
-            dP = torch.empty(ctx.positions, device=dE.device, dtype=dE.dtype)
+            dP = dE.new_empty(ctx.positions)
         elif not ctx.needs_input_grad[1]:
             return None, None, None, None, None, None
         dW = binding.cotten_embed_bwd(ids, dE.contiguous(), ctx.rows, dP=dP, scale=ctx.scale,

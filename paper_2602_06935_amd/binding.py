@@ -238,17 +238,19 @@ def _workspace_need(B: int, H: int, N: int, d: int, is_bwd: bool, dtype: int, ca
 
 def _workspace(Q: torch.Tensor, need: int, stream_handle: int) -> torch.Tensor:
     """A workspace of this module's for a call that needs one and was given none."""
-    with torch.cuda.device(Q.device):
-        if torch.cuda.is_current_stream_capturing():
-            return torch.empty(need, dtype=torch.uint8, device=Q.device)
-        key = (Q.device.index, stream_handle)
-        ws = _workspaces.get(key)
-        if ws is None or ws.numel() < need:
-            if ws is not None:
-                _retired.append(ws)
-            ws = torch.empty(max(need, 1 << 20), dtype=torch.uint8, device=Q.device)
-            _workspaces[key] = ws
-        return ws
+    if Q.device.index != _current_device():
+        with torch.cuda.device(Q.device):
+            return _workspace(Q, need, stream_handle)
+    if torch.cuda.is_current_stream_capturing():
+        return torch.empty(need, dtype=torch.uint8, device=Q.device)
+    key = (Q.device.index, stream_handle)
+    ws = _workspaces.get(key)
+    if ws is None or ws.numel() < need:
+        if ws is not None:
+            _retired.append(ws)
+        ws = torch.empty(max(need, 1 << 20), dtype=torch.uint8, device=Q.device)
+        _workspaces[key] = ws
+    return ws
 
 
 # Handle of the current stream of a device: straight from torch's extension module where that has it (0.1 us; a
@@ -519,24 +521,25 @@ _ID_BYTES = {torch.int32: 4, torch.int64: 8}
 
 
 def _embed_params(ids: torch.Tensor, like: torch.Tensor, scale: float, padding_idx: Optional[int], positions: int,
-                  position_offset: int, workspace: Optional[torch.Tensor] = None) -> CottenEmbedParams:
-    if ids.dim() != 2 or ids.dtype not in _ID_BYTES or not ids.is_contiguous() or ids.device != like.device:
+                  position_offset: int) -> CottenEmbedParams:
+    width = _ID_BYTES.get(ids.dtype)
+    if width is None or ids.dim() != 2 or not ids.is_contiguous() or ids.device != like.device:
         raise ValueError("ids must be a contiguous int32 or int64 [B,N] tensor on the same device")
-    if padding_idx is not None and padding_idx < 0:
+    if padding_idx is None:
+        padding_idx = -1
+    elif padding_idx < 0:
         raise ValueError("padding_idx must be None or an id, counted from 0")
-    space, space_bytes = (None, 0) if workspace is None else _buffer("workspace", workspace, like.device)
-    return CottenEmbedParams(_dtype_code(like), _ID_BYTES[ids.dtype], scale, -1 if padding_idx is None else padding_idx,
-                             positions, position_offset, space, space_bytes)
+    return CottenEmbedParams(_dtype_code(like), width, scale, padding_idx, positions, position_offset)
 
 
-def _table(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None, dims: int = 2) -> torch.Tensor:
+def _check_table(name: str, t: torch.Tensor, dims: int, like: Optional[torch.Tensor] = None) -> None:
+    if t.is_cuda and t.dim() == dims and t.is_contiguous():
+        if like is None or (t.dtype is like.dtype and t.shape[-1] == like.shape[-1] and t.device == like.device):
+            return
+        raise ValueError(f"{name} must match the other tensors in width, dtype and device")
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor (there is no CPU path)")
-    if t.dim() != dims or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous {dims}-d tensor")
-    if like is not None and (t.dtype is not like.dtype or t.device != like.device or t.shape[-1] != like.shape[-1]):
-        raise ValueError(f"{name} must match the other tensors in width, dtype and device")
-    return t
+    raise ValueError(f"{name} must be a contiguous {dims}-d tensor")
 
 
 def cotten_embed_fwd(ids: torch.Tensor, W: torch.Tensor, positions: Optional[torch.Tensor] = None,
@@ -545,18 +548,21 @@ def cotten_embed_fwd(ids: torch.Tensor, W: torch.Tensor, positions: Optional[tor
     """E[b,n] = scale * W[ids[b,n]] + positions[position_offset + n]; enqueues on the stream and returns E [B,N,D].
     `ids` int32 or int64 [B,N]; a token with `padding_idx`, or an id that W has no row for, gets no row of W."""
     lib = _lib or load_library()
-    _table("W", W)
+    _check_table("W", W, 2)
+    table = rows = None
     if positions is not None:
-        _table("positions", positions, W)
-    prm = _embed_params(ids, W, scale, padding_idx, 0 if positions is None else positions.shape[0], position_offset)
+        _check_table("positions", positions, 2, W)
+        table, rows = positions.data_ptr(), positions.shape[0]
+    prm = _embed_params(ids, W, scale, padding_idx, rows or 0, position_offset)
     (B, N), (V, D) = ids.shape, W.shape
     if E is None:
-        E = torch.empty(B, N, D, device=W.device, dtype=W.dtype)
-    elif _table("E", E, W, 3).shape != (B, N, D):
-        raise ValueError("E must be [B,N,D]")
-    _on_device(W.device, lib.cotten_embed_fwd, ids.data_ptr(), W.data_ptr(),
-               None if positions is None else positions.data_ptr(), E.data_ptr(), B, N, D, V, _stream_handle(stream),
-               ctypes.byref(prm))
+        E = W.new_empty((B, N, D))
+    else:
+        _check_table("E", E, 3, W)
+        if E.shape != (B, N, D):
+            raise ValueError("E must be [B,N,D]")
+    _on_device(W.device, lib.cotten_embed_fwd, ids.data_ptr(), W.data_ptr(), table, E.data_ptr(), B, N, D, V,
+               _stream_handle(stream), ctypes.byref(prm))
     return E
 
 
@@ -566,22 +572,28 @@ def cotten_embed_bwd(ids: torch.Tensor, dE: torch.Tensor, V: int, dW: Optional[t
     """The gradient dW [V,D] of the table (written whole) for the upstream gradient dE; `dP`, the shape of the table of
     positions, receives its gradient when given."""
     lib = _lib or load_library()
-    _table("dE", dE, None, 3)
+    _check_table("dE", dE, 3)
     B, N, D = dE.shape
     if ids.shape != (B, N):
         raise ValueError("ids must be [B,N] and dE [B,N,D]")
     if dW is None:
-        dW = torch.empty(V, D, device=dE.device, dtype=dE.dtype)
-    elif _table("dW", dW, dE).shape[0] != V:
-        raise ValueError("dW must be [V,D]")
+        dW = dE.new_empty((V, D))
+    else:
+        _check_table("dW", dW, 2, dE)
+        if dW.shape[0] != V:
+            raise ValueError("dW must be [V,D]")
+    positions = rows = None
     if dP is not None:
-        _table("dP", dP, dE)
+        _check_table("dP", dP, 2, dE)
+        positions, rows = dP.data_ptr(), dP.shape[0]
     handle = _stream_handle(stream)
+    prm = _embed_params(ids, dE, scale, padding_idx, rows or 0, position_offset)
     if workspace is None:
         need = cotten_embed_workspace_bytes(B, N, D, V)
         if need != 0:
             workspace = _workspace(dE, need, handle)
-    prm = _embed_params(ids, dE, scale, padding_idx, 0 if dP is None else dP.shape[0], position_offset, workspace)
-    _on_device(dE.device, lib.cotten_embed_bwd, ids.data_ptr(), dE.data_ptr(), dW.data_ptr(),
-               None if dP is None else dP.data_ptr(), B, N, D, V, handle, ctypes.byref(prm))
+    if workspace is not None:
+        prm.workspace, prm.workspace_bytes = _buffer("workspace", workspace, dE.device)
+    _on_device(dE.device, lib.cotten_embed_bwd, ids.data_ptr(), dE.data_ptr(), dW.data_ptr(), positions, B, N, D, V, handle,
+               ctypes.byref(prm))
     return dW

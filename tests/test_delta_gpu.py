@@ -317,3 +317,25 @@ def test_another_stream_and_capture():
             again = [t.clone() for t in calls()]
             torch.cuda.synchronize()
             assert all(torch.equal(p, r) for p, r in zip(again, eager))
+
+
+@pytest.mark.parametrize("layout", ["bhnd", "bnhd"])
+def test_differentiable_function(layout):
+    """Gradients through autograd, with the final state used, unused and not asked for."""
+    from paper_2602_06935_amd.autograd import gated_delta_attention
+    x = inputs(2, 2, 45, 32, torch.float32, seed=30, mask="left", states=True)
+    names = ("q", "k", "v", "g", "beta")
+    for with_state, use_state in ((True, True), (True, False), (False, False)):
+        ref = reference(dict(x, dS1=x["dS1"] if use_state else None), scale=0.7)
+        leaves = [lay(x[n], layout).requires_grad_() for n in names] + [x["S0"].cuda().requires_grad_()]
+        got = gated_delta_attention(*leaves[:5], x["mask"].cuda(), scale=0.7, initial_state=leaves[5], return_state=with_state, layout=layout)
+        outputs = got if use_state else (got[0] if with_state else got,)
+        upstream = (lay(x["dO"], layout),) + ((x["dS1"].cuda(),) if use_state else ())
+        grads = torch.autograd.grad(outputs, leaves, upstream)
+        check("O", back(outputs[0], layout), ref["O"])
+        for n, t in zip(NAMES, grads):
+            check(n, back(t, layout), ref[n])
+        check("dS0", grads[5], ref["dS0"])
+    with torch.no_grad():
+        O, S1 = gated_delta_attention(*leaves[:5], x["mask"].cuda(), scale=0.7, initial_state=leaves[5], return_state=True, layout=layout)
+    check("S1", S1, ref["S1"])
