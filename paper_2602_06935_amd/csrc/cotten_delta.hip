@@ -142,17 +142,22 @@ __global__ __launch_bounds__(64 * (kWaves<D, WALK>), waves_per_simd(kWaves<D, WA
   } else {
     const int consumer = wave - kProducers<D, WALK>;
     const bool is_m = WALK == kTransition && consumer >= kConsumers<D>;
-    if (is_m && segment == 0) {  // (its R has the initial state in it)
+    const int tile = group * kConsumers<D> + consumer % kConsumers<D>, col = 16 * tile + (lane & 15);
+    const long long of_segment = static_cast<long long>(slice) * a.segments;
+    const float* initial = a.initial_state == nullptr ? nullptr : a.initial_state + static_cast<long long>(slice) * D * D;
+    StateColumns<D> S;
+    if (is_m && segment == 0) {
+      // nobody needs the first segment's M (its R has the initial state in it): a copy of the initial state takes the place.
+      // The next launch starts from the copy, as final_state may be initial_state and another workgroup writes it.
+      S.load(initial, col, lane);
+      S.store(a.transitions + (of_segment * 2 + 1) * D * D, col, lane);
       for (int c = first; c <= end; ++c) lds_barrier();
       return;
     }
-    const int tile = group * kConsumers<D> + consumer % kConsumers<D>, col = 16 * tile + (lane & 15);
-    const long long of_segment = static_cast<long long>(slice) * a.segments;
-    StateColumns<D> S;
     if (is_m) {
       S.unit(col, lane);
     } else if (segment == 0) {
-      S.load(a.initial_state == nullptr ? nullptr : a.initial_state + static_cast<long long>(slice) * D * D, col, lane);
+      S.load(WALK != kTransition && a.segments > 1 ? a.transitions + (of_segment * 2 + 1) * D * D : initial, col, lane);
     } else if (WALK == kTransition) {
       S.load(nullptr, col, lane);
     } else {  // from the segments before: the first one's R has the initial state in it

@@ -251,6 +251,20 @@ def test_segments_without_states():
     both(inputs(2, 1, 700, 32, torch.bfloat16, seed=21, mask="left"))
 
 
+@pytest.mark.parametrize("kept", [False, True])
+def test_segments_replace_a_state_in_place(kept):
+    """The first segment reads the state that the last one writes."""
+    from paper_2602_06935_amd import binding
+    x = inputs(2, 2, 1500, 64, torch.bfloat16, seed=31, states=True)
+    O, S1, _ = forward(x, kept=kept)
+    q, k, v, g, b, S = (x[n].cuda() for n in ("q", "k", "v", "g", "beta", "S0"))
+    held = binding.cotten_delta_kept(q) if kept else None
+    for again in range(2):
+        S.copy_(x["S0"])
+        got = binding.cotten_delta_fwd(q, k, v, g, b, None, initial_state=S, final_state=S, kept=held)
+        assert torch.equal(got, O) and torch.equal(S, S1)
+
+
 def test_segments_backward_without_kept_gives_the_same_bits():
     x = inputs(1, 3, 900, 64, torch.bfloat16, seed=22, mask="left", states=True)
     _, _, held = forward(x, kept=True)
