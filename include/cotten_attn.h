@@ -262,7 +262,8 @@ const char* cotten_status_string(int status);
  * that takes part makes the results of its column not finite from its group of 32 tokens on.
  *
  * Calls enqueue on `stream` only, allocate nothing, and give the same bits for the same
- * arguments.  d_h in {16, 32, 64, 128}.  */
+ * arguments.  d_h in {16, 32, 64, 128}; B * H up to 2^22, and the rows of a slice, or 32 of them if
+ * there are fewer, within 2^31 bytes from the first to the last (COTTEN_ERR_BAD_SHAPE beyond).  */
 typedef struct cotten_delta_params {
   int dtype;                  /* a cotten_dtype: of Q, K, V, O and their gradients               */
   float scale;                /* factor of O; <= 0 selects 1                                     */
@@ -316,7 +317,8 @@ size_t cotten_delta_workspace_bytes(int B, int H, int N, int d_h, int dtype, int
  * dense and written whole, zeros included.  The same arguments give the same bits.
  *
  * dW needs a workspace of cotten_embed_workspace_bytes() bytes (lists of the tokens sorted by id, and partial
- * sums).  Calls enqueue on `stream` only and allocate nothing. */
+ * sums).  Calls enqueue on `stream` only and allocate nothing.  D up to 65536, V below 2^30, B * N below 2^31
+ * (with dW up to 2^29), with dP up to 2^22 positions (COTTEN_ERR_BAD_SHAPE beyond). */
 typedef struct cotten_embed_params {
   int dtype;            /* a cotten_dtype: of W, P, E and their gradients                        */
   int id_bytes;         /* 4 or 8                                                                */

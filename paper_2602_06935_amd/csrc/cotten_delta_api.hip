@@ -16,7 +16,8 @@ int check_shape(int B, int H, int N, int d_h, int dtype) {
   if (dtype != COTTEN_F32 && dtype != COTTEN_BF16 && dtype != COTTEN_F16) return COTTEN_ERR_BAD_DTYPE;
   if (B < 1 || H < 1 || N < 1) return COTTEN_ERR_BAD_SHAPE;
   if (d_h != 16 && d_h != 32 && d_h != 64 && d_h != 128) return COTTEN_ERR_UNSUPPORTED_HEAD_DIM;
-  if (static_cast<long long>(B) * H > (1ll << 24) || N > (1 << 24)) return COTTEN_ERR_BAD_SHAPE;
+  // (a slice takes up to 768 threads of a launch of less than 2^32)
+  if (static_cast<long long>(B) * H > (1ll << 22) || N > (1 << 24)) return COTTEN_ERR_BAD_SHAPE;
   return COTTEN_OK;
 }
 
@@ -58,8 +59,8 @@ int prepare(cotten::delta::Args* a, const void* Q, const void* K, const void* V,
   const long long e = prm->dtype == COTTEN_F32 ? 4 : 2, row = d_h * e;
   const bool heads_first = prm->layout == COTTEN_BHND;
   const long long stride_row = heads_first ? row : H * row;
-  // the kernels address the rows of a slice with 31-bit byte offsets
-  if ((N - 1ll) * stride_row + row >= (1ll << 31)) return COTTEN_ERR_BAD_SHAPE;
+  // the kernels address the rows of a slice, and those of a chunk beyond its end, with 31-bit byte offsets
+  if ((N - 1ll) * stride_row + row >= (1ll << 31) || cotten::delta::kChunk * stride_row >= (1ll << 31)) return COTTEN_ERR_BAD_SHAPE;
   a->stride_batch = static_cast<long long>(H) * N * row;
   a->stride_head = heads_first ? static_cast<long long>(N) * row : row;
   a->stride_row = static_cast<uint32_t>(stride_row);

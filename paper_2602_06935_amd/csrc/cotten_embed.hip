@@ -72,6 +72,7 @@ struct Ids {
 // ---- forward ----------------------------------------------------------------------------------------------------------
 
 constexpr int kThreads = 256;
+constexpr long long kMostBlocks = 1ll << 22;  // of a launch, which has less than 2^32 threads
 constexpr int kUnroll = 4;  // pieces of a thread: their ids, then their rows, are on the way together
 
 // A piece is VEC elements; pieces are numbered through the rows of a workgroup's tokens.
@@ -641,11 +642,13 @@ int cotten_embed_fwd(const void* ids, const void* W, const void* P, void* E, int
     typedef typename decltype(tag)::type T;
     constexpr int VEC = decltype(tag)::vec;
     const int pieces = D / VEC;
-    int block_tokens = kThreads * kUnroll / pieces;
+    long long block_tokens = kThreads * kUnroll / pieces;
     if (block_tokens < 1) block_tokens = 1;
+    const long long fewest = (tokens + kMostBlocks - 1) / kMostBlocks;  // (more than the above for 2^31 pieces only)
+    if (block_tokens < fewest) block_tokens = fewest;
     lookup_kernel<T, VEC><<<dim3(static_cast<uint32_t>((tokens + block_tokens - 1) / block_tokens)), dim3(kThreads), 0,
                             static_cast<hipStream_t>(stream)>>>(
-        of, static_cast<const T*>(W), static_cast<const T*>(P), static_cast<T*>(E), tokens, N, D, pieces, block_tokens,
+        of, static_cast<const T*>(W), static_cast<const T*>(P), static_cast<T*>(E), tokens, N, D, pieces, static_cast<int>(block_tokens),
         params->position_offset, params->scale);
   });
   return hipGetLastError() == hipSuccess ? COTTEN_OK : COTTEN_ERR_LAUNCH;
@@ -658,6 +661,9 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
   if (!aligned16(dE) || !aligned16(dW) || !aligned16(dP)) return COTTEN_ERR_MISALIGNED;
   const long long n = static_cast<long long>(B) * N;
   const Layout at(n, D, V);
+  // (sum_kernel: 512 threads for each position, and 64 at most for each unit of tokens)
+  if (dP != nullptr && params->positions > kMostBlocks) return COTTEN_ERR_BAD_SHAPE;
+  if (dW != nullptr && n > (1ll << 29)) return COTTEN_ERR_BAD_SHAPE;
   if (dW != nullptr && (params->workspace == nullptr || params->workspace_bytes < at.words * 4)) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t err = hipSuccess;

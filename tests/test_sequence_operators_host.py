@@ -67,6 +67,24 @@ def test_delta_refusals(lib, call, ptrs):
     assert call(lib, ptrs, kept=0x10000, kept_bytes=need - 1, **room) == -6
 
 
+@pytest.mark.parametrize("call,ptrs", [(delta_fwd, FWD), (delta_bwd, BWD)])
+def test_delta_refuses_what_offsets_and_grids_cannot_reach(lib, call, ptrs):
+    """Rows so far apart that those of a chunk beyond a short sequence's end would wrap around; more slices than a launch has
+    threads for."""
+    room = dict(workspace=0x100000, workspace_bytes=1 << 60)
+    for N in (1, 2, 16):
+        assert call(lib, ptrs, (1, 1 << 20, N, 64), layout=1, **room) == -2, N     # 32 rows of 2^28 bytes
+    for dims in ((1 << 12, 1 << 11, 1, 16), (1 << 12, (1 << 10) + 1, 20, 128)):
+        assert call(lib, ptrs, dims, **room) == -2, dims
+
+
+def test_embed_refuses_what_grids_cannot_reach(lib):
+    def call(dims, ptrs=(0x1000, 0x2000, 0x3000, 0x4000), **kw):
+        return lib.cotten_embed_bwd(*ptrs, *dims, None, ctypes.byref(embed_params(workspace_bytes=1 << 60, **kw)))
+    assert call(((1 << 29) + 1, 1, 33, 100), (0x1000, 0x2000, 0x3000, None)) == -2
+    assert call((2, 40, 64, 100), positions=(1 << 22) + 1) == -2
+
+
 def test_delta_backward_needs_its_workspace(lib):
     alone = binding.cotten_delta_workspace_bytes(2, 2, 40, 32, 0, True)
     given = binding.cotten_delta_workspace_bytes(2, 2, 40, 32, 0, True, True)
