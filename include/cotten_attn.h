@@ -316,8 +316,8 @@ size_t cotten_delta_workspace_bytes(int B, int H, int N, int d_h, int dtype, int
  * its E is its position's alone, and it gives dW nothing.  Sums are fp32, rounded once.  dW and dP are
  * dense and written whole, zeros included.  The same arguments give the same bits.
  *
- * dW needs a workspace of cotten_embed_workspace_bytes() bytes (lists of the tokens sorted by id, and partial
- * sums).  Calls enqueue on `stream` only and allocate nothing.  D up to 65536, V below 2^30, B * N below 2^31
+ * The backward needs a workspace of cotten_embed_workspace_bytes() bytes (lists of the tokens sorted by id, and
+ * partial sums).  Calls enqueue on `stream` only and allocate nothing.  D up to 65536, V below 2^30, B * N below 2^31
  * (with dW up to 2^29), with dP up to 2^22 positions (COTTEN_ERR_BAD_SHAPE beyond). */
 typedef struct cotten_embed_params {
   int dtype;            /* a cotten_dtype: of W, P, E and their gradients                        */
@@ -326,7 +326,7 @@ typedef struct cotten_embed_params {
   int padding_idx;      /* -1: none                                                              */
   int positions;        /* rows of P; position_offset + N at most                                */
   int position_offset;
-  void* workspace;      /* backward with dW: 16-byte aligned device buffer                       */
+  void* workspace;      /* backward: 16-byte aligned device buffer                               */
   size_t workspace_bytes;
 } cotten_embed_params;
 

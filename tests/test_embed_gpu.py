@@ -109,6 +109,25 @@ def test_tokens_without_a_row(B, N, wide):
     run_and_check(ids, W, P, dE, padding=5, scale=0.5)
 
 
+@pytest.mark.parametrize("B,N,D", [(1, 300, 17), (2, 700, 64), (3, 40, 32), (64, 1, 64), (65, 1, 64), (200, 3, 99), (4097, 1, 256),
+                                   (5000, 1, 3), (1100, 7, 300), (300, 30, 1030)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_positions_of_few_and_many_sequences(dtype, B, N, D):
+    """Sums over the sequences in parts, in one, and over next to none."""
+    ids, W, P, dE = make(B, N, D, 40, DTYPES[dtype], seed=B + N)
+    run_and_check(ids, W, P, dE, offset=3)
+
+
+@pytest.mark.parametrize("many", [17, 1024, 1025, 1040, 2063, 2064, 2065, 65552, 70000])
+def test_rows_of_many_units(many):
+    """One id takes 64 units of sixteen tokens, a few more or fewer, or thousands, between others."""
+    ids, W, P, dE = make(1, many + 40, 8, 9, torch.float32, seed=many, positions=False)
+    ids[:] = torch.arange(many + 40) % 9
+    ids[ids == 4] = 5
+    ids[0, 30:30 + many] = 4
+    run_and_check(ids, W, None, dE)
+
+
 def test_no_token_has_a_row():
     ids, W, P, dE = make(4, 50, 16, 9, torch.float32, seed=5)
     ids[:] = 0
