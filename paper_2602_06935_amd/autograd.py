@@ -46,15 +46,15 @@ def cosine_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
 class _GatedDelta(torch.autograd.Function):
     @staticmethod
     def forward(ctx, Q, K, V, g, beta, mask, scale, eps, initial_state, layout, return_state):
+        ctx.dims = dims = binding._dims(Q, layout)
+        B, H, _, d = dims
+        state = g.new_empty((B, H, d, d)) if return_state else None
         kept = binding.cotten_delta_kept(Q, layout=layout) if any(ctx.needs_input_grad) else None
-        state = None
-        if return_state:
-            B, H, _, d = binding._dims(Q, layout)
-            state = g.new_empty((B, H, d, d))
         O = binding.cotten_delta_fwd(Q, K, V, g, beta, mask, scale=scale, eps=eps, layout=layout,
                                      initial_state=initial_state, final_state=state, kept=kept)
         ctx.save_for_backward(Q, K, V, g, beta, mask, kept, initial_state)
-        ctx.scale, ctx.eps, ctx.layout = scale, eps, layout
+        ctx.call = (binding._dtype_code(Q), 0.0 if scale is None else scale, -1.0 if eps is None else eps,
+                    binding._LAYOUTS[layout])
         ctx.set_materialize_grads(False)
         return (O, state) if return_state else O
 
@@ -65,9 +65,8 @@ class _GatedDelta(torch.autograd.Function):
         dfirst = None
         if initial_state is not None and ctx.needs_input_grad[8]:
             dfirst = torch.empty_like(initial_state)
-        grads = binding.cotten_delta_bwd(Q, K, V, g, beta, mask, dO, scale=ctx.scale, eps=ctx.eps, layout=ctx.layout,
-                                         initial_state=initial_state, dinitial_state=dfirst, kept=kept,
-                                         dfinal_state=None if dstate is None else dstate.contiguous())
+        grads = binding._delta_backward_of(binding.CottenDeltaParams(*ctx.call), ctx.dims, Q, K, V, g, beta, mask, dO,
+                                           initial_state, None if dstate is None else dstate.contiguous(), dfirst, kept)
         return (*grads, None, None, None, dfirst, None, None)
 
 

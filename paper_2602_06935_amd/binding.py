@@ -429,25 +429,17 @@ def _check_gate(name: str, t: torch.Tensor, lead, dev) -> None:
 def _delta_params(Q, dims, gates, scale, eps, layout, workspace, kept, initial_state=None, final_state=None,
                   dfinal_state=None, dinitial_state=None) -> CottenDeltaParams:
     """The checks of what the two calls share besides Q, K and V, and their parameters."""
-    B, H, N, d = dims
-    dev, lead = Q.device, Q.shape[:3]
+    B, H, _, d = dims
+    dev, lead, size = Q.device, Q.shape[:3], B * H * d * d
     for name, t in gates:
         _check_gate(name, t, lead, dev)
-    prm = CottenDeltaParams(_DTYPE_CODES[Q.dtype], 0.0 if scale is None else scale, -1.0 if eps is None else eps,
-                            _LAYOUTS[layout])
-    if initial_state is not None:
-        prm.initial_state = _f32_vector("initial_state", initial_state, B * H * d * d, dev)
-    if final_state is not None:
-        prm.final_state = _f32_vector("final_state", final_state, B * H * d * d, dev)
-    if dfinal_state is not None:
-        prm.dfinal_state = _f32_vector("dfinal_state", dfinal_state, B * H * d * d, dev)
-    if dinitial_state is not None:
-        prm.dinitial_state = _f32_vector("dinitial_state", dinitial_state, B * H * d * d, dev)
-    if workspace is not None:
-        prm.workspace, prm.workspace_bytes = _buffer("workspace", workspace, dev)
-    if kept is not None:
-        prm.kept, prm.kept_bytes = _buffer("kept", kept, dev)
-    return prm
+    first = _f32_vector("initial_state", initial_state, size, dev)
+    return CottenDeltaParams(
+        _DTYPE_CODES[Q.dtype], 0.0 if scale is None else scale, -1.0 if eps is None else eps, _LAYOUTS[layout],
+        *_buffer("workspace", workspace, dev), first,
+        first if final_state is initial_state else _f32_vector("final_state", final_state, size, dev),
+        _f32_vector("dfinal_state", dfinal_state, size, dev), _f32_vector("dinitial_state", dinitial_state, size, dev),
+        *_buffer("kept", kept, dev))
 
 
 def cotten_delta_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor, beta: torch.Tensor,
@@ -504,10 +496,35 @@ def cotten_delta_bwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch
         workspace = _workspace(Q, cotten_delta_workspace_bytes(*dims, _dtype_code(Q), True, kept is not None), handle)
     prm = _delta_params(Q, dims, (("g", g), ("beta", beta), ("dg", dg), ("dbeta", dbeta)), scale, eps, layout, workspace,
                         kept, initial_state, None, dfinal_state, dinitial_state)
-    _on_device(Q.device, lib.cotten_delta_bwd, Q.data_ptr(), K.data_ptr(), V.data_ptr(), g.data_ptr(),
-               beta.data_ptr(), _mask_ptr(mask, dims[0], dims[2], Q.device), dO.data_ptr(), dQ.data_ptr(),
-               dK.data_ptr(), dV.data_ptr(), dg.data_ptr(), dbeta.data_ptr(), *dims, handle, ctypes.byref(prm))
+    return _delta_backward(prm, dims, handle, Q, K, V, g, beta, _mask_ptr(mask, dims[0], dims[2], Q.device), dO, dQ, dK, dV,
+                           dg, dbeta)
+
+
+def _delta_backward(prm, dims, handle, Q, K, V, g, beta, mask, dO, dQ, dK, dV, dg, dbeta):
+    """The call itself: everything is checked."""
+    _on_device(Q.device, _lib.cotten_delta_bwd, Q.data_ptr(), K.data_ptr(), V.data_ptr(), g.data_ptr(), beta.data_ptr(),
+               mask, dO.data_ptr(), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), dg.data_ptr(), dbeta.data_ptr(), *dims,
+               handle, ctypes.byref(prm))
     return dQ, dK, dV, dg, dbeta
+
+
+def _delta_backward_of(prm, dims, Q, K, V, g, beta, mask, dO, initial_state, dfinal_state, dinitial_state, kept):
+    """The gradients of a forward call that has checked its tensors (the differentiable function's): `prm` holds its type,
+    scale, eps and layout, the rest of it is filled in here."""
+    handle = _stream_handle(None)
+    workspace = _workspace(Q, cotten_delta_workspace_bytes(*dims, prm.dtype, True, kept is not None), handle)
+    prm.workspace, prm.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    if kept is not None:
+        prm.kept, prm.kept_bytes = kept.data_ptr(), kept.numel()
+    if initial_state is not None:
+        prm.initial_state = initial_state.data_ptr()
+    if dfinal_state is not None:
+        prm.dfinal_state = dfinal_state.data_ptr()
+    if dinitial_state is not None:
+        prm.dinitial_state = dinitial_state.data_ptr()
+    new = torch.empty_like
+    return _delta_backward(prm, dims, handle, Q, K, V, g, beta, None if mask is None else mask.data_ptr(), dO, new(Q),
+                           new(Q), new(Q), new(g), new(beta))
 
 
 # ---- embedding of item ids -----------------------------------------------------------------------
