@@ -274,10 +274,12 @@ hipError_t launch_dim(const Args& a, int D, int slices, hipStream_t stream) {
 }  // namespace
 
 Segments segments_of(long long slices, int chunks, int D) {
-  // about two workgroups for each of the 256 compute units; not more segments than make up for the steps M S + R over them
-  // (one takes about as long as half a chunk in each of the two launches); with fewer than four the first launch takes
-  // what the second saves
-  constexpr int kWorkgroups = 512, kFewest = 4;
+  // About one workgroup for each of the 256 compute units (two take as long as one after the other): 16 x 4 x 4096 x 64
+  // bf16, forward / backward: whole 242 / 378 us, in 4 segments 135 / 287, in 8 146 / 303; 16 x 4 x 1024: whole 64 / 98, 4
+  // segments 43 / 74.  Not more segments than make up for the steps M S + R over them (one takes about as long as half a
+  // chunk in each of the two launches).  With two the first launch takes what the second saves: 32 x 4 x 2048 whole 123 /
+  // 261 us, in 2 segments 120 / 273;  20 x 4 x 2048 whole 123 / 206, in 3 93 / 183.
+  constexpr int kWorkgroups = 256, kFewest = 3;
   const long long groups = slices * (D > 64 ? D / 64 : 1);
   long long count = kWorkgroups / groups < chunks ? kWorkgroups / groups : chunks;
   while (count * count > 2ll * chunks) --count;
