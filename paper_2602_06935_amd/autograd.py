@@ -84,22 +84,22 @@ class _ItemEmbedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, ids, W, positions, scale, padding_idx, position_offset):
         ctx.save_for_backward(ids)
-        ctx.scale, ctx.padding_idx, ctx.position_offset = scale, padding_idx, position_offset
-        ctx.rows = W.shape[0]
-        ctx.positions = None if positions is None else positions.shape
+        P_shape = None if positions is None else positions.shape
+        ctx.shapes = W.shape, P_shape
+        ctx.call = (binding._dtype_code(W), ids.element_size(), scale, -1 if padding_idx is None else padding_idx,
+                    0 if P_shape is None else P_shape[0], position_offset)
         return binding.cotten_embed_fwd(ids, W, positions, scale=scale, padding_idx=padding_idx,
                                         position_offset=position_offset)
 
     @staticmethod
     def backward(ctx, dE):
         ids, = ctx.saved_tensors
-        dP = None
-        if ctx.positions is not None and ctx.needs_input_grad[2]:
-            dP = dE.new_empty(ctx.positions)
-        elif not ctx.needs_input_grad[1]:
+        W_shape, P_shape = ctx.shapes
+        _, of_W, of_P = ctx.needs_input_grad[:3]
+        if not (of_W or of_P):
             return None, None, None, None, None, None
-        dW = binding.cotten_embed_bwd(ids, dE.contiguous(), ctx.rows, dP=dP, scale=ctx.scale,
-                                      padding_idx=ctx.padding_idx, position_offset=ctx.position_offset)
+        dW, dP = binding._embed_backward_of(binding.CottenEmbedParams(*ctx.call), ids, dE.contiguous(), W_shape,
+                                            P_shape if of_P else None)
         return None, dW, dP, None, None, None
 
 

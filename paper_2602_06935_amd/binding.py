@@ -614,3 +614,17 @@ def cotten_embed_bwd(ids: torch.Tensor, dE: torch.Tensor, V: int, dW: Optional[t
     _on_device(dE.device, lib.cotten_embed_bwd, ids.data_ptr(), dE.data_ptr(), dW.data_ptr(), positions, B, N, D, V, handle,
                ctypes.byref(prm))
     return dW
+
+
+def _embed_backward_of(prm, ids, dE, W_shape, P_shape):
+    """(dW, dP) of a forward call that has checked its tensors (the differentiable function's): `prm` holds all but the
+    workspace.  `P_shape` None: dW alone."""
+    B, N, D = dE.shape
+    handle = _stream_handle(None)
+    workspace = _workspace(dE, cotten_embed_workspace_bytes(B, N, D, W_shape[0]), handle)
+    prm.workspace, prm.workspace_bytes = workspace.data_ptr(), workspace.numel()
+    dW = dE.new_empty(W_shape)
+    dP = None if P_shape is None else dE.new_empty(P_shape)
+    _on_device(dE.device, _lib.cotten_embed_bwd, ids.data_ptr(), dE.data_ptr(), dW.data_ptr(),
+               None if dP is None else dP.data_ptr(), B, N, D, W_shape[0], handle, ctypes.byref(prm))
+    return dW, dP

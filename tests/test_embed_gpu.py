@@ -128,6 +128,32 @@ def test_rows_of_many_units(many):
     run_and_check(ids, W, None, dE)
 
 
+@pytest.mark.parametrize("D", [1, 3, 8, 17, 64, 100, 300, 1030])
+@pytest.mark.parametrize("tokens", [2047, 2048, 2049, 8193])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_few_and_many_tokens_of_every_width(dtype, tokens, D):
+    """Up to 2048 tokens go in one launch, up to 8192 are sorted by one workgroup."""
+    ids, W, P, dE = make(1, tokens, D, 700, DTYPES[dtype], seed=tokens + D)
+    run_and_check(ids, W, P, dE, scale=0.5, padding=3)
+
+
+@pytest.mark.parametrize("V", [1, 2, 50, 511, 513, 3000, 120000])
+@pytest.mark.parametrize("B,N", [(1, 1), (7, 9), (40, 51), (2048, 1)])
+def test_few_tokens_of_tables_of_every_size(B, N, V):
+    ids, W, P, dE = make(B, N, 32, V, torch.bfloat16, seed=V + N)
+    run_and_check(ids, W, P, dE, offset=2)
+    run_and_check(ids.int(), W, None, dE, scale=3.0)
+
+
+@pytest.mark.parametrize("many", [15, 16, 17, 32, 1024, 1025, 1040])
+def test_a_popular_id_among_sorted_tokens(many):
+    ids, W, P, dE = make(1, 2500, 8, 9, torch.float32, seed=many, positions=False)
+    ids[:] = torch.arange(2500) % 9
+    ids[ids == 4] = 5
+    ids[0, 300:300 + many] = 4
+    run_and_check(ids, W, None, dE)
+
+
 def test_no_token_has_a_row():
     ids, W, P, dE = make(4, 50, 16, 9, torch.float32, seed=5)
     ids[:] = 0
