@@ -125,8 +125,6 @@ __global__ __launch_bounds__(kThreads) void lookup_kernel(Ids ids, const T* __re
 constexpr int kDigits = 512;
 constexpr int kStrips = 2;                                       // of 64 tokens, per wave of the sort's blocks
 constexpr int kBlockTokens = (kThreads / 64) * kStrips * 64;
-constexpr int kSoloWaves = 16, kSoloStrips = 8;                  // one workgroup sorts up to ...
-constexpr int kSoloTokens = kSoloWaves * kSoloStrips * 64;       // ... this many tokens, all passes in one launch
 
 // The launches of a sort wait more than they move: workgroups behind those of the sort write a share of dW's zeros
 // (120000 rows of 256 floats take 17 us by themselves).
@@ -197,62 +195,53 @@ __global__ __launch_bounds__(kThreads) void sums_kernel(Sort s, Zeros z) {
   if (lane == 0) s.totals[d] = before;
 }
 
-// Exclusive sums of base[0 ... 511], by 256 or more threads; `part`: a word per wave.
+// Exclusive sums of base[0 ... 511], by kThreads threads; `part`: a word per wave.
 __device__ __forceinline__ void exclusive_sums(uint32_t* base, uint32_t* part) {
+  static_assert(kThreads == kDigits / 2, "two digits a thread");
   const int t = threadIdx.x, lane = t & 63;
-  uint32_t a = 0, b = 0, x = 0;
-  if (t < kDigits / 2) {
-    a = base[2 * t];
-    b = base[2 * t + 1];
-    x = a + b;
+  const uint32_t a = base[2 * t], b = base[2 * t + 1];
+  uint32_t x = a + b;
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-      const uint32_t y = __shfl_up(x, m);
-      if (lane >= m) x += y;
-    }
-    if (lane == 63) part[t >> 6] = x;
+  for (int m = 1; m < 64; m <<= 1) {
+    const uint32_t y = __shfl_up(x, m);
+    if (lane >= m) x += y;
   }
+  if (lane == 63) part[t >> 6] = x;
   __syncthreads();
-  if (t < kDigits / 2) {
-    uint32_t before = x - a - b;
-    for (int w = 0; w < (t >> 6); ++w) before += part[w];
-    base[2 * t] = before;
-    base[2 * t + 1] = before + a;
-  }
+  uint32_t before = x - a - b;
+  for (int w = 0; w < (t >> 6); ++w) before += part[w];
+  base[2 * t] = before;
+  base[2 * t + 1] = before + a;
   __syncthreads();
 }
 
-// Tokens to their places: wave w of WAVES has `strips` (STRIPS at most) times 64 of them, from `mine` (a lane's first) on.
-// place[w][d] counts up from where wave w's next token with digit d goes.  `alone`: there is no other block, base holds
-// nothing yet.
-template <int WAVES, int STRIPS, class Put>
-__device__ __forceinline__ void move_block(const Sort& s, uint32_t mine, int strips, const uint32_t (&key)[STRIPS],
-                                           uint32_t (*place)[kDigits], uint32_t* base, uint32_t* part, bool alone, Put&& put) {
+// Tokens to their places: a wave has kStrips times 64 of them.  place[w][d] counts up from where wave w's next token with
+// digit d goes.
+__global__ __launch_bounds__(kThreads) void move_kernel(Sort s, Zeros z) {
+  if (wrote_zeros<kThreads>(z)) return;
+  constexpr int kWaves = kThreads / 64;
+  __shared__ uint32_t place[kWaves][kDigits], base[kDigits], part[kWaves];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint32_t mask = (1u << s.bits) - 1u;
-  for (uint32_t i = threadIdx.x; i < (static_cast<uint32_t>(WAVES) << s.bits); i += WAVES * 64) place[i >> s.bits][i & mask] = 0;
-  __syncthreads();
+  const uint32_t mine = blockIdx.x * kBlockTokens + wave * (kStrips * 64) + lane, mask = (1u << s.bits) - 1u;
+  uint32_t key[kStrips], token[kStrips];
 #pragma unroll
-  for (int i = 0; i < STRIPS; ++i)
-    if (i < strips && mine + 64 * i < s.n) atomicAdd(&place[wave][(key[i] >> s.shift) & mask], 1u);
-  if (!alone)
-    for (uint32_t d = threadIdx.x; d < kDigits; d += WAVES * 64) base[d] = d <= mask ? s.totals[d] : 0;
-  __syncthreads();
-  if (alone) {
-    for (uint32_t d = threadIdx.x; d < kDigits; d += WAVES * 64) {
-      uint32_t x = 0;
-      if (d <= mask)
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) x += place[w][d];
-      base[d] = x;
-    }
-    __syncthreads();
+  for (int i = 0; i < kStrips; ++i) {
+    const uint32_t at = mine + 64 * i;
+    key[i] = at < s.n ? s.key(at) : 0;
+    token[i] = at < s.n && s.keys != nullptr ? s.tokens[at] : at;
   }
-  exclusive_sums(base, part);
-  for (uint32_t d = threadIdx.x; d <= mask; d += WAVES * 64) {
-    uint32_t at = base[d] + (alone ? 0 : s.counts[static_cast<size_t>(d) * s.blocks + blockIdx.x]);
+  for (uint32_t i = threadIdx.x; i < (static_cast<uint32_t>(kWaves) << s.bits); i += kThreads) place[i >> s.bits][i & mask] = 0;
+  __syncthreads();
 #pragma unroll
-    for (int w = 0; w < WAVES; ++w) {
+  for (int i = 0; i < kStrips; ++i)
+    if (mine + 64 * i < s.n) atomicAdd(&place[wave][(key[i] >> s.shift) & mask], 1u);
+  for (uint32_t d = threadIdx.x; d < kDigits; d += kThreads) base[d] = d <= mask ? s.totals[d] : 0;
+  __syncthreads();
+  exclusive_sums(base, part);
+  for (uint32_t d = threadIdx.x; d <= mask; d += kThreads) {
+    uint32_t at = base[d] + s.counts[static_cast<size_t>(d) * s.blocks + blockIdx.x];
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
       const uint32_t x = place[w][d];
       place[w][d] = at;
       at += x;
@@ -260,8 +249,7 @@ __device__ __forceinline__ void move_block(const Sort& s, uint32_t mine, int str
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < STRIPS; ++i) {
-    if (i >= strips) break;
+  for (int i = 0; i < kStrips; ++i) {
     const bool on = mine + 64 * i < s.n;
     const uint32_t d = (key[i] >> s.shift) & mask;
     uint64_t same = __ballot(on);
@@ -277,67 +265,10 @@ __device__ __forceinline__ void move_block(const Sort& s, uint32_t mine, int str
     if (on && rank == 0) place[wave][d] = to + __popcll(same);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
     __builtin_amdgcn_wave_barrier();
-    if (on) put(i, to);
-  }
-}
-
-__global__ __launch_bounds__(kThreads) void move_kernel(Sort s, Zeros z) {
-  if (wrote_zeros<kThreads>(z)) return;
-  __shared__ uint32_t place[kThreads / 64][kDigits], base[kDigits], part[kThreads / 64];
-  const uint32_t mine = blockIdx.x * kBlockTokens + (threadIdx.x >> 6) * (kStrips * 64) + (threadIdx.x & 63);
-  uint32_t key[kStrips], token[kStrips];
-#pragma unroll
-  for (int i = 0; i < kStrips; ++i) {
-    const uint32_t at = mine + 64 * i;
-    key[i] = at < s.n ? s.key(at) : 0;
-    token[i] = at < s.n && s.keys != nullptr ? s.tokens[at] : at;
-  }
-  move_block<kThreads / 64>(s, mine, kStrips, key, place, base, part, false, [&](int i, uint32_t to) {
-    s.keys_out[to] = key[i];
-    s.tokens_out[to] = token[i];
-  });
-}
-
-// All passes of up to kSoloTokens tokens; between passes the lists stay in LDS.
-__global__ __launch_bounds__(64 * kSoloWaves) void solo_kernel(Sort s, int passes, int digit_bits, int key_bits, Zeros z) {
-  if (wrote_zeros<64 * kSoloWaves>(z)) return;
-  __shared__ uint32_t place[kSoloWaves][kDigits], base[kDigits], part[kSoloWaves];
-  __shared__ uint32_t keys[kSoloTokens];
-  __shared__ uint16_t tokens[kSoloTokens];
-  static_assert(kSoloTokens <= 1 << 16, "a token fits 16 bits");
-  const int strips = static_cast<int>((s.n + kSoloWaves * 64 - 1) / (kSoloWaves * 64));
-  const uint32_t mine = (threadIdx.x >> 6) * (strips * 64) + (threadIdx.x & 63);
-  uint32_t key[kSoloStrips], token[kSoloStrips];
-#pragma unroll
-  for (int i = 0; i < kSoloStrips; ++i) {
-    const uint32_t at = mine + 64 * i;
-    key[i] = i < strips && at < s.n ? s.key(at) : 0;
-    token[i] = at;
-  }
-  for (int p = 0; p < passes; ++p) {
-    s.shift = p * digit_bits;
-    s.bits = key_bits - s.shift < digit_bits ? key_bits - s.shift : digit_bits;
-    const bool last = p == passes - 1;
-    move_block<kSoloWaves>(s, mine, strips, key, place, base, part, true, [&](int i, uint32_t to) {
-      if (last) {
-        s.keys_out[to] = key[i];
-        s.tokens_out[to] = token[i];
-      } else {
-        keys[to] = key[i];
-        tokens[to] = static_cast<uint16_t>(token[i]);
-      }
-    });
-    if (last) return;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < kSoloStrips; ++i) {
-      const uint32_t at = mine + 64 * i;
-      if (i < strips && at < s.n) {
-        key[i] = keys[at];
-        token[i] = tokens[at];
-      }
+    if (on) {
+      s.keys_out[to] = key[i];
+      s.tokens_out[to] = token[i];
     }
-    __syncthreads();
   }
 }
 
@@ -596,24 +527,25 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(Rows s, T* __rest
 // A workgroup has a share of the table's rows to write zeros to, where no token has them: `rows_of_block` that follow one
 // another.  And it has as many rows to sum, dealt out one by one (popular ids tend to be neighbours): it picks their tokens out
 // of all ids, in order, sorts them by row and token in LDS, and sums them, a lane group per row, or the whole workgroup for a
-// row of more than kUnit.  One launch instead of three, and no wait for one workgroup's sort; every workgroup reads all ids.
-// Whole backward, bf16, in one launch / sorted: 2000 tokens, 3700 rows of 64, ids uniform 8.0 / 19.4 us (host time), uniform in
-// the logarithm 14 / 20; 120000 rows of 256 17 / 25; 80 tokens 7.9 / 14.5.
+// row of more than kUnit.  One launch instead of five to eight, and every workgroup reads all ids.  Whole backward, bf16, so /
+// sorted as below (host time: 8): 80 tokens, 3700 rows of 64, 8.0 / 14.5 us;  2000 tokens 8.1 / 19.4;  8000 tokens 13 / 30, and
+// with ids uniform in the logarithm 25 / 31;  8000 of 120000 rows of 256 29 / 40.  (8000 tokens of 50 rows of 300, a fifth of
+// them the same id, lose: 42 / 26.)
 
-constexpr int kDirectTokens = 2048;
+constexpr int kDirectTokens = 8192, kFewTokens = 2048;  // (with 2048 a workgroup needs half the LDS, and fewer steps)
 
-template <class T, int VEC>
+template <class T, int VEC, int TOKENS>
 __global__ __launch_bounds__(kSumThreads) void direct_kernel(Ids ids, Rows s, const T* __restrict__ dE, T* __restrict__ dW,
                                                              uint32_t rows_of_block, uint32_t row_blocks, Positions<T> p) {
   __shared__ float part[kSumThreads * VEC];
-  __shared__ uint32_t list[kDirectTokens], long_rows[kDirectTokens / kUnit], counts[kDirectTokens / 64], long_count;
+  __shared__ uint32_t list[TOKENS], long_rows[TOKENS / kUnit], counts[TOKENS / 64], long_count, all;
   __shared__ uint32_t taken[kZeroBytes / 2 / 32];  // a bit per row of the share
   if (blockIdx.x >= row_blocks) {
     if (blockIdx.y == 0) sum_positions<T, VEC>(p, dE, blockIdx.x - row_blocks, part);
     return;
   }
-  constexpr int kTokenBits = 11, kSteps = kDirectTokens / kSumThreads, kWaves = kSumThreads / 64, kAhead = 8;
-  static_assert(kDirectTokens == 1 << kTokenBits, "an entry is a row of the block and a token");
+  constexpr int kTokenBits = 13, kSteps = TOKENS / kSumThreads, kWaves = kSumThreads / 64, kAhead = 8;
+  static_assert(TOKENS <= 1 << kTokenBits, "an entry is a row of the block and a token");
   const uint32_t tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const uint32_t first_row = blockIdx.x * rows_of_block, left = s.V - first_row, rows = left < rows_of_block ? left : rows_of_block;
   for (uint32_t i = tid; i * 32 < rows; i += kSumThreads) taken[i] = 0;
@@ -650,18 +582,36 @@ __global__ __launch_bounds__(kSumThreads) void direct_kernel(Ids ids, Rows s, co
       if (!((taken[r / 32] >> (r % 32)) & 1u)) Vec<T, VEC>::store(out + static_cast<size_t>(i) * VEC, zeros);
     }
   }
-  uint32_t m = 0;
+  if (wave == kWaves - 1) {  // sums of the counts before each
+    constexpr int kOfLane = (kSteps * kWaves + 63) / 64;
+    uint32_t own[kOfLane], x = 0;
 #pragma unroll
-  for (int k = 0; k < kSteps * kWaves; ++k) {
+    for (int i = 0; i < kOfLane; ++i) {
+      const uint32_t k = lane * kOfLane + i;
+      own[i] = k < kSteps * kWaves ? counts[k] : 0;
+      x += own[i];
+    }
+    uint32_t before = x;
 #pragma unroll
-    for (int i = 0; i < kSteps; ++i)
-      if (k == static_cast<int>(i * kWaves + wave)) at[i] += m;
-    m += counts[k];
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t y = __shfl_up(before, d);
+      if (lane >= d) before += y;
+    }
+    if (lane == 63) all = before;
+    before -= x;
+#pragma unroll
+    for (int i = 0; i < kOfLane; ++i) {
+      const uint32_t k = lane * kOfLane + i;
+      if (k < kSteps * kWaves) counts[k] = before;
+      before += own[i];
+    }
   }
+  __syncthreads();
+  const uint32_t m = all;
   if (m == 0) return;
 #pragma unroll
   for (int i = 0; i < kSteps; ++i)
-    if (mine[i]) list[at[i]] = (row[i] << kTokenBits) | (i * kSumThreads + tid);
+    if (mine[i]) list[counts[i * kWaves + wave] + at[i]] = (row[i] << kTokenBits) | (i * kSumThreads + tid);
   uint32_t size = 1;
   while (size < m) size *= 2;
   for (uint32_t i = m + tid; i < size; i += kSumThreads) list[i] = ~0u;
@@ -681,21 +631,31 @@ __global__ __launch_bounds__(kSumThreads) void direct_kernel(Ids ids, Rows s, co
   const uint32_t groups = kSumThreads / s.lanes, group = tid / s.lanes, col = (blockIdx.y * s.lanes + tid % s.lanes) * VEC;
   const bool inside = col < static_cast<uint32_t>(s.D);
   auto row_of = [&](uint32_t e) { return list[e] >> kTokenBits; };
+  auto token_of = [&](uint32_t e) { return list[e] & ((1u << kTokenBits) - 1u); };
   auto place_of = [&](uint32_t r) { return dW + (static_cast<size_t>(r) * row_blocks + blockIdx.x) * s.D; };
   // entries e, e + step ... before `end` of a row, in order
   auto add = [&](float(&sum)[VEC], uint32_t e, uint32_t end, uint32_t step) {
-    for (; e < end; e += kAhead * step) {
+    const T* const from = dE + col;
+    for (; e + (kAhead - 1) * step < end; e += kAhead * step) {
       float x[kAhead][VEC];
 #pragma unroll
-      for (int u = 0; u < kAhead; ++u)
-        if (e + u * step < end)
-          Vec<T, VEC>::load(dE + static_cast<size_t>(list[e + u * step] & (kDirectTokens - 1)) * s.D + col, x[u]);
+      for (int u = 0; u < kAhead; ++u) Vec<T, VEC>::load(from + static_cast<size_t>(token_of(e + u * step)) * s.D, x[u]);
+      __builtin_amdgcn_sched_barrier(0);  // (all on the way before the first is waited for)
 #pragma unroll
       for (int u = 0; u < kAhead; ++u)
-        if (e + u * step < end)
 #pragma unroll
-          for (int c = 0; c < VEC; ++c) sum[c] += x[u][c];
+        for (int c = 0; c < VEC; ++c) sum[c] += x[u][c];
     }
+    if (e >= end) return;
+    float x[kAhead - 1][VEC];
+#pragma unroll
+    for (int u = 0; u < kAhead - 1; ++u)  // (those beyond the end: the first of these once more)
+      Vec<T, VEC>::load(from + static_cast<size_t>(token_of(e + u * step < end ? e + u * step : e)) * s.D, x[u]);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int u = 0; u < kAhead - 1; ++u)
+#pragma unroll
+      for (int c = 0; c < VEC; ++c) sum[c] += e + u * step < end ? x[u][c] : 0.0f;
   };
   for (uint32_t e = group; e < m; e += groups) {
     const uint32_t r = row_of(e);
@@ -906,10 +866,9 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
     sort.n = static_cast<uint32_t>(n);
     sort.blocks = at.blocks;
     const int bits = key_bits(V), last = (at.passes - 1) & 1;
-    const bool solo = n <= kSoloTokens;
     // every launch of the sort with its share of the zeros
     const size_t table = static_cast<size_t>(V) * D * (params->dtype == COTTEN_F32 ? 4 : 2);
-    const size_t launches = solo ? 1 : 3 * at.passes;
+    const size_t launches = 3 * at.passes;
     const size_t share = ((table + launches - 1) / launches + kZeroBytes - 1) / kZeroBytes * kZeroBytes;
     size_t written = 0;
     auto with_zeros = [&](uint32_t blocks, Zeros* z) {
@@ -919,26 +878,19 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
       return dim3(blocks + static_cast<uint32_t>((bytes + kZeroBytes - 1) / kZeroBytes));
     };
     Zeros z;
-    if (solo) {
-      sort.keys_out = keys[last];
-      sort.tokens_out = tokens[last];
-      const dim3 grid = with_zeros(1, &z);
-      solo_kernel<<<grid, dim3(64 * kSoloWaves), 0, s>>>(sort, at.passes, at.digit_bits, bits, z);
-    } else {
-      for (int p = 0; p < at.passes; ++p) {
-        sort.shift = p * at.digit_bits;
-        sort.bits = bits - sort.shift < at.digit_bits ? bits - sort.shift : at.digit_bits;
-        sort.keys = p == 0 ? nullptr : keys[(p - 1) & 1];
-        sort.tokens = p == 0 ? nullptr : tokens[(p - 1) & 1];
-        sort.keys_out = keys[p & 1];
-        sort.tokens_out = tokens[p & 1];
-        dim3 grid = with_zeros(at.blocks, &z);
-        count_kernel<<<grid, dim3(kThreads), 0, s>>>(sort, z);
-        grid = with_zeros(((1 << sort.bits) + kThreads / 64 - 1) / (kThreads / 64), &z);
-        sums_kernel<<<grid, dim3(kThreads), 0, s>>>(sort, z);
-        grid = with_zeros(at.blocks, &z);
-        move_kernel<<<grid, dim3(kThreads), 0, s>>>(sort, z);
-      }
+    for (int p = 0; p < at.passes; ++p) {
+      sort.shift = p * at.digit_bits;
+      sort.bits = bits - sort.shift < at.digit_bits ? bits - sort.shift : at.digit_bits;
+      sort.keys = p == 0 ? nullptr : keys[(p - 1) & 1];
+      sort.tokens = p == 0 ? nullptr : tokens[(p - 1) & 1];
+      sort.keys_out = keys[p & 1];
+      sort.tokens_out = tokens[p & 1];
+      dim3 grid = with_zeros(at.blocks, &z);
+      count_kernel<<<grid, dim3(kThreads), 0, s>>>(sort, z);
+      grid = with_zeros(((1 << sort.bits) + kThreads / 64 - 1) / (kThreads / 64), &z);
+      sums_kernel<<<grid, dim3(kThreads), 0, s>>>(sort, z);
+      grid = with_zeros(at.blocks, &z);
+      move_kernel<<<grid, dim3(kThreads), 0, s>>>(sort, z);
     }
     err = hipGetLastError();
     rows.keys = keys[last];
@@ -963,7 +915,8 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
       const size_t by_bytes = kZeroBytes / (static_cast<size_t>(D) * sizeof(T)), by_rows = (static_cast<size_t>(V) + 511) / 512;
       const uint32_t of_rows = static_cast<uint32_t>(by_bytes < 1 ? 1 : by_bytes < by_rows ? by_bytes : by_rows);
       const uint32_t row_blocks = (V + of_rows - 1) / of_rows;
-      direct_kernel<T, VEC><<<dim3(row_blocks + parts * columns, (D / VEC + rows.lanes - 1) / rows.lanes), dim3(kSumThreads), 0, s>>>(
+      const auto kernel = n <= kFewTokens ? direct_kernel<T, VEC, kFewTokens> : direct_kernel<T, VEC, kDirectTokens>;
+      kernel<<<dim3(row_blocks + parts * columns, (D / VEC + rows.lanes - 1) / rows.lanes), dim3(kSumThreads), 0, s>>>(
           Ids{ids, params->id_bytes == 8, V, params->padding_idx}, rows, static_cast<const T*>(dE), static_cast<T*>(dW), of_rows,
           row_blocks, positions);
     } else {
@@ -972,7 +925,7 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
     }
     if (parts > 1)
       join_positions_kernel<T><<<dim3(static_cast<uint32_t>((positions.total + 63) / 64)), dim3(kSumThreads), 0, s>>>(positions);
-    if (dW != nullptr && !direct && at.units > 1) {
+    if (dW != nullptr && !direct) {
       const dim3 grid((at.units + kJoinWaves - 1) / kJoinWaves);
       if (D % 4 == 0) join_kernel<T, 4><<<grid, dim3(64 * kJoinWaves), 0, s>>>(rows, static_cast<T*>(dW));
       else join_kernel<T, 1><<<grid, dim3(64 * kJoinWaves), 0, s>>>(rows, static_cast<T*>(dW));

@@ -129,10 +129,10 @@ def test_rows_of_many_units(many):
 
 
 @pytest.mark.parametrize("D", [1, 3, 8, 17, 64, 100, 300, 1030])
-@pytest.mark.parametrize("tokens", [2047, 2048, 2049, 8193])
+@pytest.mark.parametrize("tokens", [2047, 2048, 2049, 8192, 8193])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_few_and_many_tokens_of_every_width(dtype, tokens, D):
-    """Up to 2048 tokens go in one launch, up to 8192 are sorted by one workgroup."""
+    """Up to 2048 and up to 8192 tokens go in one launch, more are sorted first."""
     ids, W, P, dE = make(1, tokens, D, 700, DTYPES[dtype], seed=tokens + D)
     run_and_check(ids, W, P, dE, scale=0.5, padding=3)
 
@@ -145,10 +145,11 @@ def test_few_tokens_of_tables_of_every_size(B, N, V):
     run_and_check(ids.int(), W, None, dE, scale=3.0)
 
 
-@pytest.mark.parametrize("many", [15, 16, 17, 32, 1024, 1025, 1040])
-def test_a_popular_id_among_sorted_tokens(many):
-    ids, W, P, dE = make(1, 2500, 8, 9, torch.float32, seed=many, positions=False)
-    ids[:] = torch.arange(2500) % 9
+@pytest.mark.parametrize("tokens", [2500, 9000])
+@pytest.mark.parametrize("many", [15, 16, 17, 32, 1024, 1025, 1040, 2064])
+def test_a_popular_id(many, tokens):
+    ids, W, P, dE = make(1, tokens, 8, 9, torch.float32, seed=many, positions=False)
+    ids[:] = torch.arange(tokens) % 9
     ids[ids == 4] = 5
     ids[0, 300:300 + many] = 4
     run_and_check(ids, W, None, dE)
