@@ -8,7 +8,7 @@ namespace delta {
 
 // The role of a wave in a workgroup of WAVES.  Four waves take one SIMD each, and the producers would sit on the same two in
 // every workgroup of a compute unit: they move on by one from each 256 workgroups to the next (256 x 2 x 200 x 32 fp32,
-// forward: 23.7 -> 20.7 us; workgroups of six waves are spread by the hardware, and lose by it).
+// forward: 23.9 -> 21.2 us; workgroups of six waves are spread by the hardware, and lose by it).
 template <int WAVES>
 __device__ __forceinline__ int role_of_wave() {
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);

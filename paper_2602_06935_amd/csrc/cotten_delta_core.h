@@ -44,7 +44,7 @@ __device__ __forceinline__ void wave_fence() {
 }
 
 // A barrier for what waves pass each other through LDS: loads and stores of global memory stay on their way across it
-// (a full barrier waits for them: 2.1 us a chunk for the keys' producer, and nothing it had asked for early came early).
+// (a full barrier waits for them, and nothing that a producer had asked for a chunk ahead would come early).
 __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
   __builtin_amdgcn_s_barrier();
