@@ -98,7 +98,10 @@ class _ItemEmbedding(torch.autograd.Function):
         _, of_W, of_P = ctx.needs_input_grad[:3]
         if not (of_W or of_P):
             return None, None, None, None, None, None
-        dW, dP = binding._embed_backward_of(binding.CottenEmbedParams(*ctx.call), ids, dE.contiguous(), W_shape,
+        dE = dE.contiguous()
+        if dE.data_ptr() & 15:  # (a part of another gradient, in rows of an odd width)
+            dE = dE.clone()
+        dW, dP = binding._embed_backward_of(binding.CottenEmbedParams(*ctx.call), ids, dE, W_shape,
                                             P_shape if of_P else None)
         return None, dW, dP, None, None, None
 

@@ -184,6 +184,22 @@ def test_gradient_is_that_of_the_forward():
         assert abs(slope - along) <= 1e-4 * grad.cpu().double().norm().item() * math.sqrt(step.numel())
 
 
+def test_gradient_that_begins_anywhere():
+    """The gradient of a part of a concatenation is a view whose rows of 198 bytes begin off 16-byte boundaries."""
+    from paper_2602_06935_amd.autograd import item_embedding
+    ids, W, _, _ = make(3, 5, 99, 20, torch.float16, seed=9, positions=False)
+    w, i = W.cuda().requires_grad_(), ids.cuda()
+    g = torch.randn(6, 5, 99, generator=torch.Generator().manual_seed(10)).half()
+    both = torch.cat([item_embedding(i, w), item_embedding(i, w, scale=2.0)])
+    dw, = torch.autograd.grad(both, w, g.cuda())
+    want = torch.zeros(20, 99, dtype=torch.float64)
+    for part, scale in ((g[:3], 1.0), (g[3:], 2.0)):
+        want.index_add_(0, ids.flatten(), part.double().flatten(0, 1), alpha=scale)
+    # two gradients and their sum, each rounded once
+    size = torch.zeros(20, 99, dtype=torch.float64).index_add_(0, ids.flatten(), (g[:3].double().abs() + 2 * g[3:].double().abs()).flatten(0, 1))
+    assert ((dw.cpu().double() - want).abs() <= 2 * torch.finfo(torch.float16).eps / 2 * size + 1e-6).all()
+
+
 def test_capture_and_another_stream():
     from paper_2602_06935_amd import binding
     for B, N in ((9, 40), (90, 110)):
