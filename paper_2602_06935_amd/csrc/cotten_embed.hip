@@ -302,8 +302,8 @@ constexpr int kSumThreads = 512;
 
 // dP, by the workgroups of sum_kernel behind its units.  dE is a matrix of B rows and N * D columns here, and dP the sums of
 // its columns (positions that no token has: zeros).  A workgroup has `lanes` pieces of columns, and its lane groups deal the
-// rows of its part out among them.  Few columns of many rows are cut into parts of at least kPartRows rows until there are
-// kParts workgroups, and join_positions_kernel adds the parts.  Whole backward, fp32, D = 256, in parts / in one: 65536 x 1:
+// rows of its part out among them.  Few columns of many rows are cut into parts (four or more, of at least kPartRows rows)
+// until there are kParts workgroups, and join_positions_kernel adds the parts.  Whole backward, fp32, D = 256, in parts / in one: 65536 x 1:
 // 57 / 631 us; 16384 x 4:
 // 52 / 182 us.
 template <class T>
@@ -850,7 +850,7 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
     const auto blocks_of = [&](long long rows) { return static_cast<uint32_t>((rows * (D / vec) + lanes - 1) / lanes); };
     columns = blocks_of(params->positions);
     const uint32_t shares = (static_cast<uint32_t>(B) + kPartRows - 1) / kPartRows, most = kParts / blocks_of(N);
-    parts = most <= 1 ? 1 : shares < most ? shares : most;
+    parts = most < 4 ? 1 : shares < most ? shares : most;
     if (parts > 1 && (params->workspace == nullptr || params->workspace_bytes < at.words * 4)) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
   }
   if (dW != nullptr && (params->workspace == nullptr || params->workspace_bytes < at.words * 4)) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
