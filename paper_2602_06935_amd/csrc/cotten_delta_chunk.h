@@ -27,7 +27,7 @@ struct ChunkBuffer {
 };
 
 // Waves on a SIMD that the registers of a walk must leave room for: those of two workgroups of WAVES on a compute unit, where
-// their LDS leaves room for two (128 x 4 x 200 x 64 bf16: 26 us, and 32 where registers admit one), but not more than three
+// their LDS leaves room for two (128 x 4 x 200 x 64 bf16: 26 us, and 32 where registers admitted one), but not more than three
 // (168 registers; the nine waves of a transition would get 96, and spill).
 constexpr int waves_per_simd(int waves, int lds) {
   const int of_two = (2 * waves + 3) / 4;
