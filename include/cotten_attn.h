@@ -262,7 +262,8 @@ const char* cotten_status_string(int status);
  * that takes part makes the results of its column not finite from its group of 32 tokens on.
  *
  * Calls enqueue on `stream` only, allocate nothing, and give the same bits for the same
- * arguments.  d_h in {16, 32, 64, 128}; B * H up to 2^22, and the rows of a slice, or 32 of them if
+ * arguments.  A call is several launches that pass data through its workspace and `kept`: calls from several host threads
+ * need buffers of their own, also on one stream, where the launches of two calls may alternate.  d_h in {16, 32, 64, 128}; B * H up to 2^22, and the rows of a slice, or 32 of them if
  * there are fewer, within 2^31 bytes from the first to the last (COTTEN_ERR_BAD_SHAPE beyond).  */
 typedef struct cotten_delta_params {
   int dtype;                  /* a cotten_dtype: of Q, K, V, O and their gradients               */

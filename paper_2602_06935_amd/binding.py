@@ -5,10 +5,11 @@ used for device memory (`torch.empty`, `.data_ptr()`) and for the current stream
 There is no CPU fallback: if the library cannot be loaded, or a tensor is not on
 the GPU, the call raises.
 
-The library allocates nothing.  Shapes that need a workspace (long sequences cut over
-several workgroups) get one from here when the caller passes none: a `torch.empty` buffer
-kept per (device, stream), grown when a larger shape arrives; while a stream is being
-captured into a graph the buffer is a fresh temporary from the graph's own pool instead.
+The library allocates nothing.  Calls that need a workspace get one from here when the caller
+passes none: a `torch.empty` buffer of the call's own, given back when the call has enqueued its
+launches.  Several threads may call on one stream at a time; a workspace (or `kept` buffer) that
+they pass themselves must not be shared by calls that may overlap on the host: the launches of
+two calls could alternate on the stream.
 """
 from __future__ import annotations
 
@@ -227,30 +228,21 @@ def _params(Q: torch.Tensor, scale, eps, workspace: Optional[torch.Tensor],
                         1 if causal else 0, kept, fmap)
 
 
-_workspaces = {}    # (device index, stream handle) -> uint8 tensor
-_retired = []       # outgrown buffers: work already enqueued may still use them
-
-
 @functools.lru_cache(maxsize=1024)
 def _workspace_need(B: int, H: int, N: int, d: int, is_bwd: bool, dtype: int, causal: bool) -> int:
     return cotten_attn_workspace_bytes_ex(B, H, N, d, is_bwd, dtype=dtype, causal=causal)
 
 
-def _workspace(Q: torch.Tensor, need: int, stream_handle: int) -> torch.Tensor:
-    """A workspace of this module's for a call that needs one and was given none."""
-    if Q.device.index != _current_device():
-        with torch.cuda.device(Q.device):
-            return _workspace(Q, need, stream_handle)
-    if torch.cuda.is_current_stream_capturing():
-        return torch.empty(need, dtype=torch.uint8, device=Q.device)
-    key = (Q.device.index, stream_handle)
-    ws = _workspaces.get(key)
-    if ws is None or ws.numel() < need:
-        if ws is not None:
-            _retired.append(ws)
-        ws = torch.empty(max(need, 1 << 20), dtype=torch.uint8, device=Q.device)
-        _workspaces[key] = ws
-    return ws
+def _workspace(like: torch.Tensor, need: int, stream_handle: int) -> torch.Tensor:
+    """A workspace for one call that needs one and was given none.  It is that call's alone: the lock of the interpreter is
+    not held while the library enqueues, so another thread's launches may come between this call's on the same stream.
+    torch hands a buffer that was freed on again in the order of the stream it was allocated on, so the buffer comes
+    from the stream of the call (while that is captured, from the graph's pool) and may be dropped as soon as the call returns."""
+    device = like.device
+    if stream_handle == _current_stream_handle(device.index):
+        return torch.empty(need, dtype=torch.uint8, device=device)
+    with torch.cuda.device(device), torch.cuda.stream(torch.cuda.ExternalStream(stream_handle, device)):
+        return torch.empty(need, dtype=torch.uint8, device=device)
 
 
 # Handle of the current stream of a device: straight from torch's extension module where that has it (0.1 us; a
