@@ -1,14 +1,46 @@
 """torch.autograd plumbing around the C-ABI binding: forward calls cotten_attn_fwd, backward
 calls cotten_attn_bwd (which rebuilds the d x d state from K, V: nothing but the inputs is
 saved).  The kernels return d loss / d log(scale) per slice; the one piece of arithmetic done
-here, in torch, is its conversion to d loss / d scale (a division by the scale, [B,H] values)."""
+here, in torch, is its conversion to d loss / d scale (a division by the scale, [B,H] values).
+
+The kernels' gradients have no derivatives of their own: a second derivative raises."""
 from __future__ import annotations
 
+import functools
 from typing import Optional
 
 import torch
 
 from . import binding
+
+
+class _LastDerivative(torch.autograd.Function):
+    """The first `count` tensors as they are, tied to the others, which they depend on: going on from there raises.
+    (torch's once_differentiable ties them to nothing, and `torch.autograd.grad` takes that for a derivative of zero.)"""
+    @staticmethod
+    def forward(ctx, count, *tensors):
+        return tensors[:count]
+
+    @staticmethod
+    def backward(ctx, *upstream):
+        raise RuntimeError("the gradients of this library's kernels are not differentiable: no second derivatives")
+
+
+def _first_derivatives_only(backward):
+    """For a `backward` whose arithmetic autograd does not see."""
+    @functools.wraps(backward)
+    def run(ctx, *upstream):
+        if not torch.is_grad_enabled():
+            return backward(ctx, *upstream)
+        with torch.no_grad():    # (create_graph)
+            grads = backward(ctx, *upstream)
+        given = [t for t in grads if t is not None]
+        sources = [t for t in (*upstream, *ctx.saved_tensors) if t is not None and t.requires_grad]
+        if not given or not sources:
+            return grads
+        tied = iter(_LastDerivative.apply(len(given), *given, *sources))
+        return tuple(None if t is None else next(tied) for t in grads)
+    return run
 
 
 class _CosineAttention(torch.autograd.Function):
@@ -20,6 +52,7 @@ class _CosineAttention(torch.autograd.Function):
                                        layout=layout)
 
     @staticmethod
+    @_first_derivatives_only
     def backward(ctx, dO):
         Q, K, V, mask, slice_scale = ctx.saved_tensors
         dlog = None
@@ -59,6 +92,7 @@ class _GatedDelta(torch.autograd.Function):
         return (O, state) if return_state else O
 
     @staticmethod
+    @_first_derivatives_only
     def backward(ctx, dO, dstate=None):
         Q, K, V, g, beta, mask, kept, initial_state = ctx.saved_tensors
         dO = torch.zeros_like(Q) if dO is None else dO.contiguous()
@@ -92,6 +126,7 @@ class _ItemEmbedding(torch.autograd.Function):
                                         position_offset=position_offset)
 
     @staticmethod
+    @_first_derivatives_only
     def backward(ctx, dE):
         ids, = ctx.saved_tensors
         W_shape, P_shape = ctx.shapes

@@ -1,0 +1,70 @@
+"""What the differentiable functions do around the library's calls, with stand-ins for these on the CPU."""
+import pytest
+import torch
+
+from paper_2602_06935_amd import autograd, binding
+
+
+@pytest.fixture
+def stand_ins(monkeypatch):
+    """Forward and backward calls that compute nothing, but return tensors of the right shapes; what backwards were given."""
+    given = {}
+
+    def delta_backward(prm, dims, Q, K, V, g, beta, mask, dO, initial_state, dfinal_state, dinitial_state, kept):
+        given.update(dO=dO, dfinal_state=dfinal_state)
+        return tuple(torch.ones_like(t) for t in (Q, K, V, g, beta))
+
+    monkeypatch.setattr(binding, "cotten_attn_fwd", lambda Q, *a, **kw: Q.detach() + 1.0)
+    monkeypatch.setattr(binding, "cotten_attn_bwd", lambda Q, K, V, mask, dO, **kw: tuple(torch.ones_like(Q) for _ in range(3)))
+    monkeypatch.setattr(binding, "cotten_delta_kept", lambda Q, **kw: torch.zeros(8))
+    monkeypatch.setattr(binding, "cotten_delta_fwd", lambda Q, *a, **kw: Q.detach() + 1.0)
+    monkeypatch.setattr(binding, "_delta_backward_of", delta_backward)
+    monkeypatch.setattr(binding, "cotten_embed_fwd", lambda ids, W, *a, **kw: W.detach().new_ones(*ids.shape, W.shape[1]))
+    monkeypatch.setattr(binding, "_embed_backward_of",
+                        lambda prm, ids, dE, W_shape, P_shape, *a: (dE.new_ones(W_shape), None if P_shape is None else dE.new_ones(P_shape)))
+    return given
+
+
+def leaves(*shapes):
+    return [torch.randn(s).requires_grad_() for s in shapes]
+
+
+def outputs():
+    q, k, v, g, beta = leaves(*[(1, 1, 4, 16)] * 3, *[(1, 1, 4)] * 2)
+    yield "attention", q, autograd.cosine_attention(q, k, v)
+    yield "delta", q, autograd.gated_delta_attention(q, k, v, g, beta)
+    W, P = leaves((5, 8), (4, 8))
+    yield "embedding", W, autograd.item_embedding(torch.zeros(2, 3, dtype=torch.int64), W, P)
+
+
+def test_second_derivatives_raise(stand_ins):
+    """A penalty on the gradients would lose its term: the kernels' gradients do not say what they depend on."""
+    for name, x, y in outputs():
+        first, = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="second derivatives"):
+            torch.autograd.grad(y.sum() + first.square().sum(), x)
+            pytest.fail(name)
+        first, = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="second derivatives"):
+            (y.sum() + first.square().sum()).backward()
+            pytest.fail(name)
+
+
+def test_second_derivatives_raise_where_the_upstream_gradient_is_constant(stand_ins):
+    """... but not the inputs that it meets."""
+    for name, x, y in outputs():
+        if name == "embedding":     # linear: its gradient depends on the upstream gradient alone
+            continue
+        first, = torch.autograd.grad(y.sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError, match="second derivatives"):
+            torch.autograd.grad(y.sum() + first.square().sum(), x)
+            pytest.fail(name)
+
+
+def test_graphs_of_first_derivatives_are_allowed(stand_ins):
+    """What does not go on through the kernels' gradients does not raise, and these are what they are without a graph."""
+    for name, x, y in outputs():
+        plain, = torch.autograd.grad((y * y).sum(), x, retain_graph=True)
+        first, = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+        assert torch.equal(first, plain), name
+        torch.autograd.grad(y.sum() + first.detach().sum(), x)
