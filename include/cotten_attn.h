@@ -319,7 +319,9 @@ size_t cotten_delta_workspace_bytes(int B, int H, int N, int d_h, int dtype, int
  *
  * The backward needs a workspace of cotten_embed_workspace_bytes() bytes (lists of the tokens sorted by id, and
  * partial sums).  Calls enqueue on `stream` only and allocate nothing.  D up to 65536, V below 2^30, B * N below 2^31
- * (with dW up to 2^29), with dP up to 2^22 positions (COTTEN_ERR_BAD_SHAPE beyond). */
+ * (with dW up to 2^29), with dP up to 2^22 positions, and tables and gradients of no more than a launch reaches: a workgroup for
+ * 64 KB of zeros, for 64 pieces of up to 16 bytes of dP's columns, or for a row of more than 64 KB, of 2^23 in
+ * all (COTTEN_ERR_BAD_SHAPE beyond, before anything is enqueued). */
 typedef struct cotten_embed_params {
   int dtype;            /* a cotten_dtype: of W, P, E and their gradients                        */
   int id_bytes;         /* 4 or 8                                                                */

@@ -301,8 +301,9 @@ struct Rows {
 constexpr int kSumThreads = 512;
 
 // dP, by the workgroups of sum_kernel behind its units.  dE is a matrix of B rows and N * D columns here, and dP the sums of
-// its columns (positions that no token has: zeros).  A workgroup has `lanes` pieces of columns, and its lane groups deal the
-// rows of its part out among them.  Few columns of many rows are cut into parts (four or more, of at least kPartRows rows)
+// its columns.  A workgroup has `lanes` pieces of columns, and its lane groups deal the rows of its part out among them;
+// workgroups behind these write the zeros of positions that no token has, kZeroBytes each (one token a call and a table of 4096
+// positions: the table may be any number of times as long as the columns that there is something to sum for).  Few columns of many rows are cut into parts (four or more, of at least kPartRows rows)
 // until there are kParts workgroups, and join_positions_kernel adds the parts.  Whole backward, fp32, D = 256, in parts / in one: 65536 x 1:
 // 57 / 631 us; 16384 x 4:
 // 52 / 182 us.
@@ -317,9 +318,17 @@ constexpr int kParts = 256, kPartRows = 64, kPartLanes = 64;
 
 template <class T, int VEC>
 __device__ __forceinline__ void sum_positions(const Positions<T>& p, const T* __restrict__ dE, uint32_t index, float* shared) {
+  if (index >= p.parts * p.blocks) {
+    const size_t first = static_cast<size_t>(index - p.parts * p.blocks) * (kZeroBytes / sizeof(T)), rest = p.total - p.width;
+    const size_t end = first + kZeroBytes / sizeof(T) < rest ? first + kZeroBytes / sizeof(T) : rest;
+    const float zeros[VEC] = {};
+    for (size_t i = first + threadIdx.x * VEC; i < end; i += kSumThreads * VEC)
+      Vec<T, VEC>::store(p.dP + (i < p.start ? i : i + p.width), zeros);
+    return;
+  }
   const uint32_t groups = kSumThreads / p.lanes, group = threadIdx.x / p.lanes, part = index / p.blocks;
-  const size_t col = (static_cast<size_t>(index - part * p.blocks) * p.lanes + threadIdx.x % p.lanes) * VEC, c = col - p.start;
-  const bool inside = c < p.width;  // (columns before: beyond all, as an unsigned number)
+  const size_t c = (static_cast<size_t>(index - part * p.blocks) * p.lanes + threadIdx.x % p.lanes) * VEC;
+  const bool inside = c < p.width;
   const uint32_t share = (p.B + p.parts - 1) / p.parts, end = (part + 1) * share < p.B ? (part + 1) * share : p.B;
   const uint32_t first = part * share + group, rows = first < end ? (end - first + groups - 1) / groups : 0;
   const T* from = dE + first * p.width + c;
@@ -354,12 +363,12 @@ __device__ __forceinline__ void sum_positions(const Positions<T>& p, const T* __
       for (int e = 0; e < VEC; ++e) shared[e * kSumThreads + threadIdx.x] += shared[e * kSumThreads + threadIdx.x + half * p.lanes];
     __syncthreads();
   }
-  if (group == 0 && col < p.total) {
+  if (group == 0 && inside) {
 #pragma unroll
     for (int e = 0; e < VEC; ++e) sum[e] = shared[e * kSumThreads + threadIdx.x];
     if (p.parts == 1) {
-      Vec<T, VEC>::store(p.dP + col, sum);
-    } else if (inside) {
+      Vec<T, VEC>::store(p.dP + p.start + c, sum);
+    } else {
 #pragma unroll
       for (int e = 0; e < VEC; ++e) p.partial[part * p.width + c + e] = sum[e];
     }
@@ -372,17 +381,17 @@ __global__ __launch_bounds__(kSumThreads) void join_positions_kernel(Positions<T
   constexpr int kWaves = kSumThreads / 64;
   __shared__ float shared[kWaves][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const size_t col = static_cast<size_t>(blockIdx.x) * 64 + lane, c = col - p.start;
+  const size_t c = static_cast<size_t>(blockIdx.x) * 64 + lane;
   float sum = 0.0f;
   if (c < p.width)
 #pragma unroll 8
     for (uint32_t i = wave; i < p.parts; i += kWaves) sum += p.partial[i * p.width + c];
   shared[wave][lane] = sum;
   __syncthreads();
-  if (wave > 0 || col >= p.total) return;
+  if (wave > 0 || c >= p.width) return;
 #pragma unroll
   for (int w = 1; w < kWaves; ++w) sum += shared[w][lane];
-  p.dP[col] = static_cast<T>(sum);
+  p.dP[p.start + c] = static_cast<T>(sum);
 }
 
 template <class T, int VEC>
@@ -839,27 +848,37 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
   if (!aligned16(dE) || !aligned16(dW) || !aligned16(dP)) return COTTEN_ERR_MISALIGNED;
   const long long n = static_cast<long long>(B) * N;
   const Layout at(B, N, D, V);
-  const int vec = piece_bytes(D, params->dtype == COTTEN_F32 ? 4 : 2) / (params->dtype == COTTEN_F32 ? 4 : 2);
-  // (sum_kernel: a thread for each piece of dP, and 64 at most for each unit of tokens)
-  if (dP != nullptr && (params->positions > kMostBlocks || static_cast<long long>(params->positions) * (D / vec) > (1ll << 30)))
-    return COTTEN_ERR_BAD_SHAPE;
+  const int elem = params->dtype == COTTEN_F32 ? 4 : 2, vec = piece_bytes(D, elem) / elem, lanes_of_row = lanes_of(D / vec);
+  if (dP != nullptr && params->positions > kMostBlocks) return COTTEN_ERR_BAD_SHAPE;
   if (dW != nullptr && n > (1ll << 29)) return COTTEN_ERR_BAD_SHAPE;
+  const bool direct = dW != nullptr && n <= kDirectTokens;
+  const size_t row = static_cast<size_t>(D) * elem, table = V * row;
+  // what sums dW: of the one launch, at least 512 workgroups, if there are rows for them, and more for kZeroBytes of zeros each
+  const size_t by_bytes = kZeroBytes / row, by_rows = (static_cast<size_t>(V) + 511) / 512;
+  const uint32_t of_rows = static_cast<uint32_t>(by_bytes < 1 ? 1 : by_bytes < by_rows ? by_bytes : by_rows);
+  const uint32_t of_block = kSumThreads / lanes_of_row;
+  const uint32_t table_blocks = dW == nullptr ? 0 : direct ? (V + of_rows - 1) / of_rows : (at.units + of_block - 1) / of_block;
   uint32_t lanes = kSumThreads, parts = 0, columns = 0;  // of the sums for dP: see Positions
+  size_t position_blocks = 0;
   if (dP != nullptr) {
     while (lanes > kPartLanes && kSumThreads / lanes < static_cast<uint32_t>(B)) lanes /= 2;
-    const auto blocks_of = [&](long long rows) { return static_cast<uint32_t>((rows * (D / vec) + lanes - 1) / lanes); };
-    columns = blocks_of(params->positions);
-    const uint32_t shares = (static_cast<uint32_t>(B) + kPartRows - 1) / kPartRows, most = kParts / blocks_of(N);
-    parts = most < 4 ? 1 : shares < most ? shares : most;
+    const size_t all_columns = (static_cast<size_t>(N) * (D / vec) + lanes - 1) / lanes;
+    const size_t shares = (static_cast<size_t>(B) + kPartRows - 1) / kPartRows, most = kParts / all_columns;
+    parts = static_cast<uint32_t>(most < 4 ? 1 : shares < most ? shares : most);
+    columns = static_cast<uint32_t>(all_columns);
+    position_blocks = parts * all_columns + (static_cast<size_t>(params->positions - N) * row + kZeroBytes - 1) / kZeroBytes;
     if (parts > 1 && (params->workspace == nullptr || params->workspace_bytes < at.words * 4)) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
   }
   if (dW != nullptr && (params->workspace == nullptr || params->workspace_bytes < at.words * 4)) return COTTEN_ERR_WORKSPACE_TOO_SMALL;
+  // a launch has less than 2^32 threads (the sort's write a share of the zeros each)
+  if (table_blocks + position_blocks >= (1ull << 32) / kSumThreads || (dW != nullptr && table / kZeroBytes >= (1ull << 24)))
+    return COTTEN_ERR_BAD_SHAPE;
   const hipStream_t s = static_cast<hipStream_t>(stream);
   hipError_t err = hipSuccess;
   Rows rows{};
   rows.V = V;
   rows.D = D;
-  const bool direct = dW != nullptr && n <= kDirectTokens;
+  rows.lanes = lanes_of_row;
   if (dW != nullptr) {
     rows.n = static_cast<uint32_t>(n);
     rows.scale = params->scale;
@@ -875,7 +894,6 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
     sort.blocks = at.blocks;
     const int bits = key_bits(V), last = (at.passes - 1) & 1;
     // every launch of the sort with its share of the zeros
-    const size_t table = static_cast<size_t>(V) * D * (params->dtype == COTTEN_F32 ? 4 : 2);
     const size_t launches = 3 * at.passes;
     const size_t share = ((table + launches - 1) / launches + kZeroBytes - 1) / kZeroBytes * kZeroBytes;
     size_t written = 0;
@@ -910,33 +928,28 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
   by_type(params->dtype, D, [&](auto tag) {
     typedef typename decltype(tag)::type T;
     constexpr int VEC = decltype(tag)::vec;
-    rows.lanes = lanes_of(D / VEC);
-    const uint32_t of_block = kSumThreads / rows.lanes, unit_blocks = (rows.units + of_block - 1) / of_block;
     const Positions<T> positions{static_cast<T*>(dP),
                                  parts > 1 ? static_cast<float*>(params->workspace) + (at.words - at.positions) : nullptr,
                                  static_cast<size_t>(N) * D,
                                  static_cast<size_t>(params->position_offset) * D,
                                  static_cast<size_t>(params->positions) * D,
                                  static_cast<uint32_t>(B), lanes, parts, columns};
+    const dim3 grid(table_blocks + static_cast<uint32_t>(position_blocks), (D / VEC + rows.lanes - 1) / rows.lanes);
     if (direct) {
-      // at least 512 workgroups, if there are rows for them, and more for kZeroBytes of zeros each
-      const size_t by_bytes = kZeroBytes / (static_cast<size_t>(D) * sizeof(T)), by_rows = (static_cast<size_t>(V) + 511) / 512;
-      const uint32_t of_rows = static_cast<uint32_t>(by_bytes < 1 ? 1 : by_bytes < by_rows ? by_bytes : by_rows);
-      const uint32_t row_blocks = (V + of_rows - 1) / of_rows;
       const auto kernel = n <= kFewTokens ? direct_kernel<T, VEC, kFewTokens> : direct_kernel<T, VEC, kDirectTokens>;
-      kernel<<<dim3(row_blocks + parts * columns, (D / VEC + rows.lanes - 1) / rows.lanes), dim3(kSumThreads), 0, s>>>(
+      kernel<<<grid, dim3(kSumThreads), 0, s>>>(
           Ids{ids, params->id_bytes == 8, V, params->padding_idx}, rows, static_cast<const T*>(dE), static_cast<T*>(dW), of_rows,
-          row_blocks, positions);
+          table_blocks, positions);
     } else {
-      sum_kernel<T, VEC><<<dim3(unit_blocks + parts * columns, (D / VEC + rows.lanes - 1) / rows.lanes),
-                           dim3(kSumThreads), 0, s>>>(rows, static_cast<const T*>(dE), static_cast<T*>(dW), positions, unit_blocks);
+      sum_kernel<T, VEC><<<grid, dim3(kSumThreads), 0, s>>>(rows, static_cast<const T*>(dE), static_cast<T*>(dW), positions,
+                                                            table_blocks);
     }
     if (parts > 1)
-      join_positions_kernel<T><<<dim3(static_cast<uint32_t>((positions.total + 63) / 64)), dim3(kSumThreads), 0, s>>>(positions);
+      join_positions_kernel<T><<<dim3(static_cast<uint32_t>((positions.width + 63) / 64)), dim3(kSumThreads), 0, s>>>(positions);
     if (dW != nullptr && !direct) {
-      const dim3 grid((at.units + kJoinWaves - 1) / kJoinWaves);
-      if (D % 4 == 0) join_kernel<T, 4><<<grid, dim3(64 * kJoinWaves), 0, s>>>(rows, static_cast<T*>(dW));
-      else join_kernel<T, 1><<<grid, dim3(64 * kJoinWaves), 0, s>>>(rows, static_cast<T*>(dW));
+      const dim3 join((at.units + kJoinWaves - 1) / kJoinWaves);
+      if (D % 4 == 0) join_kernel<T, 4><<<join, dim3(64 * kJoinWaves), 0, s>>>(rows, static_cast<T*>(dW));
+      else join_kernel<T, 1><<<join, dim3(64 * kJoinWaves), 0, s>>>(rows, static_cast<T*>(dW));
     }
   });
   if (err == hipSuccess) err = hipGetLastError();

@@ -1,0 +1,29 @@
+"""Gradients of tables of positions that are much longer than the calls that use them."""
+import pytest
+import torch
+
+from paper_2602_06935_amd import binding
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("B,N,D,rows,offset", [(16384, 1, 256, 32768, 20000), (16384, 1, 256, 32768, 0), (16384, 1, 256, 32768, 32767),
+                                               (1, 1, 3, 5000, 4999), (9, 1, 512, 70000, 1), (200, 2, 99, 4096, 4094),
+                                               (300, 30, 17, 9000, 77), (7, 1, 1, 100003, 50001)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
+def test_long_tables(dtype, B, N, D, rows, offset):
+    """One token a call, at the front, in the middle and at the end: sums in parts and in one, zeros everywhere else.  fp32
+    sums of B terms, at most B / 4 + 32 roundings in a row, and one rounding to the type."""
+    gen = torch.Generator().manual_seed(B + D)
+    dE = torch.randn(B, N, D, generator=gen).to(dtype)
+    ids = torch.randint(0, 40, (B, N), generator=gen)
+    dP = torch.full((rows, D), 7.0, dtype=dtype, device="cuda")
+    dW = binding.cotten_embed_bwd(ids.cuda(), dE.cuda(), 40, dP=dP, position_offset=offset)
+    alone = binding.cotten_embed_bwd(ids.cuda(), dE.cuda(), 40)
+    torch.cuda.synchronize()
+    assert torch.equal(dW, alone)
+    got, want = dP.cpu(), dE.double().sum(0)
+    half = torch.finfo(dtype).eps / 2
+    slack = 2.0 ** -24 * (B / 4 + 32) * B ** 0.5 * 4 + (6e-8 if dtype is torch.float16 else 0)
+    assert ((got[offset:offset + N].double() - want).abs() <= half * want.abs() * 1.01 + slack).all()
+    assert (got[:offset] == 0).all() and (got[offset + N:] == 0).all()
