@@ -864,7 +864,8 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
     while (lanes > kPartLanes && kSumThreads / lanes < static_cast<uint32_t>(B)) lanes /= 2;
     const size_t all_columns = (static_cast<size_t>(N) * (D / vec) + lanes - 1) / lanes;
     const size_t shares = (static_cast<size_t>(B) + kPartRows - 1) / kPartRows, most = kParts / all_columns;
-    parts = static_cast<uint32_t>(most < 4 ? 1 : shares < most ? shares : most);
+    parts = static_cast<uint32_t>(shares < most ? shares : most);
+    if (parts < 4) parts = 1;
     columns = static_cast<uint32_t>(all_columns);
     position_blocks = parts * all_columns + (static_cast<size_t>(params->positions - N) * row + kZeroBytes - 1) / kZeroBytes;
     if (parts > 1 && (params->workspace == nullptr || params->workspace_bytes < at.words * 4)) return COTTEN_ERR_WORKSPACE_TOO_SMALL;

@@ -1,4 +1,6 @@
 """Gradients of tables of positions that are much longer than the calls that use them."""
+import ctypes
+
 import pytest
 import torch
 
@@ -27,3 +29,18 @@ def test_long_tables(dtype, B, N, D, rows, offset):
     slack = 2.0 ** -24 * (B / 4 + 32) * B ** 0.5 * 4 + (6e-8 if dtype is torch.float16 else 0)
     assert ((got[offset:offset + N].double() - want).abs() <= half * want.abs() * 1.01 + slack).all()
     assert (got[:offset] == 0).all() and (got[offset + N:] == 0).all()
+
+
+@pytest.mark.parametrize("B", [100, 192])
+def test_few_shares_are_not_cut_into_parts(B):
+    """Parts (a second launch, and room for their sums) only from four on: fewer than 193 rows need no workspace."""
+    gen = torch.Generator().manual_seed(B)
+    dE = torch.randn(B, 4, 64, generator=gen)
+    ids, g, dP = torch.zeros(B, 4, dtype=torch.int64, device="cuda"), dE.cuda(), torch.full((9, 64), 7.0, device="cuda")
+    prm = binding.CottenEmbedParams(binding.COTTEN_F32, 8, 1.0, -1, 9, 3, None, 0)
+    binding._check(binding.load_library().cotten_embed_bwd(ids.data_ptr(), g.data_ptr(), None, dP.data_ptr(), B, 4, 64, 40,
+                                                           torch.cuda.current_stream().cuda_stream, ctypes.byref(prm)))
+    torch.cuda.synchronize()
+    want = dE.double().sum(0)
+    assert ((dP[3:7].cpu().double() - want).abs() <= 2.0 ** -24 * (B / 4 + 32) * B ** 0.5 * 4).all()
+    assert (dP[:3] == 0).all() and (dP[7:] == 0).all()
