@@ -43,6 +43,13 @@ def _first_derivatives_only(backward):
     return run
 
 
+def _aligned(t: torch.Tensor) -> torch.Tensor:
+    """An upstream gradient as the library takes it: contiguous, from a 16-byte boundary on (a part of another gradient
+    may begin anywhere)."""
+    t = t.contiguous()
+    return t.clone() if t.data_ptr() & 15 else t
+
+
 class _CosineAttention(torch.autograd.Function):
     @staticmethod
     def forward(ctx, Q, K, V, mask, scale, eps, slice_scale, layout):
@@ -59,7 +66,7 @@ class _CosineAttention(torch.autograd.Function):
         if slice_scale is not None and ctx.needs_input_grad[6]:
             B, H, _, _ = binding._dims(Q, ctx.layout)
             dlog = torch.empty(B, H, device=Q.device, dtype=torch.float32)
-        dQ, dK, dV = binding.cotten_attn_bwd(Q, K, V, mask, dO.contiguous(), scale=ctx.scale,
+        dQ, dK, dV = binding.cotten_attn_bwd(Q, K, V, mask, _aligned(dO), scale=ctx.scale,
                                              eps=ctx.eps, slice_scale=slice_scale,
                                              dlog_scale=dlog, layout=ctx.layout)
         # d loss / d scale = (d loss / d log scale) / scale
@@ -95,12 +102,12 @@ class _GatedDelta(torch.autograd.Function):
     @_first_derivatives_only
     def backward(ctx, dO, dstate=None):
         Q, K, V, g, beta, mask, kept, initial_state = ctx.saved_tensors
-        dO = torch.zeros_like(Q) if dO is None else dO.contiguous()
+        dO = torch.zeros_like(Q) if dO is None else _aligned(dO)
         dfirst = None
         if initial_state is not None and ctx.needs_input_grad[8]:
             dfirst = torch.empty_like(initial_state)
         grads = binding._delta_backward_of(binding.CottenDeltaParams(*ctx.call), ctx.dims, Q, K, V, g, beta, mask, dO,
-                                           initial_state, None if dstate is None else dstate.contiguous(), dfirst, kept)
+                                           initial_state, None if dstate is None else _aligned(dstate), dfirst, kept)
         return (*grads, None, None, None, dfirst, None, None)
 
 
@@ -133,10 +140,7 @@ class _ItemEmbedding(torch.autograd.Function):
         _, of_W, of_P = ctx.needs_input_grad[:3]
         if not (of_W or of_P):
             return None, None, None, None, None, None
-        dE = dE.contiguous()
-        if dE.data_ptr() & 15:  # (a part of another gradient, in rows of an odd width)
-            dE = dE.clone()
-        dW, dP = binding._embed_backward_of(binding.CottenEmbedParams(*ctx.call), ids, dE, W_shape,
+        dW, dP = binding._embed_backward_of(binding.CottenEmbedParams(*ctx.call), ids, _aligned(dE), W_shape,
                                             P_shape if of_P else None)
         return None, dW, dP, None, None, None
 

@@ -14,8 +14,12 @@ def stand_ins(monkeypatch):
         given.update(dO=dO, dfinal_state=dfinal_state)
         return tuple(torch.ones_like(t) for t in (Q, K, V, g, beta))
 
+    def attention_backward(Q, K, V, mask, dO, **kw):
+        given.update(dO=dO)
+        return tuple(torch.ones_like(Q) for _ in range(3))
+
     monkeypatch.setattr(binding, "cotten_attn_fwd", lambda Q, *a, **kw: Q.detach() + 1.0)
-    monkeypatch.setattr(binding, "cotten_attn_bwd", lambda Q, K, V, mask, dO, **kw: tuple(torch.ones_like(Q) for _ in range(3)))
+    monkeypatch.setattr(binding, "cotten_attn_bwd", attention_backward)
     monkeypatch.setattr(binding, "cotten_delta_kept", lambda Q, **kw: torch.zeros(8))
     monkeypatch.setattr(binding, "cotten_delta_fwd", lambda Q, *a, **kw: Q.detach() + 1.0)
     monkeypatch.setattr(binding, "_delta_backward_of", delta_backward)
@@ -68,3 +72,17 @@ def test_graphs_of_first_derivatives_are_allowed(stand_ins):
         first, = torch.autograd.grad((y * y).sum(), x, create_graph=True)
         assert torch.equal(first, plain), name
         torch.autograd.grad(y.sum() + first.detach().sum(), x)
+
+
+def test_upstream_gradients_may_begin_anywhere(stand_ins):
+    """The gradient of a part behind an odd one is a contiguous view off the boundaries that the library asks for."""
+    q, k, v, g, beta = leaves(*[(1, 1, 4, 16)] * 3, *[(1, 1, 4)] * 2)
+    O, S = autograd.gated_delta_attention(q, k, v, g, beta, return_state=True)
+    for outputs, names in (((O, S), ("dO", "dfinal_state")), ((autograd.cosine_attention(q, k, v),), ("dO",))):
+        for out, name in zip(outputs, names):
+            factor = torch.randn(3 + out.numel())
+            stand_ins.clear()
+            torch.autograd.grad((torch.cat([q.flatten()[:3], out.flatten()]) * factor).sum(), q, retain_graph=True)
+            got = stand_ins[name]
+            assert got.data_ptr() % 16 == 0 and got.is_contiguous()
+            assert torch.equal(got.flatten(), factor[3:])
