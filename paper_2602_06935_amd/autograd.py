@@ -141,7 +141,7 @@ class _ItemEmbedding(torch.autograd.Function):
         if not (of_W or of_P):
             return None, None, None, None, None, None
         dW, dP = binding._embed_backward_of(binding.CottenEmbedParams(*ctx.call), ids, _aligned(dE), W_shape,
-                                            P_shape if of_P else None)
+                                            P_shape if of_P else None, of_W)
         return None, dW, dP, None, None, None
 
 

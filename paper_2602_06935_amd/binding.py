@@ -577,15 +577,19 @@ def cotten_embed_fwd(ids: torch.Tensor, W: torch.Tensor, positions: Optional[tor
 
 def cotten_embed_bwd(ids: torch.Tensor, dE: torch.Tensor, V: int, dW: Optional[torch.Tensor] = None,
                      dP: Optional[torch.Tensor] = None, *, scale: float = 1.0, padding_idx: Optional[int] = None,
-                     position_offset: int = 0, stream=None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+                     position_offset: int = 0, stream=None, workspace: Optional[torch.Tensor] = None,
+                     of_table: bool = True) -> Optional[torch.Tensor]:
     """The gradient dW [V,D] of the table (written whole) for the upstream gradient dE; `dP`, the shape of the table of
-    positions, receives its gradient when given."""
+    positions, receives its gradient when given.  `of_table=False`: dP alone (a table that is not trained), and None comes back."""
     lib = _lib or load_library()
     _check_table("dE", dE, 3)
     B, N, D = dE.shape
     if ids.shape != (B, N):
         raise ValueError("ids must be [B,N] and dE [B,N,D]")
-    if dW is None:
+    if not of_table:
+        if dW is not None or dP is None:
+            raise ValueError("of_table=False: dP is wanted, and no dW")
+    elif dW is None:
         dW = dE.new_empty((V, D))
     else:
         _check_table("dW", dW, 2, dE)
@@ -603,20 +607,20 @@ def cotten_embed_bwd(ids: torch.Tensor, dE: torch.Tensor, V: int, dW: Optional[t
             workspace = _workspace(dE, need, handle)
     if workspace is not None:
         prm.workspace, prm.workspace_bytes = _buffer("workspace", workspace, dE.device)
-    _on_device(dE.device, lib.cotten_embed_bwd, ids.data_ptr(), dE.data_ptr(), dW.data_ptr(), positions, B, N, D, V, handle,
-               ctypes.byref(prm))
+    _on_device(dE.device, lib.cotten_embed_bwd, ids.data_ptr(), dE.data_ptr(), None if dW is None else dW.data_ptr(), positions,
+               B, N, D, V, handle, ctypes.byref(prm))
     return dW
 
 
-def _embed_backward_of(prm, ids, dE, W_shape, P_shape):
+def _embed_backward_of(prm, ids, dE, W_shape, P_shape, of_table):
     """(dW, dP) of a forward call that has checked its tensors (the differentiable function's): `prm` holds all but the
-    workspace.  `P_shape` None: dW alone."""
+    workspace.  `P_shape` None: dW alone; not `of_table`: dP alone."""
     B, N, D = dE.shape
     handle = _stream_handle(None)
     workspace = _workspace(dE, cotten_embed_workspace_bytes(B, N, D, W_shape[0]), handle)
     prm.workspace, prm.workspace_bytes = workspace.data_ptr(), workspace.numel()
-    dW = dE.new_empty(W_shape)
+    dW = dE.new_empty(W_shape) if of_table else None
     dP = None if P_shape is None else dE.new_empty(P_shape)
-    _on_device(dE.device, _lib.cotten_embed_bwd, ids.data_ptr(), dE.data_ptr(), dW.data_ptr(),
-               None if dP is None else dP.data_ptr(), B, N, D, W_shape[0], handle, ctypes.byref(prm))
+    _on_device(dE.device, _lib.cotten_embed_bwd, ids.data_ptr(), dE.data_ptr(),
+               None if dW is None else dW.data_ptr(), None if dP is None else dP.data_ptr(), B, N, D, W_shape[0], handle, ctypes.byref(prm))
     return dW, dP

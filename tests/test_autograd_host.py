@@ -86,3 +86,20 @@ def test_upstream_gradients_may_begin_anywhere(stand_ins):
             got = stand_ins[name]
             assert got.data_ptr() % 16 == 0 and got.is_contiguous()
             assert torch.equal(got.flatten(), factor[3:])
+
+
+def test_gradients_that_nobody_wants_are_not_computed(monkeypatch, stand_ins):
+    """Positions that are trained over a table that is not: the table's gradient is a sort and a write of all of it."""
+    wanted = []
+
+    def backward(prm, ids, dE, W_shape, P_shape, of_table=True):
+        wanted.append((of_table, P_shape is not None))
+        return dE.new_ones(W_shape) if of_table else None, None if P_shape is None else dE.new_ones(P_shape)
+
+    monkeypatch.setattr(binding, "_embed_backward_of", backward)
+    ids = torch.zeros(2, 3, dtype=torch.int64)
+    for of_W, of_P in ((True, True), (True, False), (False, True)):
+        W, P = torch.randn(5, 8, requires_grad=of_W), torch.randn(4, 8, requires_grad=of_P)
+        autograd.item_embedding(ids, W, P).sum().backward()
+        assert wanted.pop() == (of_W, of_P)
+        assert (W.grad is not None, P.grad is not None) == (of_W, of_P)

@@ -44,3 +44,21 @@ def test_few_shares_are_not_cut_into_parts(B):
     want = dE.double().sum(0)
     assert ((dP[3:7].cpu().double() - want).abs() <= 2.0 ** -24 * (B / 4 + 32) * B ** 0.5 * 4).all()
     assert (dP[:3] == 0).all() and (dP[7:] == 0).all()
+
+
+@pytest.mark.parametrize("B,N,D", [(1, 1, 64), (5, 30, 99), (90, 110, 64), (700, 3, 256)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_positions_alone(dtype, B, N, D):
+    """The gradient of the positions without the table's: the same bits, by the call and by the differentiable function."""
+    from paper_2602_06935_amd.autograd import item_embedding
+    gen = torch.Generator().manual_seed(B + D)
+    dE = torch.randn(B, N, D, generator=gen).to(dtype).cuda()
+    ids = torch.randint(0, 40, (B, N), generator=gen).cuda()
+    W, P = torch.randn(40, D, generator=gen).to(dtype).cuda(), torch.randn(N + 9, D, generator=gen).to(dtype).cuda()
+    both, alone = torch.full_like(P, 7.0), torch.full_like(P, 7.0)
+    binding.cotten_embed_bwd(ids, dE, 40, dP=both, position_offset=2)
+    assert binding.cotten_embed_bwd(ids, dE, 40, dP=alone, position_offset=2, of_table=False) is None
+    got, = torch.autograd.grad(item_embedding(ids, W, P.requires_grad_(), position_offset=2), P, dE)
+    assert torch.equal(both, alone) and torch.equal(both, got)
+    with pytest.raises(ValueError):
+        binding.cotten_embed_bwd(ids, dE, 40, of_table=False)
