@@ -423,6 +423,8 @@ def _delta_params(Q, dims, gates, scale, eps, layout, workspace, kept, initial_s
     """The checks of what the two calls share besides Q, K and V, and their parameters."""
     B, H, _, d = dims
     dev, lead, size = Q.device, Q.shape[:3], B * H * d * d
+    if scale is not None and ctypes.c_float(scale).value <= 0:
+        raise ValueError("scale must be a positive float32, or None for 1")    # (the library takes 0 and below for 1)
     for name, t in gates:
         _check_gate(name, t, lead, dev)
     first = _f32_vector("initial_state", initial_state, size, dev)
@@ -444,7 +446,7 @@ def cotten_delta_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch
     """Gated delta rule: S_t = a_t S_{t-1} + khat_t u_t^T with u_t = beta_t (v_t - a_t S_{t-1}^T khat_t) and a_t =
     exp(g_t); O_t = scale * S_t^T qhat_t.  Enqueues on the stream and returns O.
     `g` (log decays) and `beta` are float32, [B,H,N] ([B,N,H] with layout "bnhd"); a masked token leaves the state as it is;
-    `scale` defaults to 1.  `initial_state` and `final_state` ([B,H,d_h,d_h] float32) may be the same tensor: with N = 1 that
+    `scale` is positive and defaults to 1.  `initial_state` and `final_state` ([B,H,d_h,d_h] float32) may be the same tensor: with N = 1 that
     is a server's step.  `kept` (see cotten_delta_kept) receives what the backward needs of this call."""
     lib = _lib or load_library()
     _prep_like(Q, (("K", K), ("V", V)))

@@ -1,0 +1,21 @@
+"""Arguments that the bindings of the gated delta rule refuse, with tensors on the CPU behind the checks that come first."""
+import pytest
+import torch
+
+from paper_2602_06935_amd import binding
+
+
+def parameters(B=2, H=3, N=4, d=16, **kw):
+    """The parameters that the calls build of what they are given."""
+    Q, gate = torch.zeros(B, H, N, d), torch.zeros(B, H, N)
+    given = dict(scale=None, eps=None, layout="bhnd", workspace=None, kept=None)
+    given.update(kw)
+    return binding._delta_params(Q, (B, H, N, d), (("g", gate), ("beta", gate)), **given)
+
+
+def test_scales():
+    """The library takes 0 and below for 1: a caller who asks for them would get another result than the formula's."""
+    assert parameters().scale == 0.0 and parameters(scale=0.5).scale == 0.5
+    for bad in (0, 0.0, -0.0, -1.0, -1e-30, 1e-50):
+        with pytest.raises(ValueError, match="scale"):
+            parameters(scale=bad)
