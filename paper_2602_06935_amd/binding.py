@@ -418,21 +418,29 @@ def _check_gate(name: str, t: torch.Tensor, lead, dev) -> None:
         raise ValueError(f"{name} must be a contiguous float32 tensor of shape {tuple(lead)} on the device of Q")
 
 
+def _state_ptr(name: str, t: Optional[torch.Tensor], B: int, H: int, d: int, dev) -> Optional[int]:
+    if t is None:
+        return None
+    if not (t.shape == (B, H, d, d) or t.shape == (B * H, d, d)):    # (another order of as many elements would be read as this one)
+        raise ValueError(f"{name} must be of shape {(B, H, d, d)} or {(B * H, d, d)}, not {tuple(t.shape)}")
+    return _f32_vector(name, t, t.numel(), dev)
+
+
 def _delta_params(Q, dims, gates, scale, eps, layout, workspace, kept, initial_state=None, final_state=None,
                   dfinal_state=None, dinitial_state=None) -> CottenDeltaParams:
     """The checks of what the two calls share besides Q, K and V, and their parameters."""
     B, H, _, d = dims
-    dev, lead, size = Q.device, Q.shape[:3], B * H * d * d
+    dev, lead, sizes = Q.device, Q.shape[:3], (B, H, d, Q.device)
     if scale is not None and ctypes.c_float(scale).value <= 0:
         raise ValueError("scale must be a positive float32, or None for 1")    # (the library takes 0 and below for 1)
     for name, t in gates:
         _check_gate(name, t, lead, dev)
-    first = _f32_vector("initial_state", initial_state, size, dev)
+    first = _state_ptr("initial_state", initial_state, *sizes)
     return CottenDeltaParams(
         _DTYPE_CODES[Q.dtype], 0.0 if scale is None else scale, -1.0 if eps is None else eps, _LAYOUTS[layout],
         *_buffer("workspace", workspace, dev), first,
-        first if final_state is initial_state else _f32_vector("final_state", final_state, size, dev),
-        _f32_vector("dfinal_state", dfinal_state, size, dev), _f32_vector("dinitial_state", dinitial_state, size, dev),
+        first if final_state is initial_state else _state_ptr("final_state", final_state, *sizes),
+        _state_ptr("dfinal_state", dfinal_state, *sizes), _state_ptr("dinitial_state", dinitial_state, *sizes),
         *_buffer("kept", kept, dev))
 
 

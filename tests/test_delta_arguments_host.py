@@ -19,3 +19,14 @@ def test_scales():
     for bad in (0, 0.0, -0.0, -1.0, -1e-30, 1e-50):
         with pytest.raises(ValueError, match="scale"):
             parameters(scale=bad)
+
+
+@pytest.mark.parametrize("name", ["initial_state", "final_state", "dfinal_state", "dinitial_state"])
+def test_shapes_of_states(name):
+    """As many elements in another order are not taken for a state."""
+    for shape in ((2, 3, 16, 16), (6, 16, 16)):
+        t = torch.zeros(shape)
+        assert getattr(parameters(**{name: t}), name) == t.data_ptr()
+    for shape in ((3, 2, 16, 16), (2, 16, 3, 16), (1, 6, 16, 16), (6, 256), (1536,), (2, 3, 16, 8), (3, 6, 16, 16)):
+        with pytest.raises(ValueError, match=name):
+            parameters(**{name: torch.zeros(shape)})
