@@ -418,29 +418,34 @@ def _check_gate(name: str, t: torch.Tensor, lead, dev) -> None:
         raise ValueError(f"{name} must be a contiguous float32 tensor of shape {tuple(lead)} on the device of Q")
 
 
-def _state_ptr(name: str, t: Optional[torch.Tensor], B: int, H: int, d: int, dev) -> Optional[int]:
+_LEAST_SCALE = torch.finfo(torch.float32).tiny
+
+
+def _state_ptr(name: str, t: Optional[torch.Tensor], shape, dev) -> Optional[int]:
     if t is None:
         return None
-    if not (t.shape == (B, H, d, d) or t.shape == (B * H, d, d)):    # (another order of as many elements would be read as this one)
-        raise ValueError(f"{name} must be of shape {(B, H, d, d)} or {(B * H, d, d)}, not {tuple(t.shape)}")
-    return _f32_vector(name, t, t.numel(), dev)
+    if t.shape != shape and t.shape != (shape[0] * shape[1], *shape[2:]):    # (another order of as many elements would be read as this one)
+        raise ValueError(f"{name} must be of shape {shape} or {(shape[0] * shape[1], *shape[2:])}, not {tuple(t.shape)}")
+    if t.dtype is not torch.float32 or not t.is_contiguous() or t.device != dev:
+        raise ValueError(f"{name} must be a contiguous float32 tensor on the device of Q")
+    return t.data_ptr()
 
 
 def _delta_params(Q, dims, gates, scale, eps, layout, workspace, kept, initial_state=None, final_state=None,
                   dfinal_state=None, dinitial_state=None) -> CottenDeltaParams:
     """The checks of what the two calls share besides Q, K and V, and their parameters."""
     B, H, _, d = dims
-    dev, lead, sizes = Q.device, Q.shape[:3], (B, H, d, Q.device)
-    if scale is not None and ctypes.c_float(scale).value <= 0:
-        raise ValueError("scale must be a positive float32, or None for 1")    # (the library takes 0 and below for 1)
+    dev, lead, shape = Q.device, Q.shape[:3], (B, H, d, d)
+    if scale is not None and scale < _LEAST_SCALE:    # (the library takes 0 and below for 1)
+        raise ValueError(f"scale must be None for 1, or {_LEAST_SCALE} at least")
     for name, t in gates:
         _check_gate(name, t, lead, dev)
-    first = _state_ptr("initial_state", initial_state, *sizes)
+    first = _state_ptr("initial_state", initial_state, shape, dev)
     return CottenDeltaParams(
         _DTYPE_CODES[Q.dtype], 0.0 if scale is None else scale, -1.0 if eps is None else eps, _LAYOUTS[layout],
         *_buffer("workspace", workspace, dev), first,
-        first if final_state is initial_state else _state_ptr("final_state", final_state, *sizes),
-        _state_ptr("dfinal_state", dfinal_state, *sizes), _state_ptr("dinitial_state", dinitial_state, *sizes),
+        first if final_state is initial_state else _state_ptr("final_state", final_state, shape, dev),
+        _state_ptr("dfinal_state", dfinal_state, shape, dev), _state_ptr("dinitial_state", dinitial_state, shape, dev),
         *_buffer("kept", kept, dev))
 
 
