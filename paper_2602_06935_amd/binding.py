@@ -541,6 +541,7 @@ def cotten_embed_workspace_bytes(B: int, N: int, D: int, V: int) -> int:
     return int(load_library().cotten_embed_workspace_bytes(B, N, D, V))
 
 
+_MOST_INT = 2 ** 31 - 1    # (ctypes takes the lower 32 bits of a larger number)
 _ID_BYTES = {torch.int32: 4, torch.int64: 8}
 
 
@@ -551,8 +552,10 @@ def _embed_params(ids: torch.Tensor, like: torch.Tensor, scale: float, padding_i
         raise ValueError("ids must be a contiguous int32 or int64 [B,N] tensor on the same device")
     if padding_idx is None:
         padding_idx = -1
-    elif padding_idx < 0:
-        raise ValueError("padding_idx must be None or an id, counted from 0")
+    elif not 0 <= padding_idx <= _MOST_INT:
+        raise ValueError("padding_idx must be None or an id, counted from 0, of 31 bits")
+    if abs(position_offset) > _MOST_INT or positions > _MOST_INT:
+        raise ValueError("position_offset and the rows of the positions must be numbers of 31 bits")
     return CottenEmbedParams(_dtype_code(like), width, scale, padding_idx, positions, position_offset)
 
 
@@ -579,6 +582,8 @@ def cotten_embed_fwd(ids: torch.Tensor, W: torch.Tensor, positions: Optional[tor
         table, rows = positions.data_ptr(), positions.shape[0]
     prm = _embed_params(ids, W, scale, padding_idx, rows or 0, position_offset)
     (B, N), (V, D) = ids.shape, W.shape
+    if V > _MOST_INT:
+        raise ValueError("W must have fewer than 2^31 rows")
     if E is None:
         E = W.new_empty((B, N, D))
     else:
@@ -601,6 +606,8 @@ def cotten_embed_bwd(ids: torch.Tensor, dE: torch.Tensor, V: int, dW: Optional[t
     B, N, D = dE.shape
     if ids.shape != (B, N):
         raise ValueError("ids must be [B,N] and dE [B,N,D]")
+    if V > _MOST_INT:
+        raise ValueError("V, the rows of the table, must be fewer than 2^31")
     if not of_table:
         if dW is not None or dP is None:
             raise ValueError("of_table=False: dP is wanted, and no dW")
