@@ -255,9 +255,9 @@ _current_stream_handle = getattr(torch._C, "_cuda_getCurrentRawStream",
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _stream_handle(stream) -> int:
-    if stream is None:  # that of the current device
-        return _current_stream_handle(_current_device())
+def _stream_handle(stream, device: torch.device) -> int:
+    if stream is None:  # the current one of the device that the tensors are on
+        return _current_stream_handle(device.index)
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
     return int(stream)
@@ -291,7 +291,7 @@ def cotten_attn_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
     _prep_like(Q, (("K", K), ("V", V)))
     B, H, N, d = _dims(Q, layout)
     O = torch.empty_like(Q) if O is None else _prep("O", O, Q)
-    handle = _stream_handle(stream)
+    handle = _stream_handle(stream, Q.device)
     if workspace is None:
         need = _workspace_need(B, H, N, d, False, _dtype_code(Q), bool(causal))
         if need != 0:
@@ -326,7 +326,7 @@ def cotten_attn_bwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
     dQ = torch.empty_like(Q) if dQ is None else _prep("dQ", dQ, Q)
     dK = torch.empty_like(Q) if dK is None else _prep("dK", dK, Q)
     dV = torch.empty_like(Q) if dV is None else _prep("dV", dV, Q)
-    handle = _stream_handle(stream)
+    handle = _stream_handle(stream, Q.device)
     if static_scratch:
         workspace = None
     elif workspace is None:
@@ -361,7 +361,7 @@ def cotten_normaliser_fwd(m: torch.Tensor, n: Optional[torch.Tensor], B: int, N:
     with torch.cuda.device(m.device):
         _check(lib.cotten_normaliser_fwd(m.data_ptr(), _lengths_ptr(n, B, m.device),
                                          _f32_vector("slice_scale", slice_scale, B * H, m.device),
-                                         B, H, N, _stream_handle(stream)))
+                                         B, H, N, _stream_handle(stream, m.device)))
     return slice_scale
 
 
@@ -378,7 +378,7 @@ def cotten_normaliser_bwd(dlog_scale: torch.Tensor, n: Optional[torch.Tensor], N
     with torch.cuda.device(dev):
         _check(lib.cotten_normaliser_bwd(_f32_vector("dlog_scale", dlog_scale, B * H, dev),
                                          _lengths_ptr(n, B, dev), _f32_vector("dm", dm, H, dev),
-                                         B, H, N, _stream_handle(stream)))
+                                         B, H, N, _stream_handle(stream, dev)))
     return dm
 
 
@@ -466,7 +466,7 @@ def cotten_delta_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch
     dims = _dims(Q, layout)
     dtype = _dtype_code(Q)
     O = torch.empty_like(Q) if O is None else _prep("O", O, Q)
-    handle = _stream_handle(stream)
+    handle = _stream_handle(stream, Q.device)
     if workspace is None and kept is None:
         need = cotten_delta_workspace_bytes(*dims, dtype, False)
         if need != 0:
@@ -498,7 +498,7 @@ def cotten_delta_bwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch
     dV = torch.empty_like(Q) if dV is None else _prep("dV", dV, Q)
     dg = torch.empty_like(g) if dg is None else dg
     dbeta = torch.empty_like(beta) if dbeta is None else dbeta
-    handle = _stream_handle(stream)
+    handle = _stream_handle(stream, Q.device)
     if workspace is None:
         workspace = _workspace(Q, cotten_delta_workspace_bytes(*dims, _dtype_code(Q), True, kept is not None), handle)
     prm = _delta_params(Q, dims, (("g", g), ("beta", beta), ("dg", dg), ("dbeta", dbeta)), scale, eps, layout, workspace,
@@ -518,7 +518,7 @@ def _delta_backward(prm, dims, handle, Q, K, V, g, beta, mask, dO, dQ, dK, dV, d
 def _delta_backward_of(prm, dims, Q, K, V, g, beta, mask, dO, initial_state, dfinal_state, dinitial_state, kept):
     """The gradients of a forward call that has checked its tensors (the differentiable function's): `prm` holds its type,
     scale, eps and layout, the rest of it is filled in here."""
-    handle = _stream_handle(None)
+    handle = _stream_handle(None, Q.device)
     workspace = _workspace(Q, cotten_delta_workspace_bytes(*dims, prm.dtype, True, kept is not None), handle)
     prm.workspace, prm.workspace_bytes = workspace.data_ptr(), workspace.numel()
     if kept is not None:
@@ -591,7 +591,7 @@ def cotten_embed_fwd(ids: torch.Tensor, W: torch.Tensor, positions: Optional[tor
         if E.shape != (B, N, D):
             raise ValueError("E must be [B,N,D]")
     _on_device(W.device, lib.cotten_embed_fwd, ids.data_ptr(), W.data_ptr(), table, E.data_ptr(), B, N, D, V,
-               _stream_handle(stream), ctypes.byref(prm))
+               _stream_handle(stream, W.device), ctypes.byref(prm))
     return E
 
 
@@ -621,7 +621,7 @@ def cotten_embed_bwd(ids: torch.Tensor, dE: torch.Tensor, V: int, dW: Optional[t
     if dP is not None:
         _check_table("dP", dP, 2, dE)
         positions, rows = dP.data_ptr(), dP.shape[0]
-    handle = _stream_handle(stream)
+    handle = _stream_handle(stream, dE.device)
     prm = _embed_params(ids, dE, scale, padding_idx, rows or 0, position_offset)
     if workspace is None:
         need = cotten_embed_workspace_bytes(B, N, D, V)
@@ -638,7 +638,7 @@ def _embed_backward_of(prm, ids, dE, W_shape, P_shape, of_table):
     """(dW, dP) of a forward call that has checked its tensors (the differentiable function's): `prm` holds all but the
     workspace.  `P_shape` None: dW alone; not `of_table`: dP alone."""
     B, N, D = dE.shape
-    handle = _stream_handle(None)
+    handle = _stream_handle(None, dE.device)
     workspace = _workspace(dE, cotten_embed_workspace_bytes(B, N, D, W_shape[0]), handle)
     prm.workspace, prm.workspace_bytes = workspace.data_ptr(), workspace.numel()
     dW = dE.new_empty(W_shape) if of_table else None

@@ -13,3 +13,12 @@ def test_every_call_has_its_own_workspace(monkeypatch):
     first, second = binding._workspace(like, 3000, 0), binding._workspace(like, 2000, 0)
     assert first.numel() >= 3000 and second.numel() >= 2000
     assert first.data_ptr() != second.data_ptr()
+
+
+def test_the_stream_is_that_of_the_tensors_device(monkeypatch):
+    """A call on another GPU than the current one goes to that GPU's current stream."""
+    monkeypatch.setattr(binding, "_current_device", lambda: 0)
+    monkeypatch.setattr(binding, "_current_stream_handle", lambda device: 100 + device)
+    assert binding._stream_handle(None, torch.device("cuda", 1)) == 101
+    assert binding._stream_handle(None, torch.device("cuda", 0)) == 100
+    assert binding._stream_handle(77, torch.device("cuda", 1)) == 77
