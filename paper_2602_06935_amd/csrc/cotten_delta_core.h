@@ -557,21 +557,64 @@ struct Scratch {  // of the wave that solves
   float t[2][kSquare];  // diagonal blocks of T
 };
 
-// x + (a of lane J of each 16 lanes) * t, in one instruction.
-template <int J>
-__device__ __forceinline__ float add_from_lane(float a, float t, float x) {
-  asm("v_fmac_f32_dpp %0, %1, %2 row_newbcast:%3 row_mask:0xf bank_mask:0xf" : "+v"(x) : "v"(a), "v"(t), "n"(J));
-  return x;
-}
-template <int J, int M>
-__device__ __forceinline__ float solve_sum(const float (&A)[16], const float (&t)[16], float x) {
-  if constexpr (M > J) return solve_sum<J, M - 1>(A, t, add_from_lane<J>(A[M], t[M], x));
-  else return x;
-}
-template <int J>
-__device__ __forceinline__ void solve_row(const float (&A)[16], float (&t)[16], int i) {
-  t[J] = solve_sum<J, 15>(A, t, i == J ? 1.0f : 0.0f);
-  if constexpr (J > 0) solve_row<J - 1>(A, t, i);
+// t_J = [i = J] - sum_{m > J} t_m A_mJ for J = 15 ... 0, in row i = lane%16; A: minus the column lane%16, so a term is one
+// multiply-add with the value of lane J of each 16 lanes.  A row is one statement, and the two wait states between
+// a register's last write and its use in other lanes are its first instruction: whatever the compiler puts before, a copy too.
+#define COTTEN_TERM(M) "\n\tv_fmac_f32_dpp %[x], %[a" #M "], %[t" #M "] row_newbcast:%[j] row_mask:0xf bank_mask:0xf"
+#define COTTEN_PAIR(M) [a##M] "v"(A[M]), [t##M] "v"(t[M])
+#define COTTEN_TERMS_15 COTTEN_TERM(15)
+#define COTTEN_TERMS_14 COTTEN_TERMS_15 COTTEN_TERM(14)
+#define COTTEN_TERMS_13 COTTEN_TERMS_14 COTTEN_TERM(13)
+#define COTTEN_TERMS_12 COTTEN_TERMS_13 COTTEN_TERM(12)
+#define COTTEN_TERMS_11 COTTEN_TERMS_12 COTTEN_TERM(11)
+#define COTTEN_TERMS_10 COTTEN_TERMS_11 COTTEN_TERM(10)
+#define COTTEN_TERMS_9 COTTEN_TERMS_10 COTTEN_TERM(9)
+#define COTTEN_TERMS_8 COTTEN_TERMS_9 COTTEN_TERM(8)
+#define COTTEN_TERMS_7 COTTEN_TERMS_8 COTTEN_TERM(7)
+#define COTTEN_TERMS_6 COTTEN_TERMS_7 COTTEN_TERM(6)
+#define COTTEN_TERMS_5 COTTEN_TERMS_6 COTTEN_TERM(5)
+#define COTTEN_TERMS_4 COTTEN_TERMS_5 COTTEN_TERM(4)
+#define COTTEN_TERMS_3 COTTEN_TERMS_4 COTTEN_TERM(3)
+#define COTTEN_TERMS_2 COTTEN_TERMS_3 COTTEN_TERM(2)
+#define COTTEN_TERMS_1 COTTEN_TERMS_2 COTTEN_TERM(1)
+#define COTTEN_PAIRS_15 COTTEN_PAIR(15)
+#define COTTEN_PAIRS_14 COTTEN_PAIRS_15, COTTEN_PAIR(14)
+#define COTTEN_PAIRS_13 COTTEN_PAIRS_14, COTTEN_PAIR(13)
+#define COTTEN_PAIRS_12 COTTEN_PAIRS_13, COTTEN_PAIR(12)
+#define COTTEN_PAIRS_11 COTTEN_PAIRS_12, COTTEN_PAIR(11)
+#define COTTEN_PAIRS_10 COTTEN_PAIRS_11, COTTEN_PAIR(10)
+#define COTTEN_PAIRS_9 COTTEN_PAIRS_10, COTTEN_PAIR(9)
+#define COTTEN_PAIRS_8 COTTEN_PAIRS_9, COTTEN_PAIR(8)
+#define COTTEN_PAIRS_7 COTTEN_PAIRS_8, COTTEN_PAIR(7)
+#define COTTEN_PAIRS_6 COTTEN_PAIRS_7, COTTEN_PAIR(6)
+#define COTTEN_PAIRS_5 COTTEN_PAIRS_6, COTTEN_PAIR(5)
+#define COTTEN_PAIRS_4 COTTEN_PAIRS_5, COTTEN_PAIR(4)
+#define COTTEN_PAIRS_3 COTTEN_PAIRS_4, COTTEN_PAIR(3)
+#define COTTEN_PAIRS_2 COTTEN_PAIRS_3, COTTEN_PAIR(2)
+#define COTTEN_PAIRS_1 COTTEN_PAIRS_2, COTTEN_PAIR(1)
+#define COTTEN_ROW(J, M)                                                             \
+  {                                                                                  \
+    float x = i == J ? 1.0f : 0.0f;                                                  \
+    asm("s_nop 1" COTTEN_TERMS_##M : [x] "+&v"(x) : COTTEN_PAIRS_##M, [j] "n"(J));   \
+    t[J] = x;                                                                        \
+  }
+__device__ __forceinline__ void solve_rows(const float (&A)[16], float (&t)[16], int i) {
+  t[15] = i == 15 ? 1.0f : 0.0f;
+  COTTEN_ROW(14, 15)
+  COTTEN_ROW(13, 14)
+  COTTEN_ROW(12, 13)
+  COTTEN_ROW(11, 12)
+  COTTEN_ROW(10, 11)
+  COTTEN_ROW(9, 10)
+  COTTEN_ROW(8, 9)
+  COTTEN_ROW(7, 8)
+  COTTEN_ROW(6, 7)
+  COTTEN_ROW(5, 6)
+  COTTEN_ROW(4, 5)
+  COTTEN_ROW(3, 4)
+  COTTEN_ROW(2, 3)
+  COTTEN_ROW(1, 2)
+  COTTEN_ROW(0, 1)
 }
 
 // T = (I + A)^-1 for A = [[A0, 0], [A10, A1]], strictly lower: the diagonal blocks by substitution (as stable as solving
@@ -591,9 +634,7 @@ __device__ __forceinline__ void solve_blocks(Scratch* s, f32x4_t d0, f32x4_t d1,
 #pragma unroll
     for (int e = 0; e < 4; ++e) A[4 * q + e] = -w[e];
   }
-#pragma unroll
-  for (int e = 0; e < 16; ++e) asm("s_nop 1" : "+v"(A[e]));  // (two states between a result and its use in other lanes)
-  solve_row<15>(A, t, c);
+  solve_rows(A, t, c);
 #pragma unroll
   for (int q = 0; q < 4; ++q)  // (two lane groups write the same; a branch would keep the broadcasts out of the sums)
     *reinterpret_cast<f32x4_t*>(&s->t[g & 1][c * kSquareStride + 4 * q]) = f32x4_t{t[4 * q], t[4 * q + 1], t[4 * q + 2], t[4 * q + 3]};
