@@ -171,13 +171,13 @@ __global__ __launch_bounds__(64 * (kWaves<D, WALK>), waves_per_simd(kWaves<D, WA
       S.load(nullptr, col, lane);
     } else {  // from the segments before: the first one's R has the initial state in it
       S.load(a.transitions + of_segment * 2 * D * D, col, lane);
-      S.cut_all();
+      S.template cut_all<3>();
       for (int j = 1; j < segment; ++j) {
         const float* R = a.transitions + (of_segment + j) * 2 * D * D;
         advance<D, false>(S, R + D * D, R, col, lane);
       }
     }
-    S.cut_all();
+    S.template cut_all<E::kPieces>();
     ColumnTile<E> v;
     const Live lives(a, s);
     const uint32_t with_v = is_m ? 0u : ~0u;
@@ -199,7 +199,7 @@ __global__ __launch_bounds__(64 * (kWaves<D, WALK>), waves_per_simd(kWaves<D, WA
         v.load(s.of(a.V, c + 1, a.stride_row), a.stride_row, with_v & lives.bits(byte, c + 1), col, lane);
         byte = lives.fetch(c + 2, lane);
       }
-      const Pieces<3> y = cut(u[0], u[1]);
+      const Pieces<3> y = cut<3>(u[0], u[1]);
       const Pieces<3> T[2] = {triangle_operand(at + B::kT, 0, lane), triangle_operand(at + B::kT, 1, lane)};
       u[0] = u[1] = f32x4_t{0, 0, 0, 0};
       mul_left(T, y, u);
@@ -209,13 +209,13 @@ __global__ __launch_bounds__(64 * (kWaves<D, WALK>), waves_per_simd(kWaves<D, WA
       if (kKept) store_rows<D>(a.rows_u + chunk * kChunk * D, u, col, lane);
       // S' = e^(G_C) S + K^^T (e^(G_C - G) U)
       const float whole = coef[B::kWhole];
-      const Pieces<3> w = cut(u[0] * by_rows(coef + B::kWriteK, 0, lane), u[1] * by_rows(coef + B::kWriteK, 1, lane));
+      const Pieces<3> w = cut<E::kPieces>(u[0] * by_rows(coef + B::kWriteK, 0, lane), u[1] * by_rows(coef + B::kWriteK, 1, lane));
 #pragma unroll
       for (int dt = 0; dt < S.kTiles; ++dt) S.s[dt] *= whole;
       add_outer<R, D>(S, at + B::kK, w, lane);
       if (kOut) {
         const __amdgpu_buffer_rsrc_t O = s.of(a.O, c, a.stride_row);
-        const Pieces<3> up = cut(u[0], u[1]);
+        const Pieces<3> up = cut<3>(u[0], u[1]);
         const Pieces<3> M[2] = {triangle_operand(at + B::kM, 0, lane), triangle_operand(at + B::kM, 1, lane)};
 #pragma unroll
         for (int tt = 0; tt < 2; ++tt) o[tt] *= coef[B::kQuery + 16 * tt + (lane & 15)];
@@ -224,7 +224,7 @@ __global__ __launch_bounds__(64 * (kWaves<D, WALK>), waves_per_simd(kWaves<D, WA
         for (int tt = 0; tt < 2; ++tt)
           E::store_four(O, static_cast<uint32_t>(16 * tt + (lane & 15)) * a.stride_row + (16 * tile + 4 * (lane >> 4)) * E::kBytes, o[tt]);
       }
-      S.cut_all();
+      S.template cut_all<E::kPieces>();
       lds_barrier();
     }
     if (WALK == kTransition) S.store(a.transitions + ((of_segment + segment) * 2 + (is_m ? 1 : 0)) * D * D, col, lane);

@@ -77,11 +77,11 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2), waves_per_simd(kConsumers
       dS.load(nullptr, col, lane);
     } else {  // from the segments behind: the last one's is whole
       dS.load(a.carries + (of_segment + a.segments - 1) * D * D, col, lane);
-      dS.cut_all();
+      dS.template cut_all<3>();
       for (int j = a.segments - 2; j > segment; --j)
         advance<D, true>(dS, a.transitions + ((of_segment + j) * 2 + 1) * D * D, a.carries + (of_segment + j) * D * D, col, lane);
     }
-    dS.cut_all();
+    dS.template cut_all<E::kPieces>();
     ColumnTile<E> g;
     g.load(s.of(a.dO, last, a.stride_row), a.stride_row, ~0u, col, lane);
     const Live lives(a, s);
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2), waves_per_simd(kConsumers
       if (!CARRY) dS.store(a.dstates + chunk * D * D, col, lane);
       const uint32_t byte = lives.fetch(c > 0 ? c - 1 : 0, lane);
       const Pieces<E::kPieces> up = cut_elements<E>(g.tile(0), g.tile(1));
-      const Pieces<3> write = cut(g.tile(0) * by_rows(coef + B::kQuery, 0, lane), g.tile(1) * by_rows(coef + B::kQuery, 1, lane));
+      const Pieces<3> write = cut<E::kPieces>(g.tile(0) * by_rows(coef + B::kQuery, 0, lane), g.tile(1) * by_rows(coef + B::kQuery, 1, lane));
       if (c > first) g.load(s.of(a.dO, c - 1, a.stride_row), a.stride_row, ~0u, col, lane);
       const Pieces<3> M[2] = {triangle_operand(at + B::kM, 0, lane), triangle_operand(at + B::kM, 1, lane)};
       f32x4_t z[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2), waves_per_simd(kConsumers
 #pragma unroll
       for (int tt = 0; tt < 2; ++tt) z[tt] *= by_rows(coef + B::kWriteK, tt, lane);
       mul_left(M, up, z);
-      const Pieces<3> y = cut(z[0], z[1]);
+      const Pieces<3> y = cut<3>(z[0], z[1]);
       const Pieces<3> T[2] = {triangle_operand(at + B::kT, 0, lane), triangle_operand(at + B::kT, 1, lane)};
       z[0] = z[1] = f32x4_t{0, 0, 0, 0};
       mul_left(T, y, z);
@@ -123,9 +123,9 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2), waves_per_simd(kConsumers
           }
         }
       }
-      const Pieces<3> w = cut(z[0] * by_rows(coef + B::kAdjoint, 0, lane), z[1] * by_rows(coef + B::kAdjoint, 1, lane));
+      const Pieces<3> w = cut<E::kPieces>(z[0] * by_rows(coef + B::kAdjoint, 0, lane), z[1] * by_rows(coef + B::kAdjoint, 1, lane));
       add_outer<R, D>(dS, at + B::kK, w, lane);
-      dS.cut_all();
+      dS.template cut_all<E::kPieces>();
       live = lives.bits(byte, c - 1);
       lds_barrier();
     }
@@ -261,11 +261,11 @@ __device__ __forceinline__ void make_triangle(f32x4_t (&m)[3], const unsigned ch
     pair_sums(d00, d11, d10, pairs + (JOB >> 1) * kChunk, lane);
   }
 }
-template <int JOB>
+template <int JOB, int OTHER>
 __device__ __forceinline__ void put_tiles(unsigned char* at, const f32x4_t (&m)[3], int lane) {
   const f32x4_t zero = {0, 0, 0, 0};
-  put_triangle(at + JOB * kTriangleBytes, 0, lane, m[0], (JOB & 1) ? m[2] : zero);
-  put_triangle(at + JOB * kTriangleBytes, 1, lane, (JOB & 1) ? zero : m[2], m[1]);
+  put_triangle<OTHER>(at + JOB * kTriangleBytes, 0, lane, m[0], (JOB & 1) ? m[2] : zero);
+  put_triangle<OTHER>(at + JOB * kTriangleBytes, 1, lane, (JOB & 1) ? zero : m[2], m[1]);
 }
 
 template <class E, int D>
@@ -386,7 +386,7 @@ __global__ __launch_bounds__(64 * (D / 16), D == 128 ? 2 : 3) void chunk_gradien
   float inner = 0.0f;  // <S, dS'> over the wave's columns
 #pragma unroll
   for (int kb = 0; kb < kBlocks; ++kb) {
-    const Pieces<3> S = cut(before.lo[kb], before.hi[kb]), dS = cut(after.lo[kb], after.hi[kb]);
+    const Pieces<3> S = cut<3>(before.lo[kb], before.hi[kb]), dS = cut<3>(after.lo[kb], after.hi[kb]);
     const Pieces<E::kPieces> up[2] = {R::row_operand(smem + L::kG, 0, kb, lane), R::row_operand(smem + L::kG, 1, kb, lane)};
     mul_right(S, up, dq);
     const Pieces<3> z[2] = {R3::row_operand(smem + L::kZ, 0, kb, lane), R3::row_operand(smem + L::kZ, 1, kb, lane)};
@@ -399,23 +399,23 @@ __global__ __launch_bounds__(64 * (D / 16), D == 128 ? 2 : 3) void chunk_gradien
   lds_barrier();  // U and Z have been read
   unsigned char* triangles = smem + L::kTriangles;
   if constexpr (kWaves >= 4) {
-    if (wave == 0) put_tiles<0>(triangles, m[0], lane);
-    else if (wave == 1) put_tiles<1>(triangles, m[0], lane);
-    else if (wave == 2) put_tiles<2>(triangles, m[0], lane);
-    else if (wave == 3) put_tiles<3>(triangles, m[0], lane);
+    if (wave == 0) put_tiles<0, E::kPieces>(triangles, m[0], lane);
+    else if (wave == 1) put_tiles<1, E::kPieces>(triangles, m[0], lane);
+    else if (wave == 2) put_tiles<2, E::kPieces>(triangles, m[0], lane);
+    else if (wave == 3) put_tiles<3, E::kPieces>(triangles, m[0], lane);
   } else if constexpr (kWaves == 2) {
     if (wave == 0) {
-      put_tiles<0>(triangles, m[0], lane);
-      put_tiles<3>(triangles, m[1], lane);
+      put_tiles<0, E::kPieces>(triangles, m[0], lane);
+      put_tiles<3, E::kPieces>(triangles, m[1], lane);
     } else {
-      put_tiles<1>(triangles, m[0], lane);
-      put_tiles<2>(triangles, m[1], lane);
+      put_tiles<1, E::kPieces>(triangles, m[0], lane);
+      put_tiles<2, E::kPieces>(triangles, m[1], lane);
     }
   } else {
-    put_tiles<0>(triangles, m[0], lane);
-    put_tiles<1>(triangles, m[1], lane);
-    put_tiles<2>(triangles, m[2], lane);
-    put_tiles<3>(triangles, m[3], lane);
+    put_tiles<0, E::kPieces>(triangles, m[0], lane);
+    put_tiles<1, E::kPieces>(triangles, m[1], lane);
+    put_tiles<2, E::kPieces>(triangles, m[2], lane);
+    put_tiles<3, E::kPieces>(triangles, m[3], lane);
   }
   inner *= pow2(G_end);
   float read[2], write[2];

@@ -112,14 +112,14 @@ struct KeyProducer {
       // rows of T as operands; T10^T = -T0^T (A10^T T1^T) comes out as the operand's own layout
       const f32x4_t row1 = square_row(scratch->t[1], lane);
       const f32x4_t t10 = square_product(square_column(scratch->t[0], lane), square_product(a10, row1));
-      put_triangle(at + B::kT, 0, lane, square_row(scratch->t[0], lane), zero);
-      put_triangle(at + B::kT, 1, lane, -t10, row1);
+      put_triangle<3>(at + B::kT, 0, lane, square_row(scratch->t[0], lane), zero);
+      put_triangle<3>(at + B::kT, 1, lane, -t10, row1);
     } else {
       // rows of T^T: columns of T.  T10 = -T1 (A10 T0)
       const f32x4_t col0 = square_column(scratch->t[0], lane);
       const f32x4_t t10 = square_product(square_row(scratch->t[1], lane), square_product(a10, col0));
-      put_triangle(at + B::kT, 0, lane, col0, -t10);
-      put_triangle(at + B::kT, 1, lane, zero, square_column(scratch->t[1], lane));
+      put_triangle<3>(at + B::kT, 0, lane, col0, -t10);
+      put_triangle<3>(at + B::kT, 1, lane, zero, square_column(scratch->t[1], lane));
     }
   }
 };
@@ -188,8 +188,8 @@ struct QueryProducer {
                    : d10[r] * o.factor[0][r] * rq1 * pow2(o.Gc[1], o.G(0, r));
     }
     const f32x4_t zero = {0, 0, 0, 0};
-    put_triangle(at + B::kM, 0, lane, m00, BWD ? m10 : zero);
-    put_triangle(at + B::kM, 1, lane, BWD ? zero : m10, m11);
+    put_triangle<3>(at + B::kM, 0, lane, m00, BWD ? m10 : zero);
+    put_triangle<3>(at + B::kM, 1, lane, BWD ? zero : m10, m11);
   }
 };
 
@@ -252,9 +252,10 @@ struct StateColumns {
 #pragma unroll
       for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(s[dt][i]), r, first + (16 * dt + i) * D * 4, 0, 0);
   }
+  template <int OTHER>
   __device__ __forceinline__ void cut_all() {
 #pragma unroll
-    for (int kb = 0; kb < kBlocks; ++kb) p[kb] = cut(s[2 * kb], s[2 * kb + 1]);
+    for (int kb = 0; kb < kBlocks; ++kb) p[kb] = cut<OTHER>(s[2 * kb], s[2 * kb + 1]);
   }
 };
 
@@ -283,15 +284,15 @@ __device__ __forceinline__ void advance(StateColumns<D>& S, const float* M, cons
       StateColumns<D> m;
       m.load(M, 16 * dt + (lane & 15), lane);
 #pragma unroll
-      for (int kb = 0; kb < S.kBlocks; ++kb) S.s[dt] = mul(cut(m.s[2 * kb], m.s[2 * kb + 1]), S.p[kb], S.s[dt]);
+      for (int kb = 0; kb < S.kBlocks; ++kb) S.s[dt] = mul(cut<3>(m.s[2 * kb], m.s[2 * kb + 1]), S.p[kb], S.s[dt]);
     } else {
       StateRows<D> m;
       m.load(M, dt, lane);
 #pragma unroll
-      for (int kb = 0; kb < S.kBlocks; ++kb) S.s[dt] = mul(cut(m.lo[kb], m.hi[kb]), S.p[kb], S.s[dt]);
+      for (int kb = 0; kb < S.kBlocks; ++kb) S.s[dt] = mul(cut<3>(m.lo[kb], m.hi[kb]), S.p[kb], S.s[dt]);
     }
   }
-  S.cut_all();
+  S.template cut_all<3>();
 }
 
 // A pair of result tiles (tokens 16 tt + 4g + r, column `col`) into the rows of a chunk [32][D].

@@ -65,21 +65,37 @@ struct Pieces {
   bf16x8_t p[P];  // p[0] the leading bits
 };
 
-// Eight values as three pieces of eight significant bits each: h the upper half of the word, m the upper half of what is left,
-// l the rest, which fits.  Exact, and without conversions, which take longer than bit operations (m rounded by one: 16 x 4 x
-// 4096 x 64 bf16 forward 135 us, and 125 so; 64 x 2 x 197 x 128 fp16 backward 97 and 95).
+// Eight values as three pieces of eight significant bits each, exactly: h the upper half of the word, m of what is left, l
+// the rest, which fits.  OTHER: how many pieces the operand has that they meet.  With one, every product is kept, and m is the upper
+// half of what is left.  With more, the products of m and l with l are left out (see mul), and m is rounded: an m cut off leaves
+// an l of x's sign, and products left out that add up (mean 0.69 and 1.0 rms of 2^-24 of a product; rounded 0 and 0.38).
+// Conversions take longer than bit operations: all operands with m cut off / as they are / all rounded, 16 x 4 x 4096 x 64 bf16
+// forward 126.4 / 128.6 / 135 us, 128 x 4 x 200 x 64 bf16 24.7 / 25.2 / 25.9, 64 x 2 x 197 x 128 fp16 29.2 / 30.2 / 30.4.  (Half a
+// step of m added to its bits in place of the conversion: 129.0, 25.0 and 29.8, but fp32, where all are rounded, 256 x 2 x
+// 200 x 32 21.5 for 21.0, 128 x 4 x 200 x 64 45.0 for 44.0.)
 __device__ __forceinline__ float upper(float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); }
 __device__ __forceinline__ uint32_t uppers(float lo, float hi) {
   return __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
 }
+template <int OTHER>
 __device__ __forceinline__ Pieces<3> cut(const float (&x)[8]) {
   u32x4_t h, m, l;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const float a = x[2 * i], b = x[2 * i + 1], ra = a - upper(a), rb = b - upper(b);
     h[i] = uppers(a, b);
-    m[i] = uppers(ra, rb);
-    l[i] = uppers(ra - upper(ra), rb - upper(rb));
+    if constexpr (OTHER > 1) {
+      bf16x2_t v;
+      v[0] = static_cast<__bf16>(ra);
+      v[1] = static_cast<__bf16>(rb);
+      uint32_t w = __builtin_bit_cast(uint32_t, v);
+      asm("" : "+v"(w));  // (both halves from the one conversion: the compiler would make the lower one again)
+      m[i] = w;
+      l[i] = uppers(ra - __uint_as_float(w << 16), rb - upper(__uint_as_float(w)));
+    } else {
+      m[i] = uppers(ra, rb);
+      l[i] = uppers(ra - upper(ra), rb - upper(rb));
+    }
   }
   Pieces<3> r;
   r.p[0] = __builtin_bit_cast(bf16x8_t, h);
@@ -87,15 +103,16 @@ __device__ __forceinline__ Pieces<3> cut(const float (&x)[8]) {
   r.p[2] = __builtin_bit_cast(bf16x8_t, l);
   return r;
 }
+template <int OTHER>
 __device__ __forceinline__ Pieces<3> cut(f32x4_t a, f32x4_t b) {
   const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-  return cut(x);
+  return cut<OTHER>(x);
 }
 
-// The pieces that values of E's are made of (fewer than three where they are 16-bit values).
+// The pieces that values of E's are made of (fewer than three where they are 16-bit values: nothing is left for l).
 template <class E>
 __device__ __forceinline__ Pieces<E::kPieces> cut_elements(f32x4_t a, f32x4_t b) {
-  const Pieces<3> c = cut(a, b);
+  const Pieces<3> c = cut<E::kPieces == 3 ? 3 : 1>(a, b);
   Pieces<E::kPieces> r;
 #pragma unroll
   for (int i = 0; i < E::kPieces; ++i) r.p[i] = c.p[i];
@@ -103,7 +120,7 @@ __device__ __forceinline__ Pieces<E::kPieces> cut_elements(f32x4_t a, f32x4_t b)
 }
 
 // c += A B, the products of pieces that reach 24 bits, the small ones first.  (Of two operands in three pieces, m l is left
-// out: 2^-24 of a product in the mean, 2^-21 at most.)
+// out: with rounded m 0.38 rms of 2^-24 of a product, 2^-22 at most, of either sign.)
 template <int PA, int PB>
 __device__ __forceinline__ f32x4_t mul(const Pieces<PA>& a, const Pieces<PB>& b, f32x4_t c) {
 #pragma unroll
@@ -157,7 +174,7 @@ struct F32 {
   static __device__ __forceinline__ Pieces<3> pieces(const Raw& w) {
     float x[8];
     unpack(w, x);
-    return cut(x);
+    return cut<3>(x);
   }
   typedef uint32_t One;  // an element as it was loaded: turned into a float where it is used, not where it would be waited for
   static __device__ __forceinline__ One load_one(__amdgpu_buffer_rsrc_t r, uint32_t off) {
@@ -223,7 +240,7 @@ struct F16 : Half<_Float16> {  // 11 significant bits: two pieces
   static __device__ __forceinline__ Pieces<2> pieces(const Raw& w) {
     float x[8];
     unpack(w, x);
-    const Pieces<3> c = cut(x);
+    const Pieces<3> c = cut<1>(x);
     Pieces<2> r;
     r.p[0] = c.p[0];
     r.p[1] = c.p[1];
@@ -467,8 +484,9 @@ struct Rows {
 
 // A 32 x 32 triangular operand in LDS in the order the products read it: [tile][piece][lane] 16 bytes.
 constexpr int kTriangleBytes = 2 * 3 * 64 * 16;
+template <int OTHER>
 __device__ __forceinline__ void put_triangle(unsigned char* at, int tile, int lane, f32x4_t lo, f32x4_t hi) {
-  const Pieces<3> x = cut(lo, hi);
+  const Pieces<3> x = cut<OTHER>(lo, hi);
 #pragma unroll
   for (int i = 0; i < 3; ++i) *reinterpret_cast<bf16x8_t*>(at + ((tile * 3 + i) * 64 + lane) * 16) = x.p[i];
 }
