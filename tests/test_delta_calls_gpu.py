@@ -51,3 +51,29 @@ def test_fp32_is_as_near_as_the_definition_in_32_bits(d):
         return sum(((t[n].cpu().double() - ref[n]).norm() / ref[n].norm()).item() for n in names) / len(names)
 
     assert off(got) <= 1.1 * off(plain), (off(got), off(plain))
+
+
+@pytest.mark.parametrize("N", [1, 2, 5, 6])
+@pytest.mark.parametrize("layout", ["bhnd", "bnhd"])
+@pytest.mark.parametrize("d", [16, 32, 64, 128])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_recurrence(dtype, d, layout, N):
+    """Calls of few tokens and few slices, which run token by token: strides of both layouts, masks, states."""
+    x = inputs(3, 2, N, d, DTYPES[dtype], seed=50 + d + N, mask="holes" if N > 1 else None, states=True)
+    ref = reference(x, scale=0.5, grads=False)
+    O, S1, _ = forward(x, layout, scale=0.5)
+    check("O", O, ref["O"])
+    check("S1", S1, ref["S1"])
+
+
+@pytest.mark.parametrize("layout", ["bhnd", "bnhd"])
+@pytest.mark.parametrize("d,slices,N", [(64, 2051, 1), (64, 2051, 7), (128, 1031, 3), (128, 1031, 10), (32, 4099, 2), (16, 4097, 10)])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_recurrence_of_many_slices(dtype, d, slices, N, layout):
+    """More than 4096 waves, four to a workgroup, the last of which is not full but for d = 128; up to ten tokens."""
+    B = {2051: 293, 4097: 241}.get(slices, slices)
+    x = inputs(B, slices // B, N, d, DTYPES[dtype], seed=60 + d + N, mask="holes" if N > 1 else None, states=True)
+    ref = reference(x, scale=0.5, grads=False)
+    O, S1, _ = forward(x, layout, scale=0.5)
+    check("O", O, ref["O"])
+    check("S1", S1, ref["S1"])
