@@ -26,10 +26,10 @@ int check_shape(int B, int H, int N, int d_h, int dtype) {
 struct Sizes {
   size_t states, rows, transitions, carries;
   cotten::delta::Segments segments;
-  Sizes(int B, int H, int N, int d_h) {
+  Sizes(int B, int H, int N, int d_h, int dtype) {
     const size_t slices = static_cast<size_t>(B) * H, state = static_cast<size_t>(d_h) * d_h;
     const size_t chunks = (static_cast<size_t>(N) + cotten::delta::kChunk - 1) / cotten::delta::kChunk;
-    segments = cotten::delta::segments_of(static_cast<long long>(slices), static_cast<int>(chunks), d_h);
+    segments = cotten::delta::segments_of(static_cast<long long>(slices), static_cast<int>(chunks), d_h, dtype);
     states = slices * chunks * state;
     rows = slices * chunks * cotten::delta::kChunk * d_h;
     carries = segments.count > 1 ? slices * segments.count * state : 0;
@@ -93,12 +93,12 @@ void use_kept(cotten::delta::Args* a, float* at, const Sizes& size) {
 extern "C" {
 
 size_t cotten_delta_kept_bytes(int B, int H, int N, int d_h, int dtype) {
-  return check_shape(B, H, N, d_h, dtype) == COTTEN_OK ? Sizes(B, H, N, d_h).kept() : 0;
+  return check_shape(B, H, N, d_h, dtype) == COTTEN_OK ? Sizes(B, H, N, d_h, dtype).kept() : 0;
 }
 
 size_t cotten_delta_workspace_bytes(int B, int H, int N, int d_h, int dtype, int is_bwd, int with_kept) {
   if (check_shape(B, H, N, d_h, dtype) != COTTEN_OK) return 0;
-  const Sizes size(B, H, N, d_h);
+  const Sizes size(B, H, N, d_h, dtype);
   return is_bwd ? size.backward(with_kept != 0) : size.forward(with_kept != 0);
 }
 
@@ -110,7 +110,7 @@ int cotten_delta_fwd(const void* Q, const void* K, const void* V, const float* g
   if (!aligned16(O)) return COTTEN_ERR_MISALIGNED;
   a.O = static_cast<unsigned char*>(O);
   a.final_state = params->final_state;
-  const Sizes size(B, H, N, d_h);
+  const Sizes size(B, H, N, d_h, params->dtype);
   a.segments = size.segments.count;
   a.segment_chunks = size.segments.chunks;
   if (params->kept != nullptr) {
@@ -134,7 +134,7 @@ int cotten_delta_bwd(const void* Q, const void* K, const void* V, const float* g
   if (int rc = prepare(&a, Q, K, V, g, beta, mask, B, H, N, d_h, params)) return rc;
   if (!aligned16(dO) || !aligned16(dQ) || !aligned16(dK) || !aligned16(dV)) return COTTEN_ERR_MISALIGNED;
   if ((reinterpret_cast<uintptr_t>(dg) | reinterpret_cast<uintptr_t>(dbeta)) & 3u) return COTTEN_ERR_MISALIGNED;
-  const Sizes size(B, H, N, d_h);
+  const Sizes size(B, H, N, d_h, params->dtype);
   a.segments = size.segments.count;
   a.segment_chunks = size.segments.chunks;
   const bool kept = params->kept != nullptr;

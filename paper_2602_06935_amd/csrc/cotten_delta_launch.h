@@ -16,7 +16,7 @@ struct Args;
 struct Segments {
   int count, chunks;
 };
-Segments segments_of(long long slices, int chunks, int D);
+Segments segments_of(long long slices, int chunks, int D, int dtype);
 
 // O, final_state, states and rows_u, each where its pointer is given.
 hipError_t launch_forward(const Args& a, int dtype, int D, int slices, hipStream_t stream);

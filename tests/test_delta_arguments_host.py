@@ -30,3 +30,15 @@ def test_shapes_of_states(name):
     for shape in ((3, 2, 16, 16), (2, 16, 3, 16), (1, 6, 16, 16), (6, 256), (1536,), (2, 3, 16, 8), (3, 6, 16, 16)):
         with pytest.raises(ValueError, match=name):
             parameters(**{name: torch.zeros(shape)})
+
+
+def test_short_sequences_are_not_cut_into_segments():
+    """Segments take a second launch and a step over each: few chunks of 32 tokens do not make up for them (a forward without
+    `kept` needs a workspace for segments only)."""
+    F32, BF16, F16 = binding.COTTEN_F32, binding.COTTEN_BF16, binding.COTTEN_F16
+    for d in (16, 32, 64, 128):
+        for dtype in (F32, BF16, F16):
+            shortest = 8 if d <= 32 else 9 if d == 64 or dtype == F32 else 17
+            for B, H in ((1, 1), (4, 4)):
+                cut = [c for c in range(1, 40) if binding.cotten_delta_workspace_bytes(B, H, 32 * c, d, dtype, False) != 0]
+                assert cut == list(range(shortest, 40)), (B, H, d, dtype)
