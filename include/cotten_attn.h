@@ -263,8 +263,10 @@ const char* cotten_status_string(int status);
  *
  * Calls enqueue on `stream` only, allocate nothing, and give the same bits for the same
  * arguments.  A call is several launches that pass data through its workspace and `kept`: calls from several host threads
- * need buffers of their own, also on one stream, where the launches of two calls may alternate.  d_h in {16, 32, 64, 128}; B * H up to 2^22, and the rows of a slice, or 32 of them if
- * there are fewer, within 2^31 bytes from the first to the last (COTTEN_ERR_BAD_SHAPE beyond).  */
+ * need buffers of their own, also on one stream, where the launches of two calls may alternate.
+ *
+ * d_h in {16, 32, 64, 128}; B * H up to 2^22, and the rows of a slice, or 32 of them if there are fewer, within 2^31 bytes
+ * from the first to the last (COTTEN_ERR_BAD_SHAPE beyond).  */
 typedef struct cotten_delta_params {
   int dtype;                  /* a cotten_dtype: of Q, K, V, O and their gradients               */
   float scale;                /* factor of O; <= 0 selects 1                                     */
@@ -309,16 +311,17 @@ size_t cotten_delta_workspace_bytes(int B, int H, int N, int d_h, int dtype, int
  * The input of the layers (Cotten4Rec, "Model Description": E_t = s_t + P_t), with a factor:
  *
  *     E[b,n] = scale * W[ids[b,n]] + P[position_offset + n]
- *     dW[i]  = scale * sum of dE[b,n] over the tokens with ids[b,n] = i, in the order of the tokens
+ *     dW[i]  = scale * sum of dE[b,n] over the tokens with ids[b,n] = i, in a fixed order
  *     dP[position_offset + n] = sum_b dE[b,n]
  *
  * W is [V, D], P [positions, D] (or NULL: none), E and dE [B, N, D], contiguous, all of one element type;
  * ids [B, N], int32 or int64.  A token with padding_idx, or with an id outside 0 ... V-1, has no row:
  * its E is its position's alone, and it gives dW nothing.  Sums are fp32, rounded once.  dW and dP are
- * dense and written whole, zeros included.  The same arguments give the same bits.
+ * dense and written whole, zeros included.  The same arguments give the same bits (sums of more than sixteen tokens are
+ * sums of partial sums).
  *
  * The backward needs a workspace of cotten_embed_workspace_bytes() bytes (lists of the tokens sorted by id, and
- * partial sums).  Calls enqueue on `stream` only and allocate nothing.  D up to 65536, V below 2^30, B * N below 2^31
+ * partial sums), which calls from several host threads must not share, as above.  Calls enqueue on `stream` only and allocate nothing.  D up to 65536, V below 2^30, B * N below 2^31
  * (with dW up to 2^29), with dP up to 2^22 positions, and tables and gradients of no more than a launch reaches: a workgroup for
  * 64 KB of zeros, for 64 pieces of up to 16 bytes of dP's columns, or for a row of more than 64 KB, of 2^23 in
  * all (COTTEN_ERR_BAD_SHAPE beyond, before anything is enqueued). */

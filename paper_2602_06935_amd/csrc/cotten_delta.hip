@@ -100,9 +100,10 @@ __global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
 // instructions and the trips to LDS between them.  A chunk of d = 64 in bf16 takes 2160 vector and 270 matrix instructions
 // over the six waves, 900 of them to cut results into pieces: 1.8 us for a workgroup alone on a compute unit (producers without
 // consumers 1.5, consumers without producers 1.45) and 1.6 for each of two that share one (1.6 and 1.1: the consumers hide).
-// Times of calls in a loop: 128 x 4 x 200 x 64 bf16 24.6 us, 4.3 TB/s of its tensors;  256 x 2 x 200 x 32 fp32
-// 20.8;  64 x 2 x 197 x 128 fp16 29.2;  16 x 4 x 4096 x 64 bf16 in four segments 125, half of it for the segments' R and M (nine waves
-// a workgroup).
+// Times of calls in a loop: 128 x 4 x 200 x 64 bf16 25.2 us, 4.2 TB/s of its tensors;  256 x 2 x 200 x 32 fp32
+// 21.0;  64 x 2 x 197 x 128 fp16 30.2;  16 x 4 x 4096 x 64 bf16 in four segments 129, half of it for the segments' R and M (nine waves
+// a workgroup).  Timed apart: 256 x 2 x 200 x 16 bf16 16.8, fp32 22.3;  128 x 2 x 200 x 128 bf16 39.4, fp32 110 (80 registers of a
+// lane are spilled there).
 template <int D>
 constexpr int kConsumers = D / 16 < 4 ? D / 16 : 4;  // of a workgroup; d = 128 takes two (of ten waves, none would have the registers)
 
@@ -284,7 +285,7 @@ hipError_t launch_dim(const Args& a, int D, int slices, hipStream_t stream) {
 
 Segments segments_of(long long slices, int chunks, int D, int dtype) {
   // About one workgroup for each of the 256 compute units (two take as long as one after the other): 16 x 4 x 4096 x 64
-  // bf16, forward / backward: whole 242 / 378 us, in 4 segments 135 / 287 (125 / 281 by now), in 8 146 / 303; 16 x 4 x 1024: whole 64 / 98, 4
+  // bf16, forward / backward: whole 242 / 378 us, in 4 segments 135 / 287 (129 / 282 by now), in 8 146 / 303; 16 x 4 x 1024: whole 64 / 98, 4
   // segments 43 / 74.  Not more segments than make up for the steps M S + R over them (one takes about as long as half a
   // chunk in each of the two launches).  With two the first launch takes what the second saves: 32 x 4 x 2048 whole 123 /
   // 261 us, in 2 segments 120 / 273;  20 x 4 x 2048 whole 123 / 206, in 3 93 / 183.

@@ -33,7 +33,7 @@ constexpr int kConsumers = D / 16 < 4 ? D / 16 : 4;
 
 // The forward's walk in reverse: two producers, and waves with 16 columns of dS each.  Writes dS' and Z for the second
 // kernel, and dV.  CARRY: only the gradient of the state before a segment, of segments 1 ...  Bound like the forward's walk,
-// and by 24 KB of dS' and Z a chunk (d = 64): 128 x 4 x 200 x 64 bf16 in 39 us, 256 x 2 x 200 x 32 fp32 in 26.
+// and by 24 KB of dS' and Z a chunk (d = 64): 128 x 4 x 200 x 64 bf16 in 40 us, 256 x 2 x 200 x 32 fp32 in 27.
 template <class E, int D>
 constexpr int kWalkLds = 2 * ChunkBuffer<E, D, true>::kBytes + sizeof(Scratch) + sizeof(Notes);
 
@@ -137,8 +137,9 @@ __global__ __launch_bounds__(64 * (kConsumers<D> + 2), waves_per_simd(kConsumers
 // One chunk: a wave has 16 columns (of d_h as the index of q and k) of every result.  Results are computed transposed, so
 // a lane has four columns of one token: factors by token are one value, stores are whole pieces of a row.
 //
-// What bounds it: memory, with the vector units half busy.  128 x 4 x 200 x 64 bf16: 58 us for 250 MB (states on both sides of a
-// chunk 32 KB, U and Z 16, rows 24), 4.3 TB/s;  256 x 2 x 200 x 32 fp32: 44 us;  64 x 2 x 197 x 128 fp16: 66 us.
+// What bounds it: memory, with the vector units half busy.  128 x 4 x 200 x 64 bf16: 59 us for 250 MB (states on both sides of a
+// chunk 32 KB, U and Z 16, rows 24), 4.2 TB/s;  256 x 2 x 200 x 32 fp32: 45 us;  64 x 2 x 197 x 128 fp16: 66 us.  At d = 16 the
+// registers for three waves a SIMD do not hold it: 39 of a lane are spilled in fp32, 25 and 23 in 16 bits.
 template <class E, int D>
 struct GradientLds {
   typedef Rows<D, E::kPieces> R;

@@ -1,6 +1,6 @@
 // Embedding of item ids, E[b,n] = scale * W[id] + P[offset + n], and its gradient:
 //
-//     dW[i] = scale * sum over the tokens with id i of dE (in the order of the tokens)      dP[offset + n] = sum_b dE[b,n]
+//     dW[i] = scale * sum over the tokens with id i of dE (in a fixed order)      dP[offset + n] = sum_b dE[b,n]
 //
 // Everything here moves memory.  The gradient of the table sorts the tokens by id (stable, so a row's sum has one order
 // and a call one result) and sums the sorted rows in units of a few tokens, whatever ids they have: a popular item is
@@ -305,8 +305,7 @@ constexpr int kSumThreads = 512;
 // workgroups behind these write the zeros of positions that no token has, kZeroBytes each (one token a call and a table of 4096
 // positions: the table may be any number of times as long as the columns that there is something to sum for).  Few columns of many rows are cut into parts (four or more, of at least kPartRows rows)
 // until there are kParts workgroups, and join_positions_kernel adds the parts.  Whole backward, fp32, D = 256, in parts / in one: 65536 x 1:
-// 57 / 631 us; 16384 x 4:
-// 52 / 182 us.
+// 55 / 631 us; 16384 x 4: 51 / 182 us.
 template <class T>
 struct Positions {
   T* dP;           // nullptr: not wanted
@@ -546,8 +545,8 @@ __global__ __launch_bounds__(64 * kJoinWaves) void join_kernel(Rows s, T* __rest
 // of all ids, in order, sorts them by row and token in LDS, and sums them, a lane group per row, or the whole workgroup for a
 // row of more than kUnit.  One launch instead of five to eight, and every workgroup reads all ids.  Whole backward, bf16, so /
 // sorted as below (host time: 8): 80 tokens, 3700 rows of 64, 8.0 / 14.5 us;  2000 tokens 8.1 / 19.4;  8000 tokens 13 / 30, and
-// with ids uniform in the logarithm 25 / 31;  8000 of 120000 rows of 256 29 / 40.  (8000 tokens of 50 rows of 300, a fifth of
-// them the same id, lose: 42 / 26.)
+// with ids uniform in the logarithm 25 / 31;  8000 of 120000 rows of 256 29 / 40.  (8000 tokens with such
+// ids lose at rows of 300, which go in 8-byte pieces: 50 rows 40 / 25, 700 41 / 33, 30000 39 / 35; and at 8 rows of 256, 41 / 22.)
 
 constexpr int kDirectTokens = 8192, kFewTokens = 2048;  // (with 2048 a workgroup needs half the LDS, and fewer steps)
 
