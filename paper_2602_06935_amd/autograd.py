@@ -85,11 +85,11 @@ def cosine_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
 
 class _GatedDelta(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, Q, K, V, g, beta, mask, scale, eps, initial_state, layout, return_state):
+    def forward(ctx, Q, K, V, g, beta, mask, scale, eps, initial_state, layout, return_state, recorded):
         ctx.dims = dims = binding._dims(Q, layout)
         B, H, _, d = dims
         state = g.new_empty((B, H, d, d)) if return_state else None
-        kept = binding.cotten_delta_kept(Q, layout=layout) if any(ctx.needs_input_grad) else None
+        kept = binding.cotten_delta_kept(Q, layout=layout) if recorded and any(ctx.needs_input_grad) else None
         O = binding.cotten_delta_fwd(Q, K, V, g, beta, mask, scale=scale, eps=eps, layout=layout,
                                      initial_state=initial_state, final_state=state, kept=kept)
         ctx.save_for_backward(Q, K, V, g, beta, mask, kept, initial_state)
@@ -108,7 +108,7 @@ class _GatedDelta(torch.autograd.Function):
             dfirst = torch.empty_like(initial_state)
         grads = binding._delta_backward_of(binding.CottenDeltaParams(*ctx.call), ctx.dims, Q, K, V, g, beta, mask, dO,
                                            initial_state, None if dstate is None else _aligned(dstate), dfirst, kept)
-        return (*grads, None, None, None, dfirst, None, None)
+        return (*grads, None, None, None, dfirst, None, None, None)
 
 
 def gated_delta_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor, beta: torch.Tensor,
@@ -117,8 +117,8 @@ def gated_delta_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: 
                           return_state: bool = False, layout: str = "bhnd"):
     """The gated delta rule of `binding.cotten_delta_fwd`, differentiable in Q, K, V, g, beta and the initial state;
     with `return_state` (O, final state).  The states before every 32 tokens and a float32 row per token are kept for the
-    backward."""
-    return _GatedDelta.apply(Q, K, V, g, beta, mask, scale, eps, initial_state, layout, return_state)
+    backward (not under `torch.no_grad`, whatever the tensors ask for)."""
+    return _GatedDelta.apply(Q, K, V, g, beta, mask, scale, eps, initial_state, layout, return_state, torch.is_grad_enabled())
 
 
 class _ItemEmbedding(torch.autograd.Function):

@@ -103,3 +103,17 @@ def test_gradients_that_nobody_wants_are_not_computed(monkeypatch, stand_ins):
         autograd.item_embedding(ids, W, P).sum().backward()
         assert wanted.pop() == (of_W, of_P)
         assert (W.grad is not None, P.grad is not None) == (of_W, of_P)
+
+
+def test_nothing_is_kept_for_a_backward_that_cannot_come(monkeypatch, stand_ins):
+    """Under no_grad tensors still say that they want gradients; the states of all chunks are not written for that."""
+    kept = []
+    monkeypatch.setattr(binding, "cotten_delta_fwd", lambda Q, *a, **kw: kept.append(kw["kept"]) or Q.detach() + 1.0)
+    q, k, v, g, beta = leaves(*[(1, 1, 4, 16)] * 3, *[(1, 1, 4)] * 2)
+    autograd.gated_delta_attention(q, k, v, g, beta)
+    assert kept.pop() is not None
+    with torch.no_grad():
+        autograd.gated_delta_attention(q, k, v, g, beta)
+    assert kept.pop() is None
+    autograd.gated_delta_attention(*(t.detach() for t in (q, k, v, g, beta)))
+    assert kept.pop() is None
