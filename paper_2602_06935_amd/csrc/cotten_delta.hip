@@ -291,11 +291,11 @@ Segments segments_of(long long slices, int chunks, int D, int dtype) {
   // 261 us, in 2 segments 120 / 273;  20 x 4 x 2048 whole 123 / 206, in 3 93 / 183.
   //
   // Few chunks do not make up for the second launch and the steps, which take four times as long at twice the width.  In
-  // segments / whole, us: d = 16 and 32, seven chunks 12 ... 14 % longer for bf16 and 6 ... 11 % for fp32, eight (16 x 4 x 256 x 32 bf16) forward
-  // 13.9 / 15.2, backward 22.6 / 25.2;  d = 64 bf16, 16 x 4 of eight chunks 21.5 / 18.2 and 32.3 / 34.9, of nine 20.6 / 19.9 and
-  // 37.9 / 39.6, of 12 25.2 / 25.2 and 39.9 / 45.1, fp32 of nine 26.1 / 27.3 and 49.9 / 52.1;  d = 128 bf16, 4 x 4 of 12 41 / 31 and
-  // 53 / 54, of 17 45.5 / 42.5 and 77 / 78, with the states kept 47.5 / 47.9, of 24 60 / 58.5, 63 / 65.5 and 84 / 96, fp16 of 17 55 / 66 and
-  // 90 / 104, fp32 of nine 49 / 60 and 86 / 91.
+  // segments / whole, us: d = 16 and 32, seven chunks 12 ... 14 % longer for bf16 and 6 ... 11 % for fp32, eight (16 x 4 x 256 x
+  // 32 bf16) forward 13.9 / 15.2, backward 22.6 / 25.2;  d = 64 bf16, 16 x 4 of eight chunks 21.5 / 18.2 and 32.3 / 34.9, of nine
+  // 20.6 / 19.9 and 37.9 / 39.6, of 12 25.2 / 25.2 and 39.9 / 45.1, fp32 of nine 26.1 / 27.3 and 49.9 / 52.1;  d = 128 bf16, 4 x 4
+  // of 12 41 / 31 and 53 / 54, of 17 45.5 / 42.5 and 77 / 78, with the states kept 47.5 / 47.9, of 24 60 / 58.5, 63 / 65.5 and
+  // 84 / 96, fp16 of 17 55 / 66 and 90 / 104, fp32 of nine 49 / 60 and 86 / 91.
   constexpr int kWorkgroups = 256, kFewest = 3;
   const long long groups = slices * (D > 64 ? D / 64 : 1);
   long long count = kWorkgroups / groups < chunks ? kWorkgroups / groups : chunks;

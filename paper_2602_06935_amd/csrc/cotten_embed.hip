@@ -302,10 +302,10 @@ constexpr int kSumThreads = 512;
 
 // dP, by the workgroups of sum_kernel behind its units.  dE is a matrix of B rows and N * D columns here, and dP the sums of
 // its columns.  A workgroup has `lanes` pieces of columns, and its lane groups deal the rows of its part out among them;
-// workgroups behind these write the zeros of positions that no token has, kZeroBytes each (one token a call and a table of 4096
-// positions: the table may be any number of times as long as the columns that there is something to sum for).  Few columns of many rows are cut into parts (four or more, of at least kPartRows rows)
-// until there are kParts workgroups, and join_positions_kernel adds the parts.  Whole backward, fp32, D = 256, in parts / in one: 65536 x 1:
-// 55 / 631 us; 16384 x 4: 51 / 182 us.
+// workgroups behind these write the zeros of positions that no token has, kZeroBytes each (16384 x 1 x 256 fp32: 36 us for a table
+// of 4096 positions as for one of 8).  Few columns of many rows are cut into parts (four or more, of at least kPartRows
+// rows) until there are kParts workgroups, and join_positions_kernel adds the parts.  Whole backward, fp32, D = 256, in
+// parts / in one: 65536 x 1: 55 / 631 us; 16384 x 4: 51 / 182 us.
 template <class T>
 struct Positions {
   T* dP;           // nullptr: not wanted
