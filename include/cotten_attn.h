@@ -344,6 +344,80 @@ int cotten_embed_bwd(const void* ids, const void* dE, void* dW, void* dP, int B,
 /* 0 for invalid arguments; host only. */
 size_t cotten_embed_workspace_bytes(int B, int N, int D, int V);
 
+/* ---- Dropout and the seam between two blocks --------------------------------------------------
+ *
+ * Dropout draws from a counter-based generator, Philox4x32 with ten rounds: the same (seed, offset) and
+ * number of an element give the same decision, so no mask is stored, and the backward is the same call on
+ * the upstream gradient.  Eight elements, numbered through the tensor, share a counter (number / 8, offset)
+ * under the key `seed` and take 16 bits each, in order (of a word the lower half first); an element is
+ * dropped where they are below t = floor(65536 p + 1/2), so p counts as t / 65536:
+ *
+ *     y = x * 65536 / (65536 - t), or 0 where dropped (whatever x holds there)
+ *
+ * Other offsets are other draws: a program counts its calls.  `step`, a device number that is added to offset,
+ * lets a captured graph draw anew in every replay.  The seam, rows of D elements:
+ *
+ *     Y = X + alpha * gate * drop(N(F; post_weight, post_bias))        H = N(Y; next_weight, next_bias)
+ *     N(x; w, b) = w (x - mu) / sqrt(mean (x - mu)^2 + eps) + b        mu = mean x, or 0 (COTTEN_NORM_RMS)
+ *
+ * Without post_weight F goes in as it is, without next_weight there is no H, without gate it is 1; the number of an
+ * element is that in F.  X, F, Y, H and their gradients are [B, N, D], contiguous; weights, biases and
+ * the gate are [D], the gate with gate_per_sequence [B, D]; all are of one element type.  Sums are fp32, in a fixed
+ * order, every result is rounded once (H comes from the row Y before its rounding).  D up to 16384, B * N below 2^31, up to
+ * 2^40 elements for the dropout by itself.  y may be x, Y may be X, and H may be F (no others overlap).  The backward keeps nothing: it makes the rows again from
+ * X and F, which have to hold what the forward saw.  A row is one of N = 1 for single tokens. */
+typedef enum cotten_norm {
+  COTTEN_NORM_RMS = 0,
+  COTTEN_NORM_LAYER = 1
+} cotten_norm;
+
+typedef struct cotten_dropout_params {
+  int dtype;           /* a cotten_dtype                                                         */
+  double p;            /* 0 <= p, and below 1 as it counts (COTTEN_ERR_BAD_PARAM)                */
+  uint64_t seed;
+  uint64_t offset;     /* the number of the call                                                 */
+  const int64_t* step; /* device, or NULL: added to offset                                       */
+} cotten_dropout_params;
+
+int cotten_dropout(const void* x, void* y, size_t n, void* stream, const cotten_dropout_params* params);
+
+typedef struct cotten_residual_params {
+  int dtype;             /* a cotten_dtype                                                       */
+  int norm;              /* a cotten_norm: of both norms                                         */
+  const void* post_weight;
+  const void* post_bias; /* (only with post_weight)                                              */
+  const void* gate;
+  const void* next_weight;
+  const void* next_bias; /* (only with next_weight)                                              */
+  int gate_per_sequence;
+  float alpha;           /* finite                                                               */
+  float eps;             /* < 0 selects 1e-6; 0 allowed                                          */
+  double p;              /* of the dropout, as above; 0: none                                    */
+  uint64_t seed;
+  uint64_t offset;
+  const int64_t* step;
+  void* workspace;       /* backward: 16-byte aligned device buffer                              */
+  size_t workspace_bytes;
+} cotten_residual_params;
+
+/* What the backward writes besides dX and dF: each NULL where it is not wanted. */
+typedef struct cotten_residual_grads {
+  void* post_weight;
+  void* post_bias;
+  void* gate;
+  void* next_weight;
+  void* next_bias;
+} cotten_residual_grads;
+
+/* H is NULL exactly where next_weight is. */
+int cotten_residual_fwd(const void* X, const void* F, void* Y, void* H, int B, int N, int D, void* stream,
+                        const cotten_residual_params* params);
+/* dY or dH may be NULL (zeros), not both. */
+int cotten_residual_bwd(const void* X, const void* F, const void* dY, const void* dH, void* dX, void* dF, int B, int N, int D,
+                        void* stream, const cotten_residual_params* params, const cotten_residual_grads* grads);
+/* 0 for invalid arguments; host only. */
+size_t cotten_residual_workspace_bytes(int B, int N, int D, int gate_per_sequence);
+
 #ifdef __cplusplus
 }
 #endif

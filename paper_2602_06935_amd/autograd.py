@@ -150,3 +150,58 @@ def item_embedding(ids: torch.Tensor, W: torch.Tensor, positions: Optional[torch
     """scale * W[ids] + positions[position_offset + n] (see `binding.cotten_embed_fwd`), differentiable in W and the
     positions; both gradients are dense."""
     return _ItemEmbedding.apply(ids, W, positions, scale, padding_idx, position_offset)
+
+
+class _Dropout(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, p, seed, offset, step):
+        ctx.save_for_backward(step)
+        ctx.call = p, seed, offset
+        return binding.cotten_dropout(x, p, seed=seed, offset=offset, step=step)
+
+    @staticmethod
+    @_first_derivatives_only
+    def backward(ctx, dy):
+        step, = ctx.saved_tensors
+        p, seed, offset = ctx.call
+        return binding.cotten_dropout(_aligned(dy), p, seed=seed, offset=offset, step=step), None, None, None, None
+
+
+def dropout(x: torch.Tensor, p: float, *, seed: int, offset: int = 0, step: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """`binding.cotten_dropout`, differentiable in x; nothing but `step` is kept (it must not change before the backward, which
+    draws the mask again)."""
+    return _Dropout.apply(x, p, seed, offset, step)
+
+
+class _ResidualNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, X, F, post_weight, post_bias, gate, next_weight, next_bias, step, norm, alpha, eps, p, seed, offset):
+        ctx.save_for_backward(X, F, post_weight, post_bias, gate, next_weight, next_bias, step)
+        ctx.call = norm, alpha, eps, p, seed, offset
+        ctx.set_materialize_grads(False)
+        return binding.cotten_residual_fwd(X, F, norm=norm, post_weight=post_weight, post_bias=post_bias, gate=gate, alpha=alpha,
+                                           next_weight=next_weight, next_bias=next_bias, eps=eps, p=p, seed=seed, offset=offset,
+                                           step=step)
+
+    @staticmethod
+    @_first_derivatives_only
+    def backward(ctx, dY, dH=None):
+        X, F, post_weight, post_bias, gate, next_weight, next_bias, step = ctx.saved_tensors
+        norm, alpha, eps, p, seed, offset = ctx.call
+        if dY is None and dH is None:
+            return (None,) * 14
+        grads = binding.cotten_residual_bwd(X, F, None if dY is None else _aligned(dY), None if dH is None else _aligned(dH),
+                                            norm=norm, post_weight=post_weight, post_bias=post_bias, gate=gate, alpha=alpha,
+                                            next_weight=next_weight, next_bias=next_bias, eps=eps, p=p, seed=seed, offset=offset,
+                                            step=step, wanted=ctx.needs_input_grad[2:7])
+        return (*grads, *(None,) * 7)
+
+
+def residual_norm(X: torch.Tensor, F: torch.Tensor, *, norm: str = "rms", post_weight: Optional[torch.Tensor] = None,
+                  post_bias: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, alpha: float = 1.0,
+                  next_weight: Optional[torch.Tensor] = None, next_bias: Optional[torch.Tensor] = None,
+                  eps: Optional[float] = None, p: float = 0.0, seed: int = 0, offset: int = 0,
+                  step: Optional[torch.Tensor] = None):
+    """(Y, H) of `binding.cotten_residual_fwd`, H None without `next_weight`; differentiable in X, F, the weights, the biases and
+    the gate.  Nothing but the inputs is kept."""
+    return _ResidualNorm.apply(X, F, post_weight, post_bias, gate, next_weight, next_bias, step, norm, alpha, eps, p, seed, offset)

@@ -38,6 +38,7 @@ EXPORTS = (
     "cotten_attn_workspace_bytes_ex",
     "cotten_delta_fwd", "cotten_delta_bwd", "cotten_delta_kept_bytes", "cotten_delta_workspace_bytes",
     "cotten_embed_fwd", "cotten_embed_bwd", "cotten_embed_workspace_bytes",
+    "cotten_dropout", "cotten_residual_fwd", "cotten_residual_bwd", "cotten_residual_workspace_bytes",
 )
 
 
@@ -61,6 +62,24 @@ class CottenEmbedParams(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int), ("id_bytes", ctypes.c_int), ("scale", ctypes.c_float),
                 ("padding_idx", ctypes.c_int), ("positions", ctypes.c_int), ("position_offset", ctypes.c_int),
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class CottenDropoutParams(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64),
+                ("step", ctypes.c_void_p)]
+
+
+class CottenResidualParams(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("norm", ctypes.c_int), ("post_weight", ctypes.c_void_p),
+                ("post_bias", ctypes.c_void_p), ("gate", ctypes.c_void_p), ("next_weight", ctypes.c_void_p),
+                ("next_bias", ctypes.c_void_p), ("gate_per_sequence", ctypes.c_int), ("alpha", ctypes.c_float),
+                ("eps", ctypes.c_float), ("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("offset", ctypes.c_uint64),
+                ("step", ctypes.c_void_p), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class CottenResidualGrads(ctypes.Structure):
+    _fields_ = [("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p), ("gate", ctypes.c_void_p),
+                ("next_weight", ctypes.c_void_p), ("next_bias", ctypes.c_void_p)]
 
 
 class CottenError(RuntimeError):
@@ -110,6 +129,14 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.cotten_embed_fwd.restype = lib.cotten_embed_bwd.restype = ctypes.c_int
     lib.cotten_embed_workspace_bytes.argtypes = [ip] * 4
     lib.cotten_embed_workspace_bytes.restype = ctypes.c_size_t
+    lib.cotten_dropout.argtypes = [vp, vp, ctypes.c_size_t, vp, ctypes.POINTER(CottenDropoutParams)]
+    lib.cotten_residual_fwd.argtypes = [vp] * 4 + [ip] * 3 + [vp, ctypes.POINTER(CottenResidualParams)]
+    lib.cotten_residual_bwd.argtypes = [vp] * 6 + [ip] * 3 + [vp, ctypes.POINTER(CottenResidualParams),
+                                                             ctypes.POINTER(CottenResidualGrads)]
+    for f in (lib.cotten_dropout, lib.cotten_residual_fwd, lib.cotten_residual_bwd):
+        f.restype = ctypes.c_int
+    lib.cotten_residual_workspace_bytes.argtypes = [ip] * 4
+    lib.cotten_residual_workspace_bytes.restype = ctypes.c_size_t
     lib.cotten_status_string.argtypes = [ip]
     lib.cotten_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -646,3 +673,150 @@ def _embed_backward_of(prm, ids, dE, W_shape, P_shape, of_table):
     _on_device(dE.device, _lib.cotten_embed_bwd, ids.data_ptr(), dE.data_ptr(),
                None if dW is None else dW.data_ptr(), None if dP is None else dP.data_ptr(), B, N, D, W_shape[0], handle, ctypes.byref(prm))
     return dW, dP
+
+
+# ---- dropout, and the seam between two blocks --------------------------------------------------------
+
+_NORMS = {"rms": 0, "layer": 1}
+_MOST_UINT64 = 2 ** 64 - 1
+
+
+def _check_generator(p: float, seed: int, offset: int, step: Optional[torch.Tensor], dev) -> Optional[int]:
+    """Refuses what the C call would not see; returns the address of `step`."""
+    if not 0.0 <= p < 1.0:
+        raise ValueError("p must be from 0 on and below 1")
+    if not (0 <= seed <= _MOST_UINT64 and 0 <= offset <= _MOST_UINT64):    # (ctypes takes the lower 64 bits of other numbers)
+        raise ValueError("seed and offset must be from 0 on, and of 64 bits")
+    if step is None:
+        return None
+    if step.dtype is not torch.int64 or step.numel() != 1 or step.device != dev:
+        raise ValueError("step must be one int64 number on the device of the other tensors")
+    return step.data_ptr()
+
+
+def cotten_dropout(x: torch.Tensor, p: float, *, seed: int, offset: int = 0, step: Optional[torch.Tensor] = None,
+                   out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """x / (1 - p) where the generator keeps an element and 0 elsewhere; p counts in multiples of 2^-16.  The same seed and
+    offset (the number of the call) give the same decisions: the backward is this call on the upstream gradient.  `step`, one
+    int64 number on the device, is added to the offset when the kernel runs: a captured graph draws anew when the program
+    changes it between replays.  `out` may be x."""
+    lib = _lib or load_library()
+    if not (x.is_cuda and x.is_contiguous()):
+        raise ValueError("x must be a contiguous GPU tensor (there is no CPU path)")
+    prm = CottenDropoutParams(_dtype_code(x), p, seed, offset, _check_generator(p, seed, offset, step, x.device))
+    if out is None:
+        out = torch.empty_like(x)
+    elif out.shape != x.shape or out.dtype is not x.dtype or out.device != x.device or not out.is_contiguous():
+        raise ValueError("out must be a contiguous tensor like x")
+    if x.numel() == 0:
+        return out
+    _on_device(x.device, lib.cotten_dropout, x.data_ptr(), out.data_ptr(), x.numel(), _stream_handle(stream, x.device),
+               ctypes.byref(prm))
+    return out
+
+
+@functools.lru_cache(maxsize=1024)
+def cotten_residual_workspace_bytes(B: int, N: int, D: int, gate_per_sequence: bool = False) -> int:
+    return int(load_library().cotten_residual_workspace_bytes(B, N, D, int(bool(gate_per_sequence))))
+
+
+def _seam_vector(name: str, t: Optional[torch.Tensor], X: torch.Tensor) -> Optional[int]:
+    if t is None:
+        return None
+    if t.dtype is not X.dtype or t.shape != X.shape[2:] or t.device != X.device or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous [{X.shape[2]}] tensor of the type and on the device of X")
+    return t.data_ptr()
+
+
+def _residual_params(X, F, norm, post_weight, post_bias, gate, alpha, next_weight, next_bias, eps, p, seed, offset,
+                     step) -> CottenResidualParams:
+    """The checks of what the two calls share, and their parameters."""
+    if X.dim() != 3:
+        raise ValueError("X must be [B,N,D]")
+    _check_like("X", X, X)
+    _check_like("F", F, X)
+    kind = _NORMS.get(norm)
+    if kind is None:
+        raise ValueError("norm must be 'rms' or 'layer'")
+    if (post_bias is not None and post_weight is None) or (next_bias is not None and next_weight is None):
+        raise ValueError("a norm's bias goes with its weight")
+    per_sequence = gate is not None and gate.dim() == 2
+    if per_sequence:
+        if gate.dtype is not X.dtype or gate.shape != (X.shape[0], X.shape[2]) or gate.device != X.device or not gate.is_contiguous():
+            raise ValueError("gate must be a contiguous [D] or [B,D] tensor of the type and on the device of X")
+        gates = gate.data_ptr()
+    else:
+        gates = _seam_vector("gate", gate, X)
+    return CottenResidualParams(
+        _dtype_code(X), kind, _seam_vector("post_weight", post_weight, X), _seam_vector("post_bias", post_bias, X), gates,
+        _seam_vector("next_weight", next_weight, X), _seam_vector("next_bias", next_bias, X), int(per_sequence), alpha,
+        -1.0 if eps is None else eps, p, seed, offset, _check_generator(p, seed, offset, step, X.device))
+
+
+def _check_like(name: str, t: torch.Tensor, X: torch.Tensor) -> None:
+    if not (t.is_cuda and t.is_contiguous() and t.shape == X.shape and t.dtype is X.dtype and t.device == X.device):
+        raise ValueError(f"{name} must be a contiguous GPU tensor [B,N,D], like X (there is no CPU path)")
+
+
+def cotten_residual_fwd(X: torch.Tensor, F: torch.Tensor, Y: Optional[torch.Tensor] = None, H: Optional[torch.Tensor] = None, *,
+                        norm: str = "rms", post_weight: Optional[torch.Tensor] = None,
+                        post_bias: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, alpha: float = 1.0,
+                        next_weight: Optional[torch.Tensor] = None, next_bias: Optional[torch.Tensor] = None,
+                        eps: Optional[float] = None, p: float = 0.0, seed: int = 0, offset: int = 0,
+                        step: Optional[torch.Tensor] = None, stream=None):
+    """(Y, H): Y = X + alpha * gate * drop(N(F; post_weight, post_bias)), H = N(Y; next_weight, next_bias), with `norm` "rms" or
+    "layer" for both; enqueues on the stream.  F is not normalised without `post_weight`, H is None without `next_weight`; `gate`
+    is [D], or [B,D] for a row per sequence; `p`, `seed`, `offset` and `step` are those of cotten_dropout.  Y may be X and H may be F."""
+    lib = _lib or load_library()
+    prm = _residual_params(X, F, norm, post_weight, post_bias, gate, alpha, next_weight, next_bias, eps, p, seed, offset, step)
+    if Y is None:
+        Y = torch.empty_like(X)
+    else:
+        _check_like("Y", Y, X)
+    if next_weight is None:
+        if H is not None:
+            raise ValueError("H comes from next_weight")
+    elif H is None:
+        H = torch.empty_like(X)
+    else:
+        _check_like("H", H, X)
+    _on_device(X.device, lib.cotten_residual_fwd, X.data_ptr(), F.data_ptr(), Y.data_ptr(), None if H is None else H.data_ptr(),
+               *X.shape, _stream_handle(stream, X.device), ctypes.byref(prm))
+    return Y, H
+
+
+def cotten_residual_bwd(X: torch.Tensor, F: torch.Tensor, dY: Optional[torch.Tensor], dH: Optional[torch.Tensor], *,
+                        norm: str = "rms", post_weight: Optional[torch.Tensor] = None,
+                        post_bias: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None, alpha: float = 1.0,
+                        next_weight: Optional[torch.Tensor] = None, next_bias: Optional[torch.Tensor] = None,
+                        eps: Optional[float] = None, p: float = 0.0, seed: int = 0, offset: int = 0,
+                        step: Optional[torch.Tensor] = None, stream=None, workspace: Optional[torch.Tensor] = None,
+                        wanted: Tuple[bool, bool, bool, bool, bool] = (True,) * 5):
+    """(dX, dF, dpost_weight, dpost_bias, dgate, dnext_weight, dnext_bias) of the forward call with the same arguments for the
+    upstream gradients dY and dH (None: zeros; not both); None for what the call does not have.  `wanted`: which of the
+    last five are."""
+    lib = _lib or load_library()
+    prm = _residual_params(X, F, norm, post_weight, post_bias, gate, alpha, next_weight, next_bias, eps, p, seed, offset, step)
+    if dY is None and dH is None:
+        raise ValueError("dY or dH must be given")
+    if dH is not None and next_weight is None:
+        raise ValueError("dH goes with next_weight")
+    for name, t in (("dY", dY), ("dH", dH)):
+        if t is not None:
+            _check_like(name, t, X)
+    return _residual_backward(prm, _stream_handle(stream, X.device), workspace, X, F, dY, dH,
+                              (post_weight, post_bias, gate, next_weight, next_bias), wanted)
+
+
+def _residual_backward(prm, handle, workspace, X, F, dY, dH, vectors, wanted):
+    """The call itself: everything but the workspace is checked."""
+    if workspace is None:
+        workspace = _workspace(X, cotten_residual_workspace_bytes(*X.shape, bool(prm.gate_per_sequence)), handle)
+    prm.workspace, prm.workspace_bytes = _buffer("workspace", workspace, X.device)
+    dX, dF = torch.empty_like(X), torch.empty_like(X)
+    grads = [torch.empty_like(t) if t is not None and w else None for t, w in zip(vectors, wanted)]
+    to = CottenResidualGrads(*(None if t is None else t.data_ptr() for t in grads))
+    _on_device(X.device, _lib.cotten_residual_bwd, X.data_ptr(), F.data_ptr(), None if dY is None else dY.data_ptr(),
+               None if dH is None else dH.data_ptr(), dX.data_ptr(), dF.data_ptr(), *X.shape, handle, ctypes.byref(prm),
+               ctypes.byref(to))
+    return (dX, dF, *grads)
