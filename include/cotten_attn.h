@@ -418,6 +418,39 @@ int cotten_residual_bwd(const void* X, const void* F, const void* dY, const void
 /* 0 for invalid arguments; host only. */
 size_t cotten_residual_workspace_bytes(int B, int N, int D, int gate_per_sequence);
 
+/* ---- A step of a beam search -----------------------------------------------------------------
+ *
+ * Of every sequence's K beams with their scores (sums of logarithms) and the logits of V items for each, the K
+ * best continuations:
+ *
+ *     total[k, v] = scores[k] + logits[k, v] - log sum_v' exp(logits[k, v'])
+ *
+ * in falling order, of equal totals the one with the lower k * V + v.  A beam that ended (finished byte not 0)
+ * goes on with the item `pad` alone, at its score; its logits are not read.  What else an ended beam could
+ * go on with, and everything of a beam whose score, or sum of exponentials, is not finite, has the total -inf (taken
+ * where nothing else is left).  A NaN among the logits counts as -inf.  Totals are compared in 64 bits, with sums of exponentials right to
+ * about 1e-8: candidates of different beams that are nearer than that may come in either order.
+ * logits [B, K, V] of one element type, contiguous; scores, new_scores float [B, K] (new_scores may be scores);
+ * finished [B, K] bytes or NULL; parents (the beam 0 ... K-1 that is continued) and tokens (the item) int32 [B, K].  K up to 32, B * K
+ * below 2^22, V below 2^30.  The workspace holds cotten_beam_workspace_bytes(); calls from several host threads must not share
+ * one, as above.
+ *
+ * cotten_beam_reorder gives beam k what beam parents[k] of its sequence had, in place, for `bytes` bytes of
+ * every beam (states of the delta rule or of the decay attention, [B, K, ...]; histories of items; flags): any contiguous tensor [B, K, ...].  Beams that stay
+ * are not touched; a parent outside 0 ... K-1 leaves its beam as it is. */
+typedef struct cotten_beam_params {
+  int dtype;              /* a cotten_dtype: of the logits                                       */
+  int pad;                /* 0 ... V-1 where finished is given (COTTEN_ERR_BAD_PARAM)            */
+  void* workspace;        /* 16-byte aligned device buffer                                       */
+  size_t workspace_bytes;
+} cotten_beam_params;
+
+int cotten_beam_select(const void* logits, const float* scores, const uint8_t* finished, float* new_scores, int32_t* parents,
+                       int32_t* tokens, int B, int K, int V, void* stream, const cotten_beam_params* params);
+int cotten_beam_reorder(void* state, const int32_t* parents, int B, int K, size_t bytes, void* stream);
+/* 0 for invalid arguments; host only. */
+size_t cotten_beam_workspace_bytes(int B, int K, int V);
+
 #ifdef __cplusplus
 }
 #endif

@@ -39,6 +39,7 @@ EXPORTS = (
     "cotten_delta_fwd", "cotten_delta_bwd", "cotten_delta_kept_bytes", "cotten_delta_workspace_bytes",
     "cotten_embed_fwd", "cotten_embed_bwd", "cotten_embed_workspace_bytes",
     "cotten_dropout", "cotten_residual_fwd", "cotten_residual_bwd", "cotten_residual_workspace_bytes",
+    "cotten_beam_select", "cotten_beam_reorder", "cotten_beam_workspace_bytes",
 )
 
 
@@ -80,6 +81,11 @@ class CottenResidualParams(ctypes.Structure):
 class CottenResidualGrads(ctypes.Structure):
     _fields_ = [("post_weight", ctypes.c_void_p), ("post_bias", ctypes.c_void_p), ("gate", ctypes.c_void_p),
                 ("next_weight", ctypes.c_void_p), ("next_bias", ctypes.c_void_p)]
+
+
+class CottenBeamParams(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("pad", ctypes.c_int), ("workspace", ctypes.c_void_p),
+                ("workspace_bytes", ctypes.c_size_t)]
 
 
 class CottenError(RuntimeError):
@@ -137,6 +143,11 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
         f.restype = ctypes.c_int
     lib.cotten_residual_workspace_bytes.argtypes = [ip] * 4
     lib.cotten_residual_workspace_bytes.restype = ctypes.c_size_t
+    lib.cotten_beam_select.argtypes = [vp] * 6 + [ip] * 3 + [vp, ctypes.POINTER(CottenBeamParams)]
+    lib.cotten_beam_reorder.argtypes = [vp, vp, ip, ip, ctypes.c_size_t, vp]
+    lib.cotten_beam_select.restype = lib.cotten_beam_reorder.restype = ctypes.c_int
+    lib.cotten_beam_workspace_bytes.argtypes = [ip] * 3
+    lib.cotten_beam_workspace_bytes.restype = ctypes.c_size_t
     lib.cotten_status_string.argtypes = [ip]
     lib.cotten_status_string.restype = ctypes.c_char_p
     _lib = lib
@@ -820,3 +831,68 @@ def _residual_backward(prm, handle, workspace, X, F, dY, dH, vectors, wanted):
                None if dH is None else dH.data_ptr(), dX.data_ptr(), dF.data_ptr(), *X.shape, handle, ctypes.byref(prm),
                ctypes.byref(to))
     return (dX, dF, *grads)
+
+
+# ---- a step of a beam search -----------------------------------------------------------------------------
+
+@functools.lru_cache(maxsize=1024)
+def cotten_beam_workspace_bytes(B: int, K: int, V: int) -> int:
+    return int(load_library().cotten_beam_workspace_bytes(B, K, V))
+
+
+def _of_beams(name: str, t: torch.Tensor, dtype: torch.dtype, shape, dev) -> int:
+    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {tuple(shape)} on the same device")
+    return t.data_ptr()
+
+
+def cotten_beam_select(logits: torch.Tensor, scores: torch.Tensor, *, finished: Optional[torch.Tensor] = None, pad: int = 0,
+                       new_scores: Optional[torch.Tensor] = None, parents: Optional[torch.Tensor] = None,
+                       tokens: Optional[torch.Tensor] = None, stream=None, workspace: Optional[torch.Tensor] = None
+                       ) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(new_scores, parents, tokens), each [B,K]: of every sequence the K best of scores[k] + log_softmax(logits[k])[v], in falling
+    order, the lower k * V + v of equal ones first; parents says which beam is continued, tokens with which item (int32).  `logits`
+    [B,K,V], `scores` [B,K] float32; a beam that is not 0 in `finished` ([B,K] uint8) goes on with the item `pad` alone, at its
+    score.  `new_scores` may be `scores`."""
+    lib = _lib or load_library()
+    if not (logits.is_cuda and logits.is_contiguous()):
+        raise ValueError("logits must be a contiguous GPU tensor (there is no CPU path)")
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B,K,V]")
+    B, K, V = logits.shape
+    if max(B, K, V) > _MOST_INT or not 0 <= pad <= _MOST_INT:
+        raise ValueError("sizes and pad must be numbers of 31 bits")
+    dev, shape = logits.device, logits.shape[:2]
+    new_scores = torch.empty_like(scores) if new_scores is None else new_scores
+    parents = torch.empty(shape, dtype=torch.int32, device=dev) if parents is None else parents
+    tokens = torch.empty(shape, dtype=torch.int32, device=dev) if tokens is None else tokens
+    dtype = _dtype_code(logits)
+    given = (_of_beams("scores", scores, torch.float32, shape, dev),
+             None if finished is None else _of_beams("finished", finished, torch.uint8, shape, dev),
+             _of_beams("new_scores", new_scores, torch.float32, shape, dev), _of_beams("parents", parents, torch.int32, shape, dev),
+             _of_beams("tokens", tokens, torch.int32, shape, dev))
+    handle = _stream_handle(stream, dev)
+    if workspace is None:
+        workspace = _workspace(logits, cotten_beam_workspace_bytes(B, K, V), handle)
+    prm = CottenBeamParams(dtype, pad, *_buffer("workspace", workspace, dev))
+    _on_device(dev, lib.cotten_beam_select, logits.data_ptr(), *given, B, K, V, handle, ctypes.byref(prm))
+    return new_scores, parents, tokens
+
+
+def cotten_beam_reorder(state: torch.Tensor, parents: torch.Tensor, *, stream=None) -> torch.Tensor:
+    """state[b,k] <- state[b,parents[b,k]] in place, for any contiguous [B,K,...] tensor (or [B*K,...]): states of the gated delta
+    rule and of the decay attention, histories, flags.  `parents` [B,K] int32, as cotten_beam_select writes it."""
+    lib = _lib or load_library()
+    if not (state.is_cuda and state.is_contiguous()):
+        raise ValueError("state must be a contiguous GPU tensor (there is no CPU path)")
+    if parents.dim() != 2:
+        raise ValueError("parents must be [B,K]")
+    B, K = parents.shape
+    _of_beams("parents", parents, torch.int32, parents.shape, state.device)
+    if state.shape[:2] != parents.shape and state.shape[:1] != (B * K,):
+        raise ValueError(f"state must be [{B},{K},...] or [{B * K},...]")
+    if state.numel() == 0:
+        return state
+    _on_device(state.device, lib.cotten_beam_reorder, state.data_ptr(), parents.data_ptr(), B, K,
+               state.numel() // (B * K) * state.element_size(), _stream_handle(stream, state.device))
+    return state

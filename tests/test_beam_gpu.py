@@ -1,0 +1,227 @@
+"""The step of a beam search on the GPU, against a sort of all candidates in 64 bits.
+
+Scores: the sums of exponentials are right to about 1e-8 and a score is rounded to fp32 once, so it is within 2^-24 of its own
+size and 4e-8 of the formula.  Parents and items have to be equal: between candidates of different beams the inputs leave gaps far
+above 1e-8, or ties that are exact on both sides."""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+DTYPES = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}
+
+
+def totals(logits, scores, finished=None, pad=0):
+    x = logits.cpu().double()
+    x = torch.where(torch.isnan(x), -math.inf, x)
+    top = x.amax(-1, keepdim=True)
+    lse = top + torch.log(torch.exp(x - top).sum(-1, keepdim=True))
+    add = scores.cpu().double().unsqueeze(-1) - lse
+    if finished is not None:
+        ended = (finished.cpu() != 0).unsqueeze(-1)
+        only = torch.full_like(x, -math.inf)
+        only[..., pad] = 0.0
+        x = torch.where(ended, only, x)
+        add = torch.where(ended, scores.cpu().double().unsqueeze(-1), add)
+    total = torch.where(torch.isfinite(add), x + add, -math.inf)
+    return torch.where(torch.isnan(total), -math.inf, total)
+
+
+def expected(logits, scores, finished=None, pad=0):
+    B, K, V = logits.shape
+    total = totals(logits, scores, finished, pad).reshape(B, K * V)
+    best, at = torch.sort(total, dim=-1, descending=True, stable=True)
+    return best[:, :K], at[:, :K] // V, at[:, :K] % V
+
+
+def compare(logits, scores, finished=None, pad=0):
+    from paper_2602_06935_amd import binding
+    got = binding.cotten_beam_select(logits, scores, finished=finished, pad=pad)
+    best, parents, tokens = expected(logits, scores, finished, pad)
+    assert torch.equal(got[1].cpu().long(), parents)
+    assert torch.equal(got[2].cpu().long(), tokens)
+    s = got[0].cpu().double()
+    low = torch.isinf(best)
+    assert torch.equal(s[low], best[low])
+    assert ((s - best).abs() <= best.abs() * 2.0 ** -24 + 4e-8)[~low].all()
+    return got
+
+
+def draw(B, K, V, dtype, seed, spread=2.0):
+    gen = torch.Generator().manual_seed(seed)
+    logits = (torch.randn(B, K, V, generator=gen) * spread).to(dtype)
+    scores = -torch.randn(B, K, generator=gen).abs() * 2.0 - 5.0
+    return logits.cuda(), scores.cuda()
+
+
+@pytest.mark.parametrize("V", [1, 2, 7, 63, 64, 65, 511, 512, 1023, 1024, 1025, 2049, 3700, 16601])
+@pytest.mark.parametrize("K", [1, 2, 5, 8, 32])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_sizes(dtype, K, V):
+    compare(*draw(3, K, V, DTYPES[dtype], seed=100 * K + V))
+
+
+@pytest.mark.parametrize("B,K,V", [(1, 1, 120001), (1, 32, 60000), (300, 8, 2000), (1100, 8, 1500), (2, 16, 300001)])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_shapes(dtype, B, K, V):
+    """From one long row, cut into as many parts as there are, to rows enough to be walked whole."""
+    compare(*draw(B, K, V, DTYPES[dtype], seed=B + K + V))
+
+
+@pytest.mark.parametrize("V,pad", [(1, 0), (50, 0), (50, 49), (3000, 17)])
+@pytest.mark.parametrize("K", [1, 4, 32])
+def test_ended_beams(K, V, pad):
+    logits, scores = draw(6, K, V, torch.float32, seed=K + V)
+    gen = torch.Generator().manual_seed(1)
+    finished = (torch.rand(6, K, generator=gen) < 0.5).to(torch.uint8)
+    finished[0] = 1
+    finished[1] = 0
+    logits[(finished != 0).cuda()] = float("nan")               # not looked at
+    compare(logits, scores, (finished * 3).cuda(), pad)
+
+
+def test_the_first_step():
+    """One beam has a score, the others none: all that is chosen continues it, or, where it has too few items, the lowest of the
+    others."""
+    for V in (1, 3, 8, 500):
+        logits, scores = draw(4, 8, V, torch.float32, seed=V)
+        scores[:, 1:] = -math.inf
+        _, parents, tokens = compare(logits, scores)
+        assert (parents.cpu()[:, :min(V, 8)] == 0).all()
+
+
+def test_ties():
+    """Equal logits within a beam, equal rows under equal scores: the lower index first."""
+    for dtype in DTYPES.values():
+        logits = torch.zeros(3, 4, 2600, dtype=dtype)
+        logits[1] = torch.arange(2600).remainder(7).to(dtype)
+        logits[2, :, 100::3] = 2.5
+        scores = torch.full((3, 4), -1.5)
+        scores[2, 0] = -3.0
+        compare(logits.cuda(), scores.cuda())
+        rows, row_scores = draw(2, 1, 900, dtype, seed=8)
+        compare(rows.expand(2, 5, 900).contiguous(), row_scores.expand(2, 5).contiguous())
+    signs = torch.zeros(1, 2, 100)
+    signs[:, :, ::2] = -0.0
+    compare(signs.cuda(), torch.zeros(1, 2).cuda())
+
+
+def test_order_of_arrival():
+    """Every logit ahead of, or behind, all before it: every piece or none passes the comparison with what is kept."""
+    for K in (1, 7, 32):
+        rising = torch.linspace(-8.0, 8.0, 9000)
+        x = torch.stack([rising, rising.flip(0), torch.where(torch.arange(9000) % 2 == 0, rising, -rising)])
+        x = x.unsqueeze(1).expand(3, K, 9000).contiguous()
+        scores = -torch.arange(K).float().mul(0.0137).expand(3, K).contiguous()
+        compare(x.cuda(), scores.cuda())
+
+
+def test_values_that_are_not_finite():
+    logits, scores = draw(8, 4, 700, torch.float32, seed=3)
+    logits[0, 1] = -math.inf                       # a beam with no item left
+    logits[1] = -math.inf                          # none of the beams has one
+    logits[2, :, 5:] = -math.inf                   # five items each
+    logits[3, 2, 9] = math.inf                     # no sum
+    logits[4, 0, ::3] = float("nan")
+    scores[5, 3] = math.inf
+    scores[6, 0] = float("nan")
+    scores[7] = -math.inf
+    compare(logits, scores)
+
+
+@pytest.mark.parametrize("offset", [0.0, 300.0, -300.0])
+def test_sums_of_unusual_size(offset):
+    """Peaked, flat and shifted rows: the order over beams hangs on their sums."""
+    logits, scores = draw(16, 6, 5000, torch.float32, seed=4, spread=0.05)
+    logits[4:8] *= 400.0
+    logits[8:12, :, 17] += 12.0
+    compare(logits + offset, scores)
+
+
+def test_scores_in_place_and_runs_alike():
+    from paper_2602_06935_amd import binding
+    logits, scores = draw(40, 8, 9001, torch.bfloat16, seed=5)
+    first = compare(logits, scores)
+    again = binding.cotten_beam_select(logits, scores, new_scores=scores)
+    assert again[0] is scores and all(torch.equal(a, b) for a, b in zip(first, again))
+
+
+@pytest.mark.parametrize("K", [1, 3, 4, 8, 13, 16, 32])
+@pytest.mark.parametrize("shape,dtype", [((2, 16, 16), torch.float32), ((5,), torch.int64), ((7,), torch.uint8), ((3, 5), torch.bfloat16),
+                                         ((), torch.uint8), ((4099,), torch.float32), ((3, 128, 128), torch.float32)])
+def test_reorder(K, shape, dtype):
+    from paper_2602_06935_amd import binding
+    B = 9
+    gen = torch.Generator().manual_seed(K)
+    x = torch.randint(0, 120, (B, K, *shape), generator=gen).to(dtype)
+    parents = torch.randint(0, K, (B, K), generator=gen, dtype=torch.int32)
+    parents[0] = torch.arange(K)                    # nothing moves
+    parents[1] = torch.arange(K).flip(0)            # beams change places
+    parents[2] = K - 1                              # all go on from one
+    want = x[torch.arange(B)[:, None], parents.long()]
+    y = x.cuda()
+    assert binding.cotten_beam_reorder(y, parents.cuda()) is y
+    assert torch.equal(y.cpu(), want)
+    flat = x.reshape(B * K, *shape).cuda()
+    assert torch.equal(binding.cotten_beam_reorder(flat, parents.cuda()).cpu(), want.reshape(B * K, *shape))
+
+
+def test_reorder_of_views_and_of_no_parents():
+    """Beginnings off 16-byte boundaries; parents that are no beam leave theirs as it was, and nothing behind the last is touched."""
+    from paper_2602_06935_amd import binding
+    buffer = torch.arange(4 * 3 * 33 + 7, dtype=torch.uint8, device="cuda")
+    before = buffer.clone()
+    parents = torch.tensor([[2, -1, 0], [3, 1, 1], [0, 0, 0], [1, 2, 2 ** 31 - 1]], dtype=torch.int32)
+    view = buffer[1:1 + 4 * 3 * 33].reshape(4, 3, 33)
+    want = view.cpu().clone()
+    for b in range(4):
+        for k in range(3):
+            p = parents[b, k].item()
+            if 0 <= p < 3:
+                want[b, k] = before[1:1 + 4 * 3 * 33].reshape(4, 3, 33).cpu()[b, p]
+    binding.cotten_beam_reorder(view, parents.cuda())
+    assert torch.equal(view.cpu(), want)
+    assert torch.equal(buffer[:1], before[:1]) and torch.equal(buffer[1 + 4 * 3 * 33:], before[1 + 4 * 3 * 33:])
+
+
+def test_captured():
+    from paper_2602_06935_amd import binding
+    logits, scores = draw(5, 4, 3000, torch.float32, seed=9)
+    state = torch.randn(5, 4, 2, 16, 16, device="cuda")
+    finished = torch.zeros(5, 4, dtype=torch.uint8, device="cuda")
+
+    def step(s, x):
+        new, parents, tokens = binding.cotten_beam_select(logits, s, finished=finished, pad=1, new_scores=s)
+        binding.cotten_beam_reorder(x, parents)
+        return parents, tokens
+
+    step(scores.clone(), state.clone())
+    s, x = scores.clone(), state.clone()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step(s, x)
+    for i in range(4):
+        logits.copy_(torch.randn(5, 4, 3000, device="cuda"))
+        finished.copy_((torch.rand(5, 4, device="cuda") < 0.2 * i).to(torch.uint8))
+        s2, x2 = s.clone(), x.clone()
+        graph.replay()
+        want = step(s2, x2)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((*got, s, x), (*want, s2, x2))), i
+
+
+def test_on_another_stream():
+    from paper_2602_06935_amd import binding
+    logits, scores = draw(3, 4, 2000, torch.float32, seed=10)
+    state = torch.randn(3, 4, 64, device="cuda")
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    new, parents, tokens = binding.cotten_beam_select(logits, scores, stream=stream)
+    before = state.cpu()
+    binding.cotten_beam_reorder(state, parents, stream=stream)
+    stream.synchronize()
+    best, want_parents, want_tokens = expected(logits, scores)
+    assert torch.equal(parents.cpu().long(), want_parents) and torch.equal(tokens.cpu().long(), want_tokens)
+    assert torch.equal(state.cpu(), before[torch.arange(3)[:, None], want_parents])
