@@ -306,6 +306,46 @@ int cotten_delta_bwd(const void* Q, const void* K, const void* V, const float* g
 size_t cotten_delta_kept_bytes(int B, int H, int N, int d_h, int dtype);
 size_t cotten_delta_workspace_bytes(int B, int H, int N, int d_h, int dtype, int is_bwd, int with_kept);
 
+/* ---- Decay attention --------------------------------------------------------------------------
+ *
+ * The causal linear attention with one decay for each head, on the same unit rows: for every slice (b,h), with
+ * a = exp(g[h]) and the state S (d_h x d_h, row a, column c),
+ *
+ *     S_t = a * S_{t-1} + khat_t v_t^T          O_t = scale * S_t^T qhat_t
+ *
+ * g is float, [H]: log decays of any sign (-inf empties the state at every token).  A masked token (mask byte 0)
+ * leaves the state as it is, and its K and V are not used, so they may hold anything; O exists for all N rows (queries
+ * are not masked).  Gradients of masked K and V are exact zeros, those of g are summed over the batch in 64 bits.  A
+ * sequence without a valid token keeps its initial state.  With g = 0 and no states it is the causal variant above.
+ *
+ * Types, layouts, states, precision, streams, limits of rows and what calls may share are those of the gated delta rule;
+ * B * H up to 2^20.  A value that is not finite in a row that takes part makes the results that hang on it not finite from its group
+ * of 32 tokens on. */
+typedef struct cotten_decay_params {
+  int dtype;                  /* a cotten_dtype: of Q, K, V, O and their gradients               */
+  float scale;                /* factor of O; <= 0 selects 1                                     */
+  float eps;                  /* inside the square roots; < 0 selects 1e-6; 0 allowed            */
+  int layout;                 /* a cotten_layout                                                 */
+  void* workspace;            /* device buffer of cotten_decay_workspace_bytes(), 16-byte aligned;
+                                 may be NULL where that is 0                                     */
+  size_t workspace_bytes;
+  const float* initial_state; /* device, [B*H, d_h, d_h], or NULL: zeros                         */
+  float* final_state;         /* forward: receives the state after row N-1, or NULL.  May be
+                                 initial_state itself (a server's state, replaced in place)      */
+  const float* dfinal_state;  /* backward: gradient of the final state, or NULL: zeros           */
+  float* dinitial_state;      /* backward: receives the gradient of the initial state, or NULL   */
+} cotten_decay_params;
+
+/* `params` must not be NULL.  N = 1 with final_state == initial_state is one step of a server. */
+int cotten_decay_fwd(const void* Q, const void* K, const void* V, const float* g, const uint8_t* mask, void* O, int B, int H, int N,
+                     int d_h, void* stream, const cotten_decay_params* params);
+/* Gradients of all inputs from dO (and params->dfinal_state); dg, [H] floats, may be NULL.  Nothing of the forward call is kept:
+ * the inputs and initial_state have to hold what it saw. */
+int cotten_decay_bwd(const void* Q, const void* K, const void* V, const float* g, const uint8_t* mask, const void* dO, void* dQ,
+                     void* dK, void* dV, float* dg, int B, int H, int N, int d_h, void* stream, const cotten_decay_params* params);
+/* Bytes of params->workspace (with_dg: dg is given).  0 for invalid arguments; host only. */
+size_t cotten_decay_workspace_bytes(int B, int H, int N, int d_h, int dtype, int is_bwd, int with_dg);
+
 /* ---- Embedding of item ids -------------------------------------------------------------------
  *
  * The input of the layers (Cotten4Rec, "Model Description": E_t = s_t + P_t), with a factor:

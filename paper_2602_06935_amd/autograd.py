@@ -121,6 +121,39 @@ def gated_delta_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: 
     return _GatedDelta.apply(Q, K, V, g, beta, mask, scale, eps, initial_state, layout, return_state, torch.is_grad_enabled())
 
 
+class _Decay(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, Q, K, V, g, mask, scale, eps, initial_state, layout, return_state):
+        B, H, _, d = binding._dims(Q, layout)
+        state = g.new_empty((B, H, d, d)) if return_state else None
+        O = binding.cotten_decay_fwd(Q, K, V, g, mask, scale=scale, eps=eps, layout=layout, initial_state=initial_state,
+                                     final_state=state)
+        ctx.save_for_backward(Q, K, V, g, mask, initial_state)
+        ctx.call = dict(scale=scale, eps=eps, layout=layout)
+        ctx.set_materialize_grads(False)
+        return (O, state) if return_state else O
+
+    @staticmethod
+    @_first_derivatives_only
+    def backward(ctx, dO, dstate=None):
+        Q, K, V, g, mask, initial_state = ctx.saved_tensors
+        dO = torch.zeros_like(Q) if dO is None else _aligned(dO)
+        dg = torch.empty_like(g) if ctx.needs_input_grad[3] else None
+        dfirst = torch.empty_like(initial_state) if initial_state is not None and ctx.needs_input_grad[7] else None
+        grads = binding.cotten_decay_bwd(Q, K, V, g, mask, dO, dg=dg, initial_state=initial_state,
+                                         dfinal_state=None if dstate is None else _aligned(dstate), dinitial_state=dfirst, **ctx.call)
+        return (*grads, dg, None, None, None, dfirst, None, None)
+
+
+def decay_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor, mask: Optional[torch.Tensor] = None, *,
+                    scale: Optional[float] = None, eps: Optional[float] = None, initial_state: Optional[torch.Tensor] = None,
+                    return_state: bool = False, layout: str = "bhnd"):
+    """The linear attention with a decay for each head of `binding.cotten_decay_fwd`, differentiable in Q, K, V, the log decays g
+    and the initial state; with `return_state` (O, final state).  Nothing but the inputs is kept; decays that want no gradient
+    cost none."""
+    return _Decay.apply(Q, K, V, g, mask, scale, eps, initial_state, layout, return_state)
+
+
 class _ItemEmbedding(torch.autograd.Function):
     @staticmethod
     def forward(ctx, ids, W, positions, scale, padding_idx, position_offset):

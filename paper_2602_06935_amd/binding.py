@@ -40,6 +40,7 @@ EXPORTS = (
     "cotten_embed_fwd", "cotten_embed_bwd", "cotten_embed_workspace_bytes",
     "cotten_dropout", "cotten_residual_fwd", "cotten_residual_bwd", "cotten_residual_workspace_bytes",
     "cotten_beam_select", "cotten_beam_reorder", "cotten_beam_workspace_bytes",
+    "cotten_decay_fwd", "cotten_decay_bwd", "cotten_decay_workspace_bytes",
 )
 
 
@@ -63,6 +64,13 @@ class CottenEmbedParams(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int), ("id_bytes", ctypes.c_int), ("scale", ctypes.c_float),
                 ("padding_idx", ctypes.c_int), ("positions", ctypes.c_int), ("position_offset", ctypes.c_int),
                 ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t)]
+
+
+class CottenDecayParams(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int), ("scale", ctypes.c_float), ("eps", ctypes.c_float),
+                ("layout", ctypes.c_int), ("workspace", ctypes.c_void_p), ("workspace_bytes", ctypes.c_size_t),
+                ("initial_state", ctypes.c_void_p), ("final_state", ctypes.c_void_p),
+                ("dfinal_state", ctypes.c_void_p), ("dinitial_state", ctypes.c_void_p)]
 
 
 class CottenDropoutParams(ctypes.Structure):
@@ -135,6 +143,11 @@ def load_library(build_if_missing: bool = True) -> ctypes.CDLL:
     lib.cotten_embed_fwd.restype = lib.cotten_embed_bwd.restype = ctypes.c_int
     lib.cotten_embed_workspace_bytes.argtypes = [ip] * 4
     lib.cotten_embed_workspace_bytes.restype = ctypes.c_size_t
+    lib.cotten_decay_fwd.argtypes = [vp] * 6 + [ip] * 4 + [vp, ctypes.POINTER(CottenDecayParams)]
+    lib.cotten_decay_bwd.argtypes = [vp] * 10 + [ip] * 4 + [vp, ctypes.POINTER(CottenDecayParams)]
+    lib.cotten_decay_fwd.restype = lib.cotten_decay_bwd.restype = ctypes.c_int
+    lib.cotten_decay_workspace_bytes.argtypes = [ip] * 7
+    lib.cotten_decay_workspace_bytes.restype = ctypes.c_size_t
     lib.cotten_dropout.argtypes = [vp, vp, ctypes.c_size_t, vp, ctypes.POINTER(CottenDropoutParams)]
     lib.cotten_residual_fwd.argtypes = [vp] * 4 + [ip] * 3 + [vp, ctypes.POINTER(CottenResidualParams)]
     lib.cotten_residual_bwd.argtypes = [vp] * 6 + [ip] * 3 + [vp, ctypes.POINTER(CottenResidualParams),
@@ -570,6 +583,87 @@ def _delta_backward_of(prm, dims, Q, K, V, g, beta, mask, dO, initial_state, dfi
     new = torch.empty_like
     return _delta_backward(prm, dims, handle, Q, K, V, g, beta, None if mask is None else mask.data_ptr(), dO, new(Q),
                            new(Q), new(Q), new(g), new(beta))
+
+
+# ---- decay attention ------------------------------------------------------------------------------
+
+@functools.lru_cache(maxsize=1024)
+def cotten_decay_workspace_bytes(B: int, H: int, N: int, d_h: int, dtype: int, is_bwd: bool, with_dg: bool = False) -> int:
+    return int(load_library().cotten_decay_workspace_bytes(B, H, N, d_h, dtype, int(bool(is_bwd)), int(bool(with_dg))))
+
+
+def _check_decays(name: str, t: torch.Tensor, H: int, dev) -> int:
+    if not (t.dtype is torch.float32 and t.shape == (H,) and t.device == dev and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous float32 tensor of shape ({H},) on the device of Q")
+    return t.data_ptr()
+
+
+def _decay_params(Q, dims, scale, eps, layout, workspace, initial_state=None, final_state=None, dfinal_state=None,
+                  dinitial_state=None) -> CottenDecayParams:
+    """The checks of what the two calls share besides Q, K, V and g, and their parameters."""
+    B, H, _, d = dims
+    dev, shape = Q.device, (B, H, d, d)
+    if scale is not None and scale < _LEAST_SCALE:    # (the library takes 0 and below for 1)
+        raise ValueError(f"scale must be None for 1, or {_LEAST_SCALE} at least")
+    first = _state_ptr("initial_state", initial_state, shape, dev)
+    return CottenDecayParams(
+        _dtype_code(Q), 0.0 if scale is None else scale, -1.0 if eps is None else eps, _LAYOUTS[layout],
+        *_buffer("workspace", workspace, dev), first,
+        first if final_state is initial_state else _state_ptr("final_state", final_state, shape, dev),
+        _state_ptr("dfinal_state", dfinal_state, shape, dev), _state_ptr("dinitial_state", dinitial_state, shape, dev))
+
+
+def cotten_decay_fwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor, mask: Optional[torch.Tensor],
+                     O: Optional[torch.Tensor] = None, *, scale: Optional[float] = None, eps: Optional[float] = None,
+                     stream=None, workspace: Optional[torch.Tensor] = None, layout: str = "bhnd",
+                     initial_state: Optional[torch.Tensor] = None, final_state: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Linear attention with a decay for each head: S_t = exp(g_h) S_{t-1} + khat_t v_t^T; O_t = scale * S_t^T qhat_t.  Enqueues on
+    the stream and returns O.  `g` (log decays) is float32 [H]; a masked token leaves the state as it is; `scale` is positive and
+    defaults to 1.  `initial_state` and `final_state` ([B,H,d_h,d_h] float32) may be the same tensor: with N = 1 that is a server's
+    step."""
+    lib = _lib or load_library()
+    _prep_like(Q, (("K", K), ("V", V)))
+    dims = _dims(Q, layout)
+    decays = _check_decays("g", g, dims[1], Q.device)
+    O = torch.empty_like(Q) if O is None else _prep("O", O, Q)
+    handle = _stream_handle(stream, Q.device)
+    if workspace is None:
+        need = cotten_decay_workspace_bytes(*dims, _dtype_code(Q), False)
+        if need != 0:
+            workspace = _workspace(Q, need, handle)
+    prm = _decay_params(Q, dims, scale, eps, layout, workspace, initial_state, final_state)
+    _on_device(Q.device, lib.cotten_decay_fwd, Q.data_ptr(), K.data_ptr(), V.data_ptr(), decays,
+               _mask_ptr(mask, dims[0], dims[2], Q.device), O.data_ptr(), *dims, handle, ctypes.byref(prm))
+    return O
+
+
+def cotten_decay_bwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch.Tensor, mask: Optional[torch.Tensor],
+                     dO: torch.Tensor, dQ: Optional[torch.Tensor] = None, dK: Optional[torch.Tensor] = None,
+                     dV: Optional[torch.Tensor] = None, *, dg: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                     eps: Optional[float] = None, stream=None, workspace: Optional[torch.Tensor] = None, layout: str = "bhnd",
+                     initial_state: Optional[torch.Tensor] = None, dfinal_state: Optional[torch.Tensor] = None,
+                     dinitial_state: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """(dQ, dK, dV) for the upstream gradients dO and, when given, `dfinal_state`; `dg` ([H] float32) and `dinitial_state`, when
+    given, receive the gradients of the decays and of the initial state.  The inputs and `initial_state` have to hold what the
+    forward call saw: nothing else is kept of it."""
+    lib = _lib or load_library()
+    _prep_like(Q, (("K", K), ("V", V), ("dO", dO)))
+    dims = _dims(Q, layout)
+    decays = _check_decays("g", g, dims[1], Q.device)
+    of_decays = None if dg is None else _check_decays("dg", dg, dims[1], Q.device)
+    dQ = torch.empty_like(Q) if dQ is None else _prep("dQ", dQ, Q)
+    dK = torch.empty_like(Q) if dK is None else _prep("dK", dK, Q)
+    dV = torch.empty_like(Q) if dV is None else _prep("dV", dV, Q)
+    handle = _stream_handle(stream, Q.device)
+    if workspace is None:
+        need = cotten_decay_workspace_bytes(*dims, _dtype_code(Q), True, dg is not None)
+        if need != 0:
+            workspace = _workspace(Q, need, handle)
+    prm = _decay_params(Q, dims, scale, eps, layout, workspace, initial_state, None, dfinal_state, dinitial_state)
+    _on_device(Q.device, lib.cotten_decay_bwd, Q.data_ptr(), K.data_ptr(), V.data_ptr(), decays,
+               _mask_ptr(mask, dims[0], dims[2], Q.device), dO.data_ptr(), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(), of_decays,
+               *dims, handle, ctypes.byref(prm))
+    return dQ, dK, dV
 
 
 # ---- embedding of item ids -----------------------------------------------------------------------

@@ -1,0 +1,206 @@
+// Kernels of the decay attention (cotten_decay_core.h has the formulas): a recurrence for a few tokens, and chunks of 32 tokens
+// on the matrix cores for more.
+#include "cotten_decay_core.h"
+#include "cotten_decay_launch.h"
+#include "cotten_launch.h"
+
+namespace cotten {
+namespace decay {
+namespace {
+
+extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+
+// ---- token by token -----------------------------------------------------------------------------------------------
+//
+// A wave carries up to 32 columns of a state in registers, eight lanes to a row of 128 bytes, the rows dealt to the lane groups;
+// q^ . S is a sum over the groups by lane permutes.  One token is bound by the state, read and written once.
+template <class E, int D>
+__global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
+  constexpr int kCols = D < 32 ? D : 32;         // columns of a wave
+  constexpr int kLanes = kCols / 4;              // lanes of a row
+  constexpr int kGroups = 64 / kLanes;
+  constexpr int kRows = D / kGroups;             // rows of a lane: group, group + kGroups, ...
+  static_assert(D % kGroups == 0, "rows are dealt evenly");
+  const int lane = threadIdx.x & 63;
+  const long long unit = static_cast<long long>(blockIdx.x) * (blockDim.x >> 6) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (unit >= static_cast<long long>(parts) * (D / kCols)) return;
+  const int slice = static_cast<int>(unit / (D / kCols)), col = static_cast<int>(unit % (D / kCols)) * kCols + 4 * (lane % kLanes);
+  const int group = lane / kLanes;
+  const Slice s(a, slice, D * E::kBytes);
+  const __amdgpu_buffer_rsrc_t Q = s.of(a.Q, 0, a.stride_row), K = s.of(a.K, 0, a.stride_row), V = s.of(a.V, 0, a.stride_row),
+                               O = s.of(a.O, 0, a.stride_row);
+  f32x4_t S[kRows];
+#pragma unroll
+  for (int r = 0; r < kRows; ++r)
+    S[r] = a.initial_state == nullptr
+               ? f32x4_t{0, 0, 0, 0}
+               : *reinterpret_cast<const f32x4_t*>(a.initial_state + (static_cast<long long>(slice) * D + group + r * kGroups) * D + col);
+  const float whole = static_cast<float>(exp2(Rate(s.g).whole));
+  for (int t = 0; t < a.N; ++t) {
+    const bool live = s.mask == nullptr || s.mask[t] != 0;
+    const uint32_t row = static_cast<uint32_t>(t) * a.stride_row;
+    const f32x4_t v = E::load_four(V, live ? row + col * E::kBytes : kNowhere);
+    float k[kRows], q[kRows], kk = 0.0f, qq = 0.0f;
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const uint32_t off = row + (group + r * kGroups) * E::kBytes;
+      k[r] = E::value(E::load_one(K, live ? off : kNowhere));
+      q[r] = E::value(E::load_one(Q, off));
+      kk = fmaf(k[r], k[r], kk);
+      qq = fmaf(q[r], q[r], qq);
+    }
+#pragma unroll
+    for (int m = kLanes; m < 64; m <<= 1) {
+      kk += __shfl_xor(kk, m);
+      qq += __shfl_xor(qq, m);
+    }
+    const float rk = live ? __builtin_amdgcn_rsqf(kk + a.eps) : 0.0f, rq = a.scale * __builtin_amdgcn_rsqf(qq + a.eps), decay = live ? whole : 1.0f;
+    f32x4_t o = {0, 0, 0, 0};
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const float unit_k = k[r] * rk;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        S[r][c] = fmaf(unit_k, v[c], S[r][c] * decay);
+        o[c] = fmaf(q[r], S[r][c], o[c]);
+      }
+    }
+#pragma unroll
+    for (int m = kLanes; m < 64; m <<= 1)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] += __shfl_xor(o[c], m);
+    if (group == 0) E::store_four(O, row + col * E::kBytes, o * rq);
+  }
+  if (a.final_state != nullptr) {
+#pragma unroll
+    for (int r = 0; r < kRows; ++r)
+      *reinterpret_cast<f32x4_t*>(a.final_state + (static_cast<long long>(slice) * D + group + r * kGroups) * D + col) = S[r];
+  }
+}
+
+// ---- chunks ---------------------------------------------------------------------------------------------------------
+
+template <class E, int D, int ROLE>
+__global__ __launch_bounds__(64 * kWaves<D>) void walk_kernel(Args a) {
+  walk<E, D, ROLE>(a, blockIdx.x, smem);
+}
+
+// The backward's walks as roles of one launch.  Workgroups go to the eight XCDs in turn: the roles of a unit are eight apart,
+// so they find each other's rows in one L2.
+template <class E, int D, int ROLES>
+__global__ __launch_bounds__(64 * kWaves<D>) void grad_kernel(Args a, int units) {
+  const int turn = blockIdx.x / (8 * ROLES), rest = blockIdx.x % (8 * ROLES), role = rest / 8, unit = turn * 8 + rest % 8;
+  if (unit >= units) return;
+  if (role == 0) walk<E, D, kDq>(a, unit, smem);
+  else if (role == 1) walk<E, D, kDk>(a, unit, smem);
+  else if (role == 2) walk<E, D, kDv>(a, unit, smem);
+  else if constexpr (ROLES == 4) walk<E, D, kDecays>(a, unit, smem);
+}
+
+// What the segments add to S (with its derivative by g) and to dS.
+template <class E, int D, bool DERIVATIVES>
+__global__ __launch_bounds__(64 * kWaves<D>) void grad_states_kernel(Args a, int units) {
+  if (static_cast<int>(blockIdx.x) < units) walk<E, D, DERIVATIVES ? kStatesAndDerivatives : kStates>(a, blockIdx.x, smem);
+  else walk<E, D, kGradStates>(a, blockIdx.x - units, smem);
+}
+
+// dg of a head: the partial sums of its slices in order.
+__global__ __launch_bounds__(64) void sum_decays_kernel(const double* partial, float* dg, int B, int H, int of_slice) {
+  const int h = blockIdx.x, lane = threadIdx.x;
+  double s = 0.0;
+  for (int b = 0; b < B; ++b)
+    for (int i = lane; i < of_slice; i += 64) s += partial[(static_cast<long long>(b) * H + h) * of_slice + i];
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) s += __shfl_xor(s, m);
+  if (lane == 0) dg[h] = static_cast<float>(s);
+}
+
+constexpr int greatest(int a, int b) { return a > b ? a : b; }
+
+template <class Kernel>
+hipError_t granted(Kernel kernel, int bytes) {
+  return bytes > 64 * 1024 ? grant_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes) : hipSuccess;
+}
+
+// Up to how many tokens the recurrence is as fast as a chunk of 32.
+constexpr int kMostSteps = 4;
+
+template <class E, int D>
+hipError_t forward(const Args& a, int slices, hipStream_t s) {
+  if (a.N <= kMostSteps) {
+    constexpr int kParts = D < 32 ? 1 : D / 32;
+    const long long waves = static_cast<long long>(slices) * kParts;
+    const int of_block = waves > 4096 ? 4 : 1;
+    step_kernel<E, D><<<dim3(static_cast<unsigned>((waves + of_block - 1) / of_block)), dim3(64 * of_block), 0, s>>>(a, slices);
+    return hipGetLastError();
+  }
+  const dim3 grid(static_cast<unsigned>(slices) * a.segments), block(64 * kWaves<D>);
+  if (a.segments > 1) {
+    constexpr int kBytes = kLds<E, D, kStates>;
+    if (hipError_t rc = granted(walk_kernel<E, D, kStates>, kBytes)) return rc;
+    walk_kernel<E, D, kStates><<<grid, block, kBytes, s>>>(a);
+  }
+  constexpr int kBytes = kLds<E, D, kOut>;
+  if (hipError_t rc = granted(walk_kernel<E, D, kOut>, kBytes)) return rc;
+  walk_kernel<E, D, kOut><<<grid, block, kBytes, s>>>(a);
+  return hipGetLastError();
+}
+
+template <class E, int D, int ROLES>
+hipError_t backward(const Args& a, int slices, hipStream_t s) {
+  const int units = slices * a.segments;
+  const dim3 block(64 * kWaves<D>);
+  if (a.segments > 1) {
+    constexpr int kBytes = kLds<E, D, kStates>;
+    const auto kernel = grad_states_kernel<E, D, ROLES == 4>;
+    if (hipError_t rc = granted(kernel, kBytes)) return rc;
+    kernel<<<dim3(2u * units), block, kBytes, s>>>(a, units);
+  }
+  constexpr int kBytes = greatest(kLds<E, D, kDq>, kLds<E, D, kDv>);
+  const auto kernel = grad_kernel<E, D, ROLES>;
+  if (hipError_t rc = granted(kernel, kBytes)) return rc;
+  kernel<<<dim3(static_cast<unsigned>((units + 7) / 8) * 8u * ROLES), block, kBytes, s>>>(a, units);
+  return hipGetLastError();
+}
+
+template <class E, int D>
+hipError_t backward(const Args& a, int slices, float* dg, hipStream_t s) {
+  if (dg == nullptr) return backward<E, D, 3>(a, slices, s);
+  if (hipError_t rc = backward<E, D, 4>(a, slices, s)) return rc;
+  sum_decays_kernel<<<dim3(a.H), dim3(64), 0, s>>>(a.dg, dg, slices / a.H, a.H, a.segments * kWaves<D>);
+  return hipGetLastError();
+}
+
+template <class E>
+hipError_t forward(const Args& a, int D, int slices, hipStream_t s) {
+  return D == 16 ? forward<E, 16>(a, slices, s) : D == 32 ? forward<E, 32>(a, slices, s) : D == 64 ? forward<E, 64>(a, slices, s) : forward<E, 128>(a, slices, s);
+}
+template <class E>
+hipError_t backward(const Args& a, int D, int slices, float* dg, hipStream_t s) {
+  return D == 16   ? backward<E, 16>(a, slices, dg, s)
+         : D == 32 ? backward<E, 32>(a, slices, dg, s)
+         : D == 64 ? backward<E, 64>(a, slices, dg, s)
+                   : backward<E, 128>(a, slices, dg, s);
+}
+
+}  // namespace
+
+Segments segments_of(long long slices, int chunks, int D, bool bwd) {
+  const long long wanted = 1024 / (slices * (bwd ? 2 : 1));
+  long long count = wanted < chunks / 4 ? wanted : chunks / 4;
+  if (count < 2) return {1, chunks};
+  const int each = static_cast<int>((chunks + count - 1) / count);
+  return {(chunks + each - 1) / each, each};
+}
+
+hipError_t launch_forward(const Args& a, int dtype, int D, int slices, hipStream_t stream) {
+  return dtype == 0 ? forward<delta::F32>(a, D, slices, stream) : dtype == 1 ? forward<delta::Bf16>(a, D, slices, stream) : forward<delta::F16>(a, D, slices, stream);
+}
+hipError_t launch_backward(const Args& a, int dtype, int D, int slices, float* dg, hipStream_t stream) {
+  return dtype == 0   ? backward<delta::F32>(a, D, slices, dg, stream)
+         : dtype == 1 ? backward<delta::Bf16>(a, D, slices, dg, stream)
+                      : backward<delta::F16>(a, D, slices, dg, stream);
+}
+
+}  // namespace decay
+}  // namespace cotten
