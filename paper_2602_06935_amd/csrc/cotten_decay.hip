@@ -35,7 +35,7 @@ __global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
     S[r] = a.initial_state == nullptr
                ? f32x4_t{0, 0, 0, 0}
                : *reinterpret_cast<const f32x4_t*>(a.initial_state + (static_cast<long long>(slice) * D + group + r * kGroups) * D + col);
-  const float whole = static_cast<float>(exp2(Rate(s.g).whole));
+  const float whole = static_cast<float>(exp2(rate_of(s.g)));
   for (int t = 0; t < a.N; ++t) {
     const bool live = s.mask == nullptr || s.mask[t] != 0;
     const uint32_t row = static_cast<uint32_t>(t) * a.stride_row;
@@ -80,39 +80,53 @@ __global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
 
 // ---- chunks ---------------------------------------------------------------------------------------------------------
 
+// Waves on a SIMD that the registers of a walk leave room for.
+template <class E, int D, bool DECAYS = false>
+constexpr int kRoom = E::kBytes == 2 && D <= 64 && !DECAYS ? 3 : 2;
+
 template <class E, int D, int ROLE>
-__global__ __launch_bounds__(64 * kWaves<D>) void walk_kernel(Args a) {
+__global__ __launch_bounds__(64 * kWaves<D>, (kRoom<E, D, ROLE == kDecays>)) void walk_kernel(Args a) {
   walk<E, D, ROLE>(a, blockIdx.x, smem);
 }
 
 // The backward's walks as roles of one launch.  Workgroups go to the eight XCDs in turn: the roles of a unit are eight apart,
 // so they find each other's rows in one L2.
-template <class E, int D, int ROLES>
-__global__ __launch_bounds__(64 * kWaves<D>) void grad_kernel(Args a, int units) {
-  const int turn = blockIdx.x / (8 * ROLES), rest = blockIdx.x % (8 * ROLES), role = rest / 8, unit = turn * 8 + rest % 8;
+template <class E, int D>
+__global__ __launch_bounds__(64 * kWaves<D>, (kRoom<E, D>)) void grad_kernel(Args a, int units) {
+  const int turn = blockIdx.x / 24, rest = blockIdx.x % 24, role = rest / 8, unit = turn * 8 + rest % 8;
   if (unit >= units) return;
   if (role == 0) walk<E, D, kDq>(a, unit, smem);
   else if (role == 1) walk<E, D, kDk>(a, unit, smem);
-  else if (role == 2) walk<E, D, kDv>(a, unit, smem);
-  else if constexpr (ROLES == 4) walk<E, D, kDecays>(a, unit, smem);
+  else walk<E, D, kDv>(a, unit, smem);
 }
 
 // What the segments add to S (with its derivative by g) and to dS.
 template <class E, int D, bool DERIVATIVES>
-__global__ __launch_bounds__(64 * kWaves<D>) void grad_states_kernel(Args a, int units) {
+__global__ __launch_bounds__(64 * kWaves<D>, 2) void grad_states_kernel(Args a, int units) {
   if (static_cast<int>(blockIdx.x) < units) walk<E, D, DERIVATIVES ? kStatesAndDerivatives : kStates>(a, blockIdx.x, smem);
   else walk<E, D, kGradStates>(a, blockIdx.x - units, smem);
 }
 
-// dg of a head: the partial sums of its slices in order.
-__global__ __launch_bounds__(64) void sum_decays_kernel(const double* partial, float* dg, int B, int H, int of_slice) {
-  const int h = blockIdx.x, lane = threadIdx.x;
+// dg of a head: every thread sums some of its slices' partial sums, in the order that it finds them, and the threads are joined.
+constexpr int kSumThreads = 1024;
+__global__ __launch_bounds__(kSumThreads) void sum_decays_kernel(const double* partial, float* dg, int B, int H, int of_slice) {
+  __shared__ double of_wave[kSumThreads / 64];
+  const int h = blockIdx.x;
+  const long long n = static_cast<long long>(B) * of_slice;
   double s = 0.0;
-  for (int b = 0; b < B; ++b)
-    for (int i = lane; i < of_slice; i += 64) s += partial[(static_cast<long long>(b) * H + h) * of_slice + i];
+#pragma unroll 4
+  for (long long i = threadIdx.x; i < n; i += kSumThreads) {
+    const long long b = i / of_slice;
+    s += partial[(b * H + h) * of_slice + (i - b * of_slice)];
+  }
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) s += __shfl_xor(s, m);
-  if (lane == 0) dg[h] = static_cast<float>(s);
+  if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int w = 1; w < kSumThreads / 64; ++w) s += of_wave[w];
+    dg[h] = static_cast<float>(s);
+  }
 }
 
 constexpr int greatest(int a, int b) { return a > b ? a : b; }
@@ -146,28 +160,26 @@ hipError_t forward(const Args& a, int slices, hipStream_t s) {
   return hipGetLastError();
 }
 
-template <class E, int D, int ROLES>
-hipError_t backward(const Args& a, int slices, hipStream_t s) {
+template <class E, int D>
+hipError_t backward(const Args& a, int slices, float* dg, hipStream_t s) {
   const int units = slices * a.segments;
   const dim3 block(64 * kWaves<D>);
   if (a.segments > 1) {
     constexpr int kBytes = kLds<E, D, kStates>;
-    const auto kernel = grad_states_kernel<E, D, ROLES == 4>;
+    const auto kernel = dg != nullptr ? grad_states_kernel<E, D, true> : grad_states_kernel<E, D, false>;
     if (hipError_t rc = granted(kernel, kBytes)) return rc;
     kernel<<<dim3(2u * units), block, kBytes, s>>>(a, units);
   }
   constexpr int kBytes = greatest(kLds<E, D, kDq>, kLds<E, D, kDv>);
-  const auto kernel = grad_kernel<E, D, ROLES>;
-  if (hipError_t rc = granted(kernel, kBytes)) return rc;
-  kernel<<<dim3(static_cast<unsigned>((units + 7) / 8) * 8u * ROLES), block, kBytes, s>>>(a, units);
-  return hipGetLastError();
-}
-
-template <class E, int D>
-hipError_t backward(const Args& a, int slices, float* dg, hipStream_t s) {
-  if (dg == nullptr) return backward<E, D, 3>(a, slices, s);
-  if (hipError_t rc = backward<E, D, 4>(a, slices, s)) return rc;
-  sum_decays_kernel<<<dim3(a.H), dim3(64), 0, s>>>(a.dg, dg, slices / a.H, a.H, a.segments * kWaves<D>);
+  if (hipError_t rc = granted(grad_kernel<E, D>, kBytes)) return rc;
+  grad_kernel<E, D><<<dim3(static_cast<unsigned>((units + 7) / 8) * 24u), block, kBytes, s>>>(a, units);
+  if (dg != nullptr) {
+    // (a launch of its own: it needs the most registers, and would take them from the other roles)
+    constexpr int kOfDecays = kLds<E, D, kDecays>;
+    if (hipError_t rc = granted(walk_kernel<E, D, kDecays>, kOfDecays)) return rc;
+    walk_kernel<E, D, kDecays><<<dim3(units), block, kOfDecays, s>>>(a);
+    sum_decays_kernel<<<dim3(a.H), dim3(kSumThreads), 0, s>>>(a.dg, dg, slices / a.H, a.H, a.segments * kWaves<D>);
+  }
   return hipGetLastError();
 }
 

@@ -137,66 +137,143 @@ struct Mask {
   __device__ __forceinline__ uint32_t bits(int chunk) const { return all ? existing(N, chunk) : static_cast<uint32_t>(__ballot(byte != 0)); }
 };
 
-// g * log2(e) as two floats.  A decay to nothing (g = -inf) counts as 2^-100000: fp32 knows no difference, and no tokens are none.
-struct Rate {
-  float hi, lo;
-  double whole;
-  __device__ __forceinline__ explicit Rate(float g) {
-    whole = static_cast<double>(g) * 1.4426950408889634;
-    whole = whole < -100000.0 ? -100000.0 : whole;
-    hi = static_cast<float>(whole);
-    lo = static_cast<float>(whole - hi);
-  }
-  // a^n, n a small whole number
-  __device__ __forceinline__ float pow(float n) const {
-    const float x = n * hi, rest = fmaf(n, hi, -x) + n * lo, e = __builtin_amdgcn_exp2f(x);
-    return fmaf(e * 0.693147182f, rest, e);
-  }
+// Powers of a head's decay, in LDS: a^n for n = 0 ... 32, and what rounding took from them.
+struct Powers {
+  float hi[kChunk + 4], lo[kChunk + 4];
 };
+// g * log2(e); a decay to nothing (g = -inf) counts as 2^-100000: fp32 knows no difference, and no tokens are none
+__device__ __forceinline__ double rate_of(float g) {
+  const double x = static_cast<double>(g) * 1.4426950408889634;
+  return x < -100000.0 ? -100000.0 : x;
+}
+__device__ __forceinline__ void set_powers(Powers* to, double rate, int lane) {
+  const double w = exp2(rate * static_cast<double>(lane));
+  const float hi = static_cast<float>(w);
+  if (lane <= kChunk) {
+    to->hi[lane] = hi;
+    to->lo[lane] = hi - hi == 0.0f ? static_cast<float>(w - static_cast<double>(hi)) : 0.0f;
+  }
+}
 
 // Counts of the tokens of a chunk, and the factors that follow from them, for a lane's tokens: column 16 t + lane%16, rows 16 t + 4g + r.
-// They are the same in all chunks whose tokens all count.
+// Where all tokens from the first that counts to the last that exists count, pairs are as far apart as their numbers say, and
+// the factors of the pairs are the same in all chunks.
+// Two pieces of eight significant bits each, rounded: 16 bits, where a result of 11 or fewer is all that comes of them.
+__device__ __forceinline__ Pieces<2> cut_in_two(const float (&x)[8]) {
+  delta::u32x4_t h, m;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    delta::bf16x2_t v;
+    v[0] = static_cast<__bf16>(x[2 * i]);
+    v[1] = static_cast<__bf16>(x[2 * i + 1]);
+    uint32_t w = __builtin_bit_cast(uint32_t, v);
+    asm("" : "+v"(w));  // (both halves from the one conversion)
+    h[i] = w;
+    v[0] = static_cast<__bf16>(x[2 * i] - __uint_as_float(w << 16));
+    v[1] = static_cast<__bf16>(x[2 * i + 1] - delta::upper(__uint_as_float(w)));
+    m[i] = __builtin_bit_cast(uint32_t, v);
+  }
+  Pieces<2> r;
+  r.p[0] = __builtin_bit_cast(delta::bf16x8_t, h);
+  r.p[1] = __builtin_bit_cast(delta::bf16x8_t, m);
+  return r;
+}
+// What the rows of a result are made of: three pieces for fp32 results, two for 16-bit ones (a product is off by 2^-17, and a result
+// rounded to 2^-9 or 2^-12 of it).
+template <class E, int ROLE>
+constexpr int kOperand = E::kBytes == 4 || ROLE == kDecays ? 3 : 2;
+template <class E, int P>
+__device__ __forceinline__ Pieces<P> cut_operand(f32x4_t a, f32x4_t b) {
+  const float x[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  if constexpr (P == 3) return cut<E::kPieces>(x);
+  else return cut_in_two(x);
+}
+
 template <class R>
 struct Decays {
   uint32_t live;
+  bool together;
   float n;                  // tokens that count
   float to[2];              // of X's rows, against the state
-  float column[2];          // p of them
   float fro[2][4];          // of Z's rows, for the state
-  float row[2][4];          // p of these
   float pair[3][4];         // of the pairs of tile 0 with 0, of X tile 0 with Y tile 1 (back) or 1 with 0, of 1 with 1
   float whole_hi, whole_lo;
-  static __device__ __forceinline__ float upto(uint32_t live, int t) { return static_cast<float>(__popc(live & (0xffffffffu >> (31 - t)))); }
-  __device__ __forceinline__ void set(uint32_t bits, const Rate& rate, int lane) {
-    live = bits;
-    const int c = lane & 15, first = 4 * (lane >> 4);
-    n = static_cast<float>(__popc(bits));
-    const double w = exp2(rate.whole * static_cast<double>(n));
-    whole_hi = static_cast<float>(w);
-    whole_lo = static_cast<float>(w - static_cast<double>(whole_hi));
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      column[t] = upto(bits, 16 * t + c);
-      to[t] = rate.pow(R::kBack ? n - column[t] : column[t]);
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        row[t][r] = upto(bits, 16 * t + first + r);
-        fro[t][r] = rate.pow(R::kBack ? row[t][r] : n - row[t][r]);
-      }
-    }
+  // p of a token of the chunk
+  static __device__ __forceinline__ int upto(uint32_t live, int t) { return __popc(live & (0xffffffffu >> (31 - t))); }
+  // tokens that count between column 16 x + lane%16 and row 16 y + 4g + r
+  static __device__ __forceinline__ int apart(uint32_t live, int x, int y, int r, int lane) {
+    const int column = upto(live, 16 * x + (lane & 15)), row = upto(live, 16 * y + 4 * (lane >> 4) + r);
+    return R::kBack ? row - column : column - row;
+  }
+  __device__ __forceinline__ void set_pairs(uint32_t bits, const Powers* powers, int lane) {
     if constexpr (R::kRows) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
-        const bool in = R::kBack ? first + r >= c : first + r <= c;
-        pair[0][r] = in ? rate.pow(apart(0, 0, r)) : 0.0f;
-        pair[1][r] = R::kBack ? rate.pow(apart(0, 1, r)) : rate.pow(apart(1, 0, r));
-        pair[2][r] = in ? rate.pow(apart(1, 1, r)) : 0.0f;
+        const int row = 4 * (lane >> 4) + r;
+        const bool in = R::kBack ? row >= (lane & 15) : row <= (lane & 15);
+        const int a0 = apart(bits, 0, 0, r, lane), a1 = apart(bits, R::kBack ? 0 : 1, R::kBack ? 1 : 0, r, lane), a2 = apart(bits, 1, 1, r, lane);
+        pair[0][r] = in ? powers->hi[a0 < 0 ? 0 : a0] : 0.0f;
+        pair[1][r] = powers->hi[a1];
+        pair[2][r] = in ? powers->hi[a2 < 0 ? 0 : a2] : 0.0f;
       }
     }
   }
-  // tokens that count between column 16 x + lane%16 and row 16 y + 4g + r
-  __device__ __forceinline__ float apart(int x, int y, int r) const { return R::kBack ? row[y][r] - column[x] : column[x] - row[y][r]; }
+  __device__ __forceinline__ void begin(const Powers* powers, int lane) {
+    none();
+    together = true;
+    set_pairs(~0u, powers, lane);
+  }
+  // no token counts
+  __device__ __forceinline__ void none() {
+    live = 0;
+    n = 0.0f;
+    whole_hi = 1.0f;
+    whole_lo = 0.0f;
+    to[0] = to[1] = 1.0f;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) fro[0][r] = fro[1][r] = 1.0f;
+  }
+  // bits: at least one; `there`: the tokens that exist
+  __device__ __forceinline__ void set(uint32_t bits, uint32_t there, const Powers* powers, int lane) {
+    live = bits;
+    const int count = __popc(bits);
+    n = static_cast<float>(count);
+    whole_hi = powers->hi[count];
+    whole_lo = powers->lo[count];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int p = upto(bits, 16 * t + (lane & 15));
+      to[t] = powers->hi[R::kBack ? count - p : p];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int q = upto(bits, 16 * t + 4 * (lane >> 4) + r);
+        fro[t][r] = powers->hi[R::kBack ? q : count - q];
+      }
+    }
+    const bool now = ((bits | ~there) >> __builtin_ctz(bits)) == (0xffffffffu >> __builtin_ctz(bits));
+    if (!now || !together) set_pairs(now ? ~0u : bits, powers, lane);
+    together = now;
+  }
 };
+
+// The first chunk of begin ... end-1 with a token that counts, or `end`.
+__device__ __forceinline__ int first_live(const uint8_t* mask, int N, int begin, int end, int lane) {
+  const __amdgpu_buffer_rsrc_t r = buffer(mask, N);
+  for (int t = kChunk * begin; t < N && t < kChunk * end; t += 256) {
+    uint8_t b[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) b[u] = __builtin_amdgcn_raw_buffer_load_b8(r, static_cast<uint32_t>(t + 64 * u + lane), 0, 0);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const uint64_t votes = __ballot(b[u] != 0);
+      if (votes != 0) {
+        const int c = (t + 64 * u + static_cast<int>(__builtin_ctzll(votes))) / kChunk;
+        return c < end ? c : end;
+      }
+    }
+  }
+  return end;
+}
 
 // x by columns as they lie in a state: 16 dt + 4g + r of row `col`.
 template <int D>
@@ -222,7 +299,7 @@ template <class E, int D, bool ROWS>
 struct Place {
   typedef Rows<D, E::kPieces> R;
   static constexpr int kY = 0, kZ = R::kBytes, kX = 2 * R::kBytes, kOfX = ROWS ? 3 * R::kBytes : 2 * R::kBytes;
-  static constexpr int kOfPair = kOfX + kChunk * 4, kBytes = kOfPair + kChunk * 4;
+  static constexpr int kOfPair = kOfX + kChunk * 4, kPowers = kOfPair + kChunk * 4, kBytes = kPowers + static_cast<int>(sizeof(Powers));
 };
 template <class E, int D, int ROLE>
 constexpr int kLds = Place<E, D, Traits<ROLE>::kRows>::kBytes + (Traits<ROLE>::kThrough ? kWaves<D> * kChunk * 8 : 64);
@@ -262,12 +339,12 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
   typedef Traits<ROLE> R;
   typedef Place<E, D, R::kRows> P;
   typedef typename P::R L;
-  constexpr int kRowLanes = D / 8, kBlocks = StateColumns<D>::kBlocks;
+  constexpr int kOf = kOperand<E, ROLE>, kRowLanes = D / 8, kBlocks = StateColumns<D>::kBlocks;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int slice = unit / a.segments, segment = unit - slice * a.segments;
   const Slice s(a, slice, D * E::kBytes);
-  const Rate rate(s.g);
-  const int begin = segment * a.segment_chunks;
+  const double rate = rate_of(s.g);
+  int begin = segment * a.segment_chunks;
   const int end = begin + a.segment_chunks < a.chunks ? begin + a.segment_chunks : a.chunks;
   const int col = 16 * wave + (lane & 15), group = lane >> 4;
   const long long of_slice = static_cast<long long>(slice) * a.segments;
@@ -275,10 +352,11 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
   float* of_x = reinterpret_cast<float*>(smem + P::kOfX);
   float* of_pair = reinterpret_cast<float*>(smem + P::kOfPair);
 
-  if (D < 32) {  // narrow rows are followed by zeros
+  Powers* powers = reinterpret_cast<Powers*>(smem + P::kPowers);
+  if (D < 32)  // narrow rows are followed by zeros
     for (int i = threadIdx.x; i < P::kOfX / 16; i += 64 * kWaves<D>) reinterpret_cast<f32x4_t*>(smem)[i] = f32x4_t{0, 0, 0, 0};
-    lds_barrier();
-  }
+  if (wave == 0) set_powers(powers, rate, lane);
+  lds_barrier();
 
   // the state before the first chunk (back: behind the last)
   StateColumns<D> S, T;
@@ -305,7 +383,7 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     } else {
       load_state<D, R::kTransposed>(S, a.local_d + (of_slice + a.segments - 1) * D * D, col, lane);
       for (int j = a.segments - 2; j > segment; --j) {
-        const float w = static_cast<float>(exp2(rate.whole * static_cast<double>(a.counts[of_slice + j])));
+        const float w = static_cast<float>(exp2(rate * static_cast<double>(a.counts[of_slice + j])));
         load_state<D, R::kTransposed>(T, a.local_d + (of_slice + j) * D * D, col, lane);
 #pragma unroll
         for (int dt = 0; dt < 2 * kBlocks; ++dt) S.s[dt] = S.s[dt] * w + T.s[dt];
@@ -316,7 +394,7 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     if constexpr (R::kDerivative)
       if (segment > 0) load_state<D, false>(T, a.local_t + of_slice * D * D, col, lane);
     for (int j = 1; j < segment; ++j) {
-      const float n = a.counts[of_slice + j], w = static_cast<float>(exp2(rate.whole * static_cast<double>(n)));
+      const float n = a.counts[of_slice + j], w = static_cast<float>(exp2(rate * static_cast<double>(n)));
       if constexpr (R::kDerivative) {
         StateColumns<D> next;
         load_state<D, false>(next, a.local_t + (of_slice + j) * D * D, col, lane);
@@ -330,12 +408,27 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     }
   }
 
-  Mask mask(a, s);
-  uint32_t live, there;
-  typename E::Raw rx, ry, rz;
-  ResultRows<E> own;                        // rows of Q or K (through their norm), or of dO (decays)
+  // Chunks before the first token that counts: there is nothing in the state but what came from outside, and forwards without
+  // that, or back where nobody asks for the gradient of it, they are zeros at once.
   const int row = wave * (512 / D) + lane / kRowLanes;
   const uint32_t off = static_cast<uint32_t>(row) * a.stride_row + (lane % kRowLanes) * 8 * E::kBytes;
+  if (a.mask != nullptr && (R::kBack ? (ROLE == kDk || a.dinitial_state == nullptr) : a.initial_state == nullptr)) {
+    const int from = first_live(s.mask, a.N, begin, end, lane);
+    if constexpr (R::kRows && ROLE != kDecays) {
+      unsigned char* to = ROLE == kOut ? a.O : ROLE == kDq ? a.dQ : ROLE == kDk ? a.dK : a.dV;
+      for (int c = begin; c < from; ++c) {
+        const __amdgpu_buffer_rsrc_t r = s.of(to, c, a.stride_row);
+        E::store_four(r, off, f32x4_t{0, 0, 0, 0});
+        E::store_four(r, off + 4 * E::kBytes, f32x4_t{0, 0, 0, 0});
+      }
+    }
+    begin = from;
+  }
+
+  Mask mask(a, s);
+  uint32_t live = 0, there = 0;
+  typename E::Raw rx, ry, rz;
+  ResultRows<E> own;                        // rows of Q or K (through their norm), or of dO (decays)
   const uint32_t own_off = static_cast<uint32_t>(lane & 15) * a.stride_row + (16 * wave + 4 * group) * E::kBytes;
   auto fetch = [&](int chunk) {
     live = mask.bits(chunk);
@@ -347,12 +440,14 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     rz = E::load(s.of(R::z(a), chunk, a.stride_row), at_yz);
   };
   const int step = R::kBack ? -1 : 1, first = R::kBack ? end - 1 : begin, last = R::kBack ? begin : end - 1;
-  mask.fetch(first, lane);
-  fetch(first);
-  if (first != last) mask.fetch(first + step, lane);
-
+  const int walked = end - begin;           // (may be none)
+  if (walked > 0) {
+    mask.fetch(first, lane);
+    fetch(first);
+    if (first != last) mask.fetch(first + step, lane);
+  }
   Decays<R> decays;
-  decays.set(live, rate, lane);
+  decays.begin(powers, lane);
   float count = 0.0f;
   double sum = 0.0;
   f32x4_t held[2];                          // rows that wait for the sums over the waves
@@ -378,29 +473,37 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     }
   };
 
-  for (int c = first;; c += step) {
+  for (int i = 0, c = first; i < walked; ++i, c += step) {
     // rows to LDS
     const uint32_t now = live, now_there = there;
-    const int of_row = wave * (512 / D) + lane / kRowLanes;
+    // where no token counts, forwards nothing is added to the state, and back there are no rows
+    const bool dead = now == 0, with_rows = !R::kBack || !dead, with_sums = R::kBack || !dead;
     {
       const int kb = (lane % kRowLanes) / 4, g = (lane % kRowLanes) % 4;
       float fx = 1.0f, fyz = 1.0f;
       if constexpr (R::kRows) {
-        L::put(smem + P::kX, of_row, kb, g, E::pieces(rx));
-        if constexpr (R::kUnitX) fx = inverse_norm<E, D>(rx, a.eps);
+        if (with_rows) {
+          L::put(smem + P::kX, row, kb, g, E::pieces(rx));
+          if constexpr (R::kUnitX) fx = inverse_norm<E, D>(rx, a.eps);
+        }
       }
-      L::put(smem + P::kY, of_row, kb, g, E::pieces(ry));
-      L::put(smem + P::kZ, of_row, kb, g, E::pieces(rz));
-      fyz = inverse_norm<E, D>(R::kUnitY ? ry : rz, a.eps);
+      if (with_sums) {
+        L::put(smem + P::kY, row, kb, g, E::pieces(ry));
+        L::put(smem + P::kZ, row, kb, g, E::pieces(rz));
+        fyz = inverse_norm<E, D>(R::kUnitY ? ry : rz, a.eps);
+      }
       if (R::kScaleX) fx *= a.scale;
       else fyz *= a.scale;
       const uint32_t in_x = R::kBack ? now : now_there, in_yz = R::kBack ? now_there : now;
       if (lane % kRowLanes == 0) {
-        of_x[of_row] = ((in_x >> of_row) & 1u) ? fx : 0.0f;
-        of_pair[of_row] = ((in_yz >> of_row) & 1u) ? fyz : 0.0f;
+        of_x[row] = ((in_x >> row) & 1u) ? fx : 0.0f;
+        of_pair[row] = ((in_yz >> row) & 1u) ? fyz : 0.0f;
       }
     }
-    if (now != decays.live) decays.set(now, rate, lane);
+    if (now != decays.live) {
+      if (dead) decays.none();
+      else decays.set(now, now_there, powers, lane);
+    }
     if (c != last) {
       fetch(c + step);
       if (c + step != last) mask.fetch(c + 2 * step, lane);
@@ -408,60 +511,67 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     lds_barrier();
 
     const f32x4_t pair_factor[2] = {*reinterpret_cast<const f32x4_t*>(of_pair + 4 * group), *reinterpret_cast<const f32x4_t*>(of_pair + 16 + 4 * group)};
-    const Pieces<E::kPieces> z = L::column_operand(smem + P::kZ, wave, lane);
+    Pieces<E::kPieces> z;
+    if (with_sums) z = L::column_operand(smem + P::kZ, wave, lane);
     if constexpr (R::kRows) {
-      const float x_factor[2] = {of_x[lane & 15], of_x[16 + (lane & 15)]};
       if constexpr (R::kThrough || ROLE == kDecays)
         own.load(s.of(ROLE == kDq ? a.Q : ROLE == kDk ? a.K : a.dO, c, a.stride_row), a.stride_row, R::kBack ? now : ~0u, own_off, lane);
-      // the products of X's rows with Y's: rows Y, columns X
-      Pieces<E::kPieces> x[2][kBlocks];
-      f32x4_t d[3] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
-#pragma unroll
-      for (int kb = 0; kb < kBlocks; ++kb) {
-        const Pieces<E::kPieces> y[2] = {L::row_operand(smem + P::kY, 0, kb, lane), L::row_operand(smem + P::kY, 1, kb, lane)};
-        x[0][kb] = L::row_operand(smem + P::kX, 0, kb, lane);
-        x[1][kb] = L::row_operand(smem + P::kX, 1, kb, lane);
-        d[0] = mul(y[0], x[0][kb], d[0]);
-        d[1] = R::kBack ? mul(y[1], x[0][kb], d[1]) : mul(y[0], x[1][kb], d[1]);
-        d[2] = mul(y[1], x[1][kb], d[2]);
-      }
-      f32x4_t m[3];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        m[0][r] = d[0][r] * (pair_factor[0][r] * x_factor[0]) * decays.pair[0][r];
-        m[1][r] = d[1][r] * (pair_factor[R::kBack ? 1 : 0][r] * x_factor[R::kBack ? 0 : 1]) * decays.pair[1][r];
-        m[2][r] = d[2][r] * (pair_factor[1][r] * x_factor[1]) * decays.pair[2][r];
-        if constexpr (ROLE == kDecays) {
-          m[0][r] *= decays.apart(0, 0, r);
-          m[1][r] *= decays.apart(1, 0, r);
-          m[2][r] *= decays.apart(1, 1, r);
-        }
-      }
-      const f32x4_t none = {0, 0, 0, 0};
-      const Pieces<3> sums[2] = {R::kBack ? cut<E::kPieces>(m[0], m[1]) : cut<E::kPieces>(m[0], none),
-                                 R::kBack ? cut<E::kPieces>(none, m[2]) : cut<E::kPieces>(m[1], m[2])};
       // rows: 16 columns of this wave's (4g + r) of tokens 16 t + lane%16
       f32x4_t o[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-      S.template cut_all<E::kPieces>();
+      if (with_rows) {
+        const float x_factor[2] = {of_x[lane & 15], of_x[16 + (lane & 15)]};
+        Pieces<E::kPieces> x[2][kBlocks];
 #pragma unroll
-      for (int kb = 0; kb < kBlocks; ++kb) {
-        const Pieces<E::kPieces> both[2] = {x[0][kb], x[1][kb]};
-        mul_right(S.p[kb], both, o);
-      }
-      if constexpr (ROLE == kDecays) {
-        f32x4_t u[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-        T.template cut_all<E::kPieces>();
+        for (int kb = 0; kb < kBlocks; ++kb) {
+          x[0][kb] = L::row_operand(smem + P::kX, 0, kb, lane);
+          x[1][kb] = L::row_operand(smem + P::kX, 1, kb, lane);
+        }
 #pragma unroll
         for (int kb = 0; kb < kBlocks; ++kb) {
           const Pieces<E::kPieces> both[2] = {x[0][kb], x[1][kb]};
-          mul_right(T.p[kb], both, u);
+          mul_right(cut_operand<E, kOf>(S.s[2 * kb], S.s[2 * kb + 1]), both, o);
+        }
+        if constexpr (ROLE == kDecays) {
+          f32x4_t u[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+          for (int kb = 0; kb < kBlocks; ++kb) {
+            const Pieces<E::kPieces> both[2] = {x[0][kb], x[1][kb]};
+            mul_right(cut_operand<E, kOf>(T.s[2 * kb], T.s[2 * kb + 1]), both, u);
+          }
+#pragma unroll
+          for (int t = 0; t < 2; ++t) o[t] = o[t] * static_cast<float>(decays.upto(now, 16 * t + (lane & 15))) + u[t];
+        }
+        if (!dead) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t) o[t] *= decays.to[t];
+          // the products of X's rows with Y's: rows Y, columns X
+          f32x4_t m[3] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+          for (int kb = 0; kb < kBlocks; ++kb) {
+            const Pieces<E::kPieces> y[2] = {L::row_operand(smem + P::kY, 0, kb, lane), L::row_operand(smem + P::kY, 1, kb, lane)};
+            m[0] = mul(y[0], x[0][kb], m[0]);
+            m[1] = R::kBack ? mul(y[1], x[0][kb], m[1]) : mul(y[0], x[1][kb], m[1]);
+            m[2] = mul(y[1], x[1][kb], m[2]);
+          }
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            m[0][r] *= pair_factor[0][r] * decays.pair[0][r];
+            m[1][r] *= pair_factor[R::kBack ? 1 : 0][r] * decays.pair[1][r];
+            m[2][r] *= pair_factor[1][r] * decays.pair[2][r];
+            if constexpr (ROLE == kDecays) {
+              m[0][r] *= static_cast<float>(decays.apart(now, 0, 0, r, lane));
+              m[1][r] *= static_cast<float>(decays.apart(now, 1, 0, r, lane));
+              m[2][r] *= static_cast<float>(decays.apart(now, 1, 1, r, lane));
+            }
+          }
+          const f32x4_t none = {0, 0, 0, 0};
+          const Pieces<kOf> sums[2] = {cut_operand<E, kOf>(m[0], R::kBack ? m[1] : none),
+                                               cut_operand<E, kOf>(R::kBack ? none : m[1], m[2])};
+          mul_right(z, sums, o);
         }
 #pragma unroll
-        for (int t = 0; t < 2; ++t) o[t] = o[t] * decays.column[t] + u[t];
+        for (int t = 0; t < 2; ++t) o[t] *= x_factor[t];
       }
-#pragma unroll
-      for (int t = 0; t < 2; ++t) o[t] *= x_factor[t] * decays.to[t];
-      mul_right(z, sums, o);
       if constexpr (ROLE == kOut || ROLE == kDv) {
         const __amdgpu_buffer_rsrc_t r = s.of(ROLE == kOut ? a.O : a.dV, c, a.stride_row);
 #pragma unroll
@@ -498,38 +608,39 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     }
 
     // the state: S <- a^n S + Y^T (w Z)
-    count += decays.n;
-    float w[8];
+    if (with_sums) {
+      count += decays.n;
+      float w[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float v = 0.0f;
+      for (int i = 0; i < 8; ++i) {
+        float v = 0.0f;
 #pragma unroll
-      for (int p = E::kPieces - 1; p >= 0; --p) v += static_cast<float>(z.p[p][i]);
-      w[i] = v * (pair_factor[i >> 2][i & 3] * decays.fro[i >> 2][i & 3]);
-    }
-    if constexpr (R::kDerivative) {
-      float wt[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) wt[i] = w[i] * (decays.n - decays.row[i >> 2][i & 3]);
-      const Pieces<3> wz = cut<E::kPieces>(wt);
-#pragma unroll
-      for (int dt = 0; dt < StateColumns<D>::kTiles; ++dt) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float x = fmaf(decays.n, S.s[dt][i], T.s[dt][i]);
-          T.s[dt][i] = fmaf(x, decays.whole_hi, x * decays.whole_lo);
-        }
-        T.s[dt] = mul(L::column_operand(smem + P::kY, dt, lane), wz, T.s[dt]);
+        for (int p = E::kPieces - 1; p >= 0; --p) v += static_cast<float>(z.p[p][i]);
+        w[i] = v * (pair_factor[i >> 2][i & 3] * decays.fro[i >> 2][i & 3]);
       }
+      if constexpr (R::kDerivative) {
+        float wt[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) wt[i] = w[i] * (decays.n - static_cast<float>(decays.upto(now, 16 * (i >> 2) + 4 * group + (i & 3))));
+        const Pieces<3> wz = cut<E::kPieces>(wt);
+#pragma unroll
+        for (int dt = 0; dt < StateColumns<D>::kTiles; ++dt) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float x = fmaf(decays.n, S.s[dt][i], T.s[dt][i]);
+            T.s[dt][i] = fmaf(x, decays.whole_hi, x * decays.whole_lo);
+          }
+          T.s[dt] = mul(L::column_operand(smem + P::kY, dt, lane), wz, T.s[dt]);
+        }
+      }
+#pragma unroll
+      for (int dt = 0; dt < StateColumns<D>::kTiles; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S.s[dt][i] = fmaf(S.s[dt][i], decays.whole_hi, S.s[dt][i] * decays.whole_lo);
+      delta::add_outer<L, D>(S, smem + P::kY, cut<E::kPieces>(w), lane);
     }
-#pragma unroll
-    for (int dt = 0; dt < StateColumns<D>::kTiles; ++dt)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) S.s[dt][i] = fmaf(S.s[dt][i], decays.whole_hi, S.s[dt][i] * decays.whole_lo);
-    delta::add_outer<L, D>(S, smem + P::kY, cut<E::kPieces>(w), lane);
     lds_barrier();
     if constexpr (R::kThrough) finish(c);
-    if (c == last) break;
   }
 
   // what is behind the walk
