@@ -189,39 +189,51 @@ __device__ __forceinline__ Pieces<P> cut_operand(f32x4_t a, f32x4_t b) {
   else return cut_in_two(x);
 }
 
+// The pairs of 16-token tiles that give each other anything: tile `x` of X's rows with tile `y` of Y's.  A wave makes every
+// WAVES-th of the three.
 template <class R>
+struct Pair {
+  int x, y;
+  __device__ __forceinline__ explicit Pair(int i) : x(R::kBack ? i >> 1 : (i + 1) >> 1), y(R::kBack ? (i + 1) >> 1 : i >> 1) {}
+};
+template <class R, int WAVES>
 struct Decays {
+  static constexpr int kOwn = WAVES >= 3 ? 1 : WAVES == 2 ? 2 : 3;   // pairs of a wave, at most
   uint32_t live;
   bool together;
   float n;                  // tokens that count
   float to[2];              // of X's rows, against the state
   float fro[2][4];          // of Z's rows, for the state
-  float pair[3][4];         // of the pairs of tile 0 with 0, of X tile 0 with Y tile 1 (back) or 1 with 0, of 1 with 1
+  float pair[kOwn][4];
   float whole_hi, whole_lo;
   // p of a token of the chunk
   static __device__ __forceinline__ int upto(uint32_t live, int t) { return __popc(live & (0xffffffffu >> (31 - t))); }
   // tokens that count between column 16 x + lane%16 and row 16 y + 4g + r
-  static __device__ __forceinline__ int apart(uint32_t live, int x, int y, int r, int lane) {
-    const int column = upto(live, 16 * x + (lane & 15)), row = upto(live, 16 * y + 4 * (lane >> 4) + r);
+  static __device__ __forceinline__ int apart(uint32_t live, const Pair<R>& p, int r, int lane) {
+    const int column = upto(live, 16 * p.x + (lane & 15)), row = upto(live, 16 * p.y + 4 * (lane >> 4) + r);
     return R::kBack ? row - column : column - row;
   }
-  __device__ __forceinline__ void set_pairs(uint32_t bits, const Powers* powers, int lane) {
+  __device__ __forceinline__ void set_pairs(uint32_t bits, const Powers* powers, int wave, int lane) {
     if constexpr (R::kRows) {
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int row = 4 * (lane >> 4) + r;
-        const bool in = R::kBack ? row >= (lane & 15) : row <= (lane & 15);
-        const int a0 = apart(bits, 0, 0, r, lane), a1 = apart(bits, R::kBack ? 0 : 1, R::kBack ? 1 : 0, r, lane), a2 = apart(bits, 1, 1, r, lane);
-        pair[0][r] = in ? powers->hi[a0 < 0 ? 0 : a0] : 0.0f;
-        pair[1][r] = powers->hi[a1];
-        pair[2][r] = in ? powers->hi[a2 < 0 ? 0 : a2] : 0.0f;
+      for (int k = 0; k < kOwn; ++k) {
+        const int i = wave + k * WAVES;
+        if (i >= 3) break;
+        const Pair<R> p(i);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const int row = 4 * (lane >> 4) + r, a = apart(bits, p, r, lane);
+          const bool in = p.x != p.y || (R::kBack ? row >= (lane & 15) : row <= (lane & 15));
+          const float w = powers->hi[a < 0 ? 0 : a];
+          pair[k][r] = in ? w : 0.0f;
+        }
       }
     }
   }
-  __device__ __forceinline__ void begin(const Powers* powers, int lane) {
+  __device__ __forceinline__ void begin(const Powers* powers, int wave, int lane) {
     none();
     together = true;
-    set_pairs(~0u, powers, lane);
+    set_pairs(~0u, powers, wave, lane);
   }
   // no token counts
   __device__ __forceinline__ void none() {
@@ -234,7 +246,7 @@ struct Decays {
     for (int r = 0; r < 4; ++r) fro[0][r] = fro[1][r] = 1.0f;
   }
   // bits: at least one; `there`: the tokens that exist
-  __device__ __forceinline__ void set(uint32_t bits, uint32_t there, const Powers* powers, int lane) {
+  __device__ __forceinline__ void set(uint32_t bits, uint32_t there, const Powers* powers, int wave, int lane) {
     live = bits;
     const int count = __popc(bits);
     n = static_cast<float>(count);
@@ -251,7 +263,7 @@ struct Decays {
       }
     }
     const bool now = ((bits | ~there) >> __builtin_ctz(bits)) == (0xffffffffu >> __builtin_ctz(bits));
-    if (!now || !together) set_pairs(now ? ~0u : bits, powers, lane);
+    if (!now || !together) set_pairs(now ? ~0u : bits, powers, wave, lane);
     together = now;
   }
 };
@@ -301,8 +313,29 @@ struct Place {
   static constexpr int kY = 0, kZ = R::kBytes, kX = 2 * R::kBytes, kOfX = ROWS ? 3 * R::kBytes : 2 * R::kBytes;
   static constexpr int kOfPair = kOfX + kChunk * 4, kPowers = kOfPair + kChunk * 4, kBytes = kPowers + static_cast<int>(sizeof(Powers));
 };
+// ... followed by the products of the pairs of tiles as operands ([tile of X][piece][lane], 16 bytes), and what waves sum over all columns.
+template <int OF>
+constexpr int kPairBytes = 2 * OF * 64 * 16;
 template <class E, int D, int ROLE>
-constexpr int kLds = Place<E, D, Traits<ROLE>::kRows>::kBytes + (Traits<ROLE>::kThrough ? kWaves<D> * kChunk * 8 : 64);
+constexpr int kLds = Place<E, D, Traits<ROLE>::kRows>::kBytes + (Traits<ROLE>::kRows ? kPairBytes<kOperand<E, ROLE>> : 0) +
+                     (Traits<ROLE>::kThrough ? kWaves<D> * kChunk * 8 : 0);
+// Four values of a lane as half of an operand.
+template <class E, int OF>
+__device__ __forceinline__ void put_half(unsigned char* at, int tile, int half, int lane, f32x4_t x) {
+  const Pieces<OF> p = cut_operand<E, OF>(x, f32x4_t{0, 0, 0, 0});
+#pragma unroll
+  for (int i = 0; i < OF; ++i) {
+    const delta::u32x4_t w = __builtin_bit_cast(delta::u32x4_t, p.p[i]);
+    *reinterpret_cast<delta::u32x2_t*>(at + ((tile * OF + i) * 64 + lane) * 16 + 8 * half) = delta::u32x2_t{w[0], w[1]};
+  }
+}
+template <int OF>
+__device__ __forceinline__ Pieces<OF> pair_operand(const unsigned char* at, int tile, int lane) {
+  Pieces<OF> r;
+#pragma unroll
+  for (int i = 0; i < OF; ++i) r.p[i] = *reinterpret_cast<const delta::bf16x8_t*>(at + ((tile * OF + i) * 64 + lane) * 16);
+  return r;
+}
 
 // Sum over the LANES lanes that share a row, in all of them.
 template <int LANES>
@@ -353,8 +386,11 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
   float* of_pair = reinterpret_cast<float*>(smem + P::kOfPair);
 
   Powers* powers = reinterpret_cast<Powers*>(smem + P::kPowers);
+  unsigned char* pairs = smem + P::kBytes;
   if (D < 32)  // narrow rows are followed by zeros
     for (int i = threadIdx.x; i < P::kOfX / 16; i += 64 * kWaves<D>) reinterpret_cast<f32x4_t*>(smem)[i] = f32x4_t{0, 0, 0, 0};
+  if (R::kRows)  // so are the pairs that give each other nothing
+    for (int i = threadIdx.x; i < kPairBytes<kOf> / 16; i += 64 * kWaves<D>) reinterpret_cast<f32x4_t*>(pairs)[i] = f32x4_t{0, 0, 0, 0};
   if (wave == 0) set_powers(powers, rate, lane);
   lds_barrier();
 
@@ -446,13 +482,13 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     fetch(first);
     if (first != last) mask.fetch(first + step, lane);
   }
-  Decays<R> decays;
-  decays.begin(powers, lane);
+  Decays<R, kWaves<D>> decays;
+  decays.begin(powers, wave, lane);
   float count = 0.0f;
   double sum = 0.0;
   f32x4_t held[2];                          // rows that wait for the sums over the waves
   uint32_t held_live = 0;
-  float* parts = reinterpret_cast<float*>(smem + P::kBytes);   // [wave][token]: y . x^ and y . y
+  float* parts = reinterpret_cast<float*>(pairs + kPairBytes<kOf>);   // [wave][token]: y . x^ and y . y
   auto finish = [&](int chunk) {
     unsigned char* to = ROLE == kDq ? a.dQ : a.dK;
     const __amdgpu_buffer_rsrc_t r = s.of(to, chunk, a.stride_row);
@@ -502,7 +538,7 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     }
     if (now != decays.live) {
       if (dead) decays.none();
-      else decays.set(now, now_there, powers, lane);
+      else decays.set(now, now_there, powers, wave, lane);
     }
     if (c != last) {
       fetch(c + step);
@@ -510,68 +546,97 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     }
     lds_barrier();
 
+    if constexpr (R::kThrough)
+      if (i > 0) finish(c - step);
     const f32x4_t pair_factor[2] = {*reinterpret_cast<const f32x4_t*>(of_pair + 4 * group), *reinterpret_cast<const f32x4_t*>(of_pair + 16 + 4 * group)};
     Pieces<E::kPieces> z;
     if (with_sums) z = L::column_operand(smem + P::kZ, wave, lane);
+    // rows: 16 columns of this wave's (4g + r) of tokens 16 t + lane%16
+    f32x4_t o[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    float x_factor[2] = {0.0f, 0.0f};
     if constexpr (R::kRows) {
       if constexpr (R::kThrough || ROLE == kDecays)
         own.load(s.of(ROLE == kDq ? a.Q : ROLE == kDk ? a.K : a.dO, c, a.stride_row), a.stride_row, R::kBack ? now : ~0u, own_off, lane);
-      // rows: 16 columns of this wave's (4g + r) of tokens 16 t + lane%16
-      f32x4_t o[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-      if (with_rows) {
-        const float x_factor[2] = {of_x[lane & 15], of_x[16 + (lane & 15)]};
-        Pieces<E::kPieces> x[2][kBlocks];
+      // this wave's share of the products of X's rows with Y's (rows Y, columns X), for all
+      if (!dead) {
 #pragma unroll
-        for (int kb = 0; kb < kBlocks; ++kb) {
-          x[0][kb] = L::row_operand(smem + P::kX, 0, kb, lane);
-          x[1][kb] = L::row_operand(smem + P::kX, 1, kb, lane);
-        }
+        for (int k = 0; k < decays.kOwn; ++k) {
+          const int p = wave + k * kWaves<D>;
+          if (p >= 3) break;
+          const Pair<R> pair(p);
+          f32x4_t m = {0, 0, 0, 0};
 #pragma unroll
-        for (int kb = 0; kb < kBlocks; ++kb) {
-          const Pieces<E::kPieces> both[2] = {x[0][kb], x[1][kb]};
-          mul_right(cut_operand<E, kOf>(S.s[2 * kb], S.s[2 * kb + 1]), both, o);
-        }
-        if constexpr (ROLE == kDecays) {
-          f32x4_t u[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
-#pragma unroll
-          for (int kb = 0; kb < kBlocks; ++kb) {
-            const Pieces<E::kPieces> both[2] = {x[0][kb], x[1][kb]};
-            mul_right(cut_operand<E, kOf>(T.s[2 * kb], T.s[2 * kb + 1]), both, u);
-          }
-#pragma unroll
-          for (int t = 0; t < 2; ++t) o[t] = o[t] * static_cast<float>(decays.upto(now, 16 * t + (lane & 15))) + u[t];
-        }
-        if (!dead) {
-#pragma unroll
-          for (int t = 0; t < 2; ++t) o[t] *= decays.to[t];
-          // the products of X's rows with Y's: rows Y, columns X
-          f32x4_t m[3] = {{0, 0, 0, 0}, {0, 0, 0, 0}, {0, 0, 0, 0}};
-#pragma unroll
-          for (int kb = 0; kb < kBlocks; ++kb) {
-            const Pieces<E::kPieces> y[2] = {L::row_operand(smem + P::kY, 0, kb, lane), L::row_operand(smem + P::kY, 1, kb, lane)};
-            m[0] = mul(y[0], x[0][kb], m[0]);
-            m[1] = R::kBack ? mul(y[1], x[0][kb], m[1]) : mul(y[0], x[1][kb], m[1]);
-            m[2] = mul(y[1], x[1][kb], m[2]);
-          }
+          for (int kb = 0; kb < kBlocks; ++kb)
+            m = mul(L::row_operand(smem + P::kY, pair.y, kb, lane), L::row_operand(smem + P::kX, pair.x, kb, lane), m);
+          const f32x4_t factor = *reinterpret_cast<const f32x4_t*>(of_pair + 16 * pair.y + 4 * group);
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            m[0][r] *= pair_factor[0][r] * decays.pair[0][r];
-            m[1][r] *= pair_factor[R::kBack ? 1 : 0][r] * decays.pair[1][r];
-            m[2][r] *= pair_factor[1][r] * decays.pair[2][r];
-            if constexpr (ROLE == kDecays) {
-              m[0][r] *= static_cast<float>(decays.apart(now, 0, 0, r, lane));
-              m[1][r] *= static_cast<float>(decays.apart(now, 1, 0, r, lane));
-              m[2][r] *= static_cast<float>(decays.apart(now, 1, 1, r, lane));
-            }
+            m[r] *= factor[r] * decays.pair[k][r];
+            if constexpr (ROLE == kDecays) m[r] *= static_cast<float>(decays.apart(now, pair, r, lane));
           }
-          const f32x4_t none = {0, 0, 0, 0};
-          const Pieces<kOf> sums[2] = {cut_operand<E, kOf>(m[0], R::kBack ? m[1] : none),
-                                               cut_operand<E, kOf>(R::kBack ? none : m[1], m[2])};
-          mul_right(z, sums, o);
+          put_half<E, kOf>(pairs, pair.x, pair.y, lane, m);
+        }
+      }
+      if (with_rows) {
+        x_factor[0] = of_x[lane & 15];
+        x_factor[1] = of_x[16 + (lane & 15)];
+        f32x4_t u[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+#pragma unroll
+        for (int kb = 0; kb < kBlocks; ++kb) {
+          const Pieces<E::kPieces> both[2] = {L::row_operand(smem + P::kX, 0, kb, lane), L::row_operand(smem + P::kX, 1, kb, lane)};
+          mul_right(cut_operand<E, kOf>(S.s[2 * kb], S.s[2 * kb + 1]), both, o);
+          if constexpr (ROLE == kDecays) mul_right(cut_operand<E, kOf>(T.s[2 * kb], T.s[2 * kb + 1]), both, u);
         }
 #pragma unroll
-        for (int t = 0; t < 2; ++t) o[t] *= x_factor[t];
+        for (int t = 0; t < 2; ++t) {
+          if constexpr (ROLE == kDecays) o[t] = o[t] * static_cast<float>(decays.upto(now, 16 * t + (lane & 15))) + u[t];
+          o[t] *= decays.to[t];
+        }
       }
+    }
+
+    // the state: S <- a^n S + Y^T (w Z)
+    if (with_sums) {
+      count += decays.n;
+      float w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float v = 0.0f;
+#pragma unroll
+        for (int p = E::kPieces - 1; p >= 0; --p) v += static_cast<float>(z.p[p][j]);
+        w[j] = v * (pair_factor[j >> 2][j & 3] * decays.fro[j >> 2][j & 3]);
+      }
+      if constexpr (R::kDerivative) {
+        float wt[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) wt[j] = w[j] * (decays.n - static_cast<float>(decays.upto(now, 16 * (j >> 2) + 4 * group + (j & 3))));
+        const Pieces<3> wz = cut<E::kPieces>(wt);
+#pragma unroll
+        for (int dt = 0; dt < StateColumns<D>::kTiles; ++dt) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const float x = fmaf(decays.n, S.s[dt][j], T.s[dt][j]);
+            T.s[dt][j] = fmaf(x, decays.whole_hi, x * decays.whole_lo);
+          }
+          T.s[dt] = mul(L::column_operand(smem + P::kY, dt, lane), wz, T.s[dt]);
+        }
+      }
+#pragma unroll
+      for (int dt = 0; dt < StateColumns<D>::kTiles; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) S.s[dt][j] = fmaf(S.s[dt][j], decays.whole_hi, S.s[dt][j] * decays.whole_lo);
+      delta::add_outer<L, D>(S, smem + P::kY, cut<E::kPieces>(w), lane);
+    }
+    lds_barrier();
+
+    // what the chunk's tokens give each other; the next chunk's rows may be written from here on
+    if constexpr (R::kRows) {
+      if (!dead) {
+        const Pieces<kOf> sums[2] = {pair_operand<kOf>(pairs, 0, lane), pair_operand<kOf>(pairs, 1, lane)};
+        mul_right(z, sums, o);
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) o[t] *= x_factor[t];
       if constexpr (ROLE == kOut || ROLE == kDv) {
         const __amdgpu_buffer_rsrc_t r = s.of(ROLE == kOut ? a.O : a.dV, c, a.stride_row);
 #pragma unroll
@@ -584,7 +649,7 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) of_chunk = ((now_there >> (16 * t + (lane & 15))) & 1u) ? fmaf(own.x[t][i], o[t][i], of_chunk) : of_chunk;
+          for (int j = 0; j < 4; ++j) of_chunk = ((now_there >> (16 * t + (lane & 15))) & 1u) ? fmaf(own.x[t][j], o[t][j], of_chunk) : of_chunk;
         sum += static_cast<double>(of_chunk);
       } else {
         held_live = R::kBack ? now : ~0u;
@@ -593,9 +658,9 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
           held[t] = o[t];
           float dot = 0.0f, square = 0.0f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            dot = fmaf(own.x[t][i], o[t][i], dot);
-            square = fmaf(own.x[t][i], own.x[t][i], square);
+          for (int j = 0; j < 4; ++j) {
+            dot = fmaf(own.x[t][j], o[t][j], dot);
+            square = fmaf(own.x[t][j], own.x[t][j], square);
           }
           dot = over_groups(dot);
           square = over_groups(square);
@@ -606,41 +671,10 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
         }
       }
     }
-
-    // the state: S <- a^n S + Y^T (w Z)
-    if (with_sums) {
-      count += decays.n;
-      float w[8];
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        float v = 0.0f;
-#pragma unroll
-        for (int p = E::kPieces - 1; p >= 0; --p) v += static_cast<float>(z.p[p][i]);
-        w[i] = v * (pair_factor[i >> 2][i & 3] * decays.fro[i >> 2][i & 3]);
-      }
-      if constexpr (R::kDerivative) {
-        float wt[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) wt[i] = w[i] * (decays.n - static_cast<float>(decays.upto(now, 16 * (i >> 2) + 4 * group + (i & 3))));
-        const Pieces<3> wz = cut<E::kPieces>(wt);
-#pragma unroll
-        for (int dt = 0; dt < StateColumns<D>::kTiles; ++dt) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float x = fmaf(decays.n, S.s[dt][i], T.s[dt][i]);
-            T.s[dt][i] = fmaf(x, decays.whole_hi, x * decays.whole_lo);
-          }
-          T.s[dt] = mul(L::column_operand(smem + P::kY, dt, lane), wz, T.s[dt]);
-        }
-      }
-#pragma unroll
-      for (int dt = 0; dt < StateColumns<D>::kTiles; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) S.s[dt][i] = fmaf(S.s[dt][i], decays.whole_hi, S.s[dt][i] * decays.whole_lo);
-      delta::add_outer<L, D>(S, smem + P::kY, cut<E::kPieces>(w), lane);
-    }
+  }
+  if constexpr (R::kThrough) {
     lds_barrier();
-    if constexpr (R::kThrough) finish(c);
+    if (walked > 0) finish(first + (walked - 1) * step);
   }
 
   // what is behind the walk
