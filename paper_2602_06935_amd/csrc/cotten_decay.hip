@@ -107,6 +107,58 @@ __global__ __launch_bounds__(64 * kWaves<D>, 2) void grad_states_kernel(Args a, 
   else walk<E, D, kGradStates>(a, blockIdx.x - units, smem);
 }
 
+// From what every segment adds to the states before (behind) all: four values of a slice's states a thread, from segment to segment.
+// `back`: the gradients, from the last to the first, by workgroups behind the first `forwards`.
+constexpr int kScanThreads = 256, kScanAhead = 8;
+__global__ __launch_bounds__(kScanThreads) void scan_kernel(Args a, int state_quads, long long quads, unsigned forwards) {
+  const bool back = blockIdx.x >= forwards;
+  const long long i = static_cast<long long>(blockIdx.x - (back ? forwards : 0u)) * kScanThreads + threadIdx.x;
+  if (i >= quads) return;
+  const long long slice = i / state_quads, at = slice * a.segments * state_quads + (i - slice * state_quads);
+  const float* counts = a.counts + 2 * slice * a.segments;
+  f32x4_t* s = reinterpret_cast<f32x4_t*>(back ? a.local_d : a.local_s) + at;
+  f32x4_t* t = a.local_t == nullptr || back ? nullptr : reinterpret_cast<f32x4_t*>(a.local_t) + at;
+  const int last = a.segments - 1;
+  f32x4_t state = s[static_cast<long long>(last) * state_quads], derivative = {0, 0, 0, 0};
+  for (int base = 0; base < last; base += kScanAhead) {
+    f32x4_t ds[kScanAhead], dt[kScanAhead];
+    float n[kScanAhead], w[kScanAhead];
+#pragma unroll
+    for (int u = 0; u < kScanAhead; ++u) {
+      const int j = base + u < last ? base + u : last - 1, segment = back ? last - 1 - j : j;
+      ds[u] = s[static_cast<long long>(segment) * state_quads];
+      if (t != nullptr) dt[u] = t[static_cast<long long>(segment) * state_quads];
+      n[u] = counts[2 * segment];
+      w[u] = counts[2 * segment + 1];
+    }
+#pragma unroll
+    for (int u = 0; u < kScanAhead; ++u) {
+      const int j = base + u, segment = back ? last - 1 - j : j;
+      if (j >= last) break;
+      s[static_cast<long long>(segment) * state_quads] = state;
+      if (back) {
+        state = state * w[u] + ds[u];   // (the first segment's is nothing, and goes nowhere)
+      } else {
+        if (t != nullptr) {
+          t[static_cast<long long>(segment) * state_quads] = derivative;
+          derivative = j == 0 ? dt[u] : w[u] * (derivative + n[u] * state) + dt[u];
+        }
+        state = j == 0 ? ds[u] : state * w[u] + ds[u];   // (the first segment's has the initial state in it)
+      }
+    }
+  }
+  if (!back) {
+    s[static_cast<long long>(last) * state_quads] = state;
+    if (t != nullptr) t[static_cast<long long>(last) * state_quads] = derivative;
+  }
+}
+void launch_scan(const Args& a, int slices, int D, bool both, hipStream_t stream) {
+  const int quads = D * D / 4;
+  const long long all = static_cast<long long>(slices) * quads;
+  const unsigned blocks = static_cast<unsigned>((all + kScanThreads - 1) / kScanThreads);
+  scan_kernel<<<dim3(both ? 2 * blocks : blocks), dim3(kScanThreads), 0, stream>>>(a, quads, all, blocks);
+}
+
 // dg of a head: every thread sums some of its slices' partial sums, in the order that it finds them, and the threads are joined.
 constexpr int kSumThreads = 1024;
 __global__ __launch_bounds__(kSumThreads) void sum_decays_kernel(const double* partial, float* dg, int B, int H, int of_slice) {
@@ -153,6 +205,7 @@ hipError_t forward(const Args& a, int slices, hipStream_t s) {
     constexpr int kBytes = kLds<E, D, kStates>;
     if (hipError_t rc = granted(walk_kernel<E, D, kStates>, kBytes)) return rc;
     walk_kernel<E, D, kStates><<<grid, block, kBytes, s>>>(a);
+    launch_scan(a, slices, D, false, s);
   }
   constexpr int kBytes = kLds<E, D, kOut>;
   if (hipError_t rc = granted(walk_kernel<E, D, kOut>, kBytes)) return rc;
@@ -169,6 +222,7 @@ hipError_t backward(const Args& a, int slices, float* dg, hipStream_t s) {
     const auto kernel = dg != nullptr ? grad_states_kernel<E, D, true> : grad_states_kernel<E, D, false>;
     if (hipError_t rc = granted(kernel, kBytes)) return rc;
     kernel<<<dim3(2u * units), block, kBytes, s>>>(a, units);
+    launch_scan(a, slices, D, true, s);
   }
   constexpr int kBytes = greatest(kLds<E, D, kDq>, kLds<E, D, kDv>);
   if (hipError_t rc = granted(grad_kernel<E, D>, kBytes)) return rc;
@@ -197,10 +251,22 @@ hipError_t backward(const Args& a, int D, int slices, float* dg, hipStream_t s) 
 
 }  // namespace
 
-Segments segments_of(long long slices, int chunks, int D, bool bwd) {
-  const long long wanted = 1024 / (slices * (bwd ? 2 : 1));
-  long long count = wanted < chunks / 4 ? wanted : chunks / 4;
-  if (count < 2) return {1, chunks};
+// Segments for 2048 waves of a forward and 1024 of a backward (whose rows take three walks), of two chunks at least, where that makes
+// three or more: the states' own walk is half of the rows', so two gain nothing.  us, whole / three / four / eight / sixteen / 32 segments:
+//   bf16 d = 64, 4 x 4096 rows     forward 173 / 99 / 77 / 44 / 29 / 24      backward 216 / 112 / 87 / 50 / 33 / 29
+//                64 x 4096                 170 / 101 / 80 / 56 / 53 / 65             216 / 162 / 128 / 121 / 128 / 149
+//               128 x 1024                  46 / 42 / 37 / 37 / 49                    68 / 77 / 73 / 81 / 99
+//               256 x 1024                  46 / 54 / 56 / 65                         88 / 127 / 131 / 151
+//   fp32 d = 32, 128 x 1024                 63 / 48 / 39 / 31 / 36                    83 / 64 / 66 / 62 / 67
+//   fp16 d = 128, 64 x 1024                109 / 80 / 67 / 78 / 99                   125 / 195 / 160 / 181 / 228
+// Sequences of few chunks gain nothing: bf16 d = 64, 4 x 256 rows 14.1 / 16.1 / 15.2, fp32 20.9 / 20.2 / 17.1, fp16 d = 128 31.1 / 26.9 / 21.5;
+// bf16 4 x 512 24.4 / 22.2 / 18.4 / 15.1.
+Segments segments_of(long long slices, int chunks, int D, int dtype, bool bwd) {
+  const int least = dtype != 0 && D <= 64 ? 10 : 7, cap = chunks / 8 > 32 ? chunks / 8 : 32;
+  long long count = (bwd ? 1024 : 2048) / (slices * waves_of(D));
+  if (count > chunks / 2) count = chunks / 2;
+  if (count > cap) count = cap;
+  if (chunks < least || count < 3) return {1, chunks};
   const int each = static_cast<int>((chunks + count - 1) / count);
   return {(chunks + each - 1) / each, each};
 }

@@ -28,11 +28,11 @@ int check_shape(int B, int H, int N, int d_h, int dtype) {
 struct Sizes {
   size_t states, counts, partial;
   cotten::decay::Segments segments;
-  Sizes(int B, int H, int N, int d_h, bool bwd, bool with_dg) {
+  Sizes(int B, int H, int N, int d_h, int dtype, bool bwd, bool with_dg) {
     const size_t slices = static_cast<size_t>(B) * H;
-    segments = cotten::decay::segments_of(static_cast<long long>(slices), (N + kChunk - 1) / kChunk, d_h, bwd);
+    segments = cotten::decay::segments_of(static_cast<long long>(slices), (N + kChunk - 1) / kChunk, d_h, dtype, bwd);
     states = segments.count > 1 ? slices * segments.count * d_h * d_h : 0;
-    counts = segments.count > 1 ? (slices * segments.count + 3) / 4 * 4 : 0;
+    counts = segments.count > 1 ? (2 * slices * segments.count + 3) / 4 * 4 : 0;
     partial = bwd && with_dg ? (2 * slices * segments.count * cotten::decay::waves_of(d_h) + 3) / 4 * 4 : 0;
   }
   size_t bytes(bool bwd, bool with_dg) const { return (states * (bwd ? with_dg ? 3 : 2 : 1) + counts + partial) * sizeof(float); }
@@ -81,7 +81,7 @@ int use_workspace(Args* a, const Sizes& size, bool bwd, bool with_dg, const cott
   a->dg = reinterpret_cast<double*>(at);
   a->local_s = at + size.partial;
   a->local_d = a->local_s + size.states;
-  a->local_t = a->local_d + (bwd ? size.states : 0);
+  a->local_t = bwd && with_dg ? a->local_d + size.states : nullptr;
   a->counts = a->local_s + size.states * (bwd ? with_dg ? 3 : 2 : 1);
   return COTTEN_OK;
 }
@@ -92,7 +92,7 @@ extern "C" {
 
 size_t cotten_decay_workspace_bytes(int B, int H, int N, int d_h, int dtype, int is_bwd, int with_dg) {
   if (check_shape(B, H, N, d_h, dtype) != COTTEN_OK) return 0;
-  return Sizes(B, H, N, d_h, is_bwd != 0, with_dg != 0).bytes(is_bwd != 0, with_dg != 0);
+  return Sizes(B, H, N, d_h, dtype, is_bwd != 0, with_dg != 0).bytes(is_bwd != 0, with_dg != 0);
 }
 
 int cotten_decay_fwd(const void* Q, const void* K, const void* V, const float* g, const uint8_t* mask, void* O, int B, int H, int N,
@@ -103,7 +103,7 @@ int cotten_decay_fwd(const void* Q, const void* K, const void* V, const float* g
   if (!aligned16(O)) return COTTEN_ERR_MISALIGNED;
   a.O = static_cast<unsigned char*>(O);
   a.final_state = params->final_state;
-  if (int rc = use_workspace(&a, Sizes(B, H, N, d_h, false, false), false, false, params)) return rc;
+  if (int rc = use_workspace(&a, Sizes(B, H, N, d_h, params->dtype, false, false), false, false, params)) return rc;
   return cotten::decay::launch_forward(a, params->dtype, d_h, B * H, static_cast<hipStream_t>(stream)) == hipSuccess ? COTTEN_OK
                                                                                                                    : COTTEN_ERR_LAUNCH;
 }
@@ -114,7 +114,7 @@ int cotten_decay_bwd(const void* Q, const void* K, const void* V, const float* g
   if (dO == nullptr || dQ == nullptr || dK == nullptr || dV == nullptr) return COTTEN_ERR_NULL_POINTER;
   if (int rc = prepare(&a, Q, K, V, g, mask, B, H, N, d_h, params)) return rc;
   if (!aligned16(dO) || !aligned16(dQ) || !aligned16(dK) || !aligned16(dV) || (reinterpret_cast<uintptr_t>(dg) & 3u)) return COTTEN_ERR_MISALIGNED;
-  if (int rc = use_workspace(&a, Sizes(B, H, N, d_h, true, dg != nullptr), true, dg != nullptr, params)) return rc;
+  if (int rc = use_workspace(&a, Sizes(B, H, N, d_h, params->dtype, true, dg != nullptr), true, dg != nullptr, params)) return rc;
   a.dO = static_cast<const unsigned char*>(dO);
   a.dQ = static_cast<unsigned char*>(dQ);
   a.dK = static_cast<unsigned char*>(dK);

@@ -64,11 +64,11 @@ struct Args {
   const float* dfinal_state;
   float* dinitial_state;
   // Sequences cut into segments: what a segment alone adds to the state behind it, to its derivative by g and to the gradient
-  // of the state before it, and how many of its tokens count.
-  float* local_s;               // [slice][segment][D][D]; the last one's place holds a copy of the initial state (forward)
+  // of the state before it, and after a pass over them the state (derivative) before, and the gradient behind, each.
+  float* local_s;               // [slice][segment][D][D]; at first the last one's place holds a copy of the initial state
   float* local_t;
   float* local_d;
-  float* counts;                // [slice][segment]
+  float* counts;                // [slice][segment][2]: how many of a segment's tokens count, and what they decay a state by
   double* dg;                   // [slice][segment][part]: partial sums of the decays' gradient
   int segments, segment_chunks;
   int H, N, chunks;
@@ -155,8 +155,10 @@ __device__ __forceinline__ void set_powers(Powers* to, double rate, int lane) {
   }
 }
 
-// Counts of the tokens of a chunk, and the factors that follow from them, for a lane's tokens: column 16 t + lane%16, rows 16 t + 4g + r.
-// Where all tokens from the first that counts to the last that exists count, pairs are as far apart as their numbers say, and
+// p of a token of a chunk
+__device__ __forceinline__ int upto(uint32_t live, int t) { return __popc(live & (0xffffffffu >> (31 - t))); }
+
+// How many tokens of a chunk count, and the factors of a wave's pairs: columns lane%16 of X's tile, rows 4g + r of Y's.  Where all tokens from the first that counts to the last that exists count, pairs are as far apart as their numbers say, and
 // the factors of the pairs are the same in all chunks.
 // Two pieces of eight significant bits each, rounded: 16 bits, where a result of 11 or fewer is all that comes of them.
 __device__ __forceinline__ Pieces<2> cut_in_two(const float (&x)[8]) {
@@ -202,12 +204,8 @@ struct Decays {
   uint32_t live;
   bool together;
   float n;                  // tokens that count
-  float to[2];              // of X's rows, against the state
-  float fro[2][4];          // of Z's rows, for the state
   float pair[kOwn][4];
   float whole_hi, whole_lo;
-  // p of a token of the chunk
-  static __device__ __forceinline__ int upto(uint32_t live, int t) { return __popc(live & (0xffffffffu >> (31 - t))); }
   // tokens that count between column 16 x + lane%16 and row 16 y + 4g + r
   static __device__ __forceinline__ int apart(uint32_t live, const Pair<R>& p, int r, int lane) {
     const int column = upto(live, 16 * p.x + (lane & 15)), row = upto(live, 16 * p.y + 4 * (lane >> 4) + r);
@@ -241,9 +239,6 @@ struct Decays {
     n = 0.0f;
     whole_hi = 1.0f;
     whole_lo = 0.0f;
-    to[0] = to[1] = 1.0f;
-#pragma unroll
-    for (int r = 0; r < 4; ++r) fro[0][r] = fro[1][r] = 1.0f;
   }
   // bits: at least one; `there`: the tokens that exist
   __device__ __forceinline__ void set(uint32_t bits, uint32_t there, const Powers* powers, int wave, int lane) {
@@ -252,16 +247,6 @@ struct Decays {
     n = static_cast<float>(count);
     whole_hi = powers->hi[count];
     whole_lo = powers->lo[count];
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int p = upto(bits, 16 * t + (lane & 15));
-      to[t] = powers->hi[R::kBack ? count - p : p];
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int q = upto(bits, 16 * t + 4 * (lane >> 4) + r);
-        fro[t][r] = powers->hi[R::kBack ? q : count - q];
-      }
-    }
     const bool now = ((bits | ~there) >> __builtin_ctz(bits)) == (0xffffffffu >> __builtin_ctz(bits));
     if (!now || !together) set_pairs(now ? ~0u : bits, powers, wave, lane);
     together = now;
@@ -306,12 +291,13 @@ __device__ __forceinline__ void load_state(StateColumns<D>& S, const float* from
 template <int D>
 constexpr int kWaves = D / 16;
 
-// A chunk's place in LDS: rows in pieces, and the factors of X's rows and of the pairs of Y's and Z's.
+// A chunk's place in LDS: rows in pieces; by token the factors of X's rows and of Y's and Z's, and both with what decays between them and
+// the state.
 template <class E, int D, bool ROWS>
 struct Place {
   typedef Rows<D, E::kPieces> R;
   static constexpr int kY = 0, kZ = R::kBytes, kX = 2 * R::kBytes, kOfX = ROWS ? 3 * R::kBytes : 2 * R::kBytes;
-  static constexpr int kOfPair = kOfX + kChunk * 4, kPowers = kOfPair + kChunk * 4, kBytes = kPowers + static_cast<int>(sizeof(Powers));
+  static constexpr int kOfPair = kOfX + kChunk * 4, kTo = kOfPair + kChunk * 4, kOfState = kTo + kChunk * 4, kPowers = kOfState + kChunk * 4, kBytes = kPowers + static_cast<int>(sizeof(Powers));
 };
 // ... followed by the products of the pairs of tiles as operands ([tile of X][piece][lane], 16 bytes), and what waves sum over all columns.
 template <int OF>
@@ -384,6 +370,8 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
   const long long state_at = static_cast<long long>(slice) * D * D;
   float* of_x = reinterpret_cast<float*>(smem + P::kOfX);
   float* of_pair = reinterpret_cast<float*>(smem + P::kOfPair);
+  float* to_state = reinterpret_cast<float*>(smem + P::kTo);
+  float* of_state = reinterpret_cast<float*>(smem + P::kOfState);
 
   Powers* powers = reinterpret_cast<Powers*>(smem + P::kPowers);
   unsigned char* pairs = smem + P::kBytes;
@@ -411,37 +399,11 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
       return;
     }
     if (R::kBack && segment == 0) return;
-  } else if (a.segments == 1) {
+  } else if (a.segments == 1 || (R::kBack && segment == a.segments - 1)) {
     load_state<D, R::kTransposed>(S, outer, col, lane);
-  } else if (R::kBack) {
-    if (segment == a.segments - 1) {
-      load_state<D, R::kTransposed>(S, outer, col, lane);
-    } else {
-      load_state<D, R::kTransposed>(S, a.local_d + (of_slice + a.segments - 1) * D * D, col, lane);
-      for (int j = a.segments - 2; j > segment; --j) {
-        const float w = static_cast<float>(exp2(rate * static_cast<double>(a.counts[of_slice + j])));
-        load_state<D, R::kTransposed>(T, a.local_d + (of_slice + j) * D * D, col, lane);
-#pragma unroll
-        for (int dt = 0; dt < 2 * kBlocks; ++dt) S.s[dt] = S.s[dt] * w + T.s[dt];
-      }
-    }
   } else {
-    load_state<D, R::kTransposed>(S, a.local_s + (of_slice + (segment == 0 ? a.segments - 1 : 0)) * D * D, col, lane);
-    if constexpr (R::kDerivative)
-      if (segment > 0) load_state<D, false>(T, a.local_t + of_slice * D * D, col, lane);
-    for (int j = 1; j < segment; ++j) {
-      const float n = a.counts[of_slice + j], w = static_cast<float>(exp2(rate * static_cast<double>(n)));
-      if constexpr (R::kDerivative) {
-        StateColumns<D> next;
-        load_state<D, false>(next, a.local_t + (of_slice + j) * D * D, col, lane);
-#pragma unroll
-        for (int dt = 0; dt < 2 * kBlocks; ++dt) T.s[dt] = w * (T.s[dt] + n * S.s[dt]) + next.s[dt];
-      }
-      StateColumns<D> next;
-      load_state<D, R::kTransposed>(next, a.local_s + (of_slice + j) * D * D, col, lane);
-#pragma unroll
-      for (int dt = 0; dt < 2 * kBlocks; ++dt) S.s[dt] = S.s[dt] * w + next.s[dt];
-    }
+    load_state<D, R::kTransposed>(S, (R::kBack ? a.local_d : a.local_s) + (of_slice + segment) * D * D, col, lane);
+    if constexpr (R::kDerivative) load_state<D, false>(T, a.local_t + (of_slice + segment) * D * D, col, lane);
   }
 
   // Chunks before the first token that counts: there is nothing in the state but what came from outside, and forwards without
@@ -531,9 +493,15 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
       if (R::kScaleX) fx *= a.scale;
       else fyz *= a.scale;
       const uint32_t in_x = R::kBack ? now : now_there, in_yz = R::kBack ? now_there : now;
+      const int p = upto(now, row), behind = __popc(now) - p;
+      fyz = ((in_yz >> row) & 1u) ? fyz : 0.0f;
       if (lane % kRowLanes == 0) {
-        of_x[row] = ((in_x >> row) & 1u) ? fx : 0.0f;
-        of_pair[row] = ((in_yz >> row) & 1u) ? fyz : 0.0f;
+        if (R::kRows) {
+          of_x[row] = ((in_x >> row) & 1u) ? fx : 0.0f;
+          to_state[row] = powers->hi[R::kBack ? behind : p];
+        }
+        of_pair[row] = fyz;
+        of_state[row] = fyz * powers->hi[R::kBack ? p : behind];
       }
     }
     if (now != decays.live) {
@@ -548,7 +516,6 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
 
     if constexpr (R::kThrough)
       if (i > 0) finish(c - step);
-    const f32x4_t pair_factor[2] = {*reinterpret_cast<const f32x4_t*>(of_pair + 4 * group), *reinterpret_cast<const f32x4_t*>(of_pair + 16 + 4 * group)};
     Pieces<E::kPieces> z;
     if (with_sums) z = L::column_operand(smem + P::kZ, wave, lane);
     // rows: 16 columns of this wave's (4g + r) of tokens 16 t + lane%16
@@ -589,8 +556,8 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
         }
 #pragma unroll
         for (int t = 0; t < 2; ++t) {
-          if constexpr (ROLE == kDecays) o[t] = o[t] * static_cast<float>(decays.upto(now, 16 * t + (lane & 15))) + u[t];
-          o[t] *= decays.to[t];
+          if constexpr (ROLE == kDecays) o[t] = o[t] * static_cast<float>(upto(now, 16 * t + (lane & 15))) + u[t];
+          o[t] *= to_state[16 * t + (lane & 15)];
         }
       }
     }
@@ -598,18 +565,19 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     // the state: S <- a^n S + Y^T (w Z)
     if (with_sums) {
       count += decays.n;
+      const f32x4_t factor[2] = {*reinterpret_cast<const f32x4_t*>(of_state + 4 * group), *reinterpret_cast<const f32x4_t*>(of_state + 16 + 4 * group)};
       float w[8];
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         float v = 0.0f;
 #pragma unroll
         for (int p = E::kPieces - 1; p >= 0; --p) v += static_cast<float>(z.p[p][j]);
-        w[j] = v * (pair_factor[j >> 2][j & 3] * decays.fro[j >> 2][j & 3]);
+        w[j] = v * factor[j >> 2][j & 3];
       }
       if constexpr (R::kDerivative) {
         float wt[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) wt[j] = w[j] * (decays.n - static_cast<float>(decays.upto(now, 16 * (j >> 2) + 4 * group + (j & 3))));
+        for (int j = 0; j < 8; ++j) wt[j] = w[j] * (decays.n - static_cast<float>(upto(now, 16 * (j >> 2) + 4 * group + (j & 3))));
         const Pieces<3> wz = cut<E::kPieces>(wt);
 #pragma unroll
         for (int dt = 0; dt < StateColumns<D>::kTiles; ++dt) {
@@ -682,7 +650,10 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     float* to = (R::kBack ? a.local_d : a.local_s) + (of_slice + segment) * D * D;
     S.store(to, col, lane);
     if constexpr (R::kDerivative) T.store(a.local_t + (of_slice + segment) * D * D, col, lane);
-    if (threadIdx.x == 0) a.counts[of_slice + segment] = count;
+    if (threadIdx.x == 0) {
+      a.counts[2 * (of_slice + segment)] = count;
+      a.counts[2 * (of_slice + segment) + 1] = static_cast<float>(exp2(rate * static_cast<double>(count)));
+    }
   } else if constexpr (ROLE == kOut) {
     if (a.final_state != nullptr && segment == a.segments - 1) S.store(a.final_state + state_at, col, lane);
   } else if constexpr (ROLE == kDv) {

@@ -13,7 +13,7 @@ struct Args;
 struct Segments {
   int count, chunks;
 };
-Segments segments_of(long long slices, int chunks, int D, bool bwd);
+Segments segments_of(long long slices, int chunks, int D, int dtype, bool bwd);
 
 hipError_t launch_forward(const Args& a, int dtype, int D, int slices, hipStream_t stream);
 // dg: [H], or nullptr where the decays are not trained; partial sums go through a.dg.
