@@ -403,7 +403,7 @@ size_t cotten_embed_workspace_bytes(int B, int N, int D, int V);
  * Without post_weight F goes in as it is, without next_weight there is no H, without gate it is 1; the number of an
  * element is that in F.  X, F, Y, H and their gradients are [B, N, D], contiguous; weights, biases and
  * the gate are [D], the gate with gate_per_sequence [B, D]; all are of one element type.  Sums are fp32, in a fixed
- * order, every result is rounded once (H comes from the row Y before its rounding).  D up to 16384, B * N below 2^31, up to
+ * order, every result is rounded once (H comes from the row Y before its rounding).  D up to 8192, B * N below 2^31, up to
  * 2^40 elements for the dropout by itself.  y may be x, Y may be X, and H may be F (no others overlap).  The backward keeps nothing: it makes the rows again from
  * X and F, which have to hold what the forward saw.  A row is one of N = 1 for single tokens. */
 typedef enum cotten_norm {

@@ -143,7 +143,7 @@ __device__ __forceinline__ float sum_of_lanes(float x) {
 template <int LANES_, int P_>
 struct Shape {
   static constexpr int kLanes = LANES_, kPieces = P_;
-  static constexpr int kBlock = LANES_ > kThreads ? LANES_ : kThreads;
+  static constexpr int kBlock = LANES_ > 64 ? LANES_ : kThreads;
   static constexpr int kWaves = LANES_ / 64;         // of a row
   static constexpr int kGroups = kBlock / LANES_;    // rows that a workgroup has under way
   static constexpr int kMost = LANES_ * P_ * 8;      // elements of a row
@@ -267,7 +267,7 @@ __device__ __forceinline__ float normalise(float (&x)[S::kPieces][8], const int 
 #pragma unroll
     for (int i = 0; i < 8; ++i) square = fmaf(x[p][i], x[p][i], square);
   sums(square);
-  const float r = 1.0f / sqrtf(square * inv_D + eps);
+  const float r = __builtin_amdgcn_rsqf(fmaf(square, inv_D, eps));
 #pragma unroll
   for (int p = 0; p < S::kPieces; ++p)
 #pragma unroll
@@ -407,25 +407,72 @@ __device__ __forceinline__ void store_partial(float* to, const float (&x)[S::kPi
   }
 }
 
+// Weights, biases and a gate for all rows as fp32 in LDS, eight values of a lane as two reads that are free of conflicts: held
+// in registers they would take those of a second and a third wave.  Rows of more than 2048 elements read them from memory each time.
 template <class T, class S, bool ALIGNED>
-__global__ __launch_bounds__(S::kBlock) void seam_bwd_kernel(Args a) {
-  __shared__ float lds[S::kWaves > 1 ? 4 * S::kWaves : S::kGroups * S::kMost];
-  RowSums<S> sums{lds};
+struct Vectors {
+  static constexpr bool kInLds = S::kMost <= 2048;
+  static constexpr int kSize = kInLds ? S::kMost : 0;  // floats of one
+  const Columns<T, S, ALIGNED>& columns;
+  float* at;
+  int D;
+  __device__ __forceinline__ void set(int slot, const void* from) const {
+    if constexpr (kInLds) {
+      if (threadIdx.x < S::kLanes && from != nullptr) {
+        Raw<T> raw[S::kPieces];
+        columns.load(from, 0, D, raw);
+        float x[8];
+        unpack<T>(raw[0], x);
+        f32x4_t* to = reinterpret_cast<f32x4_t*>(at + slot * kSize) + threadIdx.x;
+        to[0] = f32x4_t{x[0], x[1], x[2], x[3]};
+        to[S::kLanes] = f32x4_t{x[4], x[5], x[6], x[7]};
+      }
+    }
+  }
+  __device__ __forceinline__ void get(int slot, const void* from, int p, float (&x)[8]) const {
+    if constexpr (kInLds) {
+      const f32x4_t* of = reinterpret_cast<const f32x4_t*>(at + slot * kSize) + threadIdx.x % S::kLanes;
+      const f32x4_t lo = of[0], hi = of[S::kLanes];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        x[e] = lo[e];
+        x[4 + e] = hi[e];
+      }
+    } else {
+      unpack<T>(residual::load<T, ALIGNED>(static_cast<const T*>(from) + columns.col[p], columns.valid[p]), x);
+    }
+  }
+};
+
+constexpr int max_of(int a, int b) { return a > b ? a : b; }
+
+// BIAS: the gradient of a bias is wanted.
+template <class T, class S, bool ALIGNED, bool BIAS>
+__global__ __launch_bounds__(S::kBlock, S::kBlock <= 256 ? 3 : S::kBlock == 512 ? 2 : 4) void seam_bwd_kernel(Args a) {
+  typedef Vectors<T, S, ALIGNED> V;
+  constexpr int P = S::kPieces;
+  enum { kW1, kB1, kGate, kW2 };
+  __shared__ __attribute__((aligned(16))) float space[max_of(4 * V::kSize, S::kWaves > 1 ? 4 : S::kGroups * S::kMost)];
+  __shared__ float sums_space[S::kWaves > 1 ? 4 * S::kWaves : 1];
+  RowSums<S> sums{sums_space};
   const Columns<T, S, ALIGNED> columns(a.D);
+  const V vectors{columns, space, a.D};
   const Lots lots(a.drop);
   const float inv_D = 1.0f / a.D;
-  constexpr int P = S::kPieces;
-  Raw<T> w1[P], b1[P], gate[P], w2[P];
-  if (a.w1 != nullptr) columns.load(a.w1, 0, a.D, w1);
-  if (a.b1 != nullptr) columns.load(a.b1, 0, a.D, b1);
-  if (a.gate != nullptr && !a.per_sequence) columns.load(a.gate, 0, a.D, gate);
-  if (a.w2 != nullptr) columns.load(a.w2, 0, a.D, w2);
-  float of_w1[P][8], of_b1[P][8], of_gate[P][8], of_w2[P][8], of_b2[P][8];
+  vectors.set(kW1, a.w1);
+  vectors.set(kB1, a.b1);
+  if (!a.per_sequence) vectors.set(kGate, a.gate);
+  vectors.set(kW2, a.w2);
+  if constexpr (V::kInLds) __syncthreads();
+  Raw<T> gate[P];
+  float of_w1[P][8], of_b1[BIAS ? P : 1][8], of_gate[P][8], of_w2[P][8], of_b2[BIAS ? P : 1][8];
   clear<S>(of_w1);
-  clear<S>(of_b1);
   clear<S>(of_gate);
   clear<S>(of_w2);
-  clear<S>(of_b2);
+  if constexpr (BIAS) {
+    clear<S>(of_b1);
+    clear<S>(of_b2);
+  }
   for (long long u = static_cast<long long>(blockIdx.x) * S::kGroups + threadIdx.x / S::kLanes; u < a.units;
        u += static_cast<long long>(gridDim.x) * S::kGroups) {
     const Unit unit(a, u);
@@ -442,67 +489,70 @@ __global__ __launch_bounds__(S::kBlock) void seam_bwd_kernel(Args a) {
       }
       if (a.dY != nullptr) columns.load(a.dY, row, a.D, ry);
     };
-    fetch(unit.first);
+    auto gate_of = [&](int p, float (&g)[8]) {
+      if (a.per_sequence) unpack<T>(gate[p], g);
+      else vectors.get(kGate, a.gate, p, g);
+    };
     for (int i = 0; i < unit.rows; ++i) {
       const long long row = unit.first + i;
-      float f[P][8], y[P][8], h[P][8], d[P][8];
-#pragma unroll
-      for (int p = 0; p < P; ++p) {
-        unpack<T>(rf[p], f[p]);
-        if (a.dH != nullptr) {
-          unpack<T>(rx[p], y[p]);
-          unpack<T>(rh[p], h[p]);
-        }
-        if (a.dY != nullptr) {
-          unpack<T>(ry[p], d[p]);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; ++e) d[p][e] = 0.0f;
-        }
-      }
-      if (i + 1 < unit.rows) fetch(row + 1);
-      float r1 = 0.0f;
-      if (a.w1 != nullptr) r1 = normalise<S>(f, columns.valid, a.layer, inv_D, a.eps, sums);
+      asm volatile("" ::: "memory");  // (what is read from LDS is read again in every row, not held over all)
+      fetch(row);
+      float f[P][8], z[P][8], d[P][8];
       uint32_t kept[P];
 #pragma unroll
+      for (int p = 0; p < P; ++p) unpack<T>(rf[p], f[p]);
+      float r1 = 0.0f;
+      if (a.w1 != nullptr) r1 = normalise<S>(f, columns.valid, a.layer, inv_D, a.eps, sums);
+      // z, what the block adds before its gate and alpha
+#pragma unroll
       for (int p = 0; p < P; ++p) {
+        if (a.w1 != nullptr) {
+          float w[8], b[8] = {};
+          vectors.get(kW1, a.w1, p, w);
+          if (a.b1 != nullptr) vectors.get(kB1, a.b1, p, b);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) z[p][e] = fmaf(f[p][e], w[e], b[e]);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) z[p][e] = f[p][e];
+        }
         kept[p] = 0xffu;
         if (a.drop.out_of != 0) {
           const u32x4_t w = lots.template of<ALIGNED>(static_cast<uint64_t>(row) * a.D + columns.col[p]);
           kept[p] = 0;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) kept[p] |= lots.keeps(w, e) ? 1u << e : 0u;
+          for (int e = 0; e < 8; ++e) {
+            const bool keeps = lots.keeps(w, e);
+            kept[p] |= keeps ? 1u << e : 0u;
+            z[p][e] = keeps ? z[p][e] * lots.factor : 0.0f;
+          }
         }
       }
-      // z, what the block adds before its gate and alpha
-      auto added = [&](int p, float (&z)[8]) {
-        float w[8], b[8] = {};
-        if (a.w1 != nullptr) unpack<T>(w1[p], w);
-        if (a.b1 != nullptr) unpack<T>(b1[p], b);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          z[e] = a.w1 != nullptr ? fmaf(f[p][e], w[e], b[e]) : f[p][e];
-          z[e] = (kept[p] >> e) & 1u ? z[e] * lots.factor : 0.0f;
-        }
-      };
       if (a.dH != nullptr) {
+        float y[P][8], h[P][8];
 #pragma unroll
         for (int p = 0; p < P; ++p) {
-          float z[8], g[8];
-          added(p, z);
-          if (a.gate != nullptr) unpack<T>(gate[p], g);
+          unpack<T>(rx[p], y[p]);
+          unpack<T>(rh[p], h[p]);
+          if (a.gate != nullptr) {
+            float g[8];
+            gate_of(p, g);
 #pragma unroll
-          for (int e = 0; e < 8; ++e) y[p][e] = fmaf(a.alpha, a.gate != nullptr ? g[e] * z[e] : z[e], y[p][e]);
+            for (int e = 0; e < 8; ++e) y[p][e] = fmaf(a.alpha * g[e], z[p][e], y[p][e]);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[p][e] = fmaf(a.alpha, z[p][e], y[p][e]);
+          }
         }
         const float r2 = normalise<S>(y, columns.valid, a.layer, inv_D, a.eps, sums);
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           float w[8];
-          unpack<T>(w2[p], w);
+          vectors.get(kW2, a.w2, p, w);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             of_w2[p][e] = fmaf(h[p][e], y[p][e], of_w2[p][e]);
-            of_b2[p][e] += h[p][e];
+            if constexpr (BIAS) of_b2[p][e] += h[p][e];
             h[p][e] *= w[e];
           }
         }
@@ -510,35 +560,44 @@ __global__ __launch_bounds__(S::kBlock) void seam_bwd_kernel(Args a) {
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
-          for (int e = 0; e < 8; ++e) d[p][e] += e < columns.valid[p] ? h[p][e] : 0.0f;
+          for (int e = 0; e < 8; ++e) d[p][e] = (ALIGNED && P == 1) || e < columns.valid[p] ? h[p][e] : 0.0f;
+      } else {
+        clear<S>(d);
       }
 #pragma unroll
       for (int p = 0; p < P; ++p) {
-        columns.store(a.dX, row, a.D, p, d[p]);
-        float z[8], g[8];
-        if (a.gate != nullptr) {
-          added(p, z);
-          unpack<T>(gate[p], g);
-        }
+        if (a.dY != nullptr) {
+          float y[8];
+          unpack<T>(ry[p], y);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          d[p][e] *= a.alpha;
-          if (a.gate != nullptr) {
-            of_gate[p][e] = fmaf(d[p][e], z[e], of_gate[p][e]);
+          for (int e = 0; e < 8; ++e) d[p][e] += y[e];
+        }
+        columns.store(a.dX, row, a.D, p, d[p]);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) d[p][e] *= a.alpha;
+        if (a.gate != nullptr) {
+          float g[8];
+          gate_of(p, g);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            of_gate[p][e] = fmaf(d[p][e], z[p][e], of_gate[p][e]);
             d[p][e] *= g[e];
           }
-          d[p][e] = (kept[p] >> e) & 1u ? d[p][e] * lots.factor : 0.0f;
+        }
+        if (a.drop.out_of != 0) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) d[p][e] = (kept[p] >> e) & 1u ? d[p][e] * lots.factor : 0.0f;
         }
       }
       if (a.w1 != nullptr) {
 #pragma unroll
         for (int p = 0; p < P; ++p) {
           float w[8];
-          unpack<T>(w1[p], w);
+          vectors.get(kW1, a.w1, p, w);
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
             of_w1[p][e] = fmaf(d[p][e], f[p][e], of_w1[p][e]);
-            of_b1[p][e] += d[p][e];
+            if constexpr (BIAS) of_b1[p][e] += d[p][e];
             d[p][e] *= w[e];
           }
         }
@@ -556,16 +615,16 @@ __global__ __launch_bounds__(S::kBlock) void seam_bwd_kernel(Args a) {
     }
   }
   float* to = a.partial + static_cast<long long>(blockIdx.x) * a.vectors * a.D;
-  auto hand_over = [&](bool wanted, const float (&x)[P][8]) {
+  auto hand_over = [&](bool wanted, const auto& x) {
     if (!wanted) return;
-    store_partial<S, ALIGNED>(to, x, columns.col, columns.valid, lds);
+    store_partial<S, ALIGNED>(to, x, columns.col, columns.valid, space);
     to += a.D;
   };
   hand_over(a.take_w1, of_w1);
-  hand_over(a.take_b1, of_b1);
+  if constexpr (BIAS) hand_over(a.take_b1, of_b1);
   hand_over(a.take_gate && !a.per_sequence, of_gate);
   hand_over(a.take_w2, of_w2);
-  hand_over(a.take_b2, of_b2);
+  if constexpr (BIAS) hand_over(a.take_b2, of_b2);
 }
 
 // ---- sums over workgroups and units ---------------------------------------------------------------------------------------
@@ -620,19 +679,21 @@ __global__ __launch_bounds__(kSumColumns* kSumWays) void sum_kernel(Sums a) {
 
 // ---- launches -----------------------------------------------------------------------------------------------------------
 
-constexpr int kMostWidth = 16384;
+constexpr int kMostWidth = 8192;
 
 // Lanes of a row: as few as take it in one piece of eight each, which leaves the sums over the row short and several rows to a wave.
-int lanes_of(int D) { return D <= 64 ? 8 : D <= 256 ? 32 : D <= 512 ? 64 : D <= 2048 ? 256 : 1024; }
+int lanes_of(int D) { return D <= 64 ? 8 : D <= 256 ? 32 : D <= 512 ? 64 : D <= 1024 ? 128 : D <= 2048 ? 256 : D <= 4096 ? 512 : 1024; }
 
 struct Plan {
   long long units, sequences;
   int unit_rows, sequence_units, sequence_rows, blocks;
   // `rows` of `sequence_rows` each where gates go by sequence; otherwise all rows count as one sequence, cut so that rows
   // numbered with 31 bits are enough (the last sequence may be shorter: then there is only one).
-  Plan(int B, int N, int D, bool per_sequence) {
-    const int lanes = lanes_of(D), block = lanes > kThreads ? lanes : kThreads, groups = block / lanes;
-    const long long most_groups = 256ll * (2048 / block) * groups / 2;  // 1024 threads to a compute unit
+  Plan(int B, int N, int D, bool per_sequence, bool bwd) {
+    const int lanes = lanes_of(D), block = lanes > 64 ? lanes : kThreads, groups = block / lanes;
+    // as many workgroups as run at once: 1024 threads to a compute unit, or 768 where the backward's registers admit no more
+    const int at_once = bwd && block <= 256 ? 768 / block : bwd ? 1 : 1024 / block;
+    const long long most_groups = 256ll * at_once * groups;
     const long long rows = static_cast<long long>(B) * N;
     sequences = per_sequence ? B : 1;
     sequence_rows = per_sequence ? N : static_cast<int>(rows);
@@ -651,16 +712,19 @@ void launch_seam(const Args& a, int blocks, bool bwd, hipStream_t s) {
 #define COTTEN_SEAM(LANES, PIECES)                                                                            \
   {                                                                                                           \
     typedef Shape<LANES, PIECES> S;                                                                           \
-    if (bwd) seam_bwd_kernel<T, S, ALIGNED><<<dim3(blocks), dim3(S::kBlock), 0, s>>>(a);                      \
-    else seam_fwd_kernel<T, S, ALIGNED><<<dim3(blocks), dim3(S::kBlock), 0, s>>>(a);                          \
+    const dim3 grid(blocks), block(S::kBlock);                                                                \
+    if (!bwd) seam_fwd_kernel<T, S, ALIGNED><<<grid, block, 0, s>>>(a);                                       \
+    else if (a.take_b1 || a.take_b2) seam_bwd_kernel<T, S, ALIGNED, true><<<grid, block, 0, s>>>(a);          \
+    else seam_bwd_kernel<T, S, ALIGNED, false><<<grid, block, 0, s>>>(a);                                     \
   }
   const int D = a.D;
   if (D <= 64) COTTEN_SEAM(8, 1)
   else if (D <= 256) COTTEN_SEAM(32, 1)
   else if (D <= 512) COTTEN_SEAM(64, 1)
+  else if (D <= 1024) COTTEN_SEAM(128, 1)
   else if (D <= 2048) COTTEN_SEAM(256, 1)
-  else if (D <= 8192) COTTEN_SEAM(1024, 1)
-  else COTTEN_SEAM(1024, 2)
+  else if (D <= 4096) COTTEN_SEAM(512, 1)
+  else COTTEN_SEAM(1024, 1)
 #undef COTTEN_SEAM
 }
 
@@ -765,7 +829,7 @@ int cotten_dropout(const void* x, void* y, size_t n, void* stream, const cotten_
 
 size_t cotten_residual_workspace_bytes(int B, int N, int D, int gate_per_sequence) {
   if (check_shape(B, N, D) != COTTEN_OK) return 0;
-  const Plan plan(B, N, D, gate_per_sequence != 0);
+  const Plan plan(B, N, D, gate_per_sequence != 0, true);
   return (static_cast<size_t>(plan.blocks) * 5 + (gate_per_sequence && plan.sequence_units > 1 ? plan.units : 0)) * D * sizeof(float);
 }
 
@@ -777,7 +841,7 @@ int cotten_residual_fwd(const void* X, const void* F, void* Y, void* H, int B, i
   if (!aligned16(Y) || !aligned16(H)) return COTTEN_ERR_MISALIGNED;
   a.Y = Y;
   a.H = H;
-  const Plan plan(B, N, D, a.per_sequence);
+  const Plan plan(B, N, D, a.per_sequence, false);
   use_plan(&a, plan);
   return launch_any(prm->dtype, a, plan, false, static_cast<hipStream_t>(stream)) == hipSuccess ? COTTEN_OK : COTTEN_ERR_LAUNCH;
 }
@@ -796,7 +860,7 @@ int cotten_residual_bwd(const void* X, const void* F, const void* dY, const void
     if (!aligned16(p.to)) return COTTEN_ERR_MISALIGNED;
   }
   if (!aligned16(dY) || !aligned16(dH) || !aligned16(dX) || !aligned16(dF)) return COTTEN_ERR_MISALIGNED;
-  const Plan plan(B, N, D, a.per_sequence);
+  const Plan plan(B, N, D, a.per_sequence, true);
   use_plan(&a, plan);
   if (prm->workspace == nullptr ||
       prm->workspace_bytes < cotten_residual_workspace_bytes(B, N, D, a.per_sequence)) return COTTEN_ERR_WORKSPACE_TOO_SMALL;

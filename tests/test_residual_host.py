@@ -68,7 +68,7 @@ def test_seam_refusals(lib, call, ptrs):
             assert call(lib, ptrs[:i] + (None,) + ptrs[i + 1:]) == -1, i
     for name in ("post_weight", "post_bias", "gate", "next_weight", "next_bias", "workspace"):
         assert call(lib, **{name: 0x10008}) == -5, name
-    for dims in ((0, 3, 64), (2, 0, 64), (2, 3, 0), (2, 3, 16385), (1 << 16, 1 << 15, 64)):
+    for dims in ((0, 3, 64), (2, 0, 64), (2, 3, 0), (2, 3, 8193), (1 << 16, 1 << 15, 64)):
         assert call(lib, dims=dims) == -2, dims
     assert call(lib, dtype=3) == -4
     assert call(lib, norm=2) == -7
