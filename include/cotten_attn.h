@@ -468,8 +468,8 @@ size_t cotten_residual_workspace_bytes(int B, int N, int D, int gate_per_sequenc
  * in falling order, of equal totals the one with the lower k * V + v.  A beam that ended (finished byte not 0)
  * goes on with the item `pad` alone, at its score; its logits are not read.  What else an ended beam could
  * go on with, and everything of a beam whose score, or sum of exponentials, is not finite, has the total -inf (taken
- * where nothing else is left).  A NaN among the logits counts as -inf.  Totals are compared in 64 bits, with sums of exponentials right to
- * about 1e-8: candidates of different beams that are nearer than that may come in either order.
+ * where nothing else is left).  A NaN among the logits counts as -inf.  Totals are compared in 64 bits, with sums in fp32 where
+ * these decide and in 64 bits where candidates of two beams are nearer than that can tell apart.
  * logits [B, K, V] of one element type, contiguous; scores, new_scores float [B, K] (new_scores may be scores);
  * finished [B, K] bytes or NULL; parents (the beam 0 ... K-1 that is continued) and tokens (the item) int32 [B, K].  K up to 32, B * K
  * below 2^22, V below 2^30.  The workspace holds cotten_beam_workspace_bytes(); calls from several host threads must not share

@@ -6,7 +6,9 @@
 //
 // The best, the lower k * V + v of equal ones first.  Within a beam the order of the totals is that of the logits, so a row of
 // logits is read once, in parts: a wave keeps the K best of its part (value and item) and the sum of the exponentials, and
-// one workgroup a sequence joins what the parts of its K rows hold, with totals in 64 bits.
+// one workgroup a sequence joins what the parts of its K rows hold, with totals in 64 bits.  The exponentials are fp32, which leaves
+// the logarithm of a row's sum right to 1e-6 at worst and some 1e-8 as a rule; where candidates of two beams come nearer than that, the sums
+// of these rows are made again in 64 bits.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -32,37 +34,63 @@ __device__ __forceinline__ uint32_t in_order(float x) {
 __device__ __forceinline__ float from_order(uint32_t u) { return __uint_as_float((u >> 31) ? u & 0x7fffffffu : ~u); }
 __device__ __forceinline__ uint64_t key_of(float x, uint32_t item) { return (static_cast<uint64_t>(in_order(x)) << 32) | ~item; }
 
-__device__ __forceinline__ uint64_t shuffle_xor(uint64_t x, int m) {
-  return (static_cast<uint64_t>(static_cast<uint32_t>(__shfl_xor(static_cast<int>(x >> 32), m))) << 32) |
-         static_cast<uint32_t>(__shfl_xor(static_cast<int>(x), m));
+// The value of lane ^ M, without a trip through LDS: quads, rows of 16 and halves of a wave have moves of their own.
+template <int CTRL>
+__device__ __forceinline__ uint32_t move(uint32_t x) {
+  return static_cast<uint32_t>(__builtin_amdgcn_update_dpp(0, static_cast<int>(x), CTRL, 0xF, 0xF, true));
+}
+template <int M>
+__device__ __forceinline__ uint32_t of_xor(uint32_t x, int lane) {
+  if constexpr (M == 1) return move<0xB1>(x);               // quad_perm 1,0,3,2
+  else if constexpr (M == 2) return move<0x4E>(x);          // quad_perm 2,3,0,1
+  else if constexpr (M == 4) return move<0x1B>(move<0x141>(x));  // the eight reversed, then the fours
+  else if constexpr (M == 8) return move<0x128>(x);         // row_ror 8
+  else if constexpr (M == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return (lane & 16) ? r[0] : r[1];
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return (lane & 32) ? r[0] : r[1];
+  }
+}
+template <int M>
+__device__ __forceinline__ uint64_t of_xor(uint64_t x, int lane) {
+  return (static_cast<uint64_t>(of_xor<M>(static_cast<uint32_t>(x >> 32), lane)) << 32) | of_xor<M>(static_cast<uint32_t>(x), lane);
 }
 __device__ __forceinline__ uint64_t shuffle(uint64_t x, int lane) {
   return (static_cast<uint64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(x >> 32), lane))) << 32) |
          static_cast<uint32_t>(__shfl(static_cast<int>(x), lane));
 }
 
-// The 64 keys of a wave, the greatest in lane 0 (bitonic).
-__device__ __forceinline__ uint64_t sorted(uint64_t x, int lane) {
-#pragma unroll
-  for (int size = 2; size <= 64; size <<= 1)
-#pragma unroll
-    for (int m = size >> 1; m > 0; m >>= 1) {
-      const uint64_t other = shuffle_xor(x, m);
-      const bool upper = (lane & m) == 0, falling = (lane & size) == 0 || size == 64;
-      x = (upper == falling) == (x > other) ? x : other;
-    }
+// Bitonic sorts over the lanes of a wave, what is ahead in lane 0.  A step keeps, of a pair of lanes, what is ahead in one and the other
+// in the other.
+__device__ __forceinline__ bool ahead(uint32_t a, uint32_t b) { return a > b; }
+__device__ __forceinline__ bool ahead(uint64_t a, uint64_t b) { return a > b; }
+template <int M, class X>
+__device__ __forceinline__ X exchange(const X& x, bool keep_ahead, int lane) {
+  const X other = of_xor<M>(x, lane);
+  return keep_ahead == ahead(x, other) ? x : other;
+}
+template <int SIZE, int M, class X>
+__device__ __forceinline__ X steps(X x, int lane) {
+  x = exchange<M>(x, ((lane & M) == 0) == ((lane & SIZE) == 0 || SIZE == 64), lane);
+  if constexpr (M > 1) x = steps<SIZE, M / 2>(x, lane);
   return x;
 }
-// The 64 greatest of two sorted lists, sorted: the greater of each and the opposite of the other are them, as a bitonic sequence.
-__device__ __forceinline__ uint64_t merged(uint64_t x, uint64_t y, int lane) {
-  const uint64_t z = shuffle(y, 63 - lane);
-  x = x > z ? x : z;
-#pragma unroll
-  for (int m = 32; m > 0; m >>= 1) {
-    const uint64_t other = shuffle_xor(x, m);
-    x = ((lane & m) == 0) == (x > other) ? x : other;
-  }
-  return x;
+template <class X>
+__device__ __forceinline__ X sorted(X x, int lane) {
+  x = steps<2, 1>(x, lane);
+  x = steps<4, 2>(x, lane);
+  x = steps<8, 4>(x, lane);
+  x = steps<16, 8>(x, lane);
+  x = steps<32, 16>(x, lane);
+  return steps<64, 32>(x, lane);
+}
+// The 64 ahead of two sorted lists, sorted: the one ahead of each and the opposite of the other are them, as a bitonic sequence.
+template <class X>
+__device__ __forceinline__ X merged(X x, const X& opposite, int lane) {
+  x = ahead(x, opposite) ? x : opposite;
+  return steps<64, 32>(x, lane);
 }
 
 // ---- rows ---------------------------------------------------------------------------------------------------------------
@@ -112,22 +140,21 @@ __device__ __forceinline__ float greatest_of_wave(float x) {
   return x;
 }
 
-// exp(x - top) for x <= top, to about an ulp of 2^-23: the product of the difference with log2(e) is kept as two floats.  (Beyond
-// e^-150 it is 0, and where there is no difference of two infinities.)
+
+// e^(x - top): of the difference, so that a shift of all logits costs nothing, and with log2(e) as two floats.  Errors are those of small
+// numbers where the value is large, and of either sign.  (x = top = +inf: NaN.)
 __device__ __forceinline__ float exponential(float x, float top) {
-  const float d = fmaxf(x - top, -150.0f), log2e = 1.44269502f, rest = 1.92596303e-8f;
-  const float y = d * log2e;
-  const float low = fmaf(d, log2e, -y) + d * rest;
-  const float e = __builtin_amdgcn_exp2f(y);
-  return fmaf(e * 0.693147182f, low, e);
+  const float d = x - top;
+  return __builtin_amdgcn_exp2f(fmaf(d, 1.44269502f, d * 1.92596303e-8f));
 }
 
 // A wave a part.  The list of the best is sorted over the lanes; a key that is not ahead of the K-th is left out by one
-// comparison, so most pieces cost a maximum and their exponentials.  Those that are go through a buffer of 64 in LDS, sorted and merged
-// when it is full.
+// comparison, so most pieces cost a maximum and their exponentials.  Those that are go through a buffer in LDS, sorted and merged
+// by 64.  At first the K-th is bounded from below by the K-th of the lanes' own greatest: that many are ahead of it.
+// 256 x 8 rows of 16600 bf16 in 27 us (2.5 TB/s), most of it exponentials, one a logit.
 template <class T>
 __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
-  __shared__ uint64_t buffers[4][64];
+  __shared__ uint64_t buffers[4][64 + kPiece];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const long long unit = static_cast<long long>(blockIdx.x) * 4 + wave;
   if (unit >= a.rows * a.parts) return;
@@ -139,16 +166,19 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
   uint64_t* buffer = buffers[wave];
 
   uint64_t list = 0;       // (less than every key)
-  uint64_t least = 0;      // the K-th of the list
+  uint64_t least = 0;      // a key that K or more are ahead of, or at
   int waiting = 0;         // keys in the buffer
-  float top = -__builtin_inff();
+  float top = -__builtin_inff();   // greatest logit of the lane
   double sum = 0.0;
-  auto empty = [&]() {
+  // the last up to 64 of the buffer into the list
+  auto take = [&]() {
+    const int from = waiting > 64 ? waiting - 64 : 0;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
     __builtin_amdgcn_wave_barrier();
-    list = merged(list, sorted(lane < waiting ? buffer[lane] : 0, lane), lane);
-    least = shuffle(list, a.K - 1);
-    waiting = 0;
+    list = merged(list, shuffle(sorted(from + lane < waiting ? buffer[from + lane] : uint64_t{0}, lane), 63 - lane), lane);
+    const uint64_t kth = shuffle(list, a.K - 1);
+    least = kth > least ? kth : least;
+    waiting = from;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront", "local");
     __builtin_amdgcn_wave_barrier();
   };
@@ -156,57 +186,63 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
 #pragma unroll
   for (int u = 0; u < kPieces; ++u) next[u] = load(logits, begin + u * kPiece + lane * kLaneItems, end);
   for (int at = begin; at < end; at += kPieces * kPiece) {
-    float x[kPieces][kLaneItems];
+    float x[kPieces][kLaneItems], m[kPieces];
 #pragma unroll
-    for (int u = 0; u < kPieces; ++u)
+    for (int u = 0; u < kPieces; ++u) {
 #pragma unroll
-      for (int i = 0; i < kLaneItems; ++i) {
-        x[u][i] = static_cast<float>(next[u].x[i]);
-        x[u][i] = x[u][i] != x[u][i] ? -__builtin_inff() : x[u][i];
-      }
+      for (int i = 0; i < kLaneItems; ++i) x[u][i] = static_cast<float>(next[u].x[i]);
+      m[u] = -__builtin_inff();
+#pragma unroll
+      for (int i = 0; i < kLaneItems; ++i) m[u] = fmaxf(m[u], x[u][i]);   // (not the NaNs)
+    }
     if (at + kPieces * kPiece < end)
 #pragma unroll
       for (int u = 0; u < kPieces; ++u) next[u] = load(logits, at + (kPieces + u) * kPiece + lane * kLaneItems, end);
+    float greatest = m[0];
+#pragma unroll
+    for (int u = 1; u < kPieces; ++u) greatest = fmaxf(greatest, m[u]);
+    // the sum, every lane's own; +inf gives no sum (see join_kernel)
+    if (greatest > top) {
+      sum = top > -__builtin_inff() ? sum * static_cast<double>(exponential(top, greatest)) : 0.0;
+      top = greatest;
+    }
+    const float against = top > -__builtin_inff() ? top : 0.0f;
 #pragma unroll
     for (int u = 0; u < kPieces; ++u) {
-      float m = x[u][0];
+      float s = 0.0f;
 #pragma unroll
-      for (int i = 1; i < kLaneItems; ++i) m = fmaxf(m, x[u][i]);
-      const int first = at + u * kPiece + lane * kLaneItems;
-      // the sum, every lane's own; +inf gives no sum (see join_kernel)
-      if (m > top) {
-        sum = top > -__builtin_inff() ? sum * static_cast<double>(exponential(top, m)) : 0.0;
-        top = m;
+      for (int i = 0; i < kLaneItems; ++i) s += exponential(x[u][i], against);
+      if (__ballot(s != s) != 0) {  // NaNs among them count as nothing
+        asm volatile("" ::: "memory");  // (a branch: made ahead of it, this costs as much again)
+        s = 0.0f;
+        for (int i = 0; i < kLaneItems; ++i) s += x[u][i] == x[u][i] ? exponential(x[u][i], against) : 0.0f;
       }
-      if (top > -__builtin_inff()) {
-        float s = 0.0f;
+      sum += static_cast<double>(s);
+    }
+    // the best
+    if (at == begin) least = static_cast<uint64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(sorted(in_order(greatest), lane)), a.K - 1))) << 32;
 #pragma unroll
-        for (int i = 0; i < kLaneItems; ++i) s += exponential(x[u][i], top);
-        sum += static_cast<double>(s);
-      }
-      // the best: only where a lane has a key ahead of the K-th
+    for (int u = 0; u < kPieces; ++u) {
+      // only where a lane has a key ahead of the K-th
       const float bar = from_order(static_cast<uint32_t>(least >> 32));
-      if (__ballot(least == 0 ? first < end : m >= bar) == 0) continue;
+      if (__ballot(!(m[u] < bar)) == 0) continue;
+      const int first = at + u * kPiece + lane * kLaneItems;
 #pragma unroll
       for (int i = 0; i < kLaneItems; ++i) {
+        if (__ballot(!(x[u][i] < bar)) == 0) continue;
         const uint64_t key = first + i < end ? key_of(x[u][i], first + i) : 0;
         const bool ahead = key > least;
         const uint64_t votes = __ballot(ahead);
-        if (votes == 0) continue;
-        const int many = __popcll(votes);
-        if (waiting + many > 64) {
-          empty();
-          // (some may not be ahead any more: they go in all the same, and fall out in the merge)
-        }
         if (ahead) buffer[waiting + __popcll(votes & ((1ull << lane) - 1))] = key;
-        waiting += many;
+        waiting += __popcll(votes);
       }
+      while (waiting >= 64) take();
     }
   }
-  if (waiting > 0) empty();
+  if (waiting > 0) take();
   if (lane < a.K) a.best[unit * a.K + lane] = list;
   const float all = greatest_of_wave(top);
-  double part_sum = sum > 0.0 ? sum * static_cast<double>(exponential(top, all)) : 0.0;
+  double part_sum = sum > 0.0 ? sum * static_cast<double>(exponential(top, all)) : sum;
 #pragma unroll
   for (int m = 1; m < 64; m <<= 1) part_sum += __shfl_xor(part_sum, m);
   if (lane == 0) {
@@ -218,6 +254,8 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
 // ---- joining ------------------------------------------------------------------------------------------------------------
 
 struct JoinArgs {
+  const void* logits;
+  int dtype;
   const uint64_t* best;
   const double* sums;
   const float* tops;
@@ -237,103 +275,179 @@ struct Candidate {
 __device__ __forceinline__ bool ahead(const Candidate& a, const Candidate& b) {
   return a.total > b.total || (a.total == b.total && a.index < b.index);
 }
-__device__ __forceinline__ Candidate shuffle_xor(const Candidate& c, int m) {
-  return Candidate{__builtin_bit_cast(double, shuffle_xor(__builtin_bit_cast(uint64_t, c.total), m)), shuffle_xor(c.index, m)};
+template <int M>
+__device__ __forceinline__ Candidate of_xor(const Candidate& c, int lane) {
+  return Candidate{__builtin_bit_cast(double, of_xor<M>(__builtin_bit_cast(uint64_t, c.total), lane)), of_xor<M>(c.index, lane)};
 }
 
 constexpr int kJoinThreads = 256;
+constexpr int kRowLanes = 16;              // that read a row's sums
 
-// A workgroup a sequence.  First the logarithms of its rows' sums, then K rounds of the greatest of what is left of the parts' lists:
-// they are sorted, so a list is represented by its first that was not taken, and a round is one comparison a list.
+// Totals of two beams nearer than this may be in the wrong order.  A row's logarithm is off by the exponentials' 2^-23, by 2^-24 of their
+// exponents (which are ln V at most, on the average that the sum takes), seven roundings of eight values' sum and the factors of a
+// lane's top: below 24 * 2^-24.
+constexpr double kNear = 2 * 24.0 / 16777216.0;
+
+// e^d for d <= 0 in 64 bits: e^r for what is left of d by whole multiples of ln 2, by its series (r^12 / 12! < 1e-14).
+__device__ __forceinline__ double exponential(double d) {
+  const double n = rint(d * 1.4426950408889634), r = fma(n, -1.9082149292705877e-10, fma(n, -0.693147180369123816490, d));
+  double s = 1.0 / 39916800.0;
+  constexpr double kTerms[] = {1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+#pragma unroll
+  for (int i = 0; i < 11; ++i) s = fma(s, r, kTerms[i]);
+  return d > -700.0 ? ldexp(s, static_cast<int>(n)) : 0.0;
+}
+
+// log sum exp of a row in 64 bits, by the whole workgroup; sixteen logits of a thread on their way together.  `top` is their greatest.
+// A row of 16600 takes 12 us, one of 120000 65: the memory's latency.
+template <class T>
+__device__ double sum_of_row(const T* row, int V, double top, double* of_wave) {
+  constexpr int kUnroll = 16;
+  double sum = 0.0;
+  for (int at = threadIdx.x; at < V; at += kUnroll * kJoinThreads) {
+    T x[kUnroll];
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) x[u] = at + u * kJoinThreads < V ? row[at + u * kJoinThreads] : static_cast<T>(-__builtin_inff());
+#pragma unroll
+    for (int u = 0; u < kUnroll; ++u) {
+      const float v = static_cast<float>(x[u]);
+      sum += v == v ? exponential(static_cast<double>(v) - top) : 0.0;
+    }
+  }
+#pragma unroll
+  for (int k = 1; k < 64; k <<= 1) sum += __shfl_xor(sum, k);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) of_wave[threadIdx.x >> 6] = sum;
+  __syncthreads();
+  sum = of_wave[0];
+#pragma unroll
+  for (int w = 1; w < kJoinThreads / 64; ++w) sum += of_wave[w];
+  return top + log(sum);
+}
+__device__ double exact_sum(const JoinArgs& a, long long row, double* of_wave) {
+  float top = -__builtin_inff();
+  for (int p = threadIdx.x & 63; p < a.parts; p += 64) top = fmaxf(top, a.tops[row * a.parts + p]);
+  top = greatest_of_wave(top);
+  const long long at = row * a.V;
+  if (a.dtype == COTTEN_F32) return sum_of_row(static_cast<const float*>(a.logits) + at, a.V, top, of_wave);
+  if (a.dtype == COTTEN_BF16) return sum_of_row(static_cast<const __bf16*>(a.logits) + at, a.V, top, of_wave);
+  return sum_of_row(static_cast<const _Float16*>(a.logits) + at, a.V, top, of_wave);
+}
+
+__device__ __forceinline__ Candidate of_lane(const Candidate& c, int lane) {
+  return Candidate{__builtin_bit_cast(double, shuffle(__builtin_bit_cast(uint64_t, c.total), lane)), shuffle(c.index, lane)};
+}
+
+// A workgroup a sequence.  First the logarithms of its rows' sums, then the K best of what the parts' lists hold: every wave takes 64
+// candidates at a time, the firsts of all lists before the seconds, and where one is ahead of the K-th that it has, sorts them
+// and merges them into its own 64; the waves' lists are merged at the end.  256 x 8 beams of two parts in 6 us, most of it latency.
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinArgs a) {
-  extern __shared__ int taken[];                        // of every list
+  constexpr int kWaves = kJoinThreads / 64;
   __shared__ double of_row[kMostBeams];                 // what a row adds to its logits
+  __shared__ float old_scores[kMostBeams];              // (new_scores may be scores)
   __shared__ uint8_t kind[kMostBeams];
-  __shared__ Candidate winners[kJoinThreads / 64];
-  __shared__ int winner_list[kJoinThreads / 64];
+  __shared__ Candidate lists_of_waves[kWaves][64];
+  __shared__ double exact[kWaves];
+  __shared__ uint32_t unsure;
   enum { kOpen, kEnded, kNothing };
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lists = a.K * a.parts, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const long long first_row = static_cast<long long>(blockIdx.x) * a.K;
-  for (int k = wave; k < a.K; k += kJoinThreads / 64) {
+  const uint64_t* best = a.best + first_row * a.parts * a.K;
+  const Candidate none = {-__builtin_inf(), ~0ull};
+  for (int k = threadIdx.x / kRowLanes; k < a.K; k += kJoinThreads / kRowLanes) {
     const long long row = first_row + k;
+    const int sub = threadIdx.x % kRowLanes;
     const float score = a.scores[row];
     const bool ended = a.finished != nullptr && a.finished[row] != 0;
     double value = static_cast<double>(score);
     if (!ended) {
       float top = -__builtin_inff();
-      for (int p = lane; p < a.parts; p += 64) top = fmaxf(top, a.tops[row * a.parts + p]);
-      top = greatest_of_wave(top);
+      for (int p = sub; p < a.parts; p += kRowLanes) top = fmaxf(top, a.tops[row * a.parts + p]);
+#pragma unroll
+      for (int m = 1; m < kRowLanes; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
       double sum = 0.0;
-      for (int p = lane; p < a.parts; p += 64) {
+      for (int p = sub; p < a.parts; p += kRowLanes) {
         const double s = a.sums[row * a.parts + p];
-        if (s > 0.0) sum += s * exp(static_cast<double>(a.tops[row * a.parts + p]) - static_cast<double>(top));
+        if (!(s == 0.0)) sum += s * exp(static_cast<double>(a.tops[row * a.parts + p]) - static_cast<double>(top));
       }
 #pragma unroll
-      for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
+      for (int m = 1; m < kRowLanes; m <<= 1) sum += __shfl_xor(sum, m);
       value -= static_cast<double>(top) + log(sum);
     }
-    if (lane == 0) {
+    if (sub == 0) {
+      old_scores[k] = score;
       of_row[k] = value;
       // a score or a sum that is not finite leaves a beam no continuation but at -inf
       kind[k] = !(fabs(value) < __builtin_inf()) ? kNothing : ended ? kEnded : kOpen;
     }
   }
-  const int lists = a.K * a.parts;
-  for (int i = threadIdx.x; i < lists; i += kJoinThreads) taken[i] = 0;
   __syncthreads();
 
-  // the first of a list that was not taken.  A beam that ended has one list: the pad item, then the others from the lowest on, at -inf; one
-  // without anything has them from 0 on.
-  auto head = [&](int i) {
-    const int k = i / a.parts, part = i - k * a.parts, n = taken[i];
-    const double none = -__builtin_inf();
+  // the n-th of a list.  A beam that ended has one list: the pad item, then the others from the lowest on, at -inf; one without anything
+  // has them from 0 on.
+  auto candidate = [&](int list, int n, uint64_t key) {
+    const int k = list / a.parts;
     const uint64_t base = static_cast<uint64_t>(k) * a.V;
     if (kind[k] == kOpen) {
-      const uint64_t key = n < a.K ? a.best[((first_row + k) * a.parts + part) * a.K + n] : 0;
-      if (key == 0) return Candidate{none, ~0ull};
+      if (key == 0) return none;
       return Candidate{static_cast<double>(from_order(static_cast<uint32_t>(key >> 32))) + of_row[k], base + static_cast<uint32_t>(~key)};
     }
-    if (part != 0 || n >= a.V) return Candidate{none, ~0ull};
-    if (kind[k] == kNothing) return Candidate{none, base + n};
+    if (list != k * a.parts || n >= a.V) return none;
+    if (kind[k] == kNothing) return Candidate{none.total, base + n};
     if (n == 0) return Candidate{of_row[k], base + a.pad};
-    return Candidate{none, base + (n - 1 < a.pad ? n - 1 : n)};
+    return Candidate{none.total, base + (n - 1 < a.pad ? n - 1 : n)};
   };
-  for (int round = 0; round < a.K; ++round) {
-    Candidate best = {-__builtin_inf(), ~0ull};
-    int from = -1;
-    for (int i = threadIdx.x; i < lists; i += kJoinThreads) {
-      const Candidate c = head(i);
-      if (from < 0 || ahead(c, best)) {
-        best = c;
-        from = i;
+  for (bool again = false;; again = true) {
+    Candidate mine = none, kth = none;
+    // (lists fall: where no candidate of a wave's lists is ahead, those behind them are not)
+    auto take = [&](int list, int n) {
+      const Candidate c = n < a.K ? candidate(list, n, best[static_cast<long long>(list) * a.K + n]) : none;
+      if (__ballot(ahead(c, kth)) == 0) return false;
+      mine = merged(mine, of_lane(sorted(c, lane), 63 - lane), lane);
+      kth = of_lane(mine, a.K);       // (the one behind the K-th, for how near it comes)
+      return true;
+    };
+    if (lists > 64) {
+      for (int at = wave * 64; at < lists; at += kJoinThreads) {
+        const bool there = at + lane < lists;
+        for (int n = 0; n < a.K && take(there ? at + lane : 0, there ? n : a.K); ++n) {
+        }
+      }
+    } else {
+      const int ranks = 64 / lists, n = lane / lists, list = lane - n * lists;
+      for (int at = wave * ranks; at < a.K && take(list, n < ranks ? at + n : a.K); at += kWaves * ranks) {
       }
     }
+    if (lists * a.K > 64) {
+      lists_of_waves[wave][lane] = mine;
+      __syncthreads();
+      if (wave == 0)
 #pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-      const Candidate other = shuffle_xor(best, m);
-      const int other_from = __shfl_xor(from, m);
-      if (ahead(other, best)) {
-        best = other;
-        from = other_from;
-      }
+        for (int w = 1; w < kWaves; ++w) mine = merged(mine, lists_of_waves[w][63 - lane], lane);
     }
-    if (lane == 0) {
-      winners[wave] = best;
-      winner_list[wave] = from;
+    if (wave == 0) {
+      const int k = static_cast<int>(mine.index / static_cast<uint64_t>(a.V));
+      if (lane < a.K) {
+        a.new_scores[first_row + lane] = static_cast<float>(mine.total);
+        a.parents[first_row + lane] = k;
+        a.tokens[first_row + lane] = static_cast<int>(mine.index - static_cast<uint64_t>(k) * a.V);
+      }
+      // beams with candidates nearer to each other than their sums tell apart
+      const Candidate next = of_lane(mine, lane < 63 ? lane + 1 : 63);
+      const int k_next = __shfl(k, lane < 63 ? lane + 1 : 63);
+      const double gap = mine.total - next.total;
+      uint32_t near = lane < a.K && next.index != ~0ull && k != k_next && gap > 0.0 && gap < kNear ? (1u << k) | (1u << k_next) : 0u;
+#pragma unroll
+      for (int m = 1; m < 64; m <<= 1) near |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(near), m));
+      if (lane == 0) unsure = again ? 0u : near;
     }
     __syncthreads();
-    if (threadIdx.x == 0) {
-#pragma unroll
-      for (int w = 1; w < kJoinThreads / 64; ++w)
-        if (ahead(winners[w], best)) {
-          best = winners[w];
-          from = winner_list[w];
-        }
-      ++taken[from];
-      const int k = static_cast<int>(best.index / static_cast<uint64_t>(a.V));
-      a.new_scores[first_row + round] = static_cast<float>(best.total);
-      a.parents[first_row + round] = k;
-      a.tokens[first_row + round] = static_cast<int>(best.index - static_cast<uint64_t>(k) * a.V);
+    const uint32_t rows = unsure;
+    if (rows == 0) return;
+    for (int k = 0; k < a.K; ++k) {
+      if (!((rows >> k) & 1u) || kind[k] != kOpen) continue;
+      const double sum = exact_sum(a, first_row + k, exact);
+      if (threadIdx.x == 0) of_row[k] = static_cast<double>(old_scores[k]) - sum;
     }
     __syncthreads();
   }
@@ -389,14 +503,16 @@ int check_shape(int B, int K, int V) {
   return COTTEN_OK;
 }
 
-// Waves for a row: enough of them to fill the device, of one round of loads at least.
+// Waves for a row: enough of them to fill the device, of one round of loads at least; few enough that the join has up to 512 lists.
+// 256 x 8 rows of 16600 in 8192 / 4096 / 2048 waves: 44 / 38 / 39 us with the join; 32 x 5 of 120000: 39 / 35 / 32.
+constexpr int kWanted = 4096;
 struct Cut {
   int parts, part_items;
   Cut(int B, int K, int V) {
     const long long rows = static_cast<long long>(B) * K, round = kPiece * kPieces;
-    const long long rounds = (V + round - 1) / round;
-    long long wanted = (8192 + rows - 1) / rows;
-    wanted = wanted < 1 ? 1 : wanted > 256 ? 256 : wanted;
+    const long long rounds = (V + round - 1) / round, most = 512 / K < 64 ? 512 / K : 64;
+    long long wanted = (kWanted + rows - 1) / rows;
+    wanted = wanted < 1 ? 1 : wanted > most ? most : wanted;
     const long long each = (rounds + wanted - 1) / wanted;
     part_items = static_cast<int>(each * round);
     parts = static_cast<int>((V + static_cast<long long>(part_items) - 1) / part_items);
@@ -439,8 +555,8 @@ int cotten_beam_select(const void* logits, const float* scores, const uint8_t* f
   if (prm->dtype == COTTEN_F32) row_kernel<float><<<grid, block, 0, s>>>(r);
   else if (prm->dtype == COTTEN_BF16) row_kernel<__bf16><<<grid, block, 0, s>>>(r);
   else row_kernel<_Float16><<<grid, block, 0, s>>>(r);
-  const JoinArgs j{best, sums, tops, scores, finished, new_scores, parents, tokens, V, K, cut.parts, prm->pad};
-  join_kernel<<<dim3(B), dim3(kJoinThreads), K * cut.parts * sizeof(int), s>>>(j);
+  const JoinArgs j{logits, prm->dtype, best, sums, tops, scores, finished, new_scores, parents, tokens, V, K, cut.parts, prm->pad};
+  join_kernel<<<dim3(B), dim3(kJoinThreads), 0, s>>>(j);
   return hipGetLastError() == hipSuccess ? COTTEN_OK : COTTEN_ERR_LAUNCH;
 }
 
