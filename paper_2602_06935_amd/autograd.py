@@ -124,12 +124,13 @@ def gated_delta_attention(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: 
 class _Decay(torch.autograd.Function):
     @staticmethod
     def forward(ctx, Q, K, V, g, mask, scale, eps, initial_state, layout, return_state):
-        B, H, _, d = binding._dims(Q, layout)
+        ctx.dims = B, H, _, d = binding._dims(Q, layout)
         state = g.new_empty((B, H, d, d)) if return_state else None
         O = binding.cotten_decay_fwd(Q, K, V, g, mask, scale=scale, eps=eps, layout=layout, initial_state=initial_state,
                                      final_state=state)
         ctx.save_for_backward(Q, K, V, g, mask, initial_state)
-        ctx.call = dict(scale=scale, eps=eps, layout=layout)
+        ctx.call = (binding._dtype_code(Q), 0.0 if scale is None else scale, -1.0 if eps is None else eps,
+                    binding._LAYOUTS[layout])
         ctx.set_materialize_grads(False)
         return (O, state) if return_state else O
 
@@ -140,8 +141,8 @@ class _Decay(torch.autograd.Function):
         dO = torch.zeros_like(Q) if dO is None else _aligned(dO)
         dg = torch.empty_like(g) if ctx.needs_input_grad[3] else None
         dfirst = torch.empty_like(initial_state) if initial_state is not None and ctx.needs_input_grad[7] else None
-        grads = binding.cotten_decay_bwd(Q, K, V, g, mask, dO, dg=dg, initial_state=initial_state,
-                                         dfinal_state=None if dstate is None else _aligned(dstate), dinitial_state=dfirst, **ctx.call)
+        grads = binding._decay_backward_of(binding.CottenDecayParams(*ctx.call), ctx.dims, Q, K, V, g, mask, dO, initial_state,
+                                           None if dstate is None else _aligned(dstate), dfirst, dg)
         return (*grads, dg, None, None, None, dfirst, None, None)
 
 
@@ -220,13 +221,10 @@ class _ResidualNorm(torch.autograd.Function):
     @_first_derivatives_only
     def backward(ctx, dY, dH=None):
         X, F, post_weight, post_bias, gate, next_weight, next_bias, step = ctx.saved_tensors
-        norm, alpha, eps, p, seed, offset = ctx.call
         if dY is None and dH is None:
             return (None,) * 14
-        grads = binding.cotten_residual_bwd(X, F, None if dY is None else _aligned(dY), None if dH is None else _aligned(dH),
-                                            norm=norm, post_weight=post_weight, post_bias=post_bias, gate=gate, alpha=alpha,
-                                            next_weight=next_weight, next_bias=next_bias, eps=eps, p=p, seed=seed, offset=offset,
-                                            step=step, wanted=ctx.needs_input_grad[2:7])
+        grads = binding._residual_backward_of(ctx.call, X, F, None if dY is None else _aligned(dY), None if dH is None else _aligned(dH),
+                                              (post_weight, post_bias, gate, next_weight, next_bias), step, ctx.needs_input_grad[2:7])
         return (*grads, *(None,) * 7)
 
 

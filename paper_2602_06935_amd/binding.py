@@ -666,6 +666,27 @@ def cotten_decay_bwd(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, g: torch
     return dQ, dK, dV
 
 
+def _decay_backward_of(prm, dims, Q, K, V, g, mask, dO, initial_state, dfinal_state, dinitial_state, dg):
+    """The gradients of a forward call that has checked its tensors (the differentiable function's): `prm` holds its type,
+    scale, eps and layout, the rest of it is filled in here."""
+    handle = _stream_handle(None, Q.device)
+    need = cotten_decay_workspace_bytes(*dims, prm.dtype, True, dg is not None)
+    if need != 0:
+        workspace = _workspace(Q, need, handle)
+        prm.workspace, prm.workspace_bytes = workspace.data_ptr(), need
+    if initial_state is not None:
+        prm.initial_state = initial_state.data_ptr()
+    if dfinal_state is not None:
+        prm.dfinal_state = dfinal_state.data_ptr()
+    if dinitial_state is not None:
+        prm.dinitial_state = dinitial_state.data_ptr()
+    dQ, dK, dV = torch.empty_like(Q), torch.empty_like(Q), torch.empty_like(Q)
+    _on_device(Q.device, _lib.cotten_decay_bwd, Q.data_ptr(), K.data_ptr(), V.data_ptr(), g.data_ptr(),
+               None if mask is None else mask.data_ptr(), dO.data_ptr(), dQ.data_ptr(), dK.data_ptr(), dV.data_ptr(),
+               None if dg is None else dg.data_ptr(), *dims, handle, ctypes.byref(prm))
+    return dQ, dK, dV
+
+
 # ---- embedding of item ids -----------------------------------------------------------------------
 
 @functools.lru_cache(maxsize=1024)
@@ -913,6 +934,17 @@ def cotten_residual_bwd(X: torch.Tensor, F: torch.Tensor, dY: Optional[torch.Ten
                               (post_weight, post_bias, gate, next_weight, next_bias), wanted)
 
 
+def _residual_backward_of(call, X, F, dY, dH, vectors, step, wanted):
+    """The gradients of a forward call that has checked its tensors (the differentiable function's): `call` is its norm, alpha,
+    eps, p, seed and offset."""
+    norm, alpha, eps, p, seed, offset = call
+    gate = vectors[2]
+    prm = CottenResidualParams(_dtype_code(X), _NORMS[norm], *(None if t is None else t.data_ptr() for t in vectors),
+                               int(gate is not None and gate.dim() == 2), alpha, -1.0 if eps is None else eps, p, seed, offset,
+                               None if step is None else step.data_ptr())
+    return _residual_backward(prm, _stream_handle(None, X.device), None, X, F, dY, dH, vectors, wanted)
+
+
 def _residual_backward(prm, handle, workspace, X, F, dY, dH, vectors, wanted):
     """The call itself: everything but the workspace is checked."""
     if workspace is None:
@@ -956,21 +988,25 @@ def cotten_beam_select(logits: torch.Tensor, scores: torch.Tensor, *, finished: 
     B, K, V = logits.shape
     if max(B, K, V) > _MOST_INT or not 0 <= pad <= _MOST_INT:
         raise ValueError("sizes and pad must be numbers of 31 bits")
-    dev, shape = logits.device, logits.shape[:2]
-    new_scores = torch.empty_like(scores) if new_scores is None else new_scores
-    parents = torch.empty(shape, dtype=torch.int32, device=dev) if parents is None else parents
-    tokens = torch.empty(shape, dtype=torch.int32, device=dev) if tokens is None else tokens
-    dtype = _dtype_code(logits)
-    given = (_of_beams("scores", scores, torch.float32, shape, dev),
-             None if finished is None else _of_beams("finished", finished, torch.uint8, shape, dev),
-             _of_beams("new_scores", new_scores, torch.float32, shape, dev), _of_beams("parents", parents, torch.int32, shape, dev),
-             _of_beams("tokens", tokens, torch.int32, shape, dev))
+    dev, shape, dtype = logits.device, logits.shape[:2], _dtype_code(logits)
+    given = [_of_beams("scores", scores, torch.float32, shape, dev),
+             None if finished is None else _of_beams("finished", finished, torch.uint8, shape, dev)]
+    results = []
+    for name, t, of in (("new_scores", new_scores, torch.float32), ("parents", parents, torch.int32), ("tokens", tokens, torch.int32)):
+        if t is None:
+            t = torch.empty(shape, dtype=of, device=dev)
+            given.append(t.data_ptr())
+        else:
+            given.append(_of_beams(name, t, of, shape, dev))
+        results.append(t)
     handle = _stream_handle(stream, dev)
     if workspace is None:
         workspace = _workspace(logits, cotten_beam_workspace_bytes(B, K, V), handle)
-    prm = CottenBeamParams(dtype, pad, *_buffer("workspace", workspace, dev))
+        prm = CottenBeamParams(dtype, pad, workspace.data_ptr(), workspace.numel())
+    else:
+        prm = CottenBeamParams(dtype, pad, *_buffer("workspace", workspace, dev))
     _on_device(dev, lib.cotten_beam_select, logits.data_ptr(), *given, B, K, V, handle, ctypes.byref(prm))
-    return new_scores, parents, tokens
+    return tuple(results)
 
 
 def cotten_beam_reorder(state: torch.Tensor, parents: torch.Tensor, *, stream=None) -> torch.Tensor:

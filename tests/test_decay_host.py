@@ -92,7 +92,7 @@ def test_bindings_refuse():
 def stand_ins(monkeypatch):
     wanted = []
 
-    def decay_bwd(Q, K, V, g, mask, dO, *, dg=None, dinitial_state=None, **kw):
+    def decay_bwd(prm, dims, Q, K, V, g, mask, dO, initial_state, dfinal_state, dinitial_state, dg):
         wanted.append((dg is not None, dinitial_state is not None, dO.data_ptr() % 16))
         for t in (dg, dinitial_state):
             if t is not None:
@@ -100,7 +100,7 @@ def stand_ins(monkeypatch):
         return tuple(torch.ones_like(Q) for _ in range(3))
 
     monkeypatch.setattr(binding, "cotten_decay_fwd", lambda Q, *a, **kw: Q.detach() + 1.0)
-    monkeypatch.setattr(binding, "cotten_decay_bwd", decay_bwd)
+    monkeypatch.setattr(binding, "_decay_backward_of", decay_bwd)
     return wanted
 
 

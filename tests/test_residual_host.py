@@ -118,7 +118,7 @@ def test_bindings_refuse():
 def test_second_derivatives_raise(monkeypatch):
     monkeypatch.setattr(binding, "cotten_dropout", lambda x, p, **kw: x.detach() * 2.0)
     monkeypatch.setattr(binding, "cotten_residual_fwd", lambda X, F, **kw: (X.detach() + F.detach(), X.detach() + 1.0))
-    monkeypatch.setattr(binding, "cotten_residual_bwd", lambda X, F, dY, dH, **kw: (torch.ones_like(X), torch.ones_like(F), *(None,) * 5))
+    monkeypatch.setattr(binding, "_residual_backward_of", lambda call, X, F, *a: (torch.ones_like(X), torch.ones_like(F), *(None,) * 5))
     for run in (lambda x: autograd.dropout(x, 0.5, seed=1), lambda x: autograd.residual_norm(x, x * 2.0)[0]):
         x = torch.randn(2, 3, 8, requires_grad=True)
         y = run(x)
