@@ -398,13 +398,13 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinArgs a) {
     return Candidate{none.total, base + (n - 1 < a.pad ? n - 1 : n)};
   };
   for (bool again = false;; again = true) {
-    Candidate mine = none, kth = none;
+    Candidate mine = none, bar = none;       // what a candidate has to be ahead of: the K-th, or as near behind it as sums may be off
     // (lists fall: where no candidate of a wave's lists is ahead, those behind them are not)
     auto take = [&](int list, int n) {
       const Candidate c = n < a.K ? candidate(list, n, best[static_cast<long long>(list) * a.K + n]) : none;
-      if (__ballot(ahead(c, kth)) == 0) return false;
+      if (__ballot(ahead(c, bar)) == 0) return false;
       mine = merged(mine, of_lane(sorted(c, lane), 63 - lane), lane);
-      kth = of_lane(mine, a.K);       // (the one behind the K-th, for how near it comes)
+      bar = Candidate{of_lane(mine, a.K - 1).total - kNear, ~0ull};
       return true;
     };
     if (lists > 64) {
@@ -432,11 +432,11 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinArgs a) {
         a.parents[first_row + lane] = k;
         a.tokens[first_row + lane] = static_cast<int>(mine.index - static_cast<uint64_t>(k) * a.V);
       }
-      // beams with candidates nearer to each other than their sums tell apart
-      const Candidate next = of_lane(mine, lane < 63 ? lane + 1 : 63);
-      const int k_next = __shfl(k, lane < 63 ? lane + 1 : 63);
-      const double gap = mine.total - next.total;
-      uint32_t near = lane < a.K && next.index != ~0ull && k != k_next && gap > 0.0 && gap < kNear ? (1u << k) | (1u << k_next) : 0u;
+      // beams with candidates nearer to each other, or to the last that is taken, than their sums tell apart
+      const int before = lane < a.K ? (lane > 0 ? lane - 1 : 0) : a.K - 1;
+      const double gap = of_lane(mine, before).total - mine.total;
+      const int k_before = __shfl(k, before);
+      uint32_t near = mine.index != ~0ull && k != k_before && gap > 0.0 && gap < kNear ? (1u << k) | (1u << k_before) : 0u;
 #pragma unroll
       for (int m = 1; m < 64; m <<= 1) near |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(near), m));
       if (lane == 0) unsure = again ? 0u : near;

@@ -13,7 +13,8 @@ extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
 // ---- token by token -----------------------------------------------------------------------------------------------
 //
 // A wave carries up to 32 columns of a state in registers, eight lanes to a row of 128 bytes, the rows dealt to the lane groups;
-// q^ . S is a sum over the groups by lane permutes.  One token is bound by the state, read and written once.
+// q^ . S is a sum over the groups by lane permutes.  One token is bound by the state, read and written once: 4096 x 2 states of 64 x 64
+// in 40.6 us, 6.6 TB/s (the memory-side cache helps); 512 x 4 in 9.6.
 template <class E, int D>
 __global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
   constexpr int kCols = D < 32 ? D : 32;         // columns of a wave
@@ -188,12 +189,16 @@ hipError_t granted(Kernel kernel, int bytes) {
   return bytes > 64 * 1024 ? grant_dynamic_lds(reinterpret_cast<const void*>(kernel), bytes) : hipSuccess;
 }
 
-// Up to how many tokens the recurrence is as fast as a chunk of 32.
-constexpr int kMostSteps = 4;
+// Up to how many tokens the recurrence is as fast as a chunk of 32, which takes the same for any number of them.  us, recurrence / chunk:
+//   bf16 d = 64, 2048 slices  5 tokens 14.6 / 15.2, 6 16.8 / 15.5     fp16 d = 128, 512 slices  6 tokens 17.8 / 17.8, 8 21.5 / 17.4; 2048  8 57 / 67
+//   bf16 d = 16, 8192         5 tokens 14.6 / 15.5, 6 16.7 / 15.6     fp32 d = 128, 512  8 tokens 20.3 / 21.4, 12 26.1 / 21.7; 2048  12 66 / 76
+//   fp32 d = 32, 2048        12 tokens 11.3 / 12.4, 16 13.8 / 12.6; 8192  12 29.8 / 34.2, 16 36.2 / 34.1
+template <class E, int D>
+constexpr int kMostSteps = E::kBytes == 4 ? (D == 128 ? 10 : 12) : (D == 128 ? 6 : 5);
 
 template <class E, int D>
 hipError_t forward(const Args& a, int slices, hipStream_t s) {
-  if (a.N <= kMostSteps) {
+  if (a.N <= kMostSteps<E, D>) {
     constexpr int kParts = D < 32 ? 1 : D / 32;
     const long long waves = static_cast<long long>(slices) * kParts;
     const int of_block = waves > 4096 ? 4 : 1;

@@ -156,6 +156,26 @@ def test_candidates_that_nearly_tie(dtype, V, K):
     compare(logits, scores.cuda())
 
 
+def test_large_offsets():
+    """More than 2^32 bytes of logits, and of states: the last sequences, read and written behind them."""
+    B, K, V = 40, 32, 1_800_001
+    logits = torch.zeros(B, K, V, dtype=torch.float16, device="cuda")
+    assert logits.numel() > 2 ** 31
+    few, scores = draw(1, K, V, torch.float16, seed=2)
+    logits[-1] = few[0]
+    from paper_2602_06935_amd import binding
+    got = binding.cotten_beam_select(logits, scores.expand(B, K).contiguous())
+    best, parents, tokens = expected(few, scores)
+    assert torch.equal(got[1][-1:].cpu().long(), parents) and torch.equal(got[2][-1:].cpu().long(), tokens)
+    del logits, few
+    state = torch.zeros(3, 4, 180_000_001, dtype=torch.uint8, device="cuda")
+    state[:, :, -1] = torch.arange(4, dtype=torch.uint8, device="cuda")
+    state = state.view(3, 4, -1)
+    turn = torch.tensor([[3, 2, 1, 0]] * 3, dtype=torch.int32, device="cuda")
+    binding.cotten_beam_reorder(state, turn)
+    assert torch.equal(state[:, :, -1].cpu(), turn.cpu().to(torch.uint8)) and not state[:, :, :-1].any()
+
+
 def test_scores_in_place_and_runs_alike():
     from paper_2602_06935_amd import binding
     logits, scores = draw(40, 8, 9001, torch.bfloat16, seed=5)

@@ -61,7 +61,7 @@ def compare(x, layout="bhnd", scale=1.0, grads=True):
 
 
 # lengths around those of the recurrence, of a chunk and of two
-@pytest.mark.parametrize("N", [1, 2, 4, 5, 31, 32, 33, 63, 65, 100])
+@pytest.mark.parametrize("N", [1, 2, 5, 6, 7, 10, 11, 12, 13, 31, 32, 33, 63, 65, 100])
 @pytest.mark.parametrize("d", [16, 32, 64, 128])
 @pytest.mark.parametrize("dtype", list(DTYPES))
 def test_lengths(dtype, d, N):
@@ -244,6 +244,28 @@ def test_gradients_against_differences():
         # 6500 outputs of size 1, off by a few 2^-24 each, times upstream values, over the step; and the third derivative
         room = (6528 ** 0.5 * 2.0 ** -24 * 8) / h + 4 * h * h * max(1.0, got[of].cpu().double().norm().item())
         assert abs(slope - want) <= room, (n, slope, want)
+
+
+def test_large_offsets():
+    """Tensors of more than 2^32 bytes: the last sequences are as they are by themselves."""
+    from paper_2602_06935_amd import binding
+    x = inputs(2, 3, 300, 128, torch.float32, seed=21, mask="left")
+    B = 9500
+    big = {n: torch.zeros(B, 300, 3, 128, device="cuda") for n in ("q", "k", "v", "dO")}
+    assert big["q"].numel() * 4 > 2 ** 32
+    for n, t in big.items():
+        t[-2:] = lay(x[n], "bnhd")
+    mask = torch.ones(B, 300, dtype=torch.uint8, device="cuda")
+    mask[-2:] = x["mask"].cuda()
+    g = x["g"].cuda()
+    O, S1 = forward(x, "bnhd")
+    got = binding.cotten_decay_fwd(big["q"], big["k"], big["v"], g, mask, layout="bnhd")
+    assert torch.equal(back(got, "bnhd")[-2:], O)
+    del got
+    want = backward(x, "bnhd", decays=False)
+    grads = binding.cotten_decay_bwd(big["q"], big["k"], big["v"], g, mask, big["dO"], layout="bnhd")
+    for n, t in zip(NAMES, grads):
+        check(n, back(t, "bnhd")[-2:], want[n].cpu())
 
 
 def test_on_another_stream_and_with_a_given_workspace():

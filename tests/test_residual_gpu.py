@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from seam_reference import DTYPES, NAMES, check, factors, inputs, reference
+from seam_reference import DTYPES, LOW, NAMES, check, factors, inputs, philox, reference
 
 pytestmark = pytest.mark.gpu
 
@@ -200,6 +200,31 @@ def test_gradients_against_differences():
         # fp32 roundings of 1920 values of size 1, times upstream values, over the step; and the third derivative
         room = (1920 ** 0.5 * 2.0 ** -24 * 4) / h + 64 * h * h
         assert abs(slope - want) <= room, (n, slope, want)
+
+
+def test_large_offsets():
+    """More than 2^32 elements dropped, and more than 2^32 bytes of rows: the last ones, and their numbers."""
+    from paper_2602_06935_amd import binding
+    n = 2 ** 32 + 12345
+    x = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    binding.cotten_dropout(x, 0.25, seed=5, offset=1, out=x)
+    first = 2 ** 32 - 40000 + 40000 % 8
+    group = torch.arange(first // 8, (n + 7) // 8).tolist()
+    words = [philox([g & LOW, g >> 32, 1, 0], (5, 0)) for g in group[-200:]]
+    lots = [h for w in words for c in w for h in (c & 0xffff, c >> 16)]
+    at = group[-200] * 8
+    want = torch.tensor([4 / 3 if h >= 16384 else 0.0 for h in lots])[:n - at].to(torch.bfloat16)
+    assert torch.equal(x[at:].cpu(), want)
+    del x
+    X = torch.zeros(1100, 1000, 2040, dtype=torch.bfloat16, device="cuda")
+    assert X.numel() > 2 ** 31
+    X[-1, -1] = torch.randn(2040, device="cuda").to(torch.bfloat16)
+    weight = torch.ones(2040, dtype=torch.bfloat16, device="cuda")
+    Y, H = binding.cotten_residual_fwd(X, X, X, next_weight=weight, alpha=1.0)
+    small = torch.zeros(1, 1, 2040, dtype=torch.bfloat16, device="cuda")
+    small[0, 0] = Y[-1, -1] / 2
+    again = binding.cotten_residual_fwd(small, small, next_weight=weight)
+    assert torch.equal(Y[-1:, -1:], again[0]) and torch.equal(H[-1:, -1:], again[1])
 
 
 def test_runs_are_alike():
