@@ -90,6 +90,14 @@ __global__ __launch_bounds__(64 * kWaves<D>, (kRoom<E, D, ROLE == kDecays>)) voi
   walk<E, D, ROLE>(a, blockIdx.x, smem);
 }
 
+// d = 128: two workgroups of four waves a unit, half of the columns each, eight apart for the same reason as the roles below.  Each loads all
+// rows, but a wave has the registers of a SIMD to itself (eight waves, two a SIMD, spill 89 of fp32's), and nobody waits for eight.
+template <class E, int D, int ROLE>
+__global__ __launch_bounds__(64 * kWaves<D> / 2) void halves_kernel(Args a, int units) {
+  const int turn = blockIdx.x / 16, rest = blockIdx.x % 16, unit = turn * 8 + rest % 8;
+  if (unit < units) walk<E, D, ROLE, 2>(a, unit, smem, rest / 8);
+}
+
 // The backward's walks as roles of one launch.  Workgroups go to the eight XCDs in turn: the roles of a unit are eight apart,
 // so they find each other's rows in one L2.
 template <class E, int D>
@@ -196,6 +204,27 @@ hipError_t granted(Kernel kernel, int bytes) {
 template <class E, int D>
 constexpr int kMostSteps = E::kBytes == 4 ? (D == 128 ? 10 : 12) : (D == 128 ? 6 : 5);
 
+// The decays' walk.  At d = 128 as halves where both find a compute unit of their own: the backward of 128 slices of 197 tokens takes 97 us
+// that way and 106 with eight waves in fp16, 75 and 77 in bf16; of 256 slices, two rounds, 160 and 139, 122 and 100.  fp32's are halves at any
+// number: 128 slices 121 and 152, 256 slices 200 and 212, 1024 slices 798 and 849, 64 slices of 2048 tokens 685 and 946 (at 192 slices no faster).
+// (The forward walk was tried as well: 1 us faster up to 128 slices, 4 to 20 % slower in segments.)
+template <class E, int D>
+hipError_t launch_decays(const Args& a, int units, hipStream_t s) {
+  constexpr int kBytes = kLds<E, D, kDecays>, kMostHalved = D != 128 ? 0 : E::kBytes == 4 ? 0x7fffffff : 128;
+  if constexpr (kMostHalved > 0) {
+    if (units <= kMostHalved) {
+      if (hipError_t rc = granted(halves_kernel<E, D, kDecays>, kBytes)) return rc;
+      halves_kernel<E, D, kDecays><<<dim3(static_cast<unsigned>((units + 7) / 8) * 16u), dim3(32 * kWaves<D>), kBytes, s>>>(a, units);
+      return hipSuccess;
+    }
+  }
+  if constexpr (kMostHalved < 0x7fffffff) {
+    if (hipError_t rc = granted(walk_kernel<E, D, kDecays>, kBytes)) return rc;
+    walk_kernel<E, D, kDecays><<<dim3(static_cast<unsigned>(units)), dim3(64 * kWaves<D>), kBytes, s>>>(a);
+  }
+  return hipSuccess;
+}
+
 template <class E, int D>
 hipError_t forward(const Args& a, int slices, hipStream_t s) {
   if (a.N <= kMostSteps<E, D>) {
@@ -234,9 +263,7 @@ hipError_t backward(const Args& a, int slices, float* dg, hipStream_t s) {
   grad_kernel<E, D><<<dim3(static_cast<unsigned>((units + 7) / 8) * 24u), block, kBytes, s>>>(a, units);
   if (dg != nullptr) {
     // (a launch of its own: it needs the most registers, and would take them from the other roles)
-    constexpr int kOfDecays = kLds<E, D, kDecays>;
-    if (hipError_t rc = granted(walk_kernel<E, D, kDecays>, kOfDecays)) return rc;
-    walk_kernel<E, D, kDecays><<<dim3(units), block, kOfDecays, s>>>(a);
+    if (hipError_t rc = launch_decays<E, D>(a, units, s)) return rc;
     sum_decays_kernel<<<dim3(a.H), dim3(kSumThreads), 0, s>>>(a.dg, dg, slices / a.H, a.H, a.segments * kWaves<D>);
   }
   return hipGetLastError();

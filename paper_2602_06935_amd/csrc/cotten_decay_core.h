@@ -351,10 +351,12 @@ struct ResultRows {
   }
 };
 
-// The walk of one unit: a slice, or a segment of it.  Every wave carries 16 columns of the state; all load the chunk's rows (a wave 512 / D of
-// each tensor, eight elements a lane) and leave them in LDS in pieces.
-template <class E, int D, int ROLE>
-__device__ void walk(const Args& a, int unit, unsigned char* smem) {
+// The walk of one unit: a slice, or a segment of it.  Every wave carries 16 columns of the state; all load the chunk's rows (eight
+// elements a lane) and leave them in LDS in pieces.  GROUPS: workgroups that share the columns of a unit, each with all rows.
+template <class E, int D, int ROLE, int GROUPS = 1>
+__device__ void walk(const Args& a, int unit, unsigned char* smem, int part = 0) {
+  static_assert(GROUPS == 1 || !Traits<ROLE>::kThrough, "sums over all columns are a workgroup's");
+  constexpr int kWavesHere = kWaves<D> / GROUPS, kRowsOfPass = kWavesHere * (512 / D);
   typedef Traits<ROLE> R;
   typedef Place<E, D, R::kRows> P;
   typedef typename P::R L;
@@ -365,7 +367,7 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
   const double rate = rate_of(s.g);
   int begin = segment * a.segment_chunks;
   const int end = begin + a.segment_chunks < a.chunks ? begin + a.segment_chunks : a.chunks;
-  const int col = 16 * wave + (lane & 15), group = lane >> 4;
+  const int tile = part * kWavesHere + wave, col = 16 * tile + (lane & 15), group = lane >> 4;
   const long long of_slice = static_cast<long long>(slice) * a.segments;
   const long long state_at = static_cast<long long>(slice) * D * D;
   float* of_x = reinterpret_cast<float*>(smem + P::kOfX);
@@ -376,9 +378,9 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
   Powers* powers = reinterpret_cast<Powers*>(smem + P::kPowers);
   unsigned char* pairs = smem + P::kBytes;
   if (D < 32)  // narrow rows are followed by zeros
-    for (int i = threadIdx.x; i < P::kOfX / 16; i += 64 * kWaves<D>) reinterpret_cast<f32x4_t*>(smem)[i] = f32x4_t{0, 0, 0, 0};
+    for (int i = threadIdx.x; i < P::kOfX / 16; i += 64 * kWavesHere) reinterpret_cast<f32x4_t*>(smem)[i] = f32x4_t{0, 0, 0, 0};
   if (R::kRows)  // so are the pairs that give each other nothing
-    for (int i = threadIdx.x; i < kPairBytes<kOf> / 16; i += 64 * kWaves<D>) reinterpret_cast<f32x4_t*>(pairs)[i] = f32x4_t{0, 0, 0, 0};
+    for (int i = threadIdx.x; i < kPairBytes<kOf> / 16; i += 64 * kWavesHere) reinterpret_cast<f32x4_t*>(pairs)[i] = f32x4_t{0, 0, 0, 0};
   if (wave == 0) set_powers(powers, rate, lane);
   lds_barrier();
 
@@ -416,8 +418,9 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
       unsigned char* to = ROLE == kOut ? a.O : ROLE == kDq ? a.dQ : ROLE == kDk ? a.dK : a.dV;
       for (int c = begin; c < from; ++c) {
         const __amdgpu_buffer_rsrc_t r = s.of(to, c, a.stride_row);
-        E::store_four(r, off, f32x4_t{0, 0, 0, 0});
-        E::store_four(r, off + 4 * E::kBytes, f32x4_t{0, 0, 0, 0});
+        // (of the columns' groups, each its share of the rows)
+        E::store_four(r, off + part * kRowsOfPass * a.stride_row, f32x4_t{0, 0, 0, 0});
+        E::store_four(r, off + part * kRowsOfPass * a.stride_row + 4 * E::kBytes, f32x4_t{0, 0, 0, 0});
       }
     }
     begin = from;
@@ -425,17 +428,21 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
 
   Mask mask(a, s);
   uint32_t live = 0, there = 0;
-  typename E::Raw rx, ry, rz;
+  typename E::Raw rx[GROUPS], ry[GROUPS], rz[GROUPS];   // by passes over the chunk's rows
   ResultRows<E> own;                        // rows of Q or K (through their norm), or of dO (decays)
-  const uint32_t own_off = static_cast<uint32_t>(lane & 15) * a.stride_row + (16 * wave + 4 * group) * E::kBytes;
+  const uint32_t own_off = static_cast<uint32_t>(lane & 15) * a.stride_row + (16 * tile + 4 * group) * E::kBytes;
   auto fetch = [&](int chunk) {
     live = mask.bits(chunk);
     there = existing(a.N, chunk);
-    // forwards the mask is that of Y and Z, back that of X
-    const uint32_t at_x = R::kBack ? offset_if(live, row, off) : off, at_yz = R::kBack ? off : offset_if(live, row, off);
-    if constexpr (R::kRows) rx = E::load(s.of(R::x(a), chunk, a.stride_row), at_x);
-    ry = E::load(s.of(R::y(a), chunk, a.stride_row), at_yz);
-    rz = E::load(s.of(R::z(a), chunk, a.stride_row), at_yz);
+#pragma unroll
+    for (int i = 0; i < GROUPS; ++i) {
+      // forwards the mask is that of Y and Z, back that of X
+      const uint32_t here = off + i * kRowsOfPass * a.stride_row, masked = offset_if(live, row + i * kRowsOfPass, here);
+      const uint32_t at_x = R::kBack ? masked : here, at_yz = R::kBack ? here : masked;
+      if constexpr (R::kRows) rx[i] = E::load(s.of(R::x(a), chunk, a.stride_row), at_x);
+      ry[i] = E::load(s.of(R::y(a), chunk, a.stride_row), at_yz);
+      rz[i] = E::load(s.of(R::z(a), chunk, a.stride_row), at_yz);
+    }
   };
   const int step = R::kBack ? -1 : 1, first = R::kBack ? end - 1 : begin, last = R::kBack ? begin : end - 1;
   const int walked = end - begin;           // (may be none)
@@ -444,7 +451,7 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     fetch(first);
     if (first != last) mask.fetch(first + step, lane);
   }
-  Decays<R, kWaves<D>> decays;
+  Decays<R, kWavesHere> decays;
   decays.begin(powers, wave, lane);
   float count = 0.0f;
   double sum = 0.0;
@@ -476,32 +483,33 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     const uint32_t now = live, now_there = there;
     // where no token counts, forwards nothing is added to the state, and back there are no rows
     const bool dead = now == 0, with_rows = !R::kBack || !dead, with_sums = R::kBack || !dead;
-    {
-      const int kb = (lane % kRowLanes) / 4, g = (lane % kRowLanes) % 4;
+#pragma unroll
+    for (int n = 0; n < GROUPS; ++n) {
+      const int kb = (lane % kRowLanes) / 4, g = (lane % kRowLanes) % 4, of = row + n * kRowsOfPass;
       float fx = 1.0f, fyz = 1.0f;
       if constexpr (R::kRows) {
         if (with_rows) {
-          L::put(smem + P::kX, row, kb, g, E::pieces(rx));
-          if constexpr (R::kUnitX) fx = inverse_norm<E, D>(rx, a.eps);
+          L::put(smem + P::kX, of, kb, g, E::pieces(rx[n]));
+          if constexpr (R::kUnitX) fx = inverse_norm<E, D>(rx[n], a.eps);
         }
       }
       if (with_sums) {
-        L::put(smem + P::kY, row, kb, g, E::pieces(ry));
-        L::put(smem + P::kZ, row, kb, g, E::pieces(rz));
-        fyz = inverse_norm<E, D>(R::kUnitY ? ry : rz, a.eps);
+        L::put(smem + P::kY, of, kb, g, E::pieces(ry[n]));
+        L::put(smem + P::kZ, of, kb, g, E::pieces(rz[n]));
+        fyz = inverse_norm<E, D>(R::kUnitY ? ry[n] : rz[n], a.eps);
       }
       if (R::kScaleX) fx *= a.scale;
       else fyz *= a.scale;
       const uint32_t in_x = R::kBack ? now : now_there, in_yz = R::kBack ? now_there : now;
-      const int p = upto(now, row), behind = __popc(now) - p;
-      fyz = ((in_yz >> row) & 1u) ? fyz : 0.0f;
+      const int p = upto(now, of), behind = __popc(now) - p;
+      fyz = ((in_yz >> of) & 1u) ? fyz : 0.0f;
       if (lane % kRowLanes == 0) {
         if (R::kRows) {
-          of_x[row] = ((in_x >> row) & 1u) ? fx : 0.0f;
-          to_state[row] = powers->hi[R::kBack ? behind : p];
+          of_x[of] = ((in_x >> of) & 1u) ? fx : 0.0f;
+          to_state[of] = powers->hi[R::kBack ? behind : p];
         }
-        of_pair[row] = fyz;
-        of_state[row] = fyz * powers->hi[R::kBack ? p : behind];
+        of_pair[of] = fyz;
+        of_state[of] = fyz * powers->hi[R::kBack ? p : behind];
       }
     }
     if (now != decays.live) {
@@ -517,7 +525,7 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     if constexpr (R::kThrough)
       if (i > 0) finish(c - step);
     Pieces<E::kPieces> z;
-    if (with_sums) z = L::column_operand(smem + P::kZ, wave, lane);
+    if (with_sums) z = L::column_operand(smem + P::kZ, tile, lane);
     // rows: 16 columns of this wave's (4g + r) of tokens 16 t + lane%16
     f32x4_t o[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
     float x_factor[2] = {0.0f, 0.0f};
@@ -528,7 +536,7 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
       if (!dead) {
 #pragma unroll
         for (int k = 0; k < decays.kOwn; ++k) {
-          const int p = wave + k * kWaves<D>;
+          const int p = wave + k * kWavesHere;
           if (p >= 3) break;
           const Pair<R> pair(p);
           f32x4_t m = {0, 0, 0, 0};
@@ -669,7 +677,7 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem) {
     }
 #pragma unroll
     for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
-    if (lane == 0) a.dg[(of_slice + segment) * kWaves<D> + wave] = sum;
+    if (lane == 0) a.dg[(of_slice + segment) * kWaves<D> + tile] = sum;
   }
 }
 
