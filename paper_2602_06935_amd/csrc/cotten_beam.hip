@@ -338,6 +338,12 @@ __device__ __forceinline__ Candidate of_lane(const Candidate& c, int lane) {
   return Candidate{__builtin_bit_cast(double, shuffle(__builtin_bit_cast(uint64_t, c.total), lane)), shuffle(c.index, lane)};
 }
 
+__device__ __forceinline__ uint32_t of_all(uint32_t bits) {
+#pragma unroll
+  for (int m = 1; m < 64; m <<= 1) bits |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(bits), m));
+  return bits;
+}
+
 // A workgroup a sequence.  First the logarithms of its rows' sums, then the K best of what the parts' lists hold: every wave takes 64
 // candidates at a time, the firsts of all lists before the seconds, and where one is ahead of the K-th that it has, sorts them
 // and merges them into its own 64; the waves' lists are merged at the end.  256 x 8 beams of two parts in 6 us, most of it latency.
@@ -436,9 +442,13 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinArgs a) {
       const int before = lane < a.K ? (lane > 0 ? lane - 1 : 0) : a.K - 1;
       const double gap = of_lane(mine, before).total - mine.total;
       const int k_before = __shfl(k, before);
-      uint32_t near = mine.index != ~0ull && k != k_before && gap > 0.0 && gap < kNear ? (1u << k) | (1u << k_before) : 0u;
-#pragma unroll
-      for (int m = 1; m < 64; m <<= 1) near |= static_cast<uint32_t>(__shfl_xor(static_cast<int>(near), m));
+      const uint32_t pair = mine.index != ~0ull && k != k_before && gap < kNear ? (1u << k) | (1u << k_before) : 0u;
+      // (equal totals are those of equal rows: they are in order, but stay equal only if both sums are made again)
+      uint32_t near = 0u, more = of_all(gap > 0.0 ? pair : 0u);
+      while (more != near) {
+        near = more;
+        more |= of_all((pair & near) != 0u ? pair : 0u);
+      }
       if (lane == 0) unsure = again ? 0u : near;
     }
     __syncthreads();

@@ -156,6 +156,18 @@ def test_candidates_that_nearly_tie(dtype, V, K):
     compare(logits, scores.cuda())
 
 
+@pytest.mark.parametrize("seed", range(8))
+@pytest.mark.parametrize("K", [3, 8])
+def test_a_tie_beside_a_near_tie(K, seed):
+    """Two equal beams, and the others' best so near behind them that their sums are made again: the equal ones stay equal."""
+    logits, _ = draw(1, 1, 5000, torch.float32, seed=seed)
+    order = torch.randperm(5000, generator=torch.Generator().manual_seed(seed))
+    logits = torch.cat([logits, logits] + [logits[..., order.cuda()]] * (K - 2), 1)
+    scores = torch.full((1, K), -1.0)
+    scores[0, 2:] -= 2.0 ** -23 * torch.arange(1, K - 1)
+    compare(logits, scores.cuda())
+
+
 def test_large_offsets():
     """More than 2^32 bytes of logits, and of states: the last sequences, read and written behind them."""
     B, K, V = 40, 32, 1_800_001
