@@ -120,3 +120,41 @@ def test_example_runs(example, monkeypatch, dtype, bar, mixer, p):
                                       "--items", "80", "--users", "32"])
     losses, far = example.main()
     assert all(math.isfinite(x) for x in losses) and far < bar
+
+
+def test_a_captured_training_pass():
+    """Forward and backward of mixer, seam and dropout in one graph; replays follow the inputs and draw anew."""
+    from paper_2602_06935_amd import autograd
+    gen = torch.Generator().manual_seed(5)
+    draw = lambda *shape: torch.randn(*shape, generator=gen).to("cuda", torch.bfloat16)        # noqa: E731
+    B, N, H, d = 3, 300, 2, 64
+    q, k, v = (draw(B, N, H, d).requires_grad_() for _ in range(3))
+    X = draw(B, N, H * d).requires_grad_()
+    g = torch.full((H,), -0.05, device="cuda").requires_grad_()
+    post, after = (draw(H * d).requires_grad_() for _ in range(2))
+    mask = (torch.rand(B, N, generator=gen) < 0.8).to(torch.uint8).cuda()
+    up = [draw(B, N, H * d) for _ in range(2)]
+    step = torch.zeros(1, dtype=torch.int64, device="cuda")
+    leaves = (q, k, v, g, X, post, after)
+
+    def run():
+        O = autograd.decay_attention(q, k, v, g, mask, layout="bnhd")
+        Y, h = autograd.residual_norm(X, O.reshape(B, N, H * d), post_weight=post, next_weight=after, p=0.1, seed=2, step=step)
+        return (Y, *torch.autograd.grad((Y, autograd.dropout(h, 0.3, seed=2, offset=1 << 40, step=step)), leaves, up))
+
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        run()
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        got = [t.detach() for t in run()]
+    for i in range(4):
+        with torch.no_grad():
+            v.mul_(-0.9)
+            step.fill_(i)
+        graph.replay()
+        want = run()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
