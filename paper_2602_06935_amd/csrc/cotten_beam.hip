@@ -346,7 +346,7 @@ __device__ __forceinline__ uint32_t of_all(uint32_t bits) {
 
 // A workgroup a sequence.  First the logarithms of its rows' sums, then the K best of what the parts' lists hold: every wave takes 64
 // candidates at a time, the firsts of all lists before the seconds, and where one is ahead of the K-th that it has, sorts them
-// and merges them into its own 64; the waves' lists are merged at the end.  256 x 8 beams of two parts in 6 us, most of it latency.
+// and merges them into its own 64; the waves' lists are merged at the end.  256 x 8 beams of two parts in 11 us, 4 x 4 in 6: latency, of one sort after the other.
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinArgs a) {
   constexpr int kWaves = kJoinThreads / 64;
   __shared__ double of_row[kMostBeams];                 // what a row adds to its logits
@@ -466,7 +466,8 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinArgs a) {
 // ---- reordering -----------------------------------------------------------------------------------------------------------
 
 // Beam k of a sequence gets what beam parents[k] had, in place: a thread owns some bytes of all K beams, and loads all that move
-// before it stores any.  A beam that stays is neither read nor written; a parent that is none leaves a beam as it is.
+// before it stores any.  A beam that stays is neither read nor written; a parent that is none leaves a beam as it is.  256 x 8 beams of
+// 64 KB (134 MB) in 28 us, for which the memory-side cache holds much of them.
 template <class Word, int MOST>
 __global__ __launch_bounds__(256) void reorder_kernel(Word* state, const int* parents, int K, long long words, int blocks) {
   const long long sequence = blockIdx.x / blocks;
