@@ -334,10 +334,21 @@ __device__ __forceinline__ float over_row(float x) {
 }
 template <class E, int D>
 __device__ __forceinline__ float inverse_norm(const typename E::Raw& raw, float eps) {
-  float x[8], s = 0.0f;
-  E::unpack(raw, x);
+  float s = 0.0f;
+  if constexpr (E::kBytes == 2 && E::kPieces == 1) {  // bf16: pairs as they are, 4 instructions for 16
+    typedef __bf16 pair __attribute__((ext_vector_type(2)));
 #pragma unroll
-  for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t w = raw[i];  // (a bit cast of an element in place takes the first)
+      const pair x = __builtin_bit_cast(pair, w);
+      s = __builtin_amdgcn_fdot2_f32_bf16(x, x, s, false);
+    }
+  } else {
+    float x[8];
+    E::unpack(raw, x);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s = fmaf(x[i], x[i], s);
+  }
   return __builtin_amdgcn_rsqf(over_row<D / 8>(s) + eps);
 }
 

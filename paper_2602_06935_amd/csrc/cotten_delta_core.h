@@ -221,10 +221,8 @@ struct Half {
     __builtin_amdgcn_raw_buffer_store_b16(bits(x), r, off, 0, 0);
   }
   static __device__ __forceinline__ void store_four(__amdgpu_buffer_rsrc_t r, uint32_t off, f32x4_t x) {
-    u32x2_t w;
-    w[0] = bits(x[0]) | (static_cast<uint32_t>(bits(x[1])) << 16);
-    w[1] = bits(x[2]) | (static_cast<uint32_t>(bits(x[3])) << 16);
-    __builtin_amdgcn_raw_buffer_store_b64(w, r, off, 0, 0);
+    typedef T quad __attribute__((ext_vector_type(4)));  // (two conversions of pairs; of one value each they would be four, and packed)
+    __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2_t, __builtin_convertvector(x, quad)), r, off, 0, 0);
   }
 };
 struct Bf16 : Half<__bf16> {
