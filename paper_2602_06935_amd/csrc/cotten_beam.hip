@@ -150,7 +150,8 @@ __device__ __forceinline__ float exponential(float x, float top) {
 
 // A wave a part.  The list of the best is sorted over the lanes; a key that is not ahead of the K-th is left out by one
 // comparison, so most pieces cost a maximum and their exponentials.  Those that are go through a buffer in LDS, sorted and merged
-// by 64.  At first the K-th is bounded from below by the K-th of the lanes' own greatest: that many are ahead of it.
+// by 64.  The K-th is bounded from below by the K-th of the lanes' own greatest, as that many are ahead of it or at it: looked up in the
+// first round, the third, and whenever the rounds have doubled (in the first alone, seven in eight of 8300 items' keys that passed were in vain).
 // 256 x 8 rows of 16600 bf16 in 27 us (2.5 TB/s), most of it exponentials, one a logit.
 template <class T>
 __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
@@ -185,7 +186,7 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
   Items<T> next[kPieces];
 #pragma unroll
   for (int u = 0; u < kPieces; ++u) next[u] = load(logits, begin + u * kPiece + lane * kLaneItems, end);
-  for (int at = begin; at < end; at += kPieces * kPiece) {
+  for (int at = begin, round = 0; at < end; at += kPieces * kPiece, ++round) {
     float x[kPieces][kLaneItems], m[kPieces];
 #pragma unroll
     for (int u = 0; u < kPieces; ++u) {
@@ -220,7 +221,10 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
       sum += static_cast<double>(s);
     }
     // the best
-    if (at == begin) least = static_cast<uint64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(sorted(in_order(greatest), lane)), a.K - 1))) << 32;
+    if ((round & (round - 1)) == 0 && round != 1) {
+      const uint64_t kth = static_cast<uint64_t>(static_cast<uint32_t>(__shfl(static_cast<int>(sorted(in_order(top), lane)), a.K - 1))) << 32;
+      least = kth > least ? kth : least;
+    }
 #pragma unroll
     for (int u = 0; u < kPieces; ++u) {
       // only where a lane has a key ahead of the K-th
