@@ -846,41 +846,41 @@ def cotten_residual_workspace_bytes(B: int, N: int, D: int, gate_per_sequence: b
     return int(load_library().cotten_residual_workspace_bytes(B, N, D, int(bool(gate_per_sequence))))
 
 
-def _seam_vector(name: str, t: Optional[torch.Tensor], X: torch.Tensor) -> Optional[int]:
-    if t is None:
-        return None
-    if t.dtype is not X.dtype or t.shape != X.shape[2:] or t.device != X.device or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous [{X.shape[2]}] tensor of the type and on the device of X")
+def _seam_vector(name: str, t: torch.Tensor, dtype: torch.dtype, shape, dev) -> int:
+    if t.dtype is not dtype or t.shape != shape or t.device != dev or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous {list(shape)} tensor of the type and on the device of X")
     return t.data_ptr()
 
 
 def _residual_params(X, F, norm, post_weight, post_bias, gate, alpha, next_weight, next_bias, eps, p, seed, offset,
                      step) -> CottenResidualParams:
     """The checks of what the two calls share, and their parameters."""
-    if X.dim() != 3:
+    shape, dtype, dev = X.shape, X.dtype, X.device   # (looked up once: every one of them is a call)
+    if len(shape) != 3:
         raise ValueError("X must be [B,N,D]")
-    _check_like("X", X, X)
-    _check_like("F", F, X)
+    _check_like("X", X, shape, dtype, dev)
+    _check_like("F", F, shape, dtype, dev)
     kind = _NORMS.get(norm)
     if kind is None:
         raise ValueError("norm must be 'rms' or 'layer'")
     if (post_bias is not None and post_weight is None) or (next_bias is not None and next_weight is None):
         raise ValueError("a norm's bias goes with its weight")
-    per_sequence = gate is not None and gate.dim() == 2
-    if per_sequence:
-        if gate.dtype is not X.dtype or gate.shape != (X.shape[0], X.shape[2]) or gate.device != X.device or not gate.is_contiguous():
-            raise ValueError("gate must be a contiguous [D] or [B,D] tensor of the type and on the device of X")
-        gates = gate.data_ptr()
-    else:
-        gates = _seam_vector("gate", gate, X)
+    width = shape[2:]
+    per_sequence, gates = False, None
+    if gate is not None:
+        per_sequence = gate.dim() == 2
+        gates = _seam_vector("gate", gate, dtype, (shape[0], shape[2]) if per_sequence else width, dev)
     return CottenResidualParams(
-        _dtype_code(X), kind, _seam_vector("post_weight", post_weight, X), _seam_vector("post_bias", post_bias, X), gates,
-        _seam_vector("next_weight", next_weight, X), _seam_vector("next_bias", next_bias, X), int(per_sequence), alpha,
-        -1.0 if eps is None else eps, p, seed, offset, _check_generator(p, seed, offset, step, X.device))
+        _dtype_code(X), kind,
+        None if post_weight is None else _seam_vector("post_weight", post_weight, dtype, width, dev),
+        None if post_bias is None else _seam_vector("post_bias", post_bias, dtype, width, dev), gates,
+        None if next_weight is None else _seam_vector("next_weight", next_weight, dtype, width, dev),
+        None if next_bias is None else _seam_vector("next_bias", next_bias, dtype, width, dev), int(per_sequence), alpha,
+        -1.0 if eps is None else eps, p, seed, offset, _check_generator(p, seed, offset, step, dev))
 
 
-def _check_like(name: str, t: torch.Tensor, X: torch.Tensor) -> None:
-    if not (t.is_cuda and t.is_contiguous() and t.shape == X.shape and t.dtype is X.dtype and t.device == X.device):
+def _check_like(name: str, t: torch.Tensor, shape, dtype: torch.dtype, dev) -> None:
+    if not (t.is_cuda and t.is_contiguous() and t.shape == shape and t.dtype is dtype and t.device == dev):
         raise ValueError(f"{name} must be a contiguous GPU tensor [B,N,D], like X (there is no CPU path)")
 
 
@@ -898,16 +898,17 @@ def cotten_residual_fwd(X: torch.Tensor, F: torch.Tensor, Y: Optional[torch.Tens
     if Y is None:
         Y = torch.empty_like(X)
     else:
-        _check_like("Y", Y, X)
+        _check_like("Y", Y, X.shape, X.dtype, X.device)
     if next_weight is None:
         if H is not None:
             raise ValueError("H comes from next_weight")
     elif H is None:
         H = torch.empty_like(X)
     else:
-        _check_like("H", H, X)
-    _on_device(X.device, lib.cotten_residual_fwd, X.data_ptr(), F.data_ptr(), Y.data_ptr(), None if H is None else H.data_ptr(),
-               *X.shape, _stream_handle(stream, X.device), ctypes.byref(prm))
+        _check_like("H", H, X.shape, X.dtype, X.device)
+    dev = X.device
+    _on_device(dev, lib.cotten_residual_fwd, X.data_ptr(), F.data_ptr(), Y.data_ptr(), None if H is None else H.data_ptr(),
+               *X.shape, _stream_handle(stream, dev), ctypes.byref(prm))
     return Y, H
 
 
@@ -929,7 +930,7 @@ def cotten_residual_bwd(X: torch.Tensor, F: torch.Tensor, dY: Optional[torch.Ten
         raise ValueError("dH goes with next_weight")
     for name, t in (("dY", dY), ("dH", dH)):
         if t is not None:
-            _check_like(name, t, X)
+            _check_like(name, t, X.shape, X.dtype, X.device)
     return _residual_backward(prm, _stream_handle(stream, X.device), workspace, X, F, dY, dH,
                               (post_weight, post_bias, gate, next_weight, next_bias), wanted)
 
@@ -994,7 +995,7 @@ def cotten_beam_select(logits: torch.Tensor, scores: torch.Tensor, *, finished: 
     results = []
     for name, t, of in (("new_scores", new_scores, torch.float32), ("parents", parents, torch.int32), ("tokens", tokens, torch.int32)):
         if t is None:
-            t = torch.empty(shape, dtype=of, device=dev)
+            t = torch.empty_like(scores) if of is torch.float32 else torch.empty_like(scores, dtype=of)
             given.append(t.data_ptr())
         else:
             given.append(_of_beams(name, t, of, shape, dev))
