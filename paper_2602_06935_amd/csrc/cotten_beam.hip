@@ -152,7 +152,7 @@ __device__ __forceinline__ float exponential(float x, float top) {
 // comparison, so most pieces cost a maximum and their exponentials.  Those that are go through a buffer in LDS, sorted and merged
 // by 64.  The K-th is bounded from below by the K-th of the lanes' own greatest, as that many are ahead of it or at it: looked up in the
 // first round, the third, and whenever the rounds have doubled (in the first alone, seven in eight of 8300 items' keys that passed were in vain).
-// 256 x 8 rows of 16600 bf16 in 27 us (2.5 TB/s), most of it exponentials, one a logit.
+// 256 x 8 rows of 16600 bf16 in 25 us (2.8 TB/s), bound by vector instructions, some 18 a logit.
 template <class T>
 __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
   __shared__ uint64_t buffers[4][64 + kPiece];
@@ -519,7 +519,7 @@ int check_shape(int B, int K, int V) {
 }
 
 // Waves for a row: enough of them to fill the device, of one round of loads at least; few enough that the join has up to 512 lists.
-// 256 x 8 rows of 16600 in 8192 / 4096 / 2048 waves: 44 / 38 / 39 us with the join; 32 x 5 of 120000: 39 / 35 / 32.
+// 256 x 8 rows of 16600 in 8192 / 4096 / 2048 waves: 44 / 38 / 39 us with the join; 32 x 5 of 120000: 39 / 35 / 32 (before the bar was raised again).
 constexpr int kWanted = 4096;
 struct Cut {
   int parts, part_items;

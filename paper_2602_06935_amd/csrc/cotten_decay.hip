@@ -85,7 +85,7 @@ __global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
 // products with it need no exchange, and a chunk costs two barriers: one behind its rows, one behind the products of its pairs, which the
 // waves share.  128 x 4 slices of 200 x 64 bf16: forward 16 us (52 MB, 3.3 TB/s), backward without dg 39 (92 MB; three walks, each with
 // its own reads, most of them found in L2).  From 768 slices on a forward moves 4.6 to 5.1 TB/s, a backward 2.6: three workgroups a compute unit keep
-// the vector units busy with cutting rows and states into pieces; with one, a chunk takes 0.9 us, its own chain of LDS, products and
+// the vector units busy with cutting rows and states into pieces; with one, a chunk takes 1.35 us, its own chain of LDS, products and
 // barriers.  Rows in two places of LDS with one barrier a chunk, and two chunks of rows ahead, were built: 16.2 to 17.8 us, 15.4 to 16.7.
 
 // Waves on a SIMD that the registers of a walk leave room for.
