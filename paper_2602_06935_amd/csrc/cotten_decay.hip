@@ -115,6 +115,14 @@ __global__ __launch_bounds__(64 * kWaves<D>, (kRoom<E, D>)) void grad_kernel(Arg
   else if (role == 1) walk<E, D, kDk>(a, unit, smem);
   else walk<E, D, kDv>(a, unit, smem);
 }
+// ... with keys and values in one.
+template <class E, int D>
+__global__ __launch_bounds__(64 * kWaves<D>, (kRoom<E, D>)) void joined_grad_kernel(Args a, int units) {
+  const int turn = blockIdx.x / 16, rest = blockIdx.x % 16, unit = turn * 8 + rest % 8;
+  if (unit >= units) return;
+  if (rest / 8 == 0) walk<E, D, kDq>(a, unit, smem);
+  else walk_back<E, D>(a, unit, smem);
+}
 
 // What the segments add to S (with its derivative by g) and to dS.
 template <class E, int D, bool DERIVATIVES>
@@ -232,6 +240,30 @@ hipError_t launch_decays(const Args& a, int units, hipStream_t s) {
   return hipSuccess;
 }
 
+// The walks of dQ, dK and dV.  At d = 128 a compute unit has room for one workgroup, and 16-bit walks take as many rounds as the workgroups need:
+// three of a unit, or two of which the joint one takes half as long again.  us, three / two: fp16 64 x 197 tokens 30.9 / 45.0, 128 x 197 58.4 / 47.9, 200 x 197
+// 84.5 / 88, 512 x 197 171 / 174, 16 x 2048 in 8 segments 97.8 / 82.7; bf16 25 / 35, 46.5 / 36.6, 64 / 67, 129 / 130, 75 / 63.  (Narrower rows,
+// several workgroups to a compute unit, are no faster joined: bf16 d = 64, 512 x 200 45 / 48, 4096 x 200 307 / 299, fp16 413 / 462.)
+template <class E, int D>
+hipError_t launch_gradients(const Args& a, int units, hipStream_t s) {
+  const unsigned eights = static_cast<unsigned>((units + 7) / 8);
+  constexpr int kUnits = 256;  // compute units
+  const auto rounds = [](long long workgroups) { return (workgroups + kUnits - 1) / kUnits; };
+  if constexpr (D == 128 && E::kBytes == 2) {
+    if (3 * rounds(2ll * units) < 2 * rounds(3ll * units)) {
+      constexpr int kBytes = greatest(kLds<E, D, kDq>, BackPlace<E, D>::kBytes);
+      static_assert(kBytes <= 160 * 1024, "a workgroup's LDS");
+      if (hipError_t rc = granted(joined_grad_kernel<E, D>, kBytes)) return rc;
+      joined_grad_kernel<E, D><<<dim3(eights * 16u), dim3(64 * kWaves<D>), kBytes, s>>>(a, units);
+      return hipSuccess;
+    }
+  }
+  constexpr int kBytes = greatest(kLds<E, D, kDq>, kLds<E, D, kDv>);
+  if (hipError_t rc = granted(grad_kernel<E, D>, kBytes)) return rc;
+  grad_kernel<E, D><<<dim3(eights * 24u), dim3(64 * kWaves<D>), kBytes, s>>>(a, units);
+  return hipSuccess;
+}
+
 template <class E, int D>
 hipError_t forward(const Args& a, int slices, hipStream_t s) {
   if (a.N <= kMostSteps<E, D>) {
@@ -265,9 +297,7 @@ hipError_t backward(const Args& a, int slices, float* dg, hipStream_t s) {
     kernel<<<dim3(2u * units), block, kBytes, s>>>(a, units);
     launch_scan(a, slices, D, true, s);
   }
-  constexpr int kBytes = greatest(kLds<E, D, kDq>, kLds<E, D, kDv>);
-  if (hipError_t rc = granted(grad_kernel<E, D>, kBytes)) return rc;
-  grad_kernel<E, D><<<dim3(static_cast<unsigned>((units + 7) / 8) * 24u), block, kBytes, s>>>(a, units);
+  if (hipError_t rc = launch_gradients<E, D>(a, units, s)) return rc;
   if (dg != nullptr) {
     // (a launch of its own: it needs the most registers, and would take them from the other roles)
     if (hipError_t rc = launch_decays<E, D>(a, units, s)) return rc;

@@ -198,9 +198,9 @@ struct Pair {
   int x, y;
   __device__ __forceinline__ explicit Pair(int i) : x(R::kBack ? i >> 1 : (i + 1) >> 1), y(R::kBack ? (i + 1) >> 1 : i >> 1) {}
 };
-template <class R, int WAVES>
+template <class R, int WAVES, int COUNT = 3>
 struct Decays {
-  static constexpr int kOwn = WAVES >= 3 ? 1 : WAVES == 2 ? 2 : 3;   // pairs of a wave, at most
+  static constexpr int kOwn = (COUNT + WAVES - 1) / WAVES;           // pairs of a wave, at most (COUNT: 3 or, of two kinds of them, 6)
   uint32_t live;
   bool together;
   float n;                  // tokens that count
@@ -216,8 +216,8 @@ struct Decays {
 #pragma unroll
       for (int k = 0; k < kOwn; ++k) {
         const int i = wave + k * WAVES;
-        if (i >= 3) break;
-        const Pair<R> p(i);
+        if (i >= COUNT) break;
+        const Pair<R> p(i % 3);
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int row = 4 * (lane >> 4) + r, a = apart(bits, p, r, lane);
@@ -690,6 +690,247 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem, int part = 0)
     for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
     if (lane == 0) a.dg[(of_slice + segment) * kWaves<D> + tile] = sum;
   }
+}
+
+// The gradients of keys and values in one walk, for wide 16-bit rows: both go back with dS, by columns in the waves, so its update and the rows
+// of Q and dO are shared.  dV takes a wave's own columns of dS, dK those of dS^T, which all waves leave in LDS in pieces, behind the second
+// barrier of a chunk, for the next.  A chunk takes half as long again as one of either gradient by itself.
+template <class E, int D>
+struct BackPlace {
+  static_assert(D >= 32 && E::kBytes == 2, "rows without zeros behind them, results of two pieces");
+  static constexpr int kOf = kOperand<E, kDv>;
+  typedef Rows<D, E::kPieces> R;
+  typedef Rows<D, kOf> M;                      // 32 columns of dS a block
+  static constexpr int kBlocks = StateColumns<D>::kBlocks;
+  static constexpr int kQ = 0, kO = R::kBytes, kK = 2 * R::kBytes, kV = 3 * R::kBytes, kState = 4 * R::kBytes, kOfK = kState + kBlocks * M::kBytes;
+  static constexpr int kOfPair = kOfK + kChunk * 4, kTo = kOfPair + kChunk * 4, kOfState = kTo + kChunk * 4, kPowers = kOfState + kChunk * 4;
+  static constexpr int kPairs = kPowers + static_cast<int>(sizeof(Powers)), kParts = kPairs + 2 * kPairBytes<kOf>;
+  static constexpr int kBytes = kParts + kWaves<D> * kChunk * 8;
+};
+template <class E, int D>
+__device__ void walk_back(const Args& a, int unit, unsigned char* smem) {
+  typedef Traits<kDv> T;
+  typedef BackPlace<E, D> P;
+  typedef typename P::R L;
+  typedef typename P::M M;
+  constexpr int kOf = P::kOf, kRowLanes = D / 8, kBlocks = P::kBlocks, kW = kWaves<D>, kEach = kPairBytes<kOf>;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int slice = unit / a.segments, segment = unit - slice * a.segments;
+  const Slice s(a, slice, D * E::kBytes);
+  int begin = segment * a.segment_chunks;
+  const int end = begin + a.segment_chunks < a.chunks ? begin + a.segment_chunks : a.chunks;
+  const int col = 16 * wave + (lane & 15), group = lane >> 4;
+  const long long of_slice = static_cast<long long>(slice) * a.segments, state_at = static_cast<long long>(slice) * D * D;
+  float* of_k = reinterpret_cast<float*>(smem + P::kOfK);
+  float* of_pair = reinterpret_cast<float*>(smem + P::kOfPair);
+  float* to_state = reinterpret_cast<float*>(smem + P::kTo);
+  float* of_state = reinterpret_cast<float*>(smem + P::kOfState);
+  float* parts = reinterpret_cast<float*>(smem + P::kParts);       // [wave][token]: k . dk^ and k . k
+  Powers* powers = reinterpret_cast<Powers*>(smem + P::kPowers);
+  unsigned char* pairs = smem + P::kPairs;                         // of dV, and behind them of dK
+  for (int i = threadIdx.x; i < 2 * kEach / 16; i += 64 * kW) reinterpret_cast<f32x4_t*>(pairs)[i] = f32x4_t{0, 0, 0, 0};
+  if (wave == 0) set_powers(powers, rate_of(s.g), lane);
+  lds_barrier();
+
+  StateColumns<D> S;
+  const bool outermost = a.segments == 1 || segment == a.segments - 1;
+  S.load(!outermost ? a.local_d + (of_slice + segment) * D * D : a.dfinal_state == nullptr ? nullptr : a.dfinal_state + state_at, col, lane);
+  auto hand_over = [&]() {
+#pragma unroll
+    for (int kb = 0; kb < kBlocks; ++kb) {
+      const Pieces<kOf> x = cut_operand<E, kOf>(S.s[2 * kb], S.s[2 * kb + 1]);
+      unsigned char* to = smem + P::kState + (col >> 5) * M::kBytes + (col & 31) * M::kStride + kb * 64 + 16 * group;
+#pragma unroll
+      for (int i = 0; i < kOf; ++i) *reinterpret_cast<delta::bf16x8_t*>(to + i * M::kPlane) = x.p[i];
+    }
+  };
+
+  const int row = wave * (512 / D) + lane / kRowLanes;
+  const uint32_t off = static_cast<uint32_t>(row) * a.stride_row + (lane % kRowLanes) * 8 * E::kBytes;
+  if (a.mask != nullptr && a.dinitial_state == nullptr) {  // chunks before the first token that counts
+    const int from = first_live(s.mask, a.N, begin, end, lane);
+    for (int c = begin; c < from; ++c) {
+      const __amdgpu_buffer_rsrc_t rk = s.of(a.dK, c, a.stride_row), rv = s.of(a.dV, c, a.stride_row);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        E::store_four(rk, off + 4 * i * E::kBytes, f32x4_t{0, 0, 0, 0});
+        E::store_four(rv, off + 4 * i * E::kBytes, f32x4_t{0, 0, 0, 0});
+      }
+    }
+    begin = from;
+  }
+
+  Mask mask(a, s);
+  uint32_t live = 0, there = 0;
+  typename E::Raw rq, ro, rk, rv;
+  ResultRows<E> own;                        // rows of K
+  const uint32_t own_off = static_cast<uint32_t>(lane & 15) * a.stride_row + (16 * wave + 4 * group) * E::kBytes;
+  auto fetch = [&](int chunk) {
+    live = mask.bits(chunk);
+    there = existing(a.N, chunk);
+    const uint32_t masked = offset_if(live, row, off);
+    rq = E::load(s.of(a.Q, chunk, a.stride_row), off);
+    ro = E::load(s.of(a.dO, chunk, a.stride_row), off);
+    rk = E::load(s.of(a.K, chunk, a.stride_row), masked);
+    rv = E::load(s.of(a.V, chunk, a.stride_row), masked);
+  };
+  const int first = end - 1, last = begin;
+  if (end > begin) {
+    mask.fetch(first, lane);
+    fetch(first);
+    if (first != last) mask.fetch(first - 1, lane);
+    hand_over();
+  }
+  Decays<T, kW, 6> decays;
+  decays.begin(powers, wave, lane);
+  f32x4_t held[2];                          // rows of dk^ that wait for the sums over the waves
+  uint32_t held_live = 0;
+  auto finish = [&](int chunk) {
+    const __amdgpu_buffer_rsrc_t r = s.of(a.dK, chunk, a.stride_row);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const int token = 16 * t + (lane & 15);
+      float dot = 0.0f, square = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kW; ++w) {
+        dot += parts[(w * kChunk + token) * 2];
+        square += parts[(w * kChunk + token) * 2 + 1];
+      }
+      const float inverse = __builtin_amdgcn_rsqf(square + a.eps), back = dot * inverse * inverse;
+      f32x4_t x;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = ((held_live >> token) & 1u) ? inverse * (held[t][i] - own.x[t][i] * back) : 0.0f;
+      E::store_four(r, own_off + 16 * t * a.stride_row, x);
+    }
+  };
+
+  for (int c = first; c >= last; --c) {
+    const uint32_t now = live, now_there = there;
+    const bool dead = now == 0;             // no rows of keys and values
+    {
+      const int kb = (lane % kRowLanes) / 4, g = (lane % kRowLanes) % 4;
+      L::put(smem + P::kQ, row, kb, g, E::pieces(rq));
+      L::put(smem + P::kO, row, kb, g, E::pieces(ro));
+      float fk = 0.0f;
+      if (!dead) {
+        L::put(smem + P::kK, row, kb, g, E::pieces(rk));
+        L::put(smem + P::kV, row, kb, g, E::pieces(rv));
+        fk = inverse_norm<E, D>(rk, a.eps);
+      }
+      const float norm = a.scale * inverse_norm<E, D>(rq, a.eps), fq = ((now_there >> row) & 1u) ? norm : 0.0f;
+      const int p = upto(now, row), behind = __popc(now) - p;
+      if (lane % kRowLanes == 0) {
+        of_k[row] = ((now >> row) & 1u) ? fk : 0.0f;
+        to_state[row] = powers->hi[behind];
+        of_pair[row] = fq;
+        of_state[row] = fq * powers->hi[p];
+      }
+    }
+    if (now != decays.live) {
+      if (dead) decays.none();
+      else decays.set(now, now_there, powers, wave, lane);
+    }
+    if (c != last) {
+      fetch(c - 1);
+      if (c - 1 != last) mask.fetch(c - 2, lane);
+    }
+    lds_barrier();
+
+    if (c != first) finish(c + 1);
+    f32x4_t of_v[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}}, of_keys[2] = {{0, 0, 0, 0}, {0, 0, 0, 0}};
+    own.load(s.of(a.K, c, a.stride_row), a.stride_row, now, own_off, lane);
+    const Pieces<E::kPieces> z = L::column_operand(smem + P::kO, wave, lane);
+    if (!dead) {
+      // this wave's share of the products of pairs, for all: q . k for dV, dO . v for dK
+#pragma unroll
+      for (int k = 0; k < decays.kOwn; ++k) {
+        const int i = wave + k * kW;
+        if (i >= 6) break;
+        const Pair<T> pair(i % 3);
+        const unsigned char* y = smem + (i < 3 ? P::kQ : P::kO);
+        const unsigned char* x = smem + (i < 3 ? P::kK : P::kV);
+        f32x4_t m = {0, 0, 0, 0};
+#pragma unroll
+        for (int kb = 0; kb < kBlocks; ++kb) m = mul(L::row_operand(y, pair.y, kb, lane), L::row_operand(x, pair.x, kb, lane), m);
+        const f32x4_t factor = *reinterpret_cast<const f32x4_t*>(of_pair + 16 * pair.y + 4 * group);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) m[r] *= factor[r] * decays.pair[k][r];
+        put_half<E, kOf>(pairs + (i < 3 ? 0 : kEach), pair.x, pair.y, lane, m);
+      }
+#pragma unroll
+      for (int kb = 0; kb < kBlocks; ++kb) {
+        const unsigned char* mine = smem + P::kState + (col >> 5) * M::kBytes + (col & 31) * M::kStride + kb * 64 + 16 * group;
+        Pieces<kOf> x;
+#pragma unroll
+        for (int i = 0; i < kOf; ++i) x.p[i] = *reinterpret_cast<const delta::bf16x8_t*>(mine + i * M::kPlane);
+        const Pieces<E::kPieces> keys[2] = {L::row_operand(smem + P::kK, 0, kb, lane), L::row_operand(smem + P::kK, 1, kb, lane)};
+        mul_right(x, keys, of_v);
+        const Pieces<E::kPieces> values[2] = {L::row_operand(smem + P::kV, 0, kb, lane), L::row_operand(smem + P::kV, 1, kb, lane)};
+        mul_right(M::column_operand(smem + P::kState + kb * M::kBytes, wave, lane), values, of_keys);
+      }
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const float w = to_state[16 * t + (lane & 15)];
+        of_v[t] *= w;
+        of_keys[t] *= w;
+      }
+    }
+
+    // the state: dS <- a^n dS + Q^T (w dO)
+    {
+      const f32x4_t factor[2] = {*reinterpret_cast<const f32x4_t*>(of_state + 4 * group), *reinterpret_cast<const f32x4_t*>(of_state + 16 + 4 * group)};
+      float w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        float v = 0.0f;
+#pragma unroll
+        for (int p = E::kPieces - 1; p >= 0; --p) v += static_cast<float>(z.p[p][j]);
+        w[j] = v * factor[j >> 2][j & 3];
+      }
+#pragma unroll
+      for (int dt = 0; dt < StateColumns<D>::kTiles; ++dt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) S.s[dt][j] = fmaf(S.s[dt][j], decays.whole_hi, S.s[dt][j] * decays.whole_lo);
+      delta::add_outer<L, D>(S, smem + P::kQ, cut<E::kPieces>(w), lane);
+    }
+    const float scale_k[2] = {of_k[lane & 15], of_k[16 + (lane & 15)]};
+    Pieces<E::kPieces> y;
+    if (!dead) y = L::column_operand(smem + P::kQ, wave, lane);
+    lds_barrier();
+
+    // what the chunk's tokens give each other; the next chunk's rows, and dS before this one, may be written from here on
+    if (c != last) hand_over();
+    if (!dead) {
+      const Pieces<kOf> for_v[2] = {pair_operand<kOf>(pairs, 0, lane), pair_operand<kOf>(pairs, 1, lane)};
+      mul_right(z, for_v, of_v);
+      const Pieces<kOf> for_k[2] = {pair_operand<kOf>(pairs + kEach, 0, lane), pair_operand<kOf>(pairs + kEach, 1, lane)};
+      mul_right(y, for_k, of_keys);
+    }
+    const __amdgpu_buffer_rsrc_t r = s.of(a.dV, c, a.stride_row);
+    held_live = now;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      of_v[t] *= scale_k[t];
+      if (!((now >> (16 * t + (lane & 15))) & 1u)) of_v[t] = f32x4_t{0, 0, 0, 0};
+      E::store_four(r, own_off + 16 * t * a.stride_row, of_v[t]);
+      held[t] = of_keys[t];
+      float dot = 0.0f, square = 0.0f;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        dot = fmaf(own.x[t][j], of_keys[t][j], dot);
+        square = fmaf(own.x[t][j], own.x[t][j], square);
+      }
+      dot = over_groups(dot);
+      square = over_groups(square);
+      if (group == 0) {
+        parts[(wave * kChunk + 16 * t + lane) * 2] = dot;
+        parts[(wave * kChunk + 16 * t + lane) * 2 + 1] = square;
+      }
+    }
+  }
+  lds_barrier();
+  if (end > begin) finish(last);
+  if (a.dinitial_state != nullptr && segment == 0) S.store(a.dinitial_state + state_at, col, lane);
 }
 
 }  // namespace decay

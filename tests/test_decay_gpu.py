@@ -103,6 +103,15 @@ def test_segments(dtype, mask, layout, B, H, N, d):
     compare(x, layout, scale=0.25)
 
 
+# numbers of slices (and of segments) for which keys' and values' gradients are one walk: 86 ... 128, 342 ... 384 at d = 128
+@pytest.mark.parametrize("B,H,N", [(29, 3, 33), (64, 2, 70), (43, 2, 64), (49, 7, 40), (16, 1, 520)])
+@pytest.mark.parametrize("mask", [None, "left", "right", "holes", "empty"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_joint_gradients(dtype, mask, B, H, N):
+    x = inputs(B, H, N, 128, DTYPES[dtype], seed=B + N, mask=mask, states=mask != "left")
+    compare(x, "bnhd" if N % 2 else "bhnd", scale=0.25)
+
+
 @pytest.mark.parametrize("d,B,H", [(64, 293, 7), (128, 150, 3), (16, 700, 2), (32, 520, 4)])
 @pytest.mark.parametrize("N", [1, 3, 40])
 def test_many_slices(N, d, B, H):
