@@ -71,6 +71,7 @@ struct Args {
   float* counts;                // [slice][segment][2]: how many of a segment's tokens count, and what they decay a state by
   double* dg;                   // [slice][segment][part]: partial sums of the decays' gradient
   int segments, segment_chunks;
+  int unscanned;                // a forward's segments find the states before them from all local ones
   int H, N, chunks;
   long long stride_batch, stride_head;  // in bytes
   uint32_t stride_row;
@@ -414,6 +415,24 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem, int part = 0)
     if (R::kBack && segment == 0) return;
   } else if (a.segments == 1 || (R::kBack && segment == a.segments - 1)) {
     load_state<D, R::kTransposed>(S, outer, col, lane);
+  } else if (ROLE == kOut && a.unscanned) {
+    // what the segments before add, the first's with the initial state in it
+    const float* local = a.local_s + of_slice * D * D;
+    S.load(local + static_cast<long long>(segment == 0 ? a.segments - 1 : 0) * D * D, col, lane);
+    constexpr int kAhead = D == 128 ? 2 : 4;  // on their way together
+    for (int i = 1; i < segment; i += kAhead) {
+      StateColumns<D> x[kAhead];
+      float w[kAhead];
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u) {
+        x[u].load(i + u < segment ? local + static_cast<long long>(i + u) * D * D : nullptr, col, lane);
+        w[u] = i + u < segment ? a.counts[2 * (of_slice + i + u) + 1] : 1.0f;
+      }
+#pragma unroll
+      for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+        for (int dt = 0; dt < 2 * kBlocks; ++dt) S.s[dt] = S.s[dt] * w[u] + x[u].s[dt];
+    }
   } else {
     load_state<D, R::kTransposed>(S, (R::kBack ? a.local_d : a.local_s) + (of_slice + segment) * D * D, col, lane);
     if constexpr (R::kDerivative) load_state<D, false>(T, a.local_t + (of_slice + segment) * D * D, col, lane);

@@ -103,6 +103,22 @@ def test_segments(dtype, mask, layout, B, H, N, d):
     compare(x, layout, scale=0.25)
 
 
+# few segments, which find the states before them themselves; also where the state is replaced in place
+@pytest.mark.parametrize("B,H,N,d", [(1, 2, 400, 64), (2, 1, 330, 128), (1, 3, 390, 32), (1, 1, 330, 16)])
+@pytest.mark.parametrize("mask", [None, "left", "holes"])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_few_segments(dtype, mask, B, H, N, d):
+    from paper_2602_06935_amd import binding
+    segments = binding.cotten_decay_workspace_bytes(B, H, N, d, binding._DTYPE_CODES[DTYPES[dtype]], False) // (4 * B * H * d * d)
+    assert 3 <= segments <= 6
+    x = inputs(B, H, N, d, DTYPES[dtype], seed=N + d, mask=mask, states=True)
+    ref = compare(x, "bnhd", scale=0.25)
+    q, k, v, g, state = (x[n].cuda() for n in ("q", "k", "v", "g", "S0"))
+    O = binding.cotten_decay_fwd(q, k, v, g, cuda(x["mask"]), scale=0.25, initial_state=state, final_state=state)
+    check("O", O, ref["O"])
+    check("S1", state, ref["S1"])
+
+
 # numbers of slices (and of segments) for which keys' and values' gradients are one walk: 86 ... 128, 342 ... 384 at d = 128
 @pytest.mark.parametrize("B,H,N", [(29, 3, 33), (64, 2, 70), (43, 2, 64), (49, 7, 40), (16, 1, 520)])
 @pytest.mark.parametrize("mask", [None, "left", "right", "holes", "empty"])
