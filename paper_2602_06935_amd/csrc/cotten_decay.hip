@@ -334,7 +334,7 @@ hipError_t backward(const Args& a, int D, int slices, float* dg, hipStream_t s) 
 //   fp32 d = 32, 128 x 1024                 63 / 48 / 39 / 31 / 36                    83 / 64 / 66 / 62 / 67
 //   fp16 d = 128, 64 x 1024                109 / 80 / 67 / 78 / 99                   125 / 195 / 160 / 181 / 228
 // Sequences of few chunks gain nothing: bf16 d = 64, 4 x 256 rows 14.1 / 16.1 / 15.2, fp32 20.9 / 20.2 / 17.1, fp16 d = 128 31.1 / 26.9 / 21.5;
-// bf16 4 x 512 24.4 / 22.2 / 18.4 / 15.1.
+// bf16 4 x 512 24.4 / 22.2 / 18.4 / 15.1.  (All forwards with a scan; where they do without, they take 2 to 4 us less.)
 Segments segments_of(long long slices, int chunks, int D, int dtype, bool bwd) {
   const int least = dtype != 0 && D <= 64 ? 10 : 7, cap = chunks / 8 > 32 ? chunks / 8 : 32;
   long long count = (bwd ? 1024 : 2048) / (slices * waves_of(D));
