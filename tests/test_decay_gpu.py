@@ -340,3 +340,54 @@ def test_captured():
         want = calls()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((*got, after), (*want, state))), i
+
+
+def mixed_masks(N):
+    """One sequence each: padded on the right, live tokens on either side of a stretch without any, padded on the left over more than half
+    of its length, live at its first token alone, without a live token."""
+    m = torch.zeros(5, N, dtype=torch.uint8)
+    m[0, :N // 5] = 1
+    m[1, :N // 6] = 1
+    m[1, 2 * N // 3:] = 1
+    m[2, 3 * N // 5:] = 1
+    m[3, 0] = 1
+    return m
+
+
+# segments that begin with masked tokens, where nothing comes in from outside and nobody asks for the gradient of that: rows of Q and dO count there
+@pytest.mark.parametrize("H,N,d", [(1, 400, 64), (1, 1500, 64), (2, 1100, 128), (1, 330, 128), (2, 900, 32), (1, 390, 32), (1, 1000, 16)])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_masked_beginnings_of_segments(dtype, H, N, d):
+    from paper_2602_06935_amd import binding
+    from paper_2602_06935_amd.autograd import decay_attention
+    code = binding._DTYPE_CODES[DTYPES[dtype]]
+    for bwd in (False, True):
+        assert binding.cotten_decay_workspace_bytes(5, H, N, d, code, bwd) > 0
+    layout = "bnhd" if N % 4 else "bhnd"
+    x = inputs(5, H, N, d, DTYPES[dtype], seed=N + d, rates=(1e-3, 1e-1))
+    x["mask"] = mixed_masks(N)
+    ref = reference(x, scale=0.25)
+    q, k, v = (lay(x[n], layout).requires_grad_() for n in ("q", "k", "v"))
+    g = x["g"].cuda().requires_grad_()
+    O = decay_attention(q, k, v, g, x["mask"].cuda(), scale=0.25, layout=layout)
+    grads = torch.autograd.grad(O, [q, k, v, g], lay(x["dO"], layout))
+    got = dict(zip(NAMES, (back(t, layout) for t in grads)), O=back(O.detach(), layout))
+    for n in ("O",) + NAMES:
+        for b in range(5):                      # (each sequence by itself: a small one's error is not lost in the others')
+            if ref[n][b].any():
+                check(f"{n}[{b}]", got[n][b], ref[n][b])
+            else:
+                assert not got[n][b].any(), (n, b)
+    check_decays(grads[3], ref)
+    # a state of zeros is no state, and a gradient that comes in behind the sequence changes nothing of what is skipped
+    zeros = torch.zeros(5, H, d, d, device="cuda")
+    check("O", back(binding.cotten_decay_fwd(q.detach(), k.detach(), v.detach(), g.detach(), x["mask"].cuda(), scale=0.25, layout=layout,
+                                             initial_state=zeros), layout), ref["O"])
+    x["dS1"] = torch.randn(5, H, d, d, generator=torch.Generator().manual_seed(d)) * 0.3
+    ref = reference(x, scale=0.25)
+    dg = torch.empty(H, device="cuda")
+    grads = binding.cotten_decay_bwd(q.detach(), k.detach(), v.detach(), g.detach(), x["mask"].cuda(), lay(x["dO"], layout), dg=dg, scale=0.25,
+                                     layout=layout, dfinal_state=x["dS1"].cuda())
+    for n, t in zip(NAMES, grads):
+        check(n, back(t, layout), ref[n])
+    check_decays(dg, ref)
