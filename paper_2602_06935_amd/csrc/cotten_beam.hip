@@ -449,6 +449,27 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinArgs a) {
       const uint32_t pair = mine.index != ~0ull && k != k_before && gap < kNear ? (1u << k) | (1u << k_before) : 0u;
       // (equal totals are those of equal rows: they are in order, but stay equal only if both sums are made again)
       uint32_t near = 0u, more = of_all(gap > 0.0 ? pair : 0u);
+      // Where the last of the 64 is that near too, others may have found no place (one beam's equal logits can take them all): every beam
+      // with a candidate that near behind the last that is taken is looked up in the lists.
+      if (!again && __ballot(lane == 63 && mine.index != ~0ull && gap < kNear) != 0) {
+        const Candidate last = of_lane(mine, a.K - 1);
+        const uint32_t of_last = 1u << __shfl(k, a.K - 1);
+        uint32_t crowd = 0u;
+        bool differ = false;
+        for (int list = lane; list < lists; list += 64) {
+          if ((of_last >> (list / a.parts)) & 1u) continue;   // (in order by itself)
+          for (int n = 0; n < a.K; ++n) {
+            const Candidate c = candidate(list, n, best[static_cast<long long>(list) * a.K + n]);
+            if (!(last.total - c.total < kNear)) break;
+            if (ahead(last, c)) {
+              crowd |= 1u << (list / a.parts);
+              differ |= c.total < last.total;
+            }
+          }
+        }
+        crowd = of_all(crowd);
+        if (crowd != 0u && (more != 0u || __ballot(differ) != 0)) more |= crowd | of_last;
+      }
       while (more != near) {
         near = more;
         more |= of_all((pair & near) != 0u ? pair : 0u);

@@ -273,3 +273,38 @@ def test_on_another_stream():
     best, want_parents, want_tokens = expected(logits, scores)
     assert torch.equal(parents.cpu().long(), want_parents) and torch.equal(tokens.cpu().long(), want_tokens)
     assert torch.equal(state.cpu(), before[torch.arange(3)[:, None], want_parents])
+
+
+@pytest.mark.parametrize("K", [8, 32])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_ties_of_many_candidates_beside_near_ties(dtype, K):
+    """Every beam has 200 equal greatest logits, more than a list holds, and the same logits in another order but for one of small weight,
+    so totals of beams are 1e-10 ... 1e-12 apart: those of the last beam are ahead of all others."""
+    B, V = 6, 20000
+    gen = torch.Generator().manual_seed(K)
+    base = (torch.randn(V, generator=gen) * 2.0).to(DTYPES[dtype])
+    base[base > 4.0] = 4.0
+    base[:200] = 4.0
+    rest = torch.logsumexp(base[:-1].double(), 0).item()
+    logits = torch.empty(B, K, V, dtype=DTYPES[dtype])
+    for b in range(B):
+        for k in range(K):
+            row = base.clone()
+            row[-1] = math.floor(rest) - 21.0 - 0.125 * k
+            logits[b, k] = row[torch.randperm(V, generator=gen)]
+    scores = torch.full((B, K), -1.0)
+    ahead = expected(logits, scores)
+    assert (ahead[1] == K - 1).all()
+    per_beam = totals(logits, scores).amax(-1)
+    gaps = per_beam[:, 1:] - per_beam[:, :-1]
+    assert gaps.min() > 1e-13 and gaps.max() < 2e-9
+    compare(logits.cuda(), scores.cuda())
+
+
+@pytest.mark.parametrize("V", [1500, 20000])
+def test_equal_beams_of_many_ties(V):
+    """All candidates equal, and beams that are equal beside one that is behind them by less than sums in 32 bits tell."""
+    logits = torch.zeros(3, 32, V)
+    logits[1:, :, V // 2] = -9.0
+    logits[2, 0, V // 3] = 2.0 ** -20
+    compare(logits.cuda(), torch.full((3, 32), -2.0).cuda())
