@@ -7,8 +7,8 @@
 // The best, the lower k * V + v of equal ones first.  Within a beam the order of the totals is that of the logits, so a row of
 // logits is read once, in parts: a wave keeps the K best of its part (value and item) and the sum of the exponentials, and
 // one workgroup a sequence joins what the parts of its K rows hold, with totals in 64 bits.  The exponentials are fp32, which leaves
-// the logarithm of a row's sum right to 1e-6 at worst and some 1e-8 as a rule; where candidates of two beams come nearer than that, the sums
-// of these rows are made again in 64 bits.
+// the logarithm of a row's sum right to 2e-6 at worst (how_near) and some 1e-8 as a rule; where candidates of two beams come nearer than
+// that, the sums of these rows are made again in 64 bits.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -100,7 +100,7 @@ struct RowArgs {
   const uint8_t* finished;   // [rows] or nullptr
   uint64_t* best;            // [rows][parts][K]
   double* sums;              // [rows][parts]: of exp(logit - top)
-  float* tops;               // [rows][parts]
+  float* tops;               // [rows][parts]: a whole number above all logits of the part, or what stands for it (see row_kernel)
   long long rows;
   int V, K, parts, part_items;  // items of a part: a multiple of kPiece
 };
@@ -134,18 +134,27 @@ __device__ __forceinline__ Items<T> load(const T* row, int first, int V) {
   return r;
 }
 
-__device__ __forceinline__ float greatest_of_wave(float x) {
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) x = fmaxf(x, __shfl_xor(x, m));
+template <int M = 1>
+__device__ __forceinline__ float greatest_of_wave(float x, int lane) {
+  x = fmaxf(x, __uint_as_float(of_xor<M>(__float_as_uint(x), lane)));
+  if constexpr (M < 32) x = greatest_of_wave<2 * M>(x, lane);
   return x;
 }
-
 
 // e^(x - top): of the difference, so that a shift of all logits costs nothing, and with log2(e) as two floats.  Errors are those of small
 // numbers where the value is large, and of either sign.  (x = top = +inf: NaN.)
 __device__ __forceinline__ float exponential(float x, float top) {
   const float d = x - top;
   return __builtin_amdgcn_exp2f(fmaf(d, 1.44269502f, d * 1.92596303e-8f));
+}
+// e^d for d <= 0 in 64 bits: e^r for what is left of d by whole multiples of ln 2, by its series (r^12 / 12! < 1e-14).
+__device__ __forceinline__ double exponential(double d) {
+  const double n = rint(d * 1.4426950408889634), r = fma(n, -1.9082149292705877e-10, fma(n, -0.693147180369123816490, d));
+  double s = 1.0 / 39916800.0;
+  constexpr double kTerms[] = {1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
+#pragma unroll
+  for (int i = 0; i < 11; ++i) s = fma(s, r, kTerms[i]);
+  return d > -700.0 ? ldexp(s, static_cast<int>(n)) : 0.0;
 }
 
 // A wave a part.  The list of the best is sorted over the lanes; a key that is not ahead of the K-th is left out by one
@@ -170,6 +179,7 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
   uint64_t least = 0;      // a key that K or more are ahead of, or at
   int waiting = 0;         // keys in the buffer
   float top = -__builtin_inff();   // greatest logit of the lane
+  float above = -__builtin_inff(); // of the wave: what exponentials are taken of differences from, at or above all of its logits
   double sum = 0.0;
   // the last up to 64 of the buffer into the list
   auto take = [&]() {
@@ -202,21 +212,26 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
     float greatest = m[0];
 #pragma unroll
     for (int u = 1; u < kPieces; ++u) greatest = fmaxf(greatest, m[u]);
-    // the sum, every lane's own; +inf gives no sum (see join_kernel)
-    if (greatest > top) {
-      sum = top > -__builtin_inff() ? sum * static_cast<double>(exponential(top, greatest)) : 0.0;
-      top = greatest;
+    // the sum, every lane's own; +inf gives no sum (see join_kernel).  What it is relative to rises for the whole wave, by more than 1 beyond the
+    // greatest logit, so seldom, and by a factor in 64 bits: one in 32 at every rise would add up over the rounds of a row that rises.
+    top = fmaxf(top, greatest);
+    if (__ballot(greatest > above) != 0) {
+      const float higher = ceilf(greatest_of_wave(greatest, lane)) + 1.0f;
+      if (__ballot(above > -__builtin_inff()) != 0) sum *= exponential(static_cast<double>(above) - static_cast<double>(higher));
+      above = higher;
     }
-    const float against = top > -__builtin_inff() ? top : 0.0f;
+    const float against = above > -__builtin_inff() ? above : 0.0f;
 #pragma unroll
     for (int u = 0; u < kPieces; ++u) {
-      float s = 0.0f;
+      float e[kLaneItems];
 #pragma unroll
-      for (int i = 0; i < kLaneItems; ++i) s += exponential(x[u][i], against);
+      for (int i = 0; i < kLaneItems; ++i) e[i] = exponential(x[u][i], against);
+      float s = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
       if (__ballot(s != s) != 0) {  // NaNs among them count as nothing
         asm volatile("" ::: "memory");  // (a branch: made ahead of it, this costs as much again)
-        s = 0.0f;
-        for (int i = 0; i < kLaneItems; ++i) s += x[u][i] == x[u][i] ? exponential(x[u][i], against) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < kLaneItems; ++i) e[i] = x[u][i] == x[u][i] ? exponential(x[u][i], against) : 0.0f;
+        s = ((e[0] + e[1]) + (e[2] + e[3])) + ((e[4] + e[5]) + (e[6] + e[7]));
       }
       sum += static_cast<double>(s);
     }
@@ -245,13 +260,11 @@ __global__ __launch_bounds__(256) void row_kernel(RowArgs a) {
   }
   if (waiting > 0) take();
   if (lane < a.K) a.best[unit * a.K + lane] = list;
-  const float all = greatest_of_wave(top);
-  double part_sum = sum > 0.0 ? sum * static_cast<double>(exponential(top, all)) : sum;
 #pragma unroll
-  for (int m = 1; m < 64; m <<= 1) part_sum += __shfl_xor(part_sum, m);
+  for (int m = 1; m < 64; m <<= 1) sum += __shfl_xor(sum, m);
   if (lane == 0) {
-    a.sums[unit] = part_sum;
-    a.tops[unit] = all;
+    a.sums[unit] = sum;
+    a.tops[unit] = above;
   }
 }
 
@@ -269,6 +282,7 @@ struct JoinArgs {
   int* parents;
   int* tokens;
   int V, K, parts, pad;
+  double near;               // see how_near
 };
 
 // One candidate: greater total first, then the lower index.
@@ -287,22 +301,7 @@ __device__ __forceinline__ Candidate of_xor(const Candidate& c, int lane) {
 constexpr int kJoinThreads = 256;
 constexpr int kRowLanes = 16;              // that read a row's sums
 
-// Totals of two beams nearer than this may be in the wrong order.  A row's logarithm is off by the exponentials' 2^-23, by 2^-24 of their
-// exponents (which are ln V at most, on the average that the sum takes), seven roundings of eight values' sum and the factors of a
-// lane's top: below 24 * 2^-24.
-constexpr double kNear = 2 * 24.0 / 16777216.0;
-
-// e^d for d <= 0 in 64 bits: e^r for what is left of d by whole multiples of ln 2, by its series (r^12 / 12! < 1e-14).
-__device__ __forceinline__ double exponential(double d) {
-  const double n = rint(d * 1.4426950408889634), r = fma(n, -1.9082149292705877e-10, fma(n, -0.693147180369123816490, d));
-  double s = 1.0 / 39916800.0;
-  constexpr double kTerms[] = {1.0 / 3628800.0, 1.0 / 362880.0, 1.0 / 40320.0, 1.0 / 5040.0, 1.0 / 720.0, 1.0 / 120.0, 1.0 / 24.0, 1.0 / 6.0, 0.5, 1.0, 1.0};
-#pragma unroll
-  for (int i = 0; i < 11; ++i) s = fma(s, r, kTerms[i]);
-  return d > -700.0 ? ldexp(s, static_cast<int>(n)) : 0.0;
-}
-
-// log sum exp of a row in 64 bits, by the whole workgroup; sixteen logits of a thread on their way together.  `top` is their greatest.
+// log sum exp of a row in 64 bits, by the whole workgroup; sixteen logits of a thread on their way together.  `top` is at or above them.
 // A row of 16600 takes 12 us, one of 120000 65: the memory's latency.
 template <class T>
 __device__ double sum_of_row(const T* row, int V, double top, double* of_wave) {
@@ -331,7 +330,7 @@ __device__ double sum_of_row(const T* row, int V, double top, double* of_wave) {
 __device__ double exact_sum(const JoinArgs& a, long long row, double* of_wave) {
   float top = -__builtin_inff();
   for (int p = threadIdx.x & 63; p < a.parts; p += 64) top = fmaxf(top, a.tops[row * a.parts + p]);
-  top = greatest_of_wave(top);
+  top = greatest_of_wave(top, threadIdx.x & 63);
   const long long at = row * a.V;
   if (a.dtype == COTTEN_F32) return sum_of_row(static_cast<const float*>(a.logits) + at, a.V, top, of_wave);
   if (a.dtype == COTTEN_BF16) return sum_of_row(static_cast<const __bf16*>(a.logits) + at, a.V, top, of_wave);
@@ -414,7 +413,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinArgs a) {
       const Candidate c = n < a.K ? candidate(list, n, best[static_cast<long long>(list) * a.K + n]) : none;
       if (__ballot(ahead(c, bar)) == 0) return false;
       mine = merged(mine, of_lane(sorted(c, lane), 63 - lane), lane);
-      bar = Candidate{of_lane(mine, a.K - 1).total - kNear, ~0ull};
+      bar = Candidate{of_lane(mine, a.K - 1).total - a.near, ~0ull};
       return true;
     };
     if (lists > 64) {
@@ -446,12 +445,12 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinArgs a) {
       const int before = lane < a.K ? (lane > 0 ? lane - 1 : 0) : a.K - 1;
       const double gap = of_lane(mine, before).total - mine.total;
       const int k_before = __shfl(k, before);
-      const uint32_t pair = mine.index != ~0ull && k != k_before && gap < kNear ? (1u << k) | (1u << k_before) : 0u;
+      const uint32_t pair = mine.index != ~0ull && k != k_before && gap < a.near ? (1u << k) | (1u << k_before) : 0u;
       // (equal totals are those of equal rows: they are in order, but stay equal only if both sums are made again)
       uint32_t near = 0u, more = of_all(gap > 0.0 ? pair : 0u);
       // Where the last of the 64 is that near too, others may have found no place (one beam's equal logits can take them all): every beam
       // with a candidate that near behind the last that is taken is looked up in the lists.
-      if (!again && __ballot(lane == 63 && mine.index != ~0ull && gap < kNear) != 0) {
+      if (!again && __ballot(lane == 63 && mine.index != ~0ull && gap < a.near) != 0) {
         const Candidate last = of_lane(mine, a.K - 1);
         const uint32_t of_last = 1u << __shfl(k, a.K - 1);
         uint32_t crowd = 0u;
@@ -460,7 +459,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(JoinArgs a) {
           if ((of_last >> (list / a.parts)) & 1u) continue;   // (in order by itself)
           for (int n = 0; n < a.K; ++n) {
             const Candidate c = candidate(list, n, best[static_cast<long long>(list) * a.K + n]);
-            if (!(last.total - c.total < kNear)) break;
+            if (!(last.total - c.total < a.near)) break;
             if (ahead(last, c)) {
               crowd |= 1u << (list / a.parts);
               differ |= c.total < last.total;
@@ -539,6 +538,12 @@ int check_shape(int B, int K, int V) {
   return COTTEN_OK;
 }
 
+// Totals of two beams nearer than this may be in the wrong order.  A row's logarithm is off by what its exponentials are on the average that
+// the sum takes: 2^-23 of the hardware's, and 2^-24 of their exponents by the difference and again by its product with log2(e).  The exponents
+// are 2 more than those from the row's greatest at most, which are ln V at most on that average.  Three roundings in a sum of eight by pairs;
+// everything after it is in 64 bits.
+double how_near(int V) { return 2.0 * (2.0 + 2.0 * (2.0 + std::log(static_cast<double>(V))) + 3.0) / 16777216.0; }
+
 // Waves for a row: enough of them to fill the device, of one round of loads at least; few enough that the join has up to 512 lists.
 // 256 x 8 rows of 16600 in 8192 / 4096 / 2048 waves: 44 / 38 / 39 us with the join; 32 x 5 of 120000: 39 / 35 / 32 (before the bar was raised again).
 constexpr int kWanted = 4096;
@@ -591,7 +596,7 @@ int cotten_beam_select(const void* logits, const float* scores, const uint8_t* f
   if (prm->dtype == COTTEN_F32) row_kernel<float><<<grid, block, 0, s>>>(r);
   else if (prm->dtype == COTTEN_BF16) row_kernel<__bf16><<<grid, block, 0, s>>>(r);
   else row_kernel<_Float16><<<grid, block, 0, s>>>(r);
-  const JoinArgs j{logits, prm->dtype, best, sums, tops, scores, finished, new_scores, parents, tokens, V, K, cut.parts, prm->pad};
+  const JoinArgs j{logits, prm->dtype, best, sums, tops, scores, finished, new_scores, parents, tokens, V, K, cut.parts, prm->pad, how_near(V)};
   join_kernel<<<dim3(B), dim3(kJoinThreads), 0, s>>>(j);
   return hipGetLastError() == hipSuccess ? COTTEN_OK : COTTEN_ERR_LAUNCH;
 }

@@ -308,3 +308,31 @@ def test_equal_beams_of_many_ties(V):
     logits[1:, :, V // 2] = -9.0
     logits[2, 0, V // 3] = 2.0 ** -20
     compare(logits.cuda(), torch.full((3, 32), -2.0).cuda())
+
+
+def test_rows_that_rise_for_long():
+    """Rows walked whole whose greatest grows in every round.  Totals near 0, where a score shows the sum: of exponentials of
+    differences d from a reference 2 above the greatest at most, each off by 2^-23 and 2^-24 |d| twice (|d| on the average that the sum takes:
+    2 + ln V at most), in sums of eight by pairs (three roundings)."""
+    V, K = 600_000, 2
+    slopes = (0.001, 0.003, 0.006, 0.00108, 0.02, 1.0)
+    logits = torch.zeros(2048, K, V, device="cuda")              # (so many rows that none is cut)
+    gen = torch.Generator().manual_seed(0)
+    few, scores = torch.empty(2 * len(slopes), K, V), torch.zeros(2048, K)
+    for i, slope in enumerate(slopes):
+        rising = (torch.arange(V, dtype=torch.float64) * (slope / 1024)).float()
+        few[2 * i:2 * i + 2, 0] = rising
+        few[2 * i:2 * i + 2, 1] = rising[torch.randperm(V, generator=gen)]
+        level = (torch.logsumexp(rising.double(), 0) - rising.double().amax()).float()
+        # far behind, where nothing is made again; and one step of the score ahead, which sums that grow another way have to tell
+        scores[2 * i] = torch.stack([level, level - 5.0])
+        scores[2 * i + 1] = torch.stack([level, torch.nextafter(level, torch.tensor(math.inf))])
+    logits[:few.shape[0]] = few.cuda()
+    from paper_2602_06935_amd import binding
+    got = binding.cotten_beam_select(logits, scores.cuda())
+    best, parents, tokens = expected(few, scores[:few.shape[0]])
+    assert (parents[::2] == 0).all() and (parents[1::2, 0] == 1).all()
+    off = (got[0][:few.shape[0]].cpu().double() - best).abs()
+    room = best.abs() * 2.0 ** -24 + (2 * (2 + math.log(V)) + 2 + 3) * 2.0 ** -24
+    assert (off <= room).all(), (off / 2.0 ** -24, room / 2.0 ** -24)
+    assert torch.equal(got[1][:few.shape[0]].cpu().long(), parents) and torch.equal(got[2][:few.shape[0]].cpu().long(), tokens)
