@@ -320,7 +320,7 @@ size_t cotten_delta_workspace_bytes(int B, int H, int N, int d_h, int dtype, int
  *
  * Types, layouts, states, precision, streams, limits of rows and what calls may share are those of the gated delta rule;
  * B * H up to 2^20.  A value that is not finite in a row that takes part makes the results that hang on it not finite from its group
- * of 32 tokens on. */
+ * of 32 tokens on; so does a growth (g > 0) whose power by the number of the group's tokens that count is above what fp32 holds. */
 typedef struct cotten_decay_params {
   int dtype;                  /* a cotten_dtype: of Q, K, V, O and their gradients               */
   float scale;                /* factor of O; <= 0 selects 1                                     */

@@ -159,8 +159,6 @@ __device__ __forceinline__ void set_powers(Powers* to, double rate, int lane) {
 // p of a token of a chunk
 __device__ __forceinline__ int upto(uint32_t live, int t) { return __popc(live & (0xffffffffu >> (31 - t))); }
 
-// How many tokens of a chunk count, and the factors of a wave's pairs: columns lane%16 of X's tile, rows 4g + r of Y's.  Where all tokens from the first that counts to the last that exists count, pairs are as far apart as their numbers say, and
-// the factors of the pairs are the same in all chunks.
 // Two pieces of eight significant bits each, rounded: 16 bits, where a result of 11 or fewer is all that comes of them.
 __device__ __forceinline__ Pieces<2> cut_in_two(const float (&x)[8]) {
   delta::u32x4_t h, m;
@@ -199,11 +197,15 @@ struct Pair {
   int x, y;
   __device__ __forceinline__ explicit Pair(int i) : x(R::kBack ? i >> 1 : (i + 1) >> 1), y(R::kBack ? (i + 1) >> 1 : i >> 1) {}
 };
+// How many tokens of a chunk count, and the factors of a wave's pairs: columns lane%16 of X's tile, rows 4g + r of Y's.  Where all tokens
+// from the first that counts to the last that exists count, pairs are as far apart as their numbers say, and the factors of the pairs are
+// the same in all chunks.
 template <class R, int WAVES, int COUNT = 3>
 struct Decays {
   static constexpr int kOwn = (COUNT + WAVES - 1) / WAVES;           // pairs of a wave, at most (COUNT: 3 or, of two kinds of them, 6)
   uint32_t live;
   bool together;
+  bool finite;              // all powers of a chunk
   float n;                  // tokens that count
   float pair[kOwn][4];
   float whole_hi, whole_lo;
@@ -222,7 +224,7 @@ struct Decays {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int row = 4 * (lane >> 4) + r, a = apart(bits, p, r, lane);
-          const bool in = p.x != p.y || (R::kBack ? row >= (lane & 15) : row <= (lane & 15));
+          const bool in = (p.x != p.y || (R::kBack ? row >= (lane & 15) : row <= (lane & 15))) && (R::kBack || ((bits >> (16 * p.y + row)) & 1u));
           const float w = powers->hi[a < 0 ? 0 : a];
           pair[k][r] = in ? w : 0.0f;
         }
@@ -232,6 +234,7 @@ struct Decays {
   __device__ __forceinline__ void begin(const Powers* powers, int wave, int lane) {
     none();
     together = true;
+    finite = powers->hi[kChunk - 1] < __builtin_inff();
     set_pairs(~0u, powers, wave, lane);
   }
   // no token counts
@@ -248,7 +251,8 @@ struct Decays {
     n = static_cast<float>(count);
     whole_hi = powers->hi[count];
     whole_lo = powers->lo[count];
-    const bool now = ((bits | ~there) >> __builtin_ctz(bits)) == (0xffffffffu >> __builtin_ctz(bits));
+    // (where the state grows, powers between tokens that do not count may be infinite, and are no factors of zeros)
+    const bool now = finite && ((bits | ~there) >> __builtin_ctz(bits)) == (0xffffffffu >> __builtin_ctz(bits));
     if (!now || !together) set_pairs(now ? ~0u : bits, powers, wave, lane);
     together = now;
   }

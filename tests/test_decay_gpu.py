@@ -391,3 +391,19 @@ def test_masked_beginnings_of_segments(dtype, H, N, d):
     for n, t in zip(NAMES, grads):
         check(n, back(t, layout), ref[n])
     check_decays(dg, ref)
+
+
+@pytest.mark.parametrize("N,mask", [(20, None), (40, "left"), (420, "left"), (420, "few")])
+@pytest.mark.parametrize("d", [16, 128])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_growth_between_tokens_that_do_not_count(dtype, d, N, mask):
+    """A state that grows by e^3 with every token that counts: e^93 of the pairs that are 31 tokens apart is above what fp32 holds, but of such
+    pairs one token here does not count or does not exist."""
+    x = inputs(2, 2, N, d, DTYPES[dtype], seed=N + d)
+    x["g"] = torch.tensor([3.0, -0.1])
+    if mask is not None:
+        x["mask"] = torch.zeros(2, N, dtype=torch.uint8)
+        x["mask"][:, -6:] = 1                                     # the last of a chunk that begins with none
+        if mask == "few":
+            x["mask"][0, 5:200:40] = 1
+    compare(x, scale=0.5)
