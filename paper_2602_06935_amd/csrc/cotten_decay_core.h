@@ -224,7 +224,7 @@ struct Decays {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const int row = 4 * (lane >> 4) + r, a = apart(bits, p, r, lane);
-          const bool in = (p.x != p.y || (R::kBack ? row >= (lane & 15) : row <= (lane & 15))) && (R::kBack || ((bits >> (16 * p.y + row)) & 1u));
+          const bool in = p.x != p.y || (R::kBack ? row >= (lane & 15) : row <= (lane & 15));
           const float w = powers->hi[a < 0 ? 0 : a];
           pair[k][r] = in ? w : 0.0f;
         }
@@ -277,19 +277,15 @@ __device__ __forceinline__ int first_live(const uint8_t* mask, int N, int begin,
   return end;
 }
 
-// Whether no token of the first `chunks` counts: 4096 of them at a time.
+// Whether no token of the first `chunks` counts: 1024 of them at a time (more would take registers that the states are in).
 __device__ __forceinline__ bool none_before(const uint8_t* mask, int chunks, int lane) {
   typedef delta::u32x4_t __attribute__((aligned(1))) bytes;  // (rows of a mask begin anywhere)
   const bytes* of = reinterpret_cast<const bytes*>(mask);
-  for (int at = lane; at - lane < 2 * chunks; at += 256) {
-    uint32_t any = 0;
-#pragma unroll
-    for (int u = 0; u < 4; ++u)
-      if (at + 64 * u < 2 * chunks) {
-        const delta::u32x4_t x = of[at + 64 * u];
-        any |= x[0] | x[1] | x[2] | x[3];
-      }
-    if (__ballot(any != 0) != 0) return false;
+#pragma unroll 1
+  for (int at = 0; at < 2 * chunks; at += 64) {  // (the same in all lanes)
+    delta::u32x4_t x = {0, 0, 0, 0};
+    if (at + lane < 2 * chunks) x = of[at + lane];
+    if (__ballot((x[0] | x[1] | x[2] | x[3]) != 0) != 0) return false;
   }
   return true;
 }
@@ -469,7 +465,7 @@ __device__ void walk(const Args& a, int unit, unsigned char* smem, int part = 0)
   if (a.mask != nullptr && (R::kBack ? (ROLE == kDk || a.dinitial_state == nullptr) : a.initial_state == nullptr)) {
     int from = first_live(s.mask, a.N, begin, end, lane);
     if constexpr (ROLE == kOut || ROLE == kDq || ROLE == kDecays || ROLE == kGradStates)
-      if (from > begin && begin > 0 && (begin > 128 * (from - begin) || !none_before(s.mask, begin, lane))) from = begin;
+      if (from > begin && begin > 0 && (begin > 32 * (from - begin) || !none_before(s.mask, begin, lane))) from = begin;
     if constexpr (R::kRows && ROLE != kDecays) {
       unsigned char* to = ROLE == kOut ? a.O : ROLE == kDq ? a.dQ : ROLE == kDk ? a.dK : a.dV;
       for (int c = begin; c < from; ++c) {
