@@ -36,7 +36,12 @@ __global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
     S[r] = a.initial_state == nullptr
                ? f32x4_t{0, 0, 0, 0}
                : *reinterpret_cast<const f32x4_t*>(a.initial_state + (static_cast<long long>(slice) * D + group + r * kGroups) * D + col);
-  const float whole = static_cast<float>(exp2(rate_of(s.g)));
+  // Near 1 (weak) the decay of a call's tokens is left for its end, a^p in two floats, and what a token adds is divided by a^p before: a server makes
+  // one call after the other, and the rounding of a factor would be the same in every one of them.  Other decays leave nothing for roundings to add up in.
+  const double rate = rate_of(s.g), whole = exp2(rate);
+  const bool weak = whole > 0.5 && whole < 2.0;
+  const float now = weak ? 1.0f : static_cast<float>(whole);
+  int count = 0;
   for (int t = 0; t < a.N; ++t) {
     const bool live = s.mask == nullptr || s.mask[t] != 0;
     const uint32_t row = static_cast<uint32_t>(t) * a.stride_row;
@@ -55,7 +60,10 @@ __global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
       kk += __shfl_xor(kk, m);
       qq += __shfl_xor(qq, m);
     }
-    const float rk = live ? __builtin_amdgcn_rsqf(kk + a.eps) : 0.0f, rq = a.scale * __builtin_amdgcn_rsqf(qq + a.eps), decay = live ? whole : 1.0f;
+    count += live ? 1 : 0;
+    const float later = weak ? static_cast<float>(rate * static_cast<double>(count)) : 0.0f;
+    const float rk = live ? __builtin_amdgcn_rsqf(kk + a.eps) * __builtin_amdgcn_exp2f(-later) : 0.0f;
+    const float rq = a.scale * __builtin_amdgcn_rsqf(qq + a.eps) * __builtin_amdgcn_exp2f(later), decay = live ? now : 1.0f;
     f32x4_t o = {0, 0, 0, 0};
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
@@ -73,6 +81,14 @@ __global__ __launch_bounds__(256) void step_kernel(Args a, int parts) {
     if (group == 0) E::store_four(O, row + col * E::kBytes, o * rq);
   }
   if (a.final_state != nullptr) {
+    if (weak && count != 0) {
+      const double left = exp2(rate * static_cast<double>(count));
+      const float hi = static_cast<float>(left), lo = static_cast<float>(left - static_cast<double>(hi));
+#pragma unroll
+      for (int r = 0; r < kRows; ++r)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) S[r][c] = fmaf(S[r][c], hi, S[r][c] * lo);
+    }
 #pragma unroll
     for (int r = 0; r < kRows; ++r)
       *reinterpret_cast<f32x4_t*>(a.final_state + (static_cast<long long>(slice) * D + group + r * kGroups) * D + col) = S[r];

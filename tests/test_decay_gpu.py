@@ -1,4 +1,6 @@
 """The decay attention on the GPU, forward, backward and single steps, against its definition in 64 bits."""
+import math
+
 import pytest
 import torch
 
@@ -407,3 +409,23 @@ def test_growth_between_tokens_that_do_not_count(dtype, d, N, mask):
         if mask == "few":
             x["mask"][0, 5:200:40] = 1
     compare(x, scale=0.5)
+
+
+@pytest.mark.parametrize("tokens", [1, 4])
+def test_many_steps_of_a_weak_decay(tokens):
+    """exp(g) as one float is off by up to 2^-25, in the same direction at every token: over 3000 of them the oldest would be off by 9e-5.  The
+    roundings of the state, one a token, are of either sign."""
+    from paper_2602_06935_amd import binding
+    N, d = 3000, 16
+    x = inputs(1, 4, N, d, torch.float32, seed=tokens)
+    # decays half way between two floats, the closest that a float g comes to them
+    x["g"] = torch.tensor([math.log1p(-(m + 0.5) * 2.0 ** -24) for m in (200, 1677, 1678, 8000)]).float()
+    ref = reference(x, grads=False)
+    S, O = torch.zeros(1, 4, d, d, device="cuda"), []
+    q, k, v = (torch.stack(x[n].split(tokens, 2)).cuda() for n in ("q", "k", "v"))
+    g = x["g"].cuda()
+    for i in range(N // tokens):
+        O.append(binding.cotten_decay_fwd(q[i], k[i], v[i], g, None, initial_state=S, final_state=S))
+    for h in range(4):
+        assert (S.cpu().double() - ref["S1"])[:, h].norm() <= FP32_BAR * ref["S1"][:, h].norm(), h
+    check("O", torch.cat(O, 2), ref["O"])
