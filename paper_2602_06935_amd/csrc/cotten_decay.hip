@@ -280,10 +280,16 @@ hipError_t launch_gradients(const Args& a, int units, hipStream_t s) {
   return hipSuccess;
 }
 
-// A forward's segments sum the states before them themselves, in place of a launch that does it for all, where there is little to read: up to five,
-// or narrow states.  us, scan / sums: bf16 d = 64, 4 x 400 (5 segments) 16.2 / 13.4, 128 x 1024 (4) 35.7 / 31.8, 64 x 1024 (8) 24.3 / 27.4; fp16
-// d = 128, 64 x 1024 (4) 66.8 / 59, 4 x 1024 (16) 26 / 35; fp32 d = 32, 4 x 4096 (32) 24.7 / 21.0, 64 x 1024 (16) 22.1 / 23.6; bf16 d = 16, 32 x 4096
-// (32) 22.5 / 18.5.
+// A forward's segments sum the states before them themselves, in place of a launch that does it for all, where there is little to read for as many
+// workgroups as there are: up to five, states of d = 16, and of d = 32 unless all compute units are busy with it (few slices leave a scan few
+// workgroups, which walk the segments one after the other).  us, scan / sums:
+//   d = 64 bf16   4 x 400 (5 segments) 16.2 / 13.4, 128 x 1024 (4) 35.7 / 31.8, 64 x 1024 (8) 24.3 / 27.4     128 fp16  64 x 1024 (4) 66.8 / 59, 4 x 1024 (16) 26 / 35
+//   d = 32 bf16   4 x 4096 (32) 19.9 / 16.5, 32 x 2048 (32) 21.3 / 22.8, 8 x 16384 (64) 35.4 / 32.3, 16 x 16384 (64) 38.8 / 42.5, 8 x 32768 (128) 48.7 / 55.3,
+//                 1 x 65536 (256) 60.6 / 50.9, 4 x 65536 (256) 68.6 / 79.7, 1 x 2^20 (1026) 230 / 195; fp32  64 x 1024 (16) 24.4 / 24.6, 4 x 65536 84.7 / 93.7
+//   d = 16 bf16   32 x 4096 (32) 22.6 / 18.8, 16 x 16384 (64) 35.1 / 29.4, 4 x 65536 (258) 62.5 / 48.9, 1 x 2^20 (2064, as many as there are) 321 / 247
+bool sums_of_its_own(int D, long long slices, int segments) {
+  return segments <= 5 || D == 16 || (D == 32 && (slices < 4 || slices * segments <= 512));
+}
 template <class E, int D>
 hipError_t forward(Args a, int slices, hipStream_t s) {
   if (a.N <= kMostSteps<E, D>) {
@@ -298,7 +304,7 @@ hipError_t forward(Args a, int slices, hipStream_t s) {
     constexpr int kBytes = kLds<E, D, kStates>;
     if (hipError_t rc = granted(walk_kernel<E, D, kStates>, kBytes)) return rc;
     walk_kernel<E, D, kStates><<<grid, block, kBytes, s>>>(a);
-    a.unscanned = D <= 32 || a.segments <= 5;
+    a.unscanned = sums_of_its_own(D, slices, a.segments);
     if (!a.unscanned) launch_scan(a, slices, D, false, s);
   }
   constexpr int kBytes = kLds<E, D, kOut>;

@@ -429,3 +429,14 @@ def test_many_steps_of_a_weak_decay(tokens):
     for h in range(4):
         assert (S.cpu().double() - ref["S1"])[:, h].norm() <= FP32_BAR * ref["S1"][:, h].norm(), h
     check("O", torch.cat(O, 2), ref["O"])
+
+
+# forwards of many segments of narrow states: with all compute units busy, and few slices of long sequences
+@pytest.mark.parametrize("B,H,N,d", [(32, 2, 1100, 32), (2, 1, 20000, 32), (4, 1, 16500, 32), (1, 1, 40000, 16)])
+def test_forwards_of_many_segments(B, H, N, d):
+    for dtype in ("f32", "bf16"):
+        x = inputs(B, H, N, d, DTYPES[dtype], seed=N, mask="left" if B > 1 else None, states=True)
+        ref = reference(x, grads=False)
+        O, S1 = forward(x, "bnhd")
+        check("O", O, ref["O"])
+        check("S1", S1, ref["S1"])
