@@ -318,8 +318,8 @@ size_t cotten_delta_workspace_bytes(int B, int H, int N, int d_h, int dtype, int
  * are not masked).  Gradients of masked K and V are exact zeros, those of g are summed over the batch in 64 bits.  A
  * sequence without a valid token keeps its initial state.  With g = 0 and no states it is the causal variant above.
  *
- * Types, layouts, states, precision, streams, limits of rows and what calls may share are those of the gated delta rule;
- * B * H up to 2^20.  A value that is not finite in a row that takes part makes the results that hang on it not finite from its group
+ * Types, layouts, states, precision, streams, limits of rows and what calls may share are those of the gated delta rule, but that
+ * the products that make rows of 16-bit results keep 16 significant bits of their operands; B * H up to 2^20.  A value that is not finite in a row that takes part makes the results that hang on it not finite from its group
  * of 32 tokens on; so does a growth (g > 0) whose power by the number of the group's tokens that count is above what fp32 holds. */
 typedef struct cotten_decay_params {
   int dtype;                  /* a cotten_dtype: of Q, K, V, O and their gradients               */
