@@ -301,7 +301,7 @@ __device__ __forceinline__ Candidate of_xor(const Candidate& c, int lane) {
 constexpr int kJoinThreads = 256;
 constexpr int kRowLanes = 16;              // that read a row's sums
 
-// log sum exp of a row in 64 bits, by the whole workgroup; sixteen logits of a thread on their way together.  `top` is at or above them.
+// log sum exp of a row in 64 bits, by the whole workgroup; sixteen logits of a thread on their way together.  `top` is their greatest.
 // A row of 16600 takes 12 us, one of 120000 65: the memory's latency.
 template <class T>
 __device__ double sum_of_row(const T* row, int V, double top, double* of_wave) {
@@ -329,7 +329,8 @@ __device__ double sum_of_row(const T* row, int V, double top, double* of_wave) {
 }
 __device__ double exact_sum(const JoinArgs& a, long long row, double* of_wave) {
   float top = -__builtin_inff();
-  for (int p = threadIdx.x & 63; p < a.parts; p += 64) top = fmaxf(top, a.tops[row * a.parts + p]);
+  // (the row's greatest itself, the heads of its lists: where it has all of the sum, its total is the score exactly; no key is no number)
+  for (int p = threadIdx.x & 63; p < a.parts; p += 64) top = fmaxf(top, from_order(static_cast<uint32_t>(a.best[(row * a.parts + p) * a.K] >> 32)));
   top = greatest_of_wave(top, threadIdx.x & 63);
   const long long at = row * a.V;
   if (a.dtype == COTTEN_F32) return sum_of_row(static_cast<const float*>(a.logits) + at, a.V, top, of_wave);

@@ -336,3 +336,15 @@ def test_rows_that_rise_for_long():
     room = best.abs() * 2.0 ** -24 + (2 * (2 + math.log(V)) + 2 + 3) * 2.0 ** -24
     assert (off <= room).all(), (off / 2.0 ** -24, room / 2.0 ** -24)
     assert torch.equal(got[1][:few.shape[0]].cpu().long(), parents) and torch.equal(got[2][:few.shape[0]].cpu().long(), tokens)
+
+
+@pytest.mark.parametrize("V", [1, 2, 3000])
+@pytest.mark.parametrize("dtype", list(DTYPES))
+def test_ended_beams_that_tie_with_certain_continuations(dtype, V):
+    """Where one item has all of a row, its total is the beam's score, and ties with an ended beam of that score: the lower index first."""
+    B, K = 4, 6
+    logits = torch.full((B, K, V), -60.0, dtype=DTYPES[dtype])
+    for b, level in enumerate((0.0, 3.0, 7.7, -11.4)):
+        logits[b, :, V // 2] = level
+    finished = torch.tensor([[0, 1, 0, 1, 1, 0]] * B, dtype=torch.uint8)
+    compare(logits.cuda(), torch.full((B, K), -3.25).cuda(), finished.cuda(), V // 2)
